@@ -30,9 +30,9 @@
  *     other's copies) and a few through which sizes and headers are read back (allocated
  *     on first use, grown when needed, held until zc_release_host_buffers() or the end of
  *     the process).  No environment variable is read.
- *   - HIP graphs: only zc_decompress_batch_run and zc_compress_noalloc may be recorded by
- *     stream capture (they launch kernels and nothing else; zc_compress_noalloc after a
- *     first call outside one).  Every other entry point that takes a stream
+ *   - HIP graphs: only zc_decompress_batch_run, zc_compress_noalloc and the operators over K/V pages
+ *     may be recorded by stream capture (they launch kernels and nothing else;
+ *     zc_compress_noalloc after a first call outside one).  Every other entry point that takes a stream
  *     copies from or to the library's page-locked buffers, may wait for what kernels leave
  *     there or on an event and may allocate page-locked memory, none of which a capture
  *     allows; a captured copy would also replay whatever a later call left in the buffer.
@@ -386,6 +386,81 @@ zc_status zc_copy_reference(const void *d_src, void *d_dst, uint64_t bytes, uint
  * used symbols.  A single used symbol gets length 1. */
 zc_status zc_build_code(const uint64_t *hist, uint32_t alphabet, uint32_t limit,
                         uint8_t *len_out, uint16_t *code_out);
+
+/* ---- Operators over K/V pages (Sec. 3.3, 5.2: a cache is kept, compressed and decoded in pages) -------------------------
+ * What runs on the pages that the decode calls above leave in memory: attention, and the choice of the tokens that stay.
+ * They are serving operators over a stored cache (there is no gradient).  All of them only launch kernels on `stream`:
+ * they never copy, wait or allocate, and may be recorded by stream capture.  They read no host array but their arguments.
+ *
+ * A page holds page_tokens consecutive tokens of one K/V head of one sequence: [page_tokens][head_dim] elements, which is what
+ * a chunk of chunk_bytes = page_tokens * head_dim * element size decodes to.  K and V have a pool of pages each, with the same
+ * page numbers.  Entry [s][h][i] of the table is the page of tokens i * page_tokens .. of sequence s and head h; a number that
+ * is not below n_pages (a negative one, for instance) says that the page is absent: its tokens are not seen.  Pages that a
+ * window has left behind can be given back that way.  What lies in a page behind a sequence's length has no influence,
+ * whatever its bits. */
+typedef struct {
+    uint32_t struct_size;       /* = sizeof(zc_kv_cache) */
+    uint32_t format;            /* ZC_FMT_BF16, ZC_FMT_FP8_E4M3 or ZC_FMT_FP8_E5M2 */
+    uint32_t n_seqs, n_heads;   /* sequences, K/V heads */
+    uint32_t head_dim;          /* 64 or 128 */
+    uint32_t page_tokens;       /* a power of two, 16 to 65,536 */
+    uint32_t table_pages;       /* table entries per sequence and head; table_pages * page_tokens < 2^30 */
+    uint32_t n_pages;           /* pages in each pool */
+    void *d_k_pages, *d_v_pages;    /* 16-byte aligned */
+    const int32_t *d_table;     /* [n_seqs][n_heads][table_pages] */
+    int32_t *d_lengths;         /* [n_seqs]: tokens in the cache (negative: 0; more than there is room for: that) */
+    const float *d_k_scales, *d_v_scales;   /* [n_seqs][n_heads], what the stored elements are multiplied with, or NULL: 1 */
+} zc_kv_cache;
+
+/* Attention of n_tokens query tokens.  Sequence s has the query tokens d_q_start[s] .. d_q_start[s + 1] (at most max_q_len of
+ * them; d_q_start non-decreasing, or NULL: n_tokens == n_seqs, token s is sequence s's), whose keys and values are in the cache
+ * already: the i-th of n is at position length - n + i.  It sees the tokens up to its own position that are among the last
+ * `window` of those (its own included; 0: all) or among the first `sinks` of the sequence.  Query head j reads K/V head
+ * j / (n_q_heads / n_heads).  With s_t = scale * k_scale * <q, k_t> over the tokens seen
+ *   out = v_scale * sum exp(s_t) v_t / sum exp(s_t),   lse = ln sum exp(s_t);
+ * a query that sees nothing (or nothing with a logit above minus infinity) has out = 0 and lse = -infinity.  Products are
+ * accumulated, and the softmax is held, in 32 bits; its weights are rounded to the type the values are multiplied in (BF16 for
+ * BF16 pages, half precision for FP8 pages), the result once to BF16.  Query tokens of no sequence are left untouched. */
+typedef struct {
+    uint32_t struct_size;       /* = sizeof(zc_attend_args) */
+    uint32_t n_tokens, n_q_heads, max_q_len;
+    uint32_t window, sinks;
+    uint32_t max_kv_len, max_prefix_len;    /* no length is above them (greater ones are taken as these); 0: what the tables have room for */
+    float scale;
+    uint32_t reserved;
+    const void *d_q;            /* BF16, 16-byte aligned; token t, head j at element t * q_token_stride + j * q_head_stride */
+    void *d_out;                /* BF16, likewise */
+    uint64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;  /* multiples of 8 */
+    const int32_t *d_q_start;
+    float *d_lse;               /* [n_tokens][n_q_heads], or NULL */
+    const float *d_weights_in;  /* [n_seqs][n_heads][table_pages * page_tokens], or NULL: zeros */
+    float *d_weights_out;       /* likewise, or NULL; may be d_weights_in */
+} zc_attend_args;
+
+/* Scratch bytes of the call below with these arguments (prefix: NULL for zc_attend); may be 0.  Host only. */
+uint64_t zc_attend_workspace_bytes(const zc_attend_args *args, const zc_kv_cache *prefix, const zc_kv_cache *cache);
+
+/* Attention over the cache.  With d_weights_out (then d_lse is needed) the attention weight that the call has given to every
+ * token of every sequence is added up, over its query tokens and the query heads that share the K/V head:
+ * weights_out[s][h][t] = weights_in[s][h][t] + sum exp(s_t - lse) for t below the length; entries behind it are left untouched.
+ * The sums have one order: the same call gives the same bits. */
+zc_status zc_attend(const zc_attend_args *args, const zc_kv_cache *cache, void *d_ws, uint64_t ws_bytes, void *stream);
+
+/* Attention of sequences that share their first tokens: `prefix` (n_seqs = 1; its length P) is read once for all of them, `cache`
+ * holds what each has of its own.  The i-th of n query tokens is at position P + length - n + i; window and sinks count from the
+ * prefix's first token.  The two caches have the same format, n_heads and head_dim.  d_weights_out is refused. */
+zc_status zc_attend_shared(const zc_attend_args *args, const zc_kv_cache *prefix, const zc_kv_cache *cache, void *d_ws, uint64_t ws_bytes, void *stream);
+
+/* Eviction.  Of every sequence and head of `from` that has more than `keep` tokens there remain the first `sinks`, the last
+ * `recent` (sinks + recent <= keep) and, of those between, the ones with the largest d_weights, keep in all; of equal ones those
+ * that come first; NaN counts as lowest.  They keep their order.  d_kept: [n_seqs][n_heads][keep], the numbers of the tokens that
+ * remain, ascending, -1 behind the last.  Keys, values and weights of the tokens that remain go to the pages of `to` (same
+ * sequences, heads, head_dim and format; pages that `from` does not name; room for min(keep, tokens of from's table)) and to
+ * d_weights_to ([n_seqs][n_heads][to's table_pages * page_tokens], or NULL, not d_weights); to's d_lengths (not from's) becomes
+ * min(length, keep).  The first length tokens' pages have to be there in both tables: a row from an absent page is zero, one to an
+ * absent page is not written.  Scales belong to sequence and head and stay as they are. */
+zc_status zc_evict(const zc_kv_cache *from, const float *d_weights, uint32_t keep, uint32_t sinks, uint32_t recent,
+                   const zc_kv_cache *to, float *d_weights_to, int32_t *d_kept, void *stream);
 
 const char *zc_status_string(zc_status s);
 

@@ -1,0 +1,222 @@
+// Host side of the operators over K/V pages: argument checks, the choice of kernels and splits, and the C entry points
+// zc_attend, zc_attend_shared, zc_attend_workspace_bytes and zc_evict.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "zc_attend.h"
+#include "zc_host.h"
+
+namespace zc {
+
+namespace {
+
+constexpr uint32_t kMaxTokens = 1u << 30;      // positions are signed 32-bit numbers in the kernels, sums of two included
+constexpr uint32_t kMaxSlots = 64;             // parts of one row: k_attend_join holds one per lane
+
+bool aligned4(const void *p) { return ((uintptr_t)p & 3) == 0; }
+
+zc_status check_cache(const zc_kv_cache *c, PagesDev *out)
+{
+    if (!c) return ZC_ERR_INVALID_ARG;
+    if (c->struct_size != sizeof(zc_kv_cache)) return ZC_ERR_UNSUPPORTED;
+    if (c->format != ZC_FMT_BF16 && c->format != ZC_FMT_FP8_E4M3 && c->format != ZC_FMT_FP8_E5M2) return ZC_ERR_UNSUPPORTED;
+    if (c->head_dim != 64 && c->head_dim != 128) return ZC_ERR_UNSUPPORTED;
+    if (c->page_tokens < 16 || c->page_tokens > 65536 || (c->page_tokens & (c->page_tokens - 1))) return ZC_ERR_INVALID_ARG;
+    if (!c->n_seqs || !c->n_heads || !c->table_pages || !c->n_pages || c->n_pages > 0x7FFFFFFFu) return ZC_ERR_INVALID_ARG;
+    const uint64_t capacity = (uint64_t)c->table_pages * c->page_tokens;
+    if (capacity >= kMaxTokens || (uint64_t)c->n_seqs * c->n_heads > 0x3FFFFFFu) return ZC_ERR_INVALID_ARG;
+    if (!c->d_k_pages || !c->d_v_pages || !c->d_table || !c->d_lengths) return ZC_ERR_INVALID_ARG;
+    if (!aligned16(c->d_k_pages) || !aligned16(c->d_v_pages) || !aligned4(c->d_table) || !aligned4(c->d_lengths) ||
+        !aligned4(c->d_k_scales) || !aligned4(c->d_v_scales)) return ZC_ERR_INVALID_ARG;
+    PagesDev d = {};
+    d.k = (const uint8_t *)c->d_k_pages;
+    d.v = (const uint8_t *)c->d_v_pages;
+    d.table = c->d_table;
+    d.lengths = c->d_lengths;
+    d.k_scales = c->d_k_scales;
+    d.v_scales = c->d_v_scales;
+    d.heads = c->n_heads;
+    d.table_pages = c->table_pages;
+    d.n_pages = c->n_pages;
+    while ((1u << d.page_shift) < c->page_tokens) d.page_shift++;
+    d.capacity = d.limit = (int32_t)capacity;
+    *out = d;
+    return ZC_OK;
+}
+
+bool same_shape(const zc_kv_cache &a, const zc_kv_cache &b) { return a.format == b.format && a.n_heads == b.n_heads && a.head_dim == b.head_dim; }
+
+// one pass of k_attend_few over a cache
+struct Pass {
+    uint32_t tiles, row_blocks, splits;
+    uint64_t blocks;
+};
+
+// rows: of one (sequence, head), or of one head of the prefix; units: how many of those; longest: tokens that a row block may have to read
+Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_splits)
+{
+    Pass p;
+    p.tiles = rows <= 16 ? 1 : 2;
+    p.row_blocks = (uint32_t)((rows + p.tiles * 16 - 1) / (p.tiles * 16));
+    const uint64_t groups = units * p.row_blocks, steps = (longest + 127) / 128;        // workgroups without splitting; steps of a workgroup
+    const uint64_t wanted = groups ? (1024 + groups - 1) / groups : 1, possible = (steps + 1) / 2;
+    uint64_t s = wanted < possible ? wanted : possible;
+    if (s > most_splits) s = most_splits;
+    p.splits = s ? (uint32_t)s : 1;
+    p.blocks = groups * p.splits;
+    return p;
+}
+
+// a call's passes and workspace, from its arguments
+struct AttendPlan {
+    AttendDev own;
+    AttendDev pre;
+    Pass own_pass, pre_pass;
+    uint32_t slots;                            // 1: the only pass writes the result itself
+    uint64_t part_o_bytes, ws_bytes;
+};
+
+zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const zc_kv_cache *cache, bool shared, AttendPlan *out)
+{
+    if (!x || !cache || (shared && !prefix)) return ZC_ERR_INVALID_ARG;
+    if (x->struct_size != sizeof(zc_attend_args)) return ZC_ERR_UNSUPPORTED;
+    AttendPlan p = {};
+    AttendDev &a = p.own;
+    zc_status st = check_cache(cache, &a.c);
+    if (st) return st;
+    if (!x->n_q_heads || x->n_q_heads % cache->n_heads || !x->max_q_len) return ZC_ERR_INVALID_ARG;
+    if (!x->d_q_start && (x->n_tokens != cache->n_seqs)) return ZC_ERR_INVALID_ARG;
+    if ((uint64_t)x->n_tokens * x->n_q_heads > 0x3FFFFFFFu || x->max_q_len >= kMaxTokens) return ZC_ERR_INVALID_ARG;
+    if (x->n_tokens && (!x->d_q || !x->d_out)) return ZC_ERR_INVALID_ARG;
+    if (!aligned16(x->d_q) || !aligned16(x->d_out) || !aligned4(x->d_q_start) || !aligned4(x->d_lse) || !aligned4(x->d_weights_in) ||
+        !aligned4(x->d_weights_out)) return ZC_ERR_INVALID_ARG;
+    if ((x->q_token_stride | x->q_head_stride | x->out_token_stride | x->out_head_stride) & 7) return ZC_ERR_INVALID_ARG;
+    if (!std::isfinite(x->scale) || x->reserved) return ZC_ERR_INVALID_ARG;
+    if (x->d_weights_out && (shared || (x->n_tokens && !x->d_lse))) return ZC_ERR_INVALID_ARG;
+    if (x->d_weights_in && !x->d_weights_out) return ZC_ERR_INVALID_ARG;
+    if (x->max_kv_len && x->max_kv_len < (uint32_t)a.c.limit) a.c.limit = (int32_t)x->max_kv_len;
+
+    a.q = (const uint16_t *)x->d_q;
+    a.out = (uint16_t *)x->d_out;
+    a.lse = x->d_lse;
+    a.q_start = x->d_q_start;
+    a.own_lengths = cache->d_lengths;
+    a.q_token_stride = x->q_token_stride;
+    a.q_head_stride = x->q_head_stride;
+    a.out_token_stride = x->out_token_stride;
+    a.out_head_stride = x->out_head_stride;
+    a.scale = x->scale;
+    a.own_limit = a.c.limit;
+    a.n_seqs = cache->n_seqs;
+    a.n_tokens = x->n_tokens;
+    a.q_heads = x->n_q_heads;
+    a.group = x->n_q_heads / cache->n_heads;
+    a.max_q_len = x->d_q_start ? (x->max_q_len < x->n_tokens ? x->max_q_len : x->n_tokens) : 1;
+    a.window = x->window < kMaxTokens ? x->window : 0;
+    a.sinks = x->sinks < kMaxTokens ? x->sinks : kMaxTokens;
+
+    auto reach = [&](int32_t limit) {          // tokens of a cache that the rows of one sequence may see
+        const uint64_t w = a.window ? (uint64_t)a.window + a.max_q_len + a.sinks + 64 : (uint64_t)limit;
+        return w < (uint64_t)limit ? w : (uint64_t)limit;
+    };
+    p.own_pass = plan_pass((uint64_t)a.max_q_len * a.group, (uint64_t)a.n_seqs * a.c.heads, reach(a.c.limit), shared ? 16 : kMaxSlots);
+    p.slots = p.own_pass.splits;
+    if (shared) {
+        AttendDev &b = p.pre;
+        PagesDev pc;
+        st = check_cache(prefix, &pc);
+        if (st) return st;
+        if (prefix->n_seqs != 1 || !same_shape(*prefix, *cache)) return ZC_ERR_INVALID_ARG;
+        if (x->max_prefix_len && x->max_prefix_len < (uint32_t)pc.limit) pc.limit = (int32_t)x->max_prefix_len;
+        if ((uint64_t)pc.limit + (uint64_t)a.c.limit >= kMaxTokens) return ZC_ERR_INVALID_ARG;
+        a.prefix_length = prefix->d_lengths;
+        a.prefix_limit = pc.limit;
+        b = a;
+        b.c = pc;
+        b.shared = 1;
+        p.pre_pass = plan_pass((uint64_t)a.n_tokens * a.group, a.c.heads, (uint64_t)pc.limit, 48);
+        b.splits = p.pre_pass.splits;
+        b.row_blocks = p.pre_pass.row_blocks;
+        b.first_slot = 0;
+        a.first_slot = b.splits;
+        p.slots += b.splits;
+    } else if (x->max_prefix_len) return ZC_ERR_INVALID_ARG;
+    a.splits = p.own_pass.splits;
+    a.row_blocks = p.own_pass.row_blocks;
+    a.direct = p.slots == 1;
+    if (p.own_pass.blocks > 0x7FFFFFFFu || p.pre_pass.blocks > 0x7FFFFFFFu) return ZC_ERR_INVALID_ARG;
+    if (p.slots > 1) {
+        const uint64_t rows = (uint64_t)a.n_tokens * a.q_heads * p.slots;
+        p.part_o_bytes = rows * cache->head_dim * 4;
+        p.ws_bytes = p.part_o_bytes + align256(rows * 8);
+    }
+    *out = p;
+    return ZC_OK;
+}
+
+zc_status attend(const zc_attend_args *x, const zc_kv_cache *prefix, const zc_kv_cache *cache, bool shared, void *d_ws, uint64_t ws_bytes, void *stream)
+{
+    AttendPlan p;
+    zc_status st = plan_attend(x, prefix, cache, shared, &p);
+    if (st) return st;
+    if (p.ws_bytes) {
+        if (!d_ws || !aligned16(d_ws)) return ZC_ERR_INVALID_ARG;
+        if (ws_bytes < p.ws_bytes) return ZC_ERR_BUFFER_TOO_SMALL;
+        p.own.part_o = p.pre.part_o = (float *)d_ws;
+        p.own.part_ml = p.pre.part_ml = (float *)((uint8_t *)d_ws + p.part_o_bytes);
+    }
+    if (x->n_tokens) {
+        if (shared) LAUNCH_TRY(launch_attend_few(p.pre, cache->format, cache->head_dim, p.pre_pass.tiles, stream));
+        LAUNCH_TRY(launch_attend_few(p.own, cache->format, cache->head_dim, p.own_pass.tiles, stream));
+        if (p.slots > 1) LAUNCH_TRY(launch_attend_join(p.own, cache->head_dim, p.slots, stream));
+    }
+    if (x->d_weights_out) LAUNCH_TRY(launch_attend_weights(p.own, WeightsDev{x->d_weights_in, x->d_weights_out}, cache->format, cache->head_dim, p.own.c.limit, stream));
+    return ZC_OK;
+}
+
+}  // namespace
+
+}  // namespace zc
+
+extern "C" uint64_t zc_attend_workspace_bytes(const zc_attend_args *args, const zc_kv_cache *prefix, const zc_kv_cache *cache)
+{
+    zc::AttendPlan p;
+    return zc::plan_attend(args, prefix, cache, prefix != nullptr, &p) ? 0 : p.ws_bytes;
+}
+
+extern "C" zc_status zc_attend(const zc_attend_args *args, const zc_kv_cache *cache, void *d_ws, uint64_t ws_bytes, void *stream)
+{
+    return zc::attend(args, nullptr, cache, false, d_ws, ws_bytes, stream);
+}
+
+extern "C" zc_status zc_attend_shared(const zc_attend_args *args, const zc_kv_cache *prefix, const zc_kv_cache *cache, void *d_ws, uint64_t ws_bytes, void *stream)
+{
+    return zc::attend(args, prefix, cache, true, d_ws, ws_bytes, stream);
+}
+
+extern "C" zc_status zc_evict(const zc_kv_cache *from, const float *d_weights, uint32_t keep, uint32_t sinks, uint32_t recent,
+                              const zc_kv_cache *to, float *d_weights_to, int32_t *d_kept, void *stream)
+{
+    zc::EvictDev e = {};
+    zc_status st = zc::check_cache(from, &e.from);
+    if (!st) st = zc::check_cache(to, &e.to);
+    if (st) return st;
+    if (!zc::same_shape(*from, *to) || from->n_seqs != to->n_seqs || from->d_lengths == to->d_lengths) return ZC_ERR_INVALID_ARG;
+    if (!d_weights || (keep && !d_kept) || !zc::aligned4(d_weights) || !zc::aligned4(d_weights_to) || !zc::aligned4(d_kept)) return ZC_ERR_INVALID_ARG;
+    if (d_weights_to == d_weights || (uint64_t)sinks + recent > keep || keep >= zc::kMaxTokens) return ZC_ERR_INVALID_ARG;
+    if (to->table_pages * (uint64_t)to->page_tokens < (keep < (uint32_t)e.from.capacity ? keep : (uint32_t)e.from.capacity)) return ZC_ERR_BUFFER_TOO_SMALL;
+    e.k_to = (uint8_t *)to->d_k_pages;
+    e.v_to = (uint8_t *)to->d_v_pages;
+    e.weights = d_weights;
+    e.weights_to = d_weights_to;
+    e.kept = d_kept;
+    e.lengths_to = to->d_lengths;
+    e.n_seqs = from->n_seqs;
+    e.keep = keep;
+    e.sinks = sinks;
+    e.recent = recent;
+    e.row_bytes = from->head_dim * (from->format == ZC_FMT_BF16 ? 2 : 1);
+    LAUNCH_TRY(zc::launch_evict(e, stream));
+    return ZC_OK;
+}

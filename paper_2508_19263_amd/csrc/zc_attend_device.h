@@ -1,0 +1,167 @@
+// Device-side helpers of the attention kernels over K/V pages: types of the matrix instructions' operands, conversion of
+// page elements, positions and visibility.  Internal to the library.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "zc_attend.h"
+
+namespace zc {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kNegInf = -__builtin_inff();
+
+template <int FMT> struct PageElem;
+template <> struct PageElem<ZC_FMT_BF16> { static constexpr int BYTES = 2; };
+template <> struct PageElem<ZC_FMT_FP8_E4M3> { static constexpr int BYTES = 1; };
+template <> struct PageElem<ZC_FMT_FP8_E5M2> { static constexpr int BYTES = 1; };
+
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint32_t bits(float x) { return __float_as_uint(x); }
+
+// the value of the lane 32 (16) further on, combined: every lane gets f(x of it, x of that lane)
+__device__ __forceinline__ float max_over_32(float x)
+{
+    const u32x2 r = __builtin_amdgcn_permlane32_swap(bits(x), bits(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_over_16(float x)
+{
+    const u32x2 r = __builtin_amdgcn_permlane16_swap(bits(x), bits(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_over_32(float x)
+{
+    const u32x2 r = __builtin_amdgcn_permlane32_swap(bits(x), bits(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float sum_over_16(float x)
+{
+    const u32x2 r = __builtin_amdgcn_permlane16_swap(bits(x), bits(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ int32_t min_over_wave(int32_t x)
+{
+    for (int d = 1; d < 64; d *= 2) x = min(x, __shfl_xor(x, d));
+    return uniform(x);
+}
+__device__ __forceinline__ int32_t max_over_wave(int32_t x)
+{
+    for (int d = 1; d < 64; d *= 2) x = max(x, __shfl_xor(x, d));
+    return uniform(x);
+}
+
+// FP8 elements are exact in BF16 and in half precision, so keys go to the type of the queries, and values to the type with
+// more mantissa: the weights they are multiplied with lie in [0, 1] and are rounded to that type too.
+// two bytes (the low or the high ones of a word)
+template <int FMT, bool HIGH> __device__ __forceinline__ uint32_t two_to_bf16(uint32_t w)
+{
+    bf16x2 r;
+    if constexpr (FMT == ZC_FMT_FP8_E4M3) r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HIGH);
+    else r = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, 1.0f, HIGH);
+    return __builtin_bit_cast(uint32_t, r);
+}
+template <int FMT, bool HIGH> __device__ __forceinline__ uint32_t two_to_half(uint32_t w)
+{
+    halfx2 r;
+    if constexpr (FMT == ZC_FMT_FP8_E4M3) r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH);
+    else r = __builtin_amdgcn_cvt_scalef32_pk_f16_bf8(w, 1.0f, HIGH);
+    return __builtin_bit_cast(uint32_t, r);
+}
+// eight FP8 elements to BF16
+template <int FMT> __device__ __forceinline__ u32x4_t eight_to_bf16(uint32_t lo, uint32_t hi)
+{
+    return u32x4_t{two_to_bf16<FMT, false>(lo), two_to_bf16<FMT, true>(lo), two_to_bf16<FMT, false>(hi), two_to_bf16<FMT, true>(hi)};
+}
+// two weights to the type the values of the format are multiplied in
+template <int FMT> __device__ __forceinline__ uint32_t pack_weights(float a, float b)
+{
+    if constexpr (FMT == ZC_FMT_BF16) return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+    else return __builtin_bit_cast(uint32_t, halfx2{(_Float16)a, (_Float16)b});
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b}); }
+
+__device__ __forceinline__ f32x4 mma16_keys(u32x4_t a, u32x4_t b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+template <int FMT> __device__ __forceinline__ f32x4 mma16_values(u32x4_t a, u32x4_t b, f32x4 c)
+{
+    if constexpr (FMT == ZC_FMT_BF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8, a), __builtin_bit_cast(halfx8, b), c, 0, 0, 0);
+}
+
+// ones over those of a word's elements that are infinities or NaN
+template <int FMT> __device__ __forceinline__ uint32_t nonfinite_mask(uint32_t w)
+{
+    if constexpr (FMT == ZC_FMT_BF16) {
+        const uint32_t t = ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;      // exponent of ones: carries into the sign's place
+        return (t >> 15) * 0xFFFFu;
+    } else {
+        // 0x7F is E4M3's only NaN (sign aside); E5M2 has an exponent of ones
+        const uint32_t t = (FMT == ZC_FMT_FP8_E4M3 ? (w & 0x7F7F7F7Fu) + 0x01010101u : (w & 0x7C7C7C7Cu) + 0x04040404u) & 0x80808080u;
+        return (t >> 7) * 0xFFu;
+    }
+}
+// one element as a float
+template <int FMT> __device__ __forceinline__ float element(const uint8_t *p)
+{
+    if constexpr (FMT == ZC_FMT_BF16) return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(p) << 16);
+    else return __uint_as_float(two_to_bf16<FMT, false>(*p) << 16);
+}
+
+// ---- sequences, rows, positions ----------------------------------------------------------------
+struct Span { int32_t first, count; };         // a sequence's query tokens
+
+__device__ __forceinline__ Span query_span(const AttendDev &a, uint32_t seq)
+{
+    if (!a.q_start) return Span{(int32_t)seq, 1};
+    const int32_t n = (int32_t)a.n_tokens;
+    const int32_t first = min(max(a.q_start[seq], 0), n), end = min(max(a.q_start[seq + 1], 0), n);
+    return Span{first, min(max(end - first, 0), (int32_t)a.max_q_len)};
+}
+__device__ __forceinline__ int32_t clamped_length(const int32_t *lengths, uint32_t seq, int32_t limit) { return min(max(lengths[seq], 0), limit); }
+__device__ __forceinline__ int32_t prefix_tokens(const AttendDev &a) { return a.prefix_length ? clamped_length(a.prefix_length, 0, a.prefix_limit) : 0; }
+
+// the sequence whose query tokens include `token`, or -1
+__device__ __forceinline__ int32_t sequence_of(const AttendDev &a, int32_t token)
+{
+    if (!a.q_start) return token;
+    int32_t lo = 0, hi = (int32_t)a.n_seqs;    // the last sequence that starts at or before the token
+    while (hi - lo > 1) {
+        const int32_t mid = (lo + hi) / 2;
+        if (a.q_start[mid] <= token) lo = mid; else hi = mid;
+    }
+    const Span s = query_span(a, (uint32_t)lo);
+    return token >= s.first && token < s.first + s.count ? lo : -1;
+}
+
+// What a query at position p sees of a cache whose token 0 is at position `offset`, as token numbers of that cache: those up
+// to `last`, of them those from `from` on and those before `sinks`.
+struct Sight { int32_t last, from, sinks; };
+
+__device__ __forceinline__ Sight sight(const AttendDev &a, int32_t position, int32_t offset, int32_t length)
+{
+    Sight s;
+    s.last = min(position - offset, length - 1);
+    s.from = a.window ? position - offset - (int32_t)a.window + 1 : 0;
+    s.sinks = (int32_t)a.sinks - offset;
+    return s;
+}
+__device__ __forceinline__ bool seen(const Sight &s, int32_t t) { return t <= s.last && (t >= s.from || t < s.sinks); }
+// the low n bits, n taken into 0 .. 4
+__device__ __forceinline__ uint32_t low_of_four(int32_t n) { return (1u << min(max(n, 0), 4)) - 1; }
+__device__ __forceinline__ uint32_t seen_of_four(const Sight &s, int32_t t) { return low_of_four(s.last - t + 1) & (~low_of_four(s.from - t) | low_of_four(s.sinks - t)); }
+// bit j: token t + j, or t + 16 + j - 4, is seen
+__device__ __forceinline__ uint32_t seen_of_eight(const Sight &s, int32_t t) { return seen_of_four(s, t) | seen_of_four(s, t + 16) << 4; }
+__device__ __forceinline__ uint32_t bit_as_mask(uint32_t x, int j) { return (uint32_t)__builtin_amdgcn_sbfe((int)x, j, 1); }
+
+}  // namespace zc

@@ -25,7 +25,8 @@ EXPORTS = ["zc_compress_bound", "zc_workspace_bytes", "zc_compress", "zc_compres
            "zc_decompress", "zc_decompress_chunks", "zc_decompress_batch", "zc_decompress_batch_plan",
            "zc_decompress_batch_run", "zc_stats", "zc_build_code", "zc_train_code", "zc_compress_with_code",
            "zc_compress_batch_with_code", "zc_compress_batch_with_code_async", "zc_compress_batch_async", "zc_code_stale",
-           "zc_validate_container", "zc_release_host_buffers", "zc_compress_noalloc", "zc_copy_reference", "zc_status_string"]
+           "zc_validate_container", "zc_release_host_buffers", "zc_compress_noalloc", "zc_copy_reference", "zc_status_string",
+           "zc_attend", "zc_attend_shared", "zc_attend_workspace_bytes", "zc_evict"]
 
 
 class Params(C.Structure):
@@ -68,6 +69,21 @@ class BatchPlan(C.Structure):
                 ("n_work", C.c_uint32), ("fast_kernel", C.c_uint32), ("fast_exp_kind", C.c_uint32), ("fast_sm_kind", C.c_uint32),
                 ("n_rings", C.c_uint32), ("xor_delta", C.c_uint32), ("scattered", C.c_uint32), ("tail_kernel", C.c_uint32),
                 ("fast_work_offset", C.c_uint64), ("work_offset", C.c_uint64)]
+
+
+class KvCache(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("format", C.c_uint32), ("n_seqs", C.c_uint32), ("n_heads", C.c_uint32),
+                ("head_dim", C.c_uint32), ("page_tokens", C.c_uint32), ("table_pages", C.c_uint32), ("n_pages", C.c_uint32),
+                ("d_k_pages", C.c_void_p), ("d_v_pages", C.c_void_p), ("d_table", C.c_void_p), ("d_lengths", C.c_void_p),
+                ("d_k_scales", C.c_void_p), ("d_v_scales", C.c_void_p)]
+
+
+class AttendArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_tokens", C.c_uint32), ("n_q_heads", C.c_uint32), ("max_q_len", C.c_uint32),
+                ("window", C.c_uint32), ("sinks", C.c_uint32), ("max_kv_len", C.c_uint32), ("max_prefix_len", C.c_uint32),
+                ("scale", C.c_float), ("reserved", C.c_uint32), ("d_q", C.c_void_p), ("d_out", C.c_void_p),
+                ("q_token_stride", C.c_uint64), ("q_head_stride", C.c_uint64), ("out_token_stride", C.c_uint64), ("out_head_stride", C.c_uint64),
+                ("d_q_start", C.c_void_p), ("d_lse", C.c_void_p), ("d_weights_in", C.c_void_p), ("d_weights_out", C.c_void_p)]
 
 
 class ZcError(RuntimeError):
@@ -131,6 +147,14 @@ def lib():
         L.zc_validate_container.argtypes = [vp, u64, u64, C.c_int, C.POINTER(Info)]
         L.zc_release_host_buffers.restype = C.c_int
         L.zc_release_host_buffers.argtypes = []
+        L.zc_attend_workspace_bytes.restype = u64
+        L.zc_attend_workspace_bytes.argtypes = [C.POINTER(AttendArgs), C.POINTER(KvCache), C.POINTER(KvCache)]
+        L.zc_attend.restype = C.c_int
+        L.zc_attend.argtypes = [C.POINTER(AttendArgs), C.POINTER(KvCache), vp, u64, vp]
+        L.zc_attend_shared.restype = C.c_int
+        L.zc_attend_shared.argtypes = [C.POINTER(AttendArgs), C.POINTER(KvCache), C.POINTER(KvCache), vp, u64, vp]
+        L.zc_evict.restype = C.c_int
+        L.zc_evict.argtypes = [C.POINTER(KvCache), vp, u32, u32, u32, C.POINTER(KvCache), vp, vp, vp]
         L.zc_build_code.restype = C.c_int
         L.zc_build_code.argtypes = [C.POINTER(u64), u32, u32, C.POINTER(C.c_uint8), C.POINTER(C.c_uint16)]
         _lib = L
@@ -436,3 +460,117 @@ class Batch:
         """Enqueue the decode kernels on the plan left in the workspace by plan_decompress()."""
         _check(lib().zc_decompress_batch_run(C.byref(self.plan), _ptr(self.ws_plan), _stream()), "zc_decompress_batch_run")
         return self.out
+
+
+class PagedCache:
+    """K and V of a batch of sequences in pages, as the attention and eviction calls take them.
+
+    k_pages, v_pages: [n_pages, page_tokens, head_dim], contiguous, as stored (any one-byte type for FP8, any two-byte type
+    for BF16); table: int32 [n_seqs, n_heads, table_pages] of page numbers (one that is no page's: absent); lengths: int32
+    [n_seqs], tokens in the cache; k_scales, v_scales: float32 [n_seqs, n_heads] or None.  The object holds the tensors
+    and the descriptor; the lengths and the table are read on the device when a call runs, so they may change between calls."""
+
+    def __init__(self, k_pages, v_pages, table, lengths, fmt, k_scales=None, v_scales=None):
+        for name, t, dtype, dims in (("table", table, torch.int32, 3), ("lengths", lengths, torch.int32, 1)):
+            if t.dtype != dtype or t.dim() != dims or not t.is_contiguous():
+                raise ValueError("PagedCache: %s has to be a contiguous %s tensor of %d dimensions" % (name, dtype, dims))
+        size = {FMT_BF16: 2, FMT_FP8_E4M3: 1, FMT_FP8_E5M2: 1}.get(fmt)
+        if size is None:
+            raise ZcError(ERR_UNSUPPORTED, "PagedCache")
+        for t in (k_pages, v_pages):
+            if t.dim() != 3 or t.element_size() != size or not t.is_contiguous() or t.shape != k_pages.shape:
+                raise ValueError("PagedCache: pages have to be contiguous [n_pages, page_tokens, head_dim] of %d bytes an element" % size)
+        if lengths.shape[0] != table.shape[0]:
+            raise ValueError("PagedCache: table and lengths are of different numbers of sequences")
+        for t in (k_scales, v_scales):
+            if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != tuple(table.shape[:2]) or not t.is_contiguous()):
+                raise ValueError("PagedCache: scales have to be contiguous float32 [n_seqs, n_heads]")
+        self.k_pages, self.v_pages, self.table, self.lengths = k_pages, v_pages, table, lengths
+        self.k_scales, self.v_scales, self.fmt = k_scales, v_scales, fmt
+        self.n_seqs, self.n_heads, self.table_pages = table.shape
+        self.n_pages, self.page_tokens, self.head_dim = k_pages.shape
+        self.capacity = self.table_pages * self.page_tokens
+        c = self.c = KvCache()
+        c.struct_size, c.format = C.sizeof(KvCache), fmt
+        c.n_seqs, c.n_heads, c.head_dim, c.page_tokens = self.n_seqs, self.n_heads, self.head_dim, self.page_tokens
+        c.table_pages, c.n_pages = self.table_pages, self.n_pages
+        c.d_k_pages, c.d_v_pages, c.d_table, c.d_lengths = k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), lengths.data_ptr()
+        c.d_k_scales = k_scales.data_ptr() if k_scales is not None else None
+        c.d_v_scales = v_scales.data_ptr() if v_scales is not None else None
+        self.ref = C.byref(c)
+
+
+def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, max_kv_len, max_prefix_len, out, lse, weights, weights_out, ws):
+    if q.dim() != 3 or q.shape[2] != cache.head_dim or q.stride(2) != 1 or q.element_size() != 2:
+        raise ValueError("%s: q has to be [n_tokens, n_q_heads, head_dim] in BF16 with contiguous rows" % what)
+    n, heads, dim = q.shape
+    if out is None:
+        out = torch.empty((n, heads, dim), dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.stride(2) != 1 or out.element_size() != 2:
+        raise ValueError("%s: out has to have q's shape and type, with contiguous rows" % what)
+    if lse is None:
+        lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
+    elif lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous():
+        raise ValueError("%s: lse has to be contiguous float32 [n_tokens, n_q_heads]" % what)
+    if q_start is not None and (q_start.dtype != torch.int32 or q_start.numel() != cache.n_seqs + 1 or not q_start.is_contiguous()):
+        raise ValueError("%s: q_start has to be contiguous int32 of n_seqs + 1 entries" % what)
+    a = AttendArgs()
+    a.struct_size = C.sizeof(AttendArgs)
+    a.n_tokens, a.n_q_heads, a.max_q_len, a.window, a.sinks = n, heads, max_q_len, window, sinks
+    a.max_kv_len, a.max_prefix_len = max_kv_len, max_prefix_len
+    a.scale = dim ** -0.5 if scale is None else scale
+    a.d_q, a.d_out, a.d_lse = q.data_ptr(), out.data_ptr(), lse.data_ptr()
+    a.q_token_stride, a.q_head_stride = q.stride(0), q.stride(1)
+    a.out_token_stride, a.out_head_stride = out.stride(0), out.stride(1)
+    if q_start is not None:
+        a.d_q_start = q_start.data_ptr()
+    for name, t in (("d_weights_in", weights), ("d_weights_out", weights_out)):
+        if t is not None:
+            if t.dtype != torch.float32 or tuple(t.shape) != (cache.n_seqs, cache.n_heads, cache.capacity) or not t.is_contiguous():
+                raise ValueError("%s: weights have to be contiguous float32 [n_seqs, n_heads, table_pages * page_tokens]" % what)
+            setattr(a, name, t.data_ptr())
+    L, ref, pre = lib(), C.byref(a), None if prefix is None else prefix.ref
+    need = L.zc_attend_workspace_bytes(ref, pre, cache.ref)
+    if ws is None and need:
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    at, size = (ws.data_ptr(), ws.numel()) if ws is not None else (None, 0)
+    if prefix is None:
+        st = L.zc_attend(ref, cache.ref, at, size, _stream())
+    else:
+        st = L.zc_attend_shared(ref, pre, cache.ref, at, size, _stream())
+    if st != OK:
+        raise ZcError(st, what)
+    return out, lse
+
+
+def attend(q, cache, q_start=None, max_q_len=1, window=0, sinks=0, scale=None, max_kv_len=0, out=None, lse=None, weights=None, weights_out=None, ws=None):
+    """Attention of BF16 queries [n_tokens, n_q_heads, head_dim] over a PagedCache; returns (out, lse).
+
+    q_start: int32 [n_seqs + 1], where each sequence's query tokens begin (None: one token per sequence); at most max_q_len
+    each.  window: how many of the latest tokens a query sees, itself included (0: all); sinks: how many of the first ones
+    it always sees.  scale: of the logits (None: head_dim ** -0.5).  max_kv_len: no length is above it (0: the table's room).
+    weights_out: also leaves weights (None: zeros) plus the attention weight given to each token there."""
+    return _attend("zc_attend", q, None, cache, q_start, max_q_len, window, sinks, scale, max_kv_len, 0, out, lse, weights, weights_out, ws)
+
+
+def attend_shared(q, prefix, cache, q_start=None, max_q_len=1, window=0, sinks=0, scale=None, max_kv_len=0, max_prefix_len=0, out=None, lse=None, ws=None):
+    """attend() for sequences whose first tokens are those of `prefix` (a PagedCache of one sequence), read once for all of
+    them; `cache` holds what follows in each."""
+    return _attend("zc_attend_shared", q, prefix, cache, q_start, max_q_len, window, sinks, scale, max_kv_len, max_prefix_len, out, lse, None, None, ws)
+
+
+def evict(cache, weights, keep, into, into_weights=None, sinks=0, recent=0, kept=None):
+    """Leaves `keep` tokens per sequence and head: the first `sinks`, the last `recent`, and of the others those with the largest
+    weights (float32 [n_seqs, n_heads, table_pages * page_tokens]); they go to the pages of `into` (another PagedCache),
+    whose lengths are set.  Returns their numbers, int32 [n_seqs, n_heads, keep], ascending, -1 behind the last."""
+    if kept is None:
+        kept = torch.empty((cache.n_seqs, cache.n_heads, keep), dtype=torch.int32, device=weights.device)
+    elif kept.dtype != torch.int32 or tuple(kept.shape) != (cache.n_seqs, cache.n_heads, keep) or not kept.is_contiguous():
+        raise ValueError("zc_evict: kept has to be contiguous int32 [n_seqs, n_heads, keep]")
+    for t, c in ((weights, cache), (into_weights, into)):
+        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (c.n_seqs, c.n_heads, c.capacity) or not t.is_contiguous()):
+            raise ValueError("zc_evict: weights have to be contiguous float32 [n_seqs, n_heads, table_pages * page_tokens]")
+    st = lib().zc_evict(cache.ref, weights.data_ptr(), keep, sinks, recent, into.ref, into_weights.data_ptr() if into_weights is not None else None,
+                        kept.data_ptr(), _stream())
+    _check(st, "zc_evict")
+    return kept

@@ -1,0 +1,164 @@
+"""Paged caches for the tests of attention and eviction, and these operators in 64 bits, written from their definitions."""
+import math
+
+import torch
+
+from paper_2508_19263_amd import workloads as wl
+from paper_2508_19263_amd import zc
+
+STORE = {zc.FMT_BF16: (torch.int16, torch.bfloat16), zc.FMT_FP8_E4M3: (torch.uint8, torch.float8_e4m3fn), zc.FMT_FP8_E5M2: (torch.uint8, torch.float8_e5m2)}
+JUNK = {zc.FMT_BF16: 0x7FC1, zc.FMT_FP8_E4M3: 0x7F, zc.FMT_FP8_E5M2: 0x7E}    # a NaN
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def stored(x, fmt):
+    """float32 -> stored elements."""
+    return {zc.FMT_BF16: wl.bf16_bits, zc.FMT_FP8_E4M3: wl.e4m3_bits, zc.FMT_FP8_E5M2: wl.e5m2_bits}[fmt](x)
+
+
+def values(bits, fmt):
+    return bits.view(STORE[fmt][1]).to(torch.float64)
+
+
+class Cache:
+    """A random cache: dense stored elements k, v [seqs, heads, tokens, dim] and the same in pages in random order (`paged`); what
+    no token of a sequence lies in holds NaN."""
+
+    def __init__(self, lens, heads, dim, fmt, page=16, seed=1, spare_pages=3, room=None, edit=None, scales=None):
+        g = gen(seed)
+        seqs, self.fmt, self.lens, self.page = len(lens), fmt, list(lens), page
+        pages = max(1, -(-max(list(lens) + [room or 0]) // page))
+        shape = (seqs, heads, pages * page, dim)
+        k, v = torch.randn(shape, generator=g, device="cuda"), torch.randn(shape, generator=g, device="cuda")
+        k[..., :: max(1, dim // 4)] *= 6.0
+        self.k, self.v = stored(k, fmt), stored(v, fmt)
+        if edit:
+            edit(self)
+        if scales is None:
+            scales = fmt != zc.FMT_BF16
+        self.ks = torch.rand((seqs, heads), generator=g, device="cuda") + 0.5 if scales else None
+        self.vs = torch.rand((seqs, heads), generator=g, device="cuda") + 0.5 if scales else None
+        self.lengths = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        used = seqs * heads * pages
+        order = torch.randperm(used + spare_pages, generator=g, device="cuda")[:used]
+        self.table = order.view(seqs, heads, pages).to(torch.int32)
+        inside = (torch.arange(pages * page, device="cuda") < self.lengths.view(-1, 1)).view(seqs, 1, -1, 1)
+        pools = []
+        for x in (self.k, self.v):
+            pool = torch.full((used + spare_pages, page, dim), JUNK[fmt], dtype=x.dtype, device="cuda")
+            pool[order] = torch.where(inside, x, torch.full_like(x, JUNK[fmt])).view(used, page, dim)
+            pools.append(pool)
+        self.paged = zc.PagedCache(pools[0], pools[1], self.table, self.lengths, fmt, self.ks, self.vs)
+
+    def rows(self, name, seq, head):
+        """Stored values times their scale, [tokens, dim] in 64 bits."""
+        x = values(getattr(self, name)[seq, head, :self.lens[seq]].contiguous(), self.fmt)
+        scale = getattr(self, name + "s")
+        return x if scale is None else x * scale[seq, head].to(torch.float64)
+
+    def present(self, seq, head):
+        """Which tokens' pages are there."""
+        ok = (self.table[seq, head] >= 0) & (self.table[seq, head] < self.paged.n_pages)
+        return ok.repeat_interleave(self.page)[:self.lens[seq]]
+
+
+def starts(q_lens):
+    return torch.tensor([sum(q_lens[:i]) for i in range(len(q_lens) + 1)], dtype=torch.int32, device="cuda")
+
+
+def attention(q, q_lens, cache, prefix=None, window=0, sinks=0, scale=None, weights=None):
+    """(out, lse, weights or None, tolerance of out, of lse, of weights).  What a query does not see takes no part: hidden elements
+    are selected away, not multiplied with zero.
+
+    Tolerances.  A logit is a sum of dim products in 32 bits: it is off by at most dim * 2^-24 * scale * sum |q_i k_i|, its scaling and
+    the exponential by 2^-22 (1 + |s|); `d`, the largest of these of a row, is the relative error of its weights and the absolute one of
+    lse.  Sums over tokens in 32 bits add (tokens) * 2^-24 relatively (each partial sum has fewer terms).  The weights of the values are
+    rounded to 8 bits of mantissa for BF16 pages and 11 for FP8 (half precision, with an absolute 2^-25 below its normal range), the result
+    to 8: out is off by at most 2^-8 |out| and by sum p |v| times (2^-9 or 2^-12) and 2 d, and the values of up to 64 parts are joined in 32
+    bits.  A factor of 2 on all of it for the terms of second order."""
+    n, heads, dim = q.shape
+    group = heads // cache.k.shape[1]
+    scale = dim ** -0.5 if scale is None else scale
+    out = torch.zeros(q.shape, dtype=torch.float64, device="cuda")
+    lse = torch.full((n, heads), -math.inf, dtype=torch.float64, device="cuda")
+    tol_out, tol_lse = torch.zeros_like(out), torch.zeros_like(lse)
+    w = None if weights is None else weights.to(torch.float64).clone()
+    tol_w = None if weights is None else weights.to(torch.float64).abs() * 2.0 ** -22
+    P, first = (prefix.lens[0] if prefix else 0), 0
+    bits = 2.0 ** -9 if cache.fmt == zc.FMT_BF16 else 2.0 ** -12
+    for s, count in enumerate(q_lens):
+        length = cache.lens[s]
+        pos = torch.arange(count, device="cuda").view(-1, 1) + P + length - count
+        key = torch.arange(P + length, device="cuda")
+        seen = key <= pos
+        if window:
+            seen = seen & ((key > pos - window) | (key < sinks))
+        for h in range(cache.k.shape[1]):
+            k, v, there = cache.rows("k", s, h), cache.rows("v", s, h), cache.present(s, h)
+            if prefix:
+                k, v = torch.cat([prefix.rows("k", 0, h), k]), torch.cat([prefix.rows("v", 0, h), v])
+                there = torch.cat([prefix.present(0, h), there])
+            on = seen & there
+            for j in range(h * group, (h + 1) * group):
+                if count == 0 or P + length == 0:
+                    continue
+                x = q[first:first + count, j].to(torch.float64)
+                logits = (x @ torch.where(k.isfinite(), k, torch.zeros_like(k)).t()) * scale
+                wild = (~k.isfinite()).any(dim=1)
+                if bool(wild.any()):
+                    logits[:, wild] = torch.stack([(x * k[t]).sum(dim=1) * scale for t in torch.nonzero(wild).flatten()], dim=1)
+                logits = torch.where(on, logits, torch.full_like(logits, -math.inf))
+                top = logits.amax(dim=1, keepdim=True)
+                top = torch.where(top == -math.inf, torch.zeros_like(top), top)
+                e = torch.where(on, torch.exp(logits - top), torch.zeros_like(logits))
+                total = e.sum(dim=1, keepdim=True)
+                empty = (total == 0)
+                p = e / torch.where(empty, torch.ones_like(total), total)
+                fine = v.isfinite()
+                o = p @ torch.where(fine, v, torch.zeros_like(v))
+                for t in torch.nonzero((~fine).any(dim=1)).flatten().tolist():
+                    o = o + torch.where(on[:, t:t + 1] & ~fine[t], p[:, t:t + 1] * v[t], torch.zeros_like(o))
+                out[first:first + count, j] = torch.where(empty, torch.zeros_like(o), o)
+                lse[first:first + count, j] = (top + torch.log(total)).squeeze(1)
+                size = (x.abs() @ torch.where(k.isfinite(), k, torch.zeros_like(k)).abs().t()) * abs(scale)
+                d = (dim * 2.0 ** -24 * size.amax(dim=1) + 2.0 ** -22 * (1 + size.amax(dim=1))).view(-1, 1)
+                sums = (P + length) * 2.0 ** -24
+                a = p @ torch.where(fine, v, torch.zeros_like(v)).abs()
+                tol_out[first:first + count, j] = 2 * (2.0 ** -8 * o.abs() + (bits + 2 * d + sums) * a + 2.0 ** -24)
+                tol_lse[first:first + count, j] = 2 * (d.squeeze(1) + sums + 2.0 ** -22 * (1 + lse[first:first + count, j].nan_to_num(0, 0, 0).abs()))
+                if w is not None:
+                    w[s, h, :length] += p.sum(dim=0)
+                    tol_w[s, h, :length] += 2 * (p * (2 * d + sums + 2.0 ** -21)).sum(dim=0) + w[s, h, :length].abs() * (n * group * 2.0 ** -24)
+        first += count
+    return out, lse, w, tol_out, tol_lse, tol_w
+
+
+def agree(got, want, tol, what):
+    """Equal where `want` is not finite, within `tol` elsewhere."""
+    got = got.to(torch.float64)
+    fine = want.isfinite()
+    assert torch.equal(fine, got.isfinite()), "%s: finite in other places" % what
+    assert torch.equal(want.isnan(), got.isnan()) and torch.equal(want[~fine & ~want.isnan()], got[~fine & ~want.isnan()]), "%s: other infinities" % what
+    off = (got - want).abs()[fine] - tol[fine]
+    assert off.numel() == 0 or float(off.max()) <= 0, "%s: off by %g more than the tolerance" % (what, float(off.max()))
+
+
+def eviction(cache, weights, keep, sinks, recent):
+    """The tokens that stay, as lists per sequence and head."""
+    kept = []
+    for s, n in enumerate(cache.lens):
+        kept.append([])
+        for h in range(cache.k.shape[1]):
+            if n <= keep:
+                kept[-1].append(list(range(n)))
+                continue
+            w = weights[s, h, :n].tolist()
+            middle = range(sinks, n - recent)
+            rank = sorted(middle, key=lambda i: (math.isnan(w[i]), -w[i] if not math.isnan(w[i]) else 0.0, i))
+            kept[-1].append(sorted(list(range(sinks)) + rank[:keep - sinks - recent] + list(range(n - recent, n))))
+    return kept

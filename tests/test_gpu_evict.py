@@ -1,0 +1,131 @@
+"""Eviction from a paged cache: the tokens that stay, and their keys, values and weights, are exactly those of the definition."""
+import pytest
+import torch
+
+from paper_2508_19263_amd import zc
+from tests.paged import Cache, eviction, gen
+
+pytestmark = pytest.mark.gpu
+
+BF16, E4M3, E5M2 = zc.FMT_BF16, zc.FMT_FP8_E4M3, zc.FMT_FP8_E5M2
+
+
+def weights_of(kind, cache, seed=3):
+    shape = (len(cache.lens), cache.k.shape[1], cache.paged.capacity)
+    w = torch.rand(shape, generator=gen(seed), device="cuda")
+    if kind == "ties":
+        w = (w * 4).floor()
+    elif kind == "same":
+        w = torch.full(shape, 0.25, device="cuda")
+    elif kind == "near":                                         # all of one exponent, the last bits decide
+        w = 1.0 + (w * 300).floor() * 2.0 ** -23
+    elif kind == "wild":
+        pick = torch.rand(shape, generator=gen(seed + 1), device="cuda")
+        w = torch.where(pick < 0.1, torch.full_like(w, float("nan")), torch.where(pick < 0.2, torch.full_like(w, float("inf")),
+            torch.where(pick < 0.3, torch.full_like(w, float("-inf")), torch.where(pick < 0.4, -w, torch.where(pick < 0.5, w * 0, torch.where(pick < 0.6, w * -0.0, w * 1e-40))))))
+    return w
+
+
+def check(cache, w, keep, sinks, recent, into_page=16, spare=0):
+    into = Cache([0] * len(cache.lens), cache.k.shape[1], cache.k.shape[3], cache.fmt, page=into_page, room=min(keep, cache.paged.capacity) + spare, seed=77)
+    w_to = torch.full((len(cache.lens), cache.k.shape[1], into.paged.capacity), -3.0, device="cuda")
+    k_before, v_before = into.paged.k_pages.clone(), into.paged.v_pages.clone()
+    kept = zc.evict(cache.paged, w, keep, into.paged, w_to, sinks=sinks, recent=recent)
+    torch.cuda.synchronize()
+    want = eviction(cache, w, keep, sinks, recent)
+    assert into.lengths.tolist() == [min(n, keep) for n in cache.lens]
+    touched = torch.zeros(k_before.shape[:2], dtype=torch.bool, device="cuda")
+    for s, n in enumerate(cache.lens):
+        for h in range(cache.k.shape[1]):
+            ids = want[s][h]
+            assert kept[s, h].tolist() == ids + [-1] * (keep - len(ids)), (s, h)
+            at = torch.tensor(ids, dtype=torch.int64, device="cuda")
+            slot = torch.arange(len(ids), device="cuda")
+            page, row = into.table[s, h].to(torch.int64)[slot // into_page], slot % into_page
+            for x, pool in ((cache.k, into.paged.k_pages), (cache.v, into.paged.v_pages)):
+                assert torch.equal(pool[page, row], x[s, h][at])
+            touched[page, row] = True
+            assert torch.equal(w_to[s, h, :len(ids)].view(torch.int32), w[s, h][at].view(torch.int32)) and bool((w_to[s, h, len(ids):] == -3.0).all())
+    for now, before in ((into.paged.k_pages, k_before), (into.paged.v_pages, v_before)):
+        assert torch.equal(now[~touched], before[~touched])      # nothing else is written
+
+
+@pytest.mark.parametrize("kind", ["random", "ties", "same", "near", "wild"])
+@pytest.mark.parametrize("keep,sinks,recent", [(100, 0, 0), (100, 4, 50), (64, 0, 64), (64, 60, 4), (1, 0, 0), (1, 1, 0), (1023, 4, 100), (700, 0, 1)])
+def test_kept_tokens(kind, keep, sinks, recent):
+    cache = Cache([1025, 0, 1, 63, 64, 65, 1000, 700, 1024], 2, 64, E4M3)
+    check(cache, weights_of(kind, cache), keep, sinks, recent)
+
+
+@pytest.mark.parametrize("fmt,dim", [(BF16, 128), (E4M3, 128), (E5M2, 64), (BF16, 64)])
+@pytest.mark.parametrize("page,into_page", [(16, 64), (128, 16)])
+def test_formats_and_pages(fmt, dim, page, into_page):
+    cache = Cache([300, 1, 222], 3, dim, fmt, page=page)
+    check(cache, weights_of("random", cache), 100, 2, 30, into_page, spare=40)
+
+
+@pytest.mark.parametrize("kind", ["random", "ties", "same"])
+def test_long_caches(kind):
+    cache = Cache([70001, 20000], 1, 64, E4M3)
+    check(cache, weights_of(kind, cache), 30000, 4, 1000)
+
+
+def test_nothing_kept_and_no_weights_moved():
+    cache = Cache([50, 20], 2, 64, E4M3)
+    into = Cache([5, 5], 2, 64, E4M3, seed=8)
+    kept = zc.evict(cache.paged, weights_of("random", cache), 0, into.paged)
+    assert kept.numel() == 0 and into.lengths.tolist() == [0, 0]
+    kept = zc.evict(cache.paged, weights_of("random", cache), 4, into.paged, recent=4)
+    assert into.lengths.tolist() == [4, 4] and kept[0, 0].tolist() == [46, 47, 48, 49]
+
+
+def test_absent_pages():
+    """A row from an absent page is zero; one whose own page is absent is not written."""
+    cache = Cache([64], 1, 64, E4M3)
+    cache.table[0, 0, 1] = -1
+    into = Cache([0], 1, 64, E4M3, room=64, seed=8)
+    into.table[0, 0, 2] = into.paged.n_pages
+    before = into.paged.k_pages.clone()
+    gone = int(Cache([0], 1, 64, E4M3, room=64, seed=8).table[0, 0, 2])
+    zc.evict(cache.paged, weights_of("random", cache), 64, into.paged)
+    table = into.table[0, 0].tolist()
+    assert not bool(into.paged.k_pages[table[1]].any()) and torch.equal(into.paged.k_pages[table[0]], cache.k[0, 0, :16])
+    assert torch.equal(into.paged.k_pages[gone], before[gone])
+
+
+def test_weights_that_attention_leaves_decide():
+    """The step as a server takes it: attention keeps account, the lightest half goes, attention goes on over the rest."""
+    cache = Cache([400, 333], 2, 128, E4M3)
+    q = torch.randn((2, 8, 128), generator=gen(4), device="cuda").to(torch.bfloat16)
+    w = torch.zeros((2, 2, cache.paged.capacity), device="cuda")
+    full, _ = zc.attend(q, cache.paged, weights_out=w)
+    check(cache, w, 200, 4, 32)
+    into = Cache([0, 0], 2, 128, E4M3, room=200, seed=6)
+    zc.evict(cache.paged, w, 200, into.paged, sinks=4, recent=32)
+    rest = zc.PagedCache(into.paged.k_pages, into.paged.v_pages, into.table, into.lengths, E4M3, cache.ks, cache.vs)
+    w_rest = torch.zeros((2, 2, into.paged.capacity), device="cuda")
+    zc.attend(q, rest, weights_out=w_rest)
+    # what is left carries all of the weight again: a softmax over 200 tokens for each of the four heads of a group
+    assert torch.allclose(w_rest.sum(dim=2), torch.full((2, 2), 4.0, device="cuda"), rtol=200 * 2.0 ** -20)
+
+
+def test_in_a_graph():
+    cache = Cache([500, 100], 2, 64, E4M3)
+    into = Cache([0, 0], 2, 64, E4M3, room=200, seed=6)
+    w = weights_of("random", cache)
+    want = zc.evict(cache.paged, w, 200, into.paged, sinks=1, recent=9)
+    k = into.paged.k_pages.clone()
+    graph = torch.cuda.CUDAGraph()
+    kept = torch.empty_like(want)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        zc.evict(cache.paged, w, 200, into.paged, sinks=1, recent=9, kept=kept)
+    for _ in range(3):
+        kept.zero_()
+        into.paged.k_pages[into.table.view(-1).to(torch.int64)] = 0
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(kept, want)
+        page = into.table[0, 0].to(torch.int64)[torch.arange(200, device="cuda") // 16]
+        assert torch.equal(into.paged.k_pages[page, torch.arange(200, device="cuda") % 16], k[page, torch.arange(200, device="cuda") % 16])
