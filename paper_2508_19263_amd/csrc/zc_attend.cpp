@@ -47,8 +47,9 @@ zc_status check_cache(const zc_kv_cache *c, PagesDev *out)
 
 bool same_shape(const zc_kv_cache &a, const zc_kv_cache &b) { return a.format == b.format && a.n_heads == b.n_heads && a.head_dim == b.head_dim; }
 
-// one pass of k_attend_few over a cache
+// one pass over a cache: k_attend_many with tiles x 128 rows to a workgroup, or k_attend_few with tiles x 16
 struct Pass {
+    bool many;
     uint32_t tiles, row_blocks, splits;
     uint64_t blocks;
 };
@@ -57,15 +58,23 @@ struct Pass {
 Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_splits)
 {
     Pass p;
-    p.tiles = rows <= 16 ? 1 : 2;
-    p.row_blocks = (uint32_t)((rows + p.tiles * 16 - 1) / (p.tiles * 16));
-    const uint64_t groups = units * p.row_blocks, steps = (longest + 127) / 128;        // workgroups without splitting; steps of a workgroup
-    const uint64_t wanted = groups ? (1024 + groups - 1) / groups : 1, possible = (steps + 1) / 2;
+    p.many = rows > 32;
+    p.tiles = p.many || rows <= 16 ? 1 : 2;
+    const uint64_t per_block = p.tiles * (p.many ? 128 : 16);
+    p.row_blocks = (uint32_t)((rows + per_block - 1) / per_block);
+    const uint64_t groups = units * p.row_blocks, steps = (longest + 127) / 128;        // workgroups without splitting; pairs of tiles, or steps of four wavefronts
+    const uint64_t enough = p.many ? 512 : 1024;
+    const uint64_t wanted = groups ? (enough + groups - 1) / groups : 1, possible = (steps + 1) / 2;
     uint64_t s = wanted < possible ? wanted : possible;
     if (s > most_splits) s = most_splits;
     p.splits = s ? (uint32_t)s : 1;
     p.blocks = groups * p.splits;
     return p;
+}
+
+int launch_pass(const AttendDev &a, const Pass &p, const zc_kv_cache &c, void *stream)
+{
+    return p.many ? launch_attend_many(a, c.format, c.head_dim, p.tiles, stream) : launch_attend_few(a, c.format, c.head_dim, p.tiles, stream);
 }
 
 // a call's passes and workspace, from its arguments
@@ -167,8 +176,8 @@ zc_status attend(const zc_attend_args *x, const zc_kv_cache *prefix, const zc_kv
         p.own.part_ml = p.pre.part_ml = (float *)((uint8_t *)d_ws + p.part_o_bytes);
     }
     if (x->n_tokens) {
-        if (shared) LAUNCH_TRY(launch_attend_few(p.pre, cache->format, cache->head_dim, p.pre_pass.tiles, stream));
-        LAUNCH_TRY(launch_attend_few(p.own, cache->format, cache->head_dim, p.own_pass.tiles, stream));
+        if (shared) LAUNCH_TRY(launch_pass(p.pre, p.pre_pass, *cache, stream));
+        LAUNCH_TRY(launch_pass(p.own, p.own_pass, *cache, stream));
         if (p.slots > 1) LAUNCH_TRY(launch_attend_join(p.own, cache->head_dim, p.slots, stream));
     }
     if (x->d_weights_out) LAUNCH_TRY(launch_attend_weights(p.own, WeightsDev{x->d_weights_in, x->d_weights_out}, cache->format, cache->head_dim, p.own.c.limit, stream));

@@ -54,6 +54,7 @@ struct EvictDev {
 
 // rows a workgroup of the kernels takes (`tiles` = 16-row tiles per wavefront there)
 int launch_attend_few(const AttendDev &a, uint32_t format, uint32_t head_dim, uint32_t tiles, void *stream);
+int launch_attend_many(const AttendDev &a, uint32_t format, uint32_t head_dim, uint32_t tiles, void *stream);
 int launch_attend_join(const AttendDev &a, uint32_t head_dim, uint32_t slots, void *stream);
 int launch_attend_weights(const AttendDev &a, const WeightsDev &w, uint32_t format, uint32_t head_dim, int32_t longest, void *stream);
 int launch_evict(const EvictDev &e, void *stream);

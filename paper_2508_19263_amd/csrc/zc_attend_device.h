@@ -17,6 +17,9 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNegInf = -__builtin_inff();
+// A row's running maximum is replaced, and what has been added up scaled, only where a logit is more than 2^kSlack above it: weights
+// then reach 2^kSlack, which the 32-bit sums and the operands' types (half precision to 2^16) hold with the same relative error.
+constexpr float kSlack = 8.0f;
 
 template <int FMT> struct PageElem;
 template <> struct PageElem<ZC_FMT_BF16> { static constexpr int BYTES = 2; };
@@ -163,5 +166,46 @@ __device__ __forceinline__ uint32_t seen_of_four(const Sight &s, int32_t t) { re
 // bit j: token t + j, or t + 16 + j - 4, is seen
 __device__ __forceinline__ uint32_t seen_of_eight(const Sight &s, int32_t t) { return seen_of_four(s, t) | seen_of_four(s, t + 16) << 4; }
 __device__ __forceinline__ uint32_t bit_as_mask(uint32_t x, int j) { return (uint32_t)__builtin_amdgcn_sbfe((int)x, j, 1); }
+
+// A row of a (sequence, K/V head), or of a head of the shared prefix: query token r / group, query head r % group of the K/V head's.
+// `span`: the query tokens the rows belong to.  token -1: there is no such row.
+struct Row { int32_t token; uint32_t q_head; Sight sight; };
+
+__device__ __forceinline__ Row row_of(const AttendDev &a, const Span &span, uint32_t head, uint32_t r, int32_t prefix, int32_t offset, int32_t length)
+{
+    Row x;
+    const uint32_t i = r / a.group;
+    x.q_head = head * a.group + r % a.group;
+    x.token = (int32_t)i < span.count ? span.first + (int32_t)i : -1;
+    int32_t position = 0;
+    if (x.token >= 0) {
+        if (a.shared) {
+            const int32_t s = sequence_of(a, x.token);
+            if (s < 0) x.token = -1;
+            else {
+                const Span own = query_span(a, (uint32_t)s);
+                position = prefix + clamped_length(a.own_lengths, (uint32_t)s, a.own_limit) - own.count + (x.token - own.first);
+            }
+        } else position = prefix + length - span.count + (int32_t)i;
+    }
+    x.sight = sight(a, position, offset, length);
+    return x;
+}
+__device__ __forceinline__ Span rows_span(const AttendDev &a, uint32_t seq) { return a.shared ? Span{0, (int32_t)a.n_tokens} : query_span(a, seq); }
+
+// The blocks of `size` tokens that some of several rows see: those with sinks, then those from the first row's window on.
+struct Blocks {
+    int32_t sinks, skipped, count;             // blocks b < sinks are block b of the cache, later ones block b + skipped
+    __device__ __forceinline__ int32_t at(int32_t b) const { return b < sinks ? b : b + skipped; }
+};
+__device__ __forceinline__ Blocks seen_blocks(int32_t size, int32_t last_max, int32_t from_min, int32_t sinks)
+{
+    Blocks x;
+    const int32_t end = last_max < 0 ? 0 : last_max / size + 1, lo = max(from_min, 0) / size;
+    x.sinks = lo > 0 ? min(min((max(sinks, 0) + size - 1) / size, lo), end) : 0;
+    x.skipped = max(lo, x.sinks) - x.sinks;
+    x.count = x.sinks + max(0, end - max(lo, x.sinks));
+    return x;
+}
 
 }  // namespace zc

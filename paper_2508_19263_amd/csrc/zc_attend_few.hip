@@ -65,34 +65,17 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
     const int32_t offset = a.shared ? 0 : prefix_tokens(a);
     const int32_t length = clamped_length(a.c.lengths, seq, a.c.limit);
     const int32_t prefix = prefix_tokens(a);
-    int32_t token[QT];
-    uint32_t q_head[QT];
-    Sight sg[QT];
+    const Span span = rows_span(a, seq);
+    Row rows[QT];
     int32_t last_min = INT32_MAX, last_max = -1, from_min = INT32_MAX, from_max = INT32_MIN;
-    Span span = {0, (int32_t)a.n_tokens};
-    if (!a.shared) span = query_span(a, seq);
 #pragma unroll
     for (int t = 0; t < QT; t++) {
-        const uint32_t r = (row_block * QT + t) * 16 + n16, i = r / a.group;
-        q_head[t] = head * a.group + r % a.group;
-        token[t] = (int32_t)i < span.count ? span.first + (int32_t)i : -1;
-        int32_t position = 0;
-        if (token[t] >= 0) {
-            if (a.shared) {
-                const int32_t s = sequence_of(a, token[t]);
-                if (s < 0) token[t] = -1;
-                else {
-                    const Span own = query_span(a, (uint32_t)s);
-                    position = prefix + clamped_length(a.own_lengths, (uint32_t)s, a.own_limit) - own.count + (token[t] - own.first);
-                }
-            } else position = prefix + length - span.count + (int32_t)i;
-        }
-        sg[t] = sight(a, position, offset, length);
-        if (token[t] >= 0) {
-            last_min = min(last_min, sg[t].last);
-            last_max = max(last_max, sg[t].last);
-            from_min = min(from_min, sg[t].from);
-            from_max = max(from_max, sg[t].from);
+        rows[t] = row_of(a, span, head, (row_block * QT + t) * 16 + n16, prefix, offset, length);
+        if (rows[t].token >= 0) {
+            last_min = min(last_min, rows[t].sight.last);
+            last_max = max(last_max, rows[t].sight.last);
+            from_min = min(from_min, rows[t].sight.from);
+            from_max = max(from_max, rows[t].sight.from);
         }
     }
     last_min = min_over_wave(last_min);
@@ -101,31 +84,28 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
     from_max = max_over_wave(from_max);
     const int32_t sinks = (int32_t)a.sinks - offset;
 
-    // ---- the blocks of 32 tokens that some row sees: those with sinks, then those from the first row's window on
-    const int32_t end_block = last_max < 0 ? 0 : last_max / 32 + 1, lo_block = max(from_min, 0) / 32;
-    const int32_t sink_blocks = lo_block > 0 ? min(min((max(sinks, 0) + 31) / 32, lo_block), end_block) : 0;
-    const int32_t n_blocks = sink_blocks + max(0, end_block - max(lo_block, sink_blocks));
-    const int32_t skipped = max(lo_block, sink_blocks) - sink_blocks;
+    const Blocks blocks = seen_blocks(32, last_max, from_min, sinks);
     // this workgroup's part, in steps that all four wavefronts take part in
-    const int32_t per_split = ((n_blocks + (int32_t)a.splits - 1) / (int32_t)a.splits + (int32_t)kWaves - 1) / (int32_t)kWaves * (int32_t)kWaves;
-    const int32_t begin = min((int32_t)split * per_split, n_blocks), end = min(begin + per_split, n_blocks);
+    const int32_t per_split = ((blocks.count + (int32_t)a.splits - 1) / (int32_t)a.splits + (int32_t)kWaves - 1) / (int32_t)kWaves * (int32_t)kWaves;
+    const int32_t begin = min((int32_t)split * per_split, blocks.count), end = min(begin + per_split, blocks.count);
 
     const float k_scale = a.c.k_scales ? a.c.k_scales[seq * a.c.heads + head] : 1.0f;
     const float v_scale = a.c.v_scales ? a.c.v_scales[seq * a.c.heads + head] : 1.0f;
     const float signed_c = a.scale * k_scale * kLog2e;
-    const float c = fabsf(signed_c);                     // logits in base 2; a negative factor goes to the queries' signs
+    // logits in base 2; a negative factor goes to the queries' signs, and 0 is made one that takes any product to 0 but minus infinity
+    const float c = fmaxf(fabsf(signed_c), 1e-30f);
     const uint32_t flip = signed_c < 0 ? 0x80008000u : 0u;
 
     u32x4_t q[QT][KS];
 #pragma unroll
     for (int t = 0; t < QT; t++) {
-        const uint16_t *row = a.q + (uint64_t)max(token[t], 0) * a.q_token_stride + (uint64_t)q_head[t] * a.q_head_stride;
+        const uint16_t *row = a.q + (uint64_t)max(rows[t].token, 0) * a.q_token_stride + (uint64_t)rows[t].q_head * a.q_head_stride;
 #pragma unroll
         for (int s = 0; s < KS; s++) {
             // the dimensions that the lane's piece of a key has
             const int dim = FMT == ZC_FMT_BF16 ? s * 32 + (int)g * 8 : (s / 2) * 64 + (int)g * 16 + (s & 1) * 8;
             u32x4_t x = {0, 0, 0, 0};
-            if (token[t] >= 0) x = *reinterpret_cast<const u32x4_t *>(row + dim);
+            if (rows[t].token >= 0) x = *reinterpret_cast<const u32x4_t *>(row + dim);
             q[t][s] = x ^ flip;
         }
     }
@@ -141,16 +121,15 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
     }
 
     const int32_t *table = a.c.table + (uint64_t)(seq * a.c.heads + head) * a.c.table_pages;
-    const uint64_t page_bytes = (uint64_t)D * ES << a.c.page_shift;
+    const uint32_t page_log = a.c.page_shift + (D == 128 ? 7 : 6) + (ES - 1);   // of a page's bytes
     const uint32_t page_mask = (1u << a.c.page_shift) - 1;
     const uint32_t k_lane = n16 * (D * ES) + g * 16, v_lane = g * 4 * (D * ES) + n16 * (DL * ES);
 
     // page ids of the wavefront's next 32 steps: lane 2i + h has that of half h of step i (-1: absent)
     int32_t ids = -1, ids_from = begin + (int32_t)wave;
-    auto block_of = [&](int32_t b) { return b < sink_blocks ? b : b + skipped; };
     auto fetch_ids = [&](int32_t b) {
         const int32_t mine = b + (int32_t)(lane >> 1) * (int32_t)kWaves;
-        const uint32_t page = ((uint32_t)block_of(mine) * 32 + (lane & 1) * 16) >> a.c.page_shift;
+        const uint32_t page = ((uint32_t)blocks.at(mine) * 32 + (lane & 1) * 16) >> a.c.page_shift;
         ids = -1;
         if (mine < end && page < a.c.table_pages) ids = table[page];
         if ((uint32_t)ids >= a.c.n_pages) ids = -1;
@@ -162,13 +141,13 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
         if (b - ids_from >= 32 * (int32_t)kWaves) fetch_ids(b);
         const int32_t i = (b - ids_from) / (int32_t)kWaves * 2;
         Place x;
-        x.t0 = block_of(b) * 32;
+        x.t0 = blocks.at(b) * 32;
         x.there = 0;
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             const int32_t page = __builtin_amdgcn_readlane(ids, i + h);
             x.there |= page >= 0 ? 1u << h : 0u;
-            x.at[h] = (uint64_t)(uint32_t)max(page, 0) * page_bytes + (((uint32_t)x.t0 + h * 16) & page_mask) * (D * ES);
+            x.at[h] = ((uint64_t)(uint32_t)max(page, 0) << page_log) + (((uint32_t)x.t0 + h * 16) & page_mask) * (D * ES);
         }
         return x;
     };
@@ -238,9 +217,8 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
         u32x4_t p[QT];
 #pragma unroll
         for (int t = 0; t < QT; t++) {
-            uint32_t mask = 0;
             if (!whole) {
-                mask = seen_of_eight(sg[t], t0 + (int32_t)g * 4) & ((there & 1 ? 0x0Fu : 0u) | (there & 2 ? 0xF0u : 0u));
+                const uint32_t mask = seen_of_eight(rows[t].sight, t0 + (int32_t)g * 4) & ((there & 1 ? 0x0Fu : 0u) | (there & 2 ? 0xF0u : 0u));
 #pragma unroll
                 for (int j = 0; j < 8; j++) {
                     const uint32_t keep = bit_as_mask(mask, j);
@@ -249,7 +227,7 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
             }
             float top = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])), fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
             top = max_over_16(max_over_32(top));
-            if (__any(top > m[t])) {
+            if (__any((top - m[t]) * c > kSlack)) {
                 const float now = fmaxf(m[t], top);
                 const float f = m[t] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f((m[t] - now) * c);   // (nothing to scale yet)
                 m[t] = now;
@@ -262,10 +240,6 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
 #pragma unroll
             for (int j = 0; j < 8; j++) {
                 e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][j / 4][j & 3], c, -mc));
-            }
-            if (!whole) {
-#pragma unroll
-                for (int j = 0; j < 8; j++) e[j] = __uint_as_float(bits(e[j]) & bit_as_mask(mask, j));
             }
             l[t] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
 #pragma unroll
@@ -280,15 +254,17 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
 #pragma unroll
                     for (uint32_t k = 1; k < 8; k++) weight = j == k ? e[k] : weight;
                     weight = __shfl(weight, (int)(n16 + gg * 16));
-                    const bool mine = seen(sg[t], tok);
-                    const uint8_t *row = a.c.v + (uint64_t)max(table[(uint32_t)tok >> a.c.page_shift], 0) * page_bytes + (uint64_t)((uint32_t)tok & page_mask) * (D * ES) + g * 4 * DL * ES;
+                    const bool mine = seen(rows[t].sight, tok);
+                    const uint8_t *row = a.c.v + ((uint64_t)(uint32_t)max(table[(uint32_t)tok >> a.c.page_shift], 0) << page_log) + (uint64_t)((uint32_t)tok & page_mask) * (D * ES) + g * 4 * DL * ES;
 #pragma unroll
-                    for (int cc = 0; cc < 4; cc++)
+                    for (int cc = 0; cc < 4; cc++) {
 #pragma unroll
                         for (int i = 0; i < DL; i++) {
                             const float x = element<FMT>(row + (cc * DL + i) * ES);
-                            if (mine && !(fabsf(x) < __builtin_inff())) o[t][i][cc] += weight * x;
+                            o[t][i][cc] += mine && !(fabsf(x) < __builtin_inff()) ? weight * x : 0.0f;
                         }
+                        __builtin_amdgcn_sched_barrier(0);       // a few at a time: this hardly ever runs and is to cost no registers
+                    }
                 }
             }
         }
