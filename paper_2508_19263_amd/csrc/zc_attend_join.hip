@@ -51,86 +51,138 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendDev a, uint32_t slots
     if (a.lse && lane == 0) a.lse[row] = top == kNegInf ? kNegInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-// weights_out[t] = weights_in[t] + sum over the rows that see t of exp(s - lse).  One wavefront per 32 tokens of a (sequence,
-// K/V head), which keeps their keys in registers and goes over the rows 16 at a time: the sum has one order, whatever the launch.
+// weights_out[t] = weights_in[t] + sum over the rows that see t of exp(s - lse).  A wavefront keeps the keys of 64 tokens in
+// registers and goes over the rows 32 at a time, straight from memory: S^T = K Q^T leaves a lane one row's products with 32 of
+// the tokens, whose exponentials it adds up token by token; the 32 lanes of a token are added at the end.  With many rows (a prompt)
+// the eight wavefronts of a workgroup share the tokens and take every eighth 32 rows, and their sums are joined in LDS; else every
+// wavefront has tokens of its own.  The sums have one order, whatever the launch.  Bound by the matrix instructions and the
+// exponentials with many rows, by the read of the keys with few.
 template <int FMT, int D>
-__global__ __launch_bounds__(256) void k_attend_weights(AttendDev a, WeightsDev wt, uint32_t blocks_per_head)
+__global__ __launch_bounds__(512) void k_attend_weights(AttendDev a, WeightsDev wt, uint32_t by_rows)
 {
-    constexpr int ES = PageElem<FMT>::BYTES, NK = D * ES / 64, KS = D / 32;
-    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
-    const uint32_t unit = blockIdx.x / blocks_per_head, head = unit % a.c.heads, seq = unit / a.c.heads;
-    const int32_t t0 = (int32_t)((blockIdx.x % blocks_per_head * 4 + wave) * 32);
+    constexpr int ES = PageElem<FMT>::BYTES, KS = D / 16;
+    __shared__ float sums[8][64];
+    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n32 = lane & 31, g = lane >> 5;
+    const uint32_t units = a.n_seqs * a.c.heads, unit = blockIdx.x % units, head = unit % a.c.heads, seq = unit / a.c.heads;
+    const uint32_t tile = by_rows ? blockIdx.x / units : blockIdx.x / units * (blockDim.x / 64) + wave;
+    const int32_t t0 = (int32_t)(tile * 64);
     const int32_t length = clamped_length(a.c.lengths, seq, a.c.limit);
-    if (t0 >= length) return;
+    if (t0 >= length) return;                                  // by rows: the whole workgroup
     const Span span = query_span(a, seq);
-    const float signed_c = a.scale * (a.c.k_scales ? a.c.k_scales[unit] : 1.0f) * kLog2e;
+    const float c = a.scale * (a.c.k_scales ? a.c.k_scales[unit] : 1.0f) * kLog2e;
 
     const int32_t *table = a.c.table + (uint64_t)unit * a.c.table_pages;
-    const uint64_t page_bytes = (uint64_t)D * ES << a.c.page_shift;
-    const uint32_t page_mask = (1u << a.c.page_shift) - 1;
+    const uint32_t page_log = a.c.page_shift + (D == 128 ? 7 : 6) + (ES - 1), page_mask = (1u << a.c.page_shift) - 1;
     u32x4_t key[2][KS];
-    bool there[2];
+    uint32_t there = 0;
+#pragma unroll
+    for (int h = 0; h < 4; h++) {
+        const uint32_t page = ((uint32_t)t0 + h * 16) >> a.c.page_shift;
+        there |= page < a.c.table_pages && (uint32_t)table[page] < a.c.n_pages ? 1u << h : 0u;
+    }
 #pragma unroll
     for (int h = 0; h < 2; h++) {
-        const uint32_t page = ((uint32_t)t0 + h * 16) >> a.c.page_shift;
+        const uint32_t t = (uint32_t)t0 + h * 32 + n32, page = t >> a.c.page_shift;
         const int32_t id = page < a.c.table_pages ? table[page] : -1;
-        there[h] = (uint32_t)id < a.c.n_pages;
-        const uint8_t *p = a.c.k + (there[h] ? (uint64_t)id : 0) * page_bytes + (uint64_t)(((uint32_t)t0 + h * 16) & page_mask) * (D * ES) + n16 * (D * ES) + g * 16;
+        const uint8_t *row = a.c.k + ((uint64_t)((uint32_t)id < a.c.n_pages ? id : 0) << page_log) + (t & page_mask) * (D * ES);
+        // the order of the dimensions in the sums is free: FP8 keys come in pieces of 16
+        if constexpr (FMT == ZC_FMT_BF16) {
 #pragma unroll
-        for (int u = 0; u < NK; u++) {
-            const u32x4_t x = *reinterpret_cast<const u32x4_t *>(p + u * 64);
-            if constexpr (FMT == ZC_FMT_BF16) key[h][u] = x;
-            else { key[h][2 * u] = eight_to_bf16<FMT>(x[0], x[1]); key[h][2 * u + 1] = eight_to_bf16<FMT>(x[2], x[3]); }
+            for (int u = 0; u < KS; u++) key[h][u] = *reinterpret_cast<const u32x4_t *>(row + u * 32 + g * 16);
+        } else {
+#pragma unroll
+            for (int u = 0; u < KS; u += 2) {
+                const u32x4_t x = *reinterpret_cast<const u32x4_t *>(row + u * 16 + g * 16);
+                key[h][u] = eight_to_bf16<FMT>(x[0], x[1]);
+                key[h][u + 1] = eight_to_bf16<FMT>(x[2], x[3]);
+            }
         }
     }
     // rows that may see one of these tokens: query tokens from position t0 on, up to the window's end unless they are sinks
-    const int32_t before = length - span.count;
-    const int32_t first = max(0, t0 - before);
+    const int32_t before = length - span.count, first = max(0, t0 - before);
     int32_t end = span.count;
-    if (a.window && t0 >= (int32_t)a.sinks) end = min(end, t0 + 31 + (int32_t)a.window - before);
-    float acc[2][4] = {};
-    for (uint32_t r0 = (uint32_t)first * a.group; (int32_t)r0 < end * (int32_t)a.group; r0 += 16) {
-        const uint32_t r = r0 + n16, i = r / a.group;
-        const bool valid = (int32_t)i < end;
-        const int32_t tok = span.first + (valid ? (int32_t)i : first);
-        const uint32_t h = head * a.group + r % a.group;
-        const uint16_t *row = a.q + (uint64_t)tok * a.q_token_stride + (uint64_t)h * a.q_head_stride;
-        f32x4 s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    if (a.window && t0 >= (int32_t)a.sinks) end = min(end, t0 + 63 + (int32_t)a.window - before);
+    const uint32_t step = by_rows ? 32 * 8 : 32, first_row = (uint32_t)first * a.group + (by_rows ? wave * 32 : 0), n_rows = (uint32_t)max(end, 0) * a.group;
+    float acc[32];
+#pragma unroll
+    for (int i = 0; i < 32; i++) acc[i] = 0.0f;
+
+    // this lane's row of the next step: query token `i` of the sequence, head `h` of the group
+    uint32_t i = (first_row + n32) / a.group, h = (first_row + n32) % a.group;
+    const uint32_t step_i = step / a.group, step_h = step % a.group;
+    u32x4_t q[KS];
+    float lse;
+    int32_t position;
+    auto fetch = [&](bool valid) {
+        const uint32_t tok = (uint32_t)span.first + (valid ? i : (uint32_t)first), q_head = head * a.group + h;
+        const uint16_t *row = a.q + (uint64_t)tok * a.q_token_stride + (uint64_t)q_head * a.q_head_stride;
+#pragma unroll
+        for (int u = 0; u < KS; u++) q[u] = *reinterpret_cast<const u32x4_t *>(row + (FMT == ZC_FMT_BF16 ? u * 16 + g * 8 : (u & ~1) * 16 + g * 16 + (u & 1) * 8));
+        lse = valid ? a.lse[(uint64_t)tok * a.q_heads + q_head] * kLog2e : kNegInf;
+        position = before + (int32_t)i;
+    };
+    if (first_row < n_rows) fetch(first_row + n32 < n_rows);
+    for (uint32_t r0 = first_row; r0 < n_rows; r0 += step) {
+        f32x16 s[2];
+#pragma unroll
+        for (int k = 0; k < 16; k++) s[0][k] = s[1][k] = 0.0f;
 #pragma unroll
         for (int u = 0; u < KS; u++) {
-            const int dim = FMT == ZC_FMT_BF16 ? u * 32 + (int)g * 8 : (u / 2) * 64 + (int)g * 16 + (u & 1) * 8;
-            const u32x4_t x = *reinterpret_cast<const u32x4_t *>(row + dim);
-#pragma unroll
-            for (int hh = 0; hh < 2; hh++) s[hh] = mma16_keys(key[hh][u], x, s[hh]);
+            s[0] = mma32_keys(key[0][u], q[u], s[0]);
+            s[1] = mma32_keys(key[1][u], q[u], s[1]);
         }
-        const float lse = valid ? a.lse[(uint64_t)tok * a.q_heads + h] * kLog2e : kNegInf;
-        const Sight sg = sight(a, before + (int32_t)i, 0, length);
+        const Sight sg = sight(a, position, 0, length);
+        const float minus = lse == kNegInf ? kNegInf : -lse;   // a row that sees nothing gives nothing
+        i += step_i;
+        h += step_h;
+        if (h >= a.group) { h -= a.group; i++; }
+        if (r0 + step < n_rows) fetch(r0 + step + n32 < n_rows);
+        // all of these rows see all of these tokens
+        const bool whole = there == 15 && !__any(!(t0 + 63 <= sg.last && (t0 >= sg.from || t0 + 64 <= sg.sinks)) || minus == kNegInf);
+        if (whole) {
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const bool on = valid && lse != kNegInf && there[j / 4] && seen(sg, t0 + (j / 4) * 16 + (int32_t)g * 4 + (j & 3));
-            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j / 4][j & 3], signed_c, -lse));
-            acc[j / 4][j & 3] += on ? e : 0.0f;
+            for (int k = 0; k < 32; k++) acc[k] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[k / 16][k & 15], c, minus));
+        } else {
+            uint32_t mask = 0;
+#pragma unroll
+            for (int n = 0; n < 8; n++) mask |= (seen_of_four(sg, t0 + n * 8 + (int32_t)g * 4) & (there >> (n / 2) & 1 ? 15u : 0u)) << (n * 4);
+            mask = minus == kNegInf ? 0u : mask;
+#pragma unroll
+            for (int k = 0; k < 32; k++) acc[k] += __uint_as_float(bits(__builtin_amdgcn_exp2f(__builtin_fmaf(s[k / 16][k & 15], c, minus))) & bit_as_mask(mask, k));
         }
     }
+    // the sum over 32 lanes of each of 32 numbers: halves are exchanged until lane n has number n
 #pragma unroll
-    for (int j = 0; j < 8; j++)
+    for (int width = 16; width > 0; width /= 2)
 #pragma unroll
-        for (int d = 1; d < 16; d *= 2) acc[j / 4][j & 3] += __shfl_xor(acc[j / 4][j & 3], d);
-    // lane n16 = j of each group writes token j of the group's eight
-    float mine = 0.0f;
-#pragma unroll
-    for (int j = 0; j < 8; j++) mine = (int)n16 == j ? acc[j / 4][j & 3] : mine;
-    const int32_t t = t0 + (int32_t)(n16 / 4 * 16 + g * 4 + (n16 & 3));
-    if (n16 < 8 && t < length) {
+        for (int k = 0; k < width; k++) {
+            const bool upper = (n32 & width) != 0;
+            const float give = upper ? acc[k] : acc[k + width], keep = upper ? acc[k + width] : acc[k];
+            acc[k] = keep + __shfl_xor(give, width);
+        }
+    // number n is token (n / 16) * 32 + (n / 4 % 4) * 8 + g * 4 + n % 4 of the tile
+    const uint32_t token = n32 / 16 * 32 + (n32 / 4 & 3) * 8 + g * 4 + (n32 & 3);
+    float sum = acc[0];
+    if (by_rows) {
+        sums[wave][token] = sum;
+        __syncthreads();
+        if (wave) return;
+        sum = 0.0f;
+        for (int w = 0; w < 8; w++) sum += sums[w][token];
+    }
+    const int32_t t = t0 + (int32_t)token;
+    if (t < length) {
         const uint64_t at = (uint64_t)unit * (uint64_t)a.c.capacity + (uint64_t)t;
-        wt.out[at] = (wt.in ? wt.in[at] : 0.0f) + mine;
+        wt.out[at] = (wt.in ? wt.in[at] : 0.0f) + sum;
     }
 }
 
-template <int FMT> void launch_weights(const AttendDev &a, const WeightsDev &w, uint32_t head_dim, uint32_t blocks, uint32_t per_head, hipStream_t s)
+template <int FMT> void launch_weights(const AttendDev &a, const WeightsDev &w, uint32_t head_dim, uint32_t tiles, hipStream_t s)
 {
-    if (head_dim == 64) hipLaunchKernelGGL((k_attend_weights<FMT, 64>), dim3(blocks), dim3(256), 0, s, a, w, per_head);
-    else hipLaunchKernelGGL((k_attend_weights<FMT, 128>), dim3(blocks), dim3(256), 0, s, a, w, per_head);
+    const uint32_t by_rows = (uint64_t)a.max_q_len * a.group > 64, per_group = by_rows ? 1 : 4, threads = by_rows ? 512 : 256;
+    const uint32_t per_head = (tiles + per_group - 1) / per_group, blocks = a.n_seqs * a.c.heads * per_head;
+    if (head_dim == 64) hipLaunchKernelGGL((k_attend_weights<FMT, 64>), dim3(blocks), dim3(threads), 0, s, a, w, by_rows);
+    else hipLaunchKernelGGL((k_attend_weights<FMT, 128>), dim3(blocks), dim3(threads), 0, s, a, w, by_rows);
 }
 
 }  // namespace
@@ -145,12 +197,11 @@ int launch_attend_join(const AttendDev &a, uint32_t head_dim, uint32_t slots, vo
 
 int launch_attend_weights(const AttendDev &a, const WeightsDev &w, uint32_t format, uint32_t head_dim, int32_t longest, void *stream)
 {
-    const uint32_t per_head = (uint32_t)(longest + 127) / 128, blocks = a.n_seqs * a.c.heads * per_head;
-    if (!blocks) return 0;
+    const uint32_t tiles = (uint32_t)(longest + 63) / 64;
     const hipStream_t s = (hipStream_t)stream;
-    if (format == ZC_FMT_BF16) launch_weights<ZC_FMT_BF16>(a, w, head_dim, blocks, per_head, s);
-    else if (format == ZC_FMT_FP8_E4M3) launch_weights<ZC_FMT_FP8_E4M3>(a, w, head_dim, blocks, per_head, s);
-    else launch_weights<ZC_FMT_FP8_E5M2>(a, w, head_dim, blocks, per_head, s);
+    if (format == ZC_FMT_BF16) launch_weights<ZC_FMT_BF16>(a, w, head_dim, tiles, s);
+    else if (format == ZC_FMT_FP8_E4M3) launch_weights<ZC_FMT_FP8_E4M3>(a, w, head_dim, tiles, s);
+    else launch_weights<ZC_FMT_FP8_E5M2>(a, w, head_dim, tiles, s);
     return (int)hipGetLastError();
 }
 

@@ -19,91 +19,126 @@ __device__ __forceinline__ uint32_t weight_key(float w)
 }
 
 // One workgroup per (sequence, head).  The keep - sinks - recent largest weights of the middle are those above a threshold and
-// the first of those equal to it; three passes over the weights (11, 11 and 10 bits of the key at a time, a histogram in LDS each)
-// find it.  Then every wavefront counts a stretch of its own, and once it knows what lies before it writes its tokens in order.
-// Bound by latency: the weights, 4 bytes a token, are read from the L2 after the first pass.
+// the first of those equal to it.  A wavefront has a stretch of tokens of its own, up to N of them per lane held as keys in
+// registers (N = 0: read anew each time).  Four passes over the keys, 8 bits at a time from the top, find the threshold: a histogram in
+// LDS has 32 copies, one per lane of half a wavefront, side by side in the banks, so that the few exponents that weights have cost
+// no waits (with one copy of 2,048 bins the passes over 65,536 tokens took 100 us).  Then every wavefront counts its stretch, and
+// once it knows what lies before it writes its tokens in order.  Bound by latency.
+template <int N>
 __global__ __launch_bounds__(kThreads) void k_evict_select(EvictDev e)
 {
-    __shared__ uint32_t hist[2048];
+    __shared__ __align__(16) uint32_t hist[256 * 32];
+    __shared__ __align__(16) uint32_t total[256];
     __shared__ uint32_t wave_sum[kGroupWaves], wave_more[kGroupWaves];
-    __shared__ uint32_t found_bin, found_above;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const uint32_t unit = blockIdx.x, head = unit % e.from.heads, seq = unit / e.from.heads;
-    const int32_t length = min(max(e.from.lengths[seq], 0), e.from.capacity);
+    const uint32_t length = (uint32_t)min(max(e.from.lengths[seq], 0), e.from.capacity);
     int32_t *kept = e.kept + (uint64_t)unit * e.keep;
-    const uint32_t count = min((uint32_t)length, e.keep);
+    const uint32_t count = min(length, e.keep);
     if (head == 0 && tid == 0) e.lengths_to[seq] = (int32_t)count;
     for (uint32_t i = count + tid; i < e.keep; i += kThreads) kept[i] = -1;
-    if ((uint32_t)length <= e.keep) {
+    if (length <= e.keep) {
         for (uint32_t i = tid; i < count; i += kThreads) kept[i] = (int32_t)i;
         return;
     }
     const float *w = e.weights + (uint64_t)unit * (uint64_t)e.from.capacity;
-    const uint32_t begin = e.sinks, end = (uint32_t)length - e.recent, need = e.keep - e.sinks - e.recent;   // the middle, of which `need` stay
+    const uint32_t begin = e.sinks, end = length - e.recent, need = e.keep - e.sinks - e.recent;   // the middle, of which `need` stay
+    const uint32_t rounds = (length + kThreads - 1) / kThreads, from = wave * rounds * 64;         // the stretch: `rounds` times 64 tokens
+
+    uint32_t keys[N ? N : 1];
+    if constexpr (N > 0) {
+#pragma unroll
+        for (int j = 0; j < N; j++) {
+            const uint32_t i = from + (uint32_t)j * 64 + lane;
+            float x = 0.0f;
+            if ((uint32_t)j < rounds && i >= begin && i < end) x = w[i];
+            keys[j] = weight_key(x);
+        }
+    }
+    // f(token, its key, whether it is of the middle) for the stretch, 64 tokens at a time
+    auto over_stretch = [&](auto f) {
+        if constexpr (N > 0) {
+#pragma unroll
+            for (int j = 0; j < N; j++)
+                if ((uint32_t)j < rounds) {
+                    const uint32_t i = from + (uint32_t)j * 64 + lane;
+                    f(i, keys[j], i >= begin && i < end);
+                }
+        } else {
+            for (uint32_t j = 0; j < rounds; j++) {
+                const uint32_t i = from + j * 64 + lane;
+                const bool middle = i >= begin && i < end;
+                f(i, middle ? weight_key(w[i]) : 0u, middle);
+            }
+        }
+    };
 
     // ---- the threshold: `above` keys of the middle are larger, and need - above of those equal to it stay
-    uint32_t prefix = 0, mask = 0, above = 0;
-    for (int pass = 0; pass < 3; pass++) {
-        const uint32_t shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
-        for (uint32_t i = tid; i < 2048; i += kThreads) hist[i] = 0;
-        __syncthreads();
-        for (uint32_t i = begin + tid; i < end; i += kThreads) {
-            const uint32_t key = weight_key(w[i]);
-            if ((key & mask) == prefix) atomicAdd(&hist[key >> shift & (bins - 1)], 1u);
+    uint32_t threshold = 0, above = 0;
+    if (need) {
+        uint32_t mask = 0;
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            for (uint32_t i = tid; i < 256 * 32 / 4; i += kThreads) reinterpret_cast<uint4 *>(hist)[i] = make_uint4(0, 0, 0, 0);
+            __syncthreads();
+            over_stretch([&](uint32_t, uint32_t key, bool middle) {
+                if (middle && (key & mask) == threshold) atomicAdd(&hist[(key >> shift & 255) * 32 + (lane & 31)], 1u);
+            });
+            __syncthreads();
+            {
+                const uint4 x = reinterpret_cast<const uint4 *>(hist)[tid * 2], y = reinterpret_cast<const uint4 *>(hist)[tid * 2 + 1];
+                uint32_t sum = x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;        // a quarter of bin tid / 4
+                sum += __shfl_xor(sum, 1);
+                sum += __shfl_xor(sum, 2);
+                if ((tid & 3) == 0) total[tid / 4] = sum;
+            }
+            __syncthreads();
+            // every wavefront for itself: lane n has bins 255 - 4 n and the three below
+            const uint4 bins = reinterpret_cast<const uint4 *>(total)[63 - lane];
+            const uint32_t four = bins.x + bins.y + bins.z + bins.w;
+            uint32_t upto = four;
+            for (uint32_t d = 1; d < 64; d *= 2) {
+                const uint32_t x = __shfl_up(upto, d);
+                if (lane >= d) upto += x;
+            }
+            const uint64_t reached = __ballot(above + upto >= need);                 // not 0: the middle has more than `need` keys
+            const int who = __ffsll((unsigned long long)reached) - 1;
+            uint32_t before = above + upto - four, bin = 255 - 4 * lane;
+            if (before + bins.w < need) {
+                before += bins.w; bin--;
+                if (before + bins.z < need) {
+                    before += bins.z; bin--;
+                    if (before + bins.y < need) { before += bins.y; bin--; }
+                }
+            }
+            above = __shfl(before, who);
+            threshold |= (uint32_t)__shfl(bin, who) << shift;
+            mask |= 255u << shift;
         }
-        __syncthreads();
-        // bins from the top: thread t has the two bins 2047 - 2t and 2046 - 2t
-        const uint32_t hi = hist[2047 - 2 * tid], lo = hist[2046 - 2 * tid];
-        uint32_t sum = hi + lo;
-        for (uint32_t d = 1; d < 64; d *= 2) {
-            const uint32_t x = __shfl_up(sum, d);
-            if (lane >= d) sum += x;
-        }
-        if (lane == 63) wave_sum[wave] = sum;
-        if (tid == 0) found_bin = 0xFFFFFFFFu;
-        __syncthreads();
-        uint32_t before = above;
-        for (uint32_t i = 0; i < wave; i++) before += wave_sum[i];
-        before += sum - hi - lo;                           // keys above this thread's bins
-        if (before < need && before + hi >= need) { found_bin = 2047 - 2 * tid; found_above = before; }
-        else if (before + hi < need && before + hi + lo >= need) { found_bin = 2046 - 2 * tid; found_above = before + hi; }
-        __syncthreads();
-        if (found_bin == 0xFFFFFFFFu) break;               // need == 0: every key is below the threshold
-        prefix |= found_bin << shift;
-        mask |= (bins - 1) << shift;
-        above = found_above;
-        __syncthreads();
     }
-    const bool none = need == 0;
-    const uint32_t threshold = prefix, ties = need - above;
+    const uint32_t ties = need - above;
+    auto sure = [&](uint32_t i, uint32_t key, bool middle) { return i < length && (!middle || (need && key > threshold)); };
+    auto equal = [&](uint32_t key, bool middle) { return middle && need && key == threshold; };
 
-    // ---- stretches of whole wavefronts: what each holds above the threshold and at it
-    const uint32_t per = ((uint32_t)length + kThreads - 1) / kThreads * 64, from = min(wave * per, (uint32_t)length), to = min(from + per, (uint32_t)length);
-    uint32_t sure = 0, equal = 0;
-    for (uint32_t i = from + lane; i < to; i += 64) {
-        const bool middle = i >= begin && i < end;
-        const uint32_t key = middle && !none ? weight_key(w[i]) : 0;
-        sure += !middle || (!none && key > threshold);
-        equal += middle && !none && key == threshold;
-    }
-    for (uint32_t d = 1; d < 64; d *= 2) { sure += __shfl_xor(sure, d); equal += __shfl_xor(equal, d); }
-    if (lane == 0) { wave_sum[wave] = sure; wave_more[wave] = equal; }
+    uint32_t n_sure = 0, n_equal = 0;
+    over_stretch([&](uint32_t i, uint32_t key, bool middle) {
+        n_sure += sure(i, key, middle);
+        n_equal += equal(key, middle);
+    });
+    for (uint32_t d = 1; d < 64; d *= 2) { n_sure += __shfl_xor(n_sure, d); n_equal += __shfl_xor(n_equal, d); }
+    if (lane == 0) { wave_sum[wave] = n_sure; wave_more[wave] = n_equal; }
     __syncthreads();
     uint32_t sure_before = 0, equal_before = 0;
     for (uint32_t i = 0; i < wave; i++) { sure_before += wave_sum[i]; equal_before += wave_more[i]; }
     const uint64_t below = (1ull << lane) - 1;
-    for (uint32_t i0 = from; i0 < to; i0 += 64) {
-        const uint32_t i = i0 + lane;
-        const bool in = i < to, middle = in && i >= begin && i < end;
-        const uint32_t key = middle && !none ? weight_key(w[i]) : 0;
-        const bool is_sure = in && (!middle || (!none && key > threshold)), is_equal = middle && !none && key == threshold;
+    over_stretch([&](uint32_t i, uint32_t key, bool middle) {
+        const bool is_sure = sure(i, key, middle), is_equal = equal(key, middle);
         const uint64_t s = __ballot(is_sure), q = __ballot(is_equal);
         const uint32_t rank = equal_before + (uint32_t)__popcll(q & below);
         const uint32_t at = sure_before + (uint32_t)__popcll(s & below) + min(rank, ties);
         if ((is_sure || (is_equal && rank < ties)) && at < e.keep) kept[at] = (int32_t)i;
         sure_before += (uint32_t)__popcll(s);
         equal_before += (uint32_t)__popcll(q);
-    }
+    });
 }
 
 // 16 bytes of a key's or value's row per thread; a workgroup takes 256 rows of one (sequence, head).  Bound by reading and writing them.
@@ -144,7 +179,10 @@ int launch_evict(const EvictDev &e, void *stream)
 {
     const hipStream_t s = (hipStream_t)stream;
     const uint32_t units = e.n_seqs * e.from.heads;
-    hipLaunchKernelGGL(k_evict_select, dim3(units), dim3(kThreads), 0, s, e);
+    const uint32_t rounds = ((uint32_t)e.from.capacity + kThreads - 1) / kThreads;
+    if (rounds <= 8) hipLaunchKernelGGL(k_evict_select<8>, dim3(units), dim3(kThreads), 0, s, e);
+    else if (rounds <= 64) hipLaunchKernelGGL(k_evict_select<64>, dim3(units), dim3(kThreads), 0, s, e);
+    else hipLaunchKernelGGL(k_evict_select<0>, dim3(units), dim3(kThreads), 0, s, e);
     int rc = (int)hipGetLastError();
     if (rc) return rc;
     const uint32_t most = e.keep < (uint32_t)e.from.capacity ? e.keep : (uint32_t)e.from.capacity, rows_per_block = 64;
