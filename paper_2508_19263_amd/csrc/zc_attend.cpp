@@ -83,7 +83,8 @@ struct AttendPlan {
     AttendDev pre;
     Pass own_pass, pre_pass;
     uint32_t slots;                            // 1: the only pass writes the result itself
-    uint64_t part_o_bytes, ws_bytes;
+    uint64_t part_o_bytes, logits_at, ws_bytes;
+    bool logits;                               // weights come from the logits that the pass leaves, else from the keys again
 };
 
 zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const zc_kv_cache *cache, bool shared, AttendPlan *out)
@@ -160,6 +161,15 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
         p.part_o_bytes = rows * cache->head_dim * 4;
         p.ws_bytes = p.part_o_bytes + align256(rows * 8);
     }
+    // Weights.  A logit is written and read again, 8 bytes per row and token; the keys are head_dim elements per token.
+    const uint64_t rows_per_head = (uint64_t)a.max_q_len * a.group;
+    p.logits = x->d_weights_out && x->n_tokens && rows_per_head <= 16 && rows_per_head * 8 <= (uint64_t)cache->head_dim * (cache->format == ZC_FMT_BF16 ? 2 : 1);
+    if (p.logits) {
+        a.logit_rows = (uint32_t)rows_per_head;
+        a.logit_stride = ((uint32_t)a.c.limit + 31) / 32 * 32;
+        p.logits_at = p.ws_bytes = align256(p.ws_bytes);
+        p.ws_bytes += (uint64_t)a.n_seqs * a.c.heads * a.logit_rows * a.logit_stride * 4;
+    }
     *out = p;
     return ZC_OK;
 }
@@ -174,13 +184,15 @@ zc_status attend(const zc_attend_args *x, const zc_kv_cache *prefix, const zc_kv
         if (ws_bytes < p.ws_bytes) return ZC_ERR_BUFFER_TOO_SMALL;
         p.own.part_o = p.pre.part_o = (float *)d_ws;
         p.own.part_ml = p.pre.part_ml = (float *)((uint8_t *)d_ws + p.part_o_bytes);
+        p.own.logits = p.logits ? (float *)((uint8_t *)d_ws + p.logits_at) : nullptr;
     }
+    const WeightsDev w = {x->d_weights_in, x->d_weights_out};
     if (x->n_tokens) {
         if (shared) LAUNCH_TRY(launch_pass(p.pre, p.pre_pass, *cache, stream));
         LAUNCH_TRY(launch_pass(p.own, p.own_pass, *cache, stream));
-        if (p.slots > 1) LAUNCH_TRY(launch_attend_join(p.own, cache->head_dim, p.slots, stream));
+        if (p.slots > 1 || p.logits) LAUNCH_TRY(launch_attend_join(p.own, w, cache->head_dim, p.slots, stream));
     }
-    if (x->d_weights_out) LAUNCH_TRY(launch_attend_weights(p.own, WeightsDev{x->d_weights_in, x->d_weights_out}, cache->format, cache->head_dim, p.own.c.limit, stream));
+    if (x->d_weights_out && !p.logits) LAUNCH_TRY(launch_attend_weights(p.own, w, cache->format, cache->head_dim, p.own.c.limit, stream));
     return ZC_OK;
 }
 

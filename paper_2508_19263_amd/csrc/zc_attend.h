@@ -28,6 +28,8 @@ struct AttendDev {
     const int32_t *prefix_length;      // length of the shared prefix or null
     float *part_o, *part_ml;           // workspace: [slot][row][dim] and [slot][row][2], rows in the order of lse
     uint64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;   // elements
+    float *logits;                     // k_attend_few with at most 16 rows, or null: [seq][head][logit_rows][logit_stride], in base 2
+    uint32_t logit_rows, logit_stride;
     float scale;
     int32_t own_limit, prefix_limit;
     uint32_t n_seqs, n_tokens, q_heads, group, max_q_len, window, sinks;
@@ -52,10 +54,11 @@ struct EvictDev {
     uint32_t n_seqs, keep, sinks, recent, row_bytes;
 };
 
-// rows a workgroup of the kernels takes (`tiles` = 16-row tiles per wavefront there)
+// tiles: of 16 rows in k_attend_few, of 128 in k_attend_many
 int launch_attend_few(const AttendDev &a, uint32_t format, uint32_t head_dim, uint32_t tiles, void *stream);
 int launch_attend_many(const AttendDev &a, uint32_t format, uint32_t head_dim, uint32_t tiles, void *stream);
-int launch_attend_join(const AttendDev &a, uint32_t head_dim, uint32_t slots, void *stream);
+// slots > 1: joins them; a.logits: adds up the weights from them
+int launch_attend_join(const AttendDev &a, const WeightsDev &w, uint32_t head_dim, uint32_t slots, void *stream);
 int launch_attend_weights(const AttendDev &a, const WeightsDev &w, uint32_t format, uint32_t head_dim, int32_t longest, void *stream);
 int launch_evict(const EvictDev &e, void *stream);
 

@@ -48,49 +48,64 @@ template <int FMT, int VW> __device__ __forceinline__ u32x4_t value_operand(cons
     return r;
 }
 
-template <int FMT, int D, int QT>
+template <int FMT, int D, int QT, bool LOGITS>
 __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_few(AttendDev a)
 {
     using Regs = BlockRegs<FMT, D>;
     constexpr int ES = Regs::ES, NK = Regs::NK, DL = Regs::DL, KS = D / 32;
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
-    uint32_t id = blockIdx.x;
-    const uint32_t split = id % a.splits;
-    id /= a.splits;
-    const uint32_t row_block = id % a.row_blocks;
-    id /= a.row_blocks;
-    const uint32_t head = id % a.c.heads, seq = id / a.c.heads;          // shared: the prefix's one "sequence" is 0
+    const uint32_t unit = blockIdx.x, split = blockIdx.y, head = unit % a.c.heads, seq = unit / a.c.heads;     // shared: the prefix's one "sequence" is 0
 
-    // ---- this lane's rows
-    const int32_t offset = a.shared ? 0 : prefix_tokens(a);
+    // ---- this lane's rows, and what all of them and any of them see
+    const int32_t prefix = prefix_tokens(a), offset = a.shared ? 0 : prefix;
     const int32_t length = clamped_length(a.c.lengths, seq, a.c.limit);
-    const int32_t prefix = prefix_tokens(a);
     const Span span = rows_span(a, seq);
-    Row rows[QT];
-    int32_t last_min = INT32_MAX, last_max = -1, from_min = INT32_MAX, from_max = INT32_MIN;
-#pragma unroll
-    for (int t = 0; t < QT; t++) {
-        rows[t] = row_of(a, span, head, (row_block * QT + t) * 16 + n16, prefix, offset, length);
-        if (rows[t].token >= 0) {
-            last_min = min(last_min, rows[t].sight.last);
-            last_max = max(last_max, rows[t].sight.last);
-            from_min = min(from_min, rows[t].sight.from);
-            from_max = max(from_max, rows[t].sight.from);
-        }
-    }
-    last_min = min_over_wave(last_min);
-    last_max = max_over_wave(last_max);
-    from_min = min_over_wave(from_min);
-    from_max = max_over_wave(from_max);
     const int32_t sinks = (int32_t)a.sinks - offset;
-
+    Row rows[QT];
+    int32_t last_min = length - span.count, last_max = span.count ? length - 1 : -1;
+    int32_t from_min = a.window ? last_min - (int32_t)a.window + 1 : 0, from_max = a.window ? length - (int32_t)a.window : 0;
+#pragma unroll
+    for (int t = 0; t < QT; t++) rows[t] = row_of(a, span, head, t * 16 + n16, prefix, offset, length);
+    if (a.shared) {
+        last_min = INT32_MAX, last_max = -1, from_min = INT32_MAX, from_max = INT32_MIN;
+#pragma unroll
+        for (int t = 0; t < QT; t++)
+            if (rows[t].token >= 0) {
+                last_min = min(last_min, rows[t].sight.last);
+                last_max = max(last_max, rows[t].sight.last);
+                from_min = min(from_min, rows[t].sight.from);
+                from_max = max(from_max, rows[t].sight.from);
+            }
+        last_min = min_over_wave(last_min);
+        last_max = max_over_wave(last_max);
+        from_min = min_over_wave(from_min);
+        from_max = max_over_wave(from_max);
+    }
     const Blocks blocks = seen_blocks(32, last_max, from_min, sinks);
     // this workgroup's part, in steps that all four wavefronts take part in
     const int32_t per_split = ((blocks.count + (int32_t)a.splits - 1) / (int32_t)a.splits + (int32_t)kWaves - 1) / (int32_t)kWaves * (int32_t)kWaves;
     const int32_t begin = min((int32_t)split * per_split, blocks.count), end = min(begin + per_split, blocks.count);
 
-    const float k_scale = a.c.k_scales ? a.c.k_scales[seq * a.c.heads + head] : 1.0f;
-    const float v_scale = a.c.v_scales ? a.c.v_scales[seq * a.c.heads + head] : 1.0f;
+    const int32_t *table = a.c.table + (uint64_t)(unit) * a.c.table_pages;
+    const uint32_t page_log = a.c.page_shift + (D == 128 ? 7 : 6) + (ES - 1);   // of a page's bytes
+    const uint32_t page_mask = (1u << a.c.page_shift) - 1;
+    const uint32_t k_lane = n16 * (D * ES) + g * 16, v_lane = g * 4 * (D * ES) + n16 * (DL * ES);
+
+    // page ids of the wavefront's next 32 steps: lane 2i + h has that of half h of step i (-1: absent)
+    int32_t ids = -1, ids_from = begin + (int32_t)wave;
+    auto fetch_ids = [&](int32_t b) {
+        const int32_t mine = b + (int32_t)(lane >> 1) * (int32_t)kWaves;
+        const uint32_t page = ((uint32_t)blocks.at(mine) * 32 + (lane & 1) * 16) >> a.c.page_shift;
+        ids = -1;
+        if (mine < end && page < a.c.table_pages) ids = table[page];
+        if ((uint32_t)ids >= a.c.n_pages) ids = -1;
+        ids_from = b;
+    };
+    int32_t b = begin + (int32_t)wave;
+    if (b < end) fetch_ids(b);
+
+    const float k_scale = a.c.k_scales ? a.c.k_scales[unit] : 1.0f;
+    const float v_scale = a.c.v_scales ? a.c.v_scales[unit] : 1.0f;
     const float signed_c = a.scale * k_scale * kLog2e;
     // logits in base 2; a negative factor goes to the queries' signs, and 0 is made one that takes any product to 0 but minus infinity
     const float c = fmaxf(fabsf(signed_c), 1e-30f);
@@ -120,21 +135,6 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
         for (int i = 0; i < DL; i++) o[t][i] = f32x4{0, 0, 0, 0};
     }
 
-    const int32_t *table = a.c.table + (uint64_t)(seq * a.c.heads + head) * a.c.table_pages;
-    const uint32_t page_log = a.c.page_shift + (D == 128 ? 7 : 6) + (ES - 1);   // of a page's bytes
-    const uint32_t page_mask = (1u << a.c.page_shift) - 1;
-    const uint32_t k_lane = n16 * (D * ES) + g * 16, v_lane = g * 4 * (D * ES) + n16 * (DL * ES);
-
-    // page ids of the wavefront's next 32 steps: lane 2i + h has that of half h of step i (-1: absent)
-    int32_t ids = -1, ids_from = begin + (int32_t)wave;
-    auto fetch_ids = [&](int32_t b) {
-        const int32_t mine = b + (int32_t)(lane >> 1) * (int32_t)kWaves;
-        const uint32_t page = ((uint32_t)blocks.at(mine) * 32 + (lane & 1) * 16) >> a.c.page_shift;
-        ids = -1;
-        if (mine < end && page < a.c.table_pages) ids = table[page];
-        if ((uint32_t)ids >= a.c.n_pages) ids = -1;
-        ids_from = b;
-    };
     // the two halves' places of a step: byte offsets into the pools, and which of their pages are present
     struct Place { uint64_t at[2]; int32_t t0; uint32_t there; };
     auto place_of = [&](int32_t b) {
@@ -166,10 +166,8 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
     };
 
     // Keys of the next step are asked for when this step's products are on their way, values when this step's are used up.
-    int32_t b = begin + (int32_t)wave;
     Place now = {};
     if (b < end) {
-        fetch_ids(b);
         now = place_of(b);
         load_keys(now);
         load_values(now);
@@ -224,6 +222,11 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
                     const uint32_t keep = bit_as_mask(mask, j);
                     s[t][j / 4][j & 3] = __uint_as_float((bits(s[t][j / 4][j & 3]) & keep) | (bits(kNegInf) & ~keep));
                 }
+            }
+            if (LOGITS && rows[t].token >= 0) {
+                float *to = a.logits + ((uint64_t)unit * a.logit_rows + n16) * a.logit_stride + (uint32_t)t0 + g * 4;
+#pragma unroll
+                for (int h = 0; h < 2; h++) *reinterpret_cast<f32x4 *>(to + h * 16) = s[t][h] * c;
             }
             float top = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])), fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
             top = max_over_16(max_over_32(top));
@@ -306,7 +309,7 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
             }
         __syncthreads();
         {
-            const uint32_t r = (row_block * QT + t) * 16 + row16, i = r / a.group;
+            const uint32_t r = t * 16 + row16, i = r / a.group;
             int32_t tok = (int32_t)i < span.count ? span.first + (int32_t)i : -1;
             if (a.shared && tok >= 0 && sequence_of(a, tok) < 0) tok = -1;
             float big = kNegInf, sum = 0.0f;
@@ -348,13 +351,14 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
     }
 }
 
-template <int FMT, int D> int launch(const AttendDev &a, uint32_t tiles, uint32_t blocks, hipStream_t s)
+template <int FMT, int D> int launch(const AttendDev &a, uint32_t tiles, dim3 blocks, hipStream_t s)
 {
-    if (tiles == 1) hipLaunchKernelGGL((k_attend_few<FMT, D, 1>), dim3(blocks), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_attend_few<FMT, D, 2>), dim3(blocks), dim3(256), 0, s, a);
+    if (a.logits) hipLaunchKernelGGL((k_attend_few<FMT, D, 1, true>), blocks, dim3(256), 0, s, a);
+    else if (tiles == 1) hipLaunchKernelGGL((k_attend_few<FMT, D, 1, false>), blocks, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_attend_few<FMT, D, 2, false>), blocks, dim3(256), 0, s, a);
     return (int)hipGetLastError();
 }
-template <int FMT> int launch(const AttendDev &a, uint32_t head_dim, uint32_t tiles, uint32_t blocks, hipStream_t s)
+template <int FMT> int launch(const AttendDev &a, uint32_t head_dim, uint32_t tiles, dim3 blocks, hipStream_t s)
 {
     return head_dim == 64 ? launch<FMT, 64>(a, tiles, blocks, s) : launch<FMT, 128>(a, tiles, blocks, s);
 }
@@ -363,7 +367,7 @@ template <int FMT> int launch(const AttendDev &a, uint32_t head_dim, uint32_t ti
 
 int launch_attend_few(const AttendDev &a, uint32_t format, uint32_t head_dim, uint32_t tiles, void *stream)
 {
-    const uint32_t blocks = (a.shared ? 1 : a.n_seqs) * a.c.heads * a.row_blocks * a.splits;
+    const dim3 blocks((a.shared ? 1 : a.n_seqs) * a.c.heads, a.splits);
     const hipStream_t s = (hipStream_t)stream;
     if (format == ZC_FMT_BF16) return launch<ZC_FMT_BF16>(a, head_dim, tiles, blocks, s);
     if (format == ZC_FMT_FP8_E4M3) return launch<ZC_FMT_FP8_E4M3>(a, head_dim, tiles, blocks, s);

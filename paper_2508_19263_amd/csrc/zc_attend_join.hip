@@ -6,49 +6,118 @@ namespace zc {
 
 namespace {
 
-// One wavefront per (query token, query head).  With (m_s, l_s, O_s) of the slots, M = max m_s:
+// One workgroup per (query token, query head).  With (m_s, l_s, O_s) of the slots, M = max m_s:
 //   out = sum O_s 2^(m_s - M) / sum l_s 2^(m_s - M),   lse = (M + log2 of that sum) ln 2.
-// A lane first holds one slot's pair (at most 64 slots), then four dimensions of every second (head_dim 128) or fourth slot.
-// Bound by the read of the parts, which the pass before has left in the L2 and the memory-side cache.
+// A lane first holds one slot's pair (at most 64 slots), then four dimensions of every eighth (head_dim 128) or sixteenth slot.
+// Bound by latency: the parts are in the L2 or the memory-side cache.
+//
+// Workgroups behind those take 1,024 tokens of a (sequence, K/V head) each and add up their weights from the logits that
+// k_attend_few has left (`logits`, where rereading these costs less than rereading the keys): four tokens to a thread, the
+// rows one after the other.
 template <int D>
-__global__ __launch_bounds__(256) void k_attend_join(AttendDev a, uint32_t slots)
+__global__ __launch_bounds__(256, 4) void k_attend_join(AttendDev a, WeightsDev wt, uint32_t slots, uint32_t join_blocks, uint32_t blocks_per_unit)
 {
-    constexpr uint32_t LD = D / 4, SUBS = 64 / LD;
-    const uint32_t lane = threadIdx.x & 63;
-    const uint64_t n_rows = (uint64_t)a.n_tokens * a.q_heads, row = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= n_rows) return;
-    const int32_t token = (int32_t)(row / a.q_heads);
-    if (sequence_of(a, token) < 0) return;
-    float m = kNegInf, l = 0.0f;
-    if (lane < slots) {
-        m = a.part_ml[(lane * n_rows + row) * 2];
-        l = a.part_ml[(lane * n_rows + row) * 2 + 1];
-    }
-    float top = m;
-    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-    const float f = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m - top);
-    float sum = m == kNegInf ? 0.0f : l * f;
-    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    const uint32_t sub = lane / LD, dim = lane % LD * 4;
-    f32x4 x = {0, 0, 0, 0};
-    for (uint32_t s0 = 0; s0 < slots; s0 += SUBS * 4) {
-#pragma unroll
-        for (uint32_t k = 0; k < 4; k++) {
-            const uint32_t s = s0 + k * SUBS + sub;
-            const float fs = __shfl(f, (int)(s & 63));
-            if (s < slots && fs != 0.0f) x += *reinterpret_cast<const f32x4 *>(a.part_o + (s * n_rows + row) * D + dim) * fs;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint64_t n_rows = (uint64_t)a.n_tokens * a.q_heads;
+    if (blockIdx.x < join_blocks) {
+        constexpr uint32_t LD = D / 4, SUBS = 256 / LD;        // lanes per slot, slots at a time
+        __shared__ f32x4 joined[4][LD];
+        const uint64_t row = blockIdx.x;
+        const int32_t token = (int32_t)(row / a.q_heads);
+        if (sequence_of(a, token) < 0) return;
+        float m = kNegInf, l = 0.0f;
+        if (lane < slots) {
+            m = a.part_ml[(lane * n_rows + row) * 2];
+            l = a.part_ml[(lane * n_rows + row) * 2 + 1];
         }
-    }
+        const uint32_t sub = tid / LD, dim = tid % LD * 4;
+        f32x4 part[64 / SUBS];
 #pragma unroll
-    for (uint32_t d = LD; d < 64; d *= 2)
+        for (uint32_t k = 0; k < 64 / SUBS; k++) {
+            const uint32_t s = k * SUBS + sub;
+            part[k] = f32x4{0, 0, 0, 0};
+            if (s < slots) part[k] = *reinterpret_cast<const f32x4 *>(a.part_o + (s * n_rows + row) * D + dim);
+        }
+        float top = m;
+        for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+        const float f = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+        float sum = m == kNegInf ? 0.0f : l * f;
+        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+        f32x4 x = {0, 0, 0, 0};
 #pragma unroll
-        for (int j = 0; j < 4; j++) x[j] += __shfl_xor(x[j], (int)d);
-    const float inv = top == kNegInf ? 0.0f : 1.0f / sum;
-    if (sub == 0) {
+        for (uint32_t k = 0; k < 64 / SUBS; k++) {
+            const float fs = __shfl(f, (int)(k * SUBS + sub));
+            x += fs == 0.0f ? f32x4{0, 0, 0, 0} : part[k] * fs;
+        }
+#pragma unroll
+        for (uint32_t d = LD; d < 64; d *= 2)
+#pragma unroll
+            for (int j = 0; j < 4; j++) x[j] += __shfl_xor(x[j], (int)d);
+        if (lane < LD) joined[wave][lane] = x;
+        __syncthreads();
+        if (tid >= LD) return;
+        x = (joined[0][tid] + joined[1][tid]) + (joined[2][tid] + joined[3][tid]);
+        const float inv = top == kNegInf ? 0.0f : 1.0f / sum;
         const u32x2 w = {pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv)};
         *reinterpret_cast<u32x2 *>(a.out + (uint64_t)token * a.out_token_stride + row % a.q_heads * a.out_head_stride + dim) = w;
+        if (a.lse && tid == 0) a.lse[row] = top == kNegInf ? kNegInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+        return;
     }
-    if (a.lse && lane == 0) a.lse[row] = top == kNegInf ? kNegInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+
+    __shared__ float lse[16];
+    const uint32_t unit = (blockIdx.x - join_blocks) / blocks_per_unit, head = unit % a.c.heads, seq = unit / a.c.heads;
+    const int32_t t = (int32_t)((blockIdx.x - join_blocks) % blocks_per_unit * 1024 + tid * 4);
+    const int32_t length = clamped_length(a.c.lengths, seq, a.c.limit);
+    const Span span = query_span(a, seq);
+    const uint32_t rows = (uint32_t)span.count * a.group;      // at most 16
+    {
+        // the rows' lse in base 2: 16 lanes for each row's slots
+        const uint32_t r = tid / 16;
+        float m = kNegInf, l = 0.0f;
+        if (r < rows) {
+            const uint64_t row = (uint64_t)(span.first + (int32_t)(r / a.group)) * a.q_heads + head * a.group + r % a.group;
+            if (slots == 1) {
+                m = a.lse[row] * kLog2e;
+                l = 1.0f;
+            } else {
+                float ms[4], ls[4];
+#pragma unroll
+                for (uint32_t k = 0; k < 4; k++) {
+                    const uint32_t s = k * 16 + (tid & 15);
+                    ms[k] = s < slots ? a.part_ml[(s * n_rows + row) * 2] : kNegInf;
+                    ls[k] = s < slots ? a.part_ml[(s * n_rows + row) * 2 + 1] : 0.0f;
+                    m = fmaxf(m, ms[k]);
+                }
+                for (int d = 1; d < 16; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+#pragma unroll
+                for (uint32_t k = 0; k < 4; k++) l += ms[k] == kNegInf ? 0.0f : ls[k] * __builtin_amdgcn_exp2f(ms[k] - m);
+                for (int d = 1; d < 16; d *= 2) l += __shfl_xor(l, d);
+            }
+        }
+        if ((tid & 15) == 0) lse[r] = m == kNegInf ? kNegInf : m + __builtin_amdgcn_logf(l);
+        __syncthreads();
+    }
+    if (t >= length) return;
+    const Sight any = sight(a, length - 1, 0, length), first = sight(a, length - span.count, 0, length);
+    // the four tokens lie in one block of those the pass has gone over, or in none
+    const bool gone_over = span.count && (t + 3 >= first.from || t < any.sinks);
+    f32x4 sum = {0, 0, 0, 0};
+    if (gone_over) {
+        const float *from = a.logits + (uint64_t)unit * a.logit_rows * a.logit_stride + (uint32_t)t;
+        for (uint32_t r = 0; r < rows; r++) {
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(from + (uint64_t)r * a.logit_stride);
+            const float minus = lse[r];
+#pragma unroll
+            for (int j = 0; j < 4; j++) sum[j] += minus == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(x[j] - minus);
+        }
+    }
+    const uint64_t at = (uint64_t)unit * (uint64_t)a.c.capacity + (uint64_t)t;
+    if (t + 4 <= length) {
+        const f32x4 before = wt.in ? *reinterpret_cast<const f32x4u *>(wt.in + at) : f32x4{0, 0, 0, 0};
+        *reinterpret_cast<f32x4u *>(wt.out + at) = before + sum;
+    } else {
+        for (int j = 0; j < 4 && t + j < length; j++) wt.out[at + j] = (wt.in ? wt.in[at + j] : 0.0f) + sum[j];
+    }
 }
 
 // weights_out[t] = weights_in[t] + sum over the rows that see t of exp(s - lse).  A wavefront keeps the keys of 64 tokens in
@@ -187,11 +256,12 @@ template <int FMT> void launch_weights(const AttendDev &a, const WeightsDev &w, 
 
 }  // namespace
 
-int launch_attend_join(const AttendDev &a, uint32_t head_dim, uint32_t slots, void *stream)
+int launch_attend_join(const AttendDev &a, const WeightsDev &w, uint32_t head_dim, uint32_t slots, void *stream)
 {
-    const uint32_t blocks = (uint32_t)(((uint64_t)a.n_tokens * a.q_heads + 3) / 4);
-    if (head_dim == 64) hipLaunchKernelGGL((k_attend_join<64>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, a, slots);
-    else hipLaunchKernelGGL((k_attend_join<128>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, a, slots);
+    const uint32_t join_blocks = slots > 1 ? (uint32_t)((uint64_t)a.n_tokens * a.q_heads) : 0;
+    const uint32_t per_unit = a.logits ? (uint32_t)(a.c.limit + 1023) / 1024 : 1, blocks = join_blocks + (a.logits ? a.n_seqs * a.c.heads * per_unit : 0);
+    if (head_dim == 64) hipLaunchKernelGGL((k_attend_join<64>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, a, w, slots, join_blocks, per_unit);
+    else hipLaunchKernelGGL((k_attend_join<128>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, a, w, slots, join_blocks, per_unit);
     return (int)hipGetLastError();
 }
 
