@@ -54,17 +54,22 @@ struct Pass {
     uint64_t blocks;
 };
 
-// rows: of one (sequence, head), or of one head of the prefix; units: how many of those; longest: tokens that a row block may have to read
-Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_splits)
+// rows: of one (sequence, head), or of one head of the prefix; units: how many of those; longest: tokens that a row block may have to read;
+// only: the call has no other pass
+Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_splits, bool only)
 {
     Pass p;
     p.many = rows > 32;
     p.tiles = p.many || rows <= 16 ? 1 : 2;
     const uint64_t per_block = p.tiles * (p.many ? 128 : 16);
     p.row_blocks = (uint32_t)((rows + per_block - 1) / per_block);
-    const uint64_t groups = units * p.row_blocks, steps = (longest + 127) / 128;        // workgroups without splitting; pairs of tiles, or steps of four wavefronts
-    const uint64_t enough = p.many ? 512 : 1024;
-    const uint64_t wanted = groups ? (enough + groups - 1) / groups : 1, possible = (steps + 1) / 2;
+    // A cache is split where there are fewer workgroups than compute units (k_attend_many: two of whose workgroups share one), but
+    // into parts of no less than two steps of 128 tokens (four of 64).  Measured with one workgroup per compute unit against two in
+    // k_attend_few: 4 FP8 caches of 8,192 tokens 17.6 against 18.3 us, 32 BF16 ones with a window of 4,096 94 against 100 us; with
+    // parts of two steps against four: one cache with a window of 512 9.0 against 9.6 us, 1,531 shared tokens 19.1 against 21.4 us.
+    // A call's only pass is left in one part up to 640 tokens: a second launch costs what its part of the work takes.
+    const uint64_t groups = units * p.row_blocks, part = 256, possible = only && longest <= 640 ? 1 : (longest + part - 1) / part;
+    const uint64_t enough = p.many ? 512 : 256, wanted = groups ? (enough + groups - 1) / groups : 1;
     uint64_t s = wanted < possible ? wanted : possible;
     if (s > most_splits) s = most_splits;
     p.splits = s ? (uint32_t)s : 1;
@@ -130,7 +135,7 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
         const uint64_t w = a.window ? (uint64_t)a.window + a.max_q_len + a.sinks + 64 : (uint64_t)limit;
         return w < (uint64_t)limit ? w : (uint64_t)limit;
     };
-    p.own_pass = plan_pass((uint64_t)a.max_q_len * a.group, (uint64_t)a.n_seqs * a.c.heads, reach(a.c.limit), shared ? 16 : kMaxSlots);
+    p.own_pass = plan_pass((uint64_t)a.max_q_len * a.group, (uint64_t)a.n_seqs * a.c.heads, reach(a.c.limit), shared ? 16 : kMaxSlots, !shared);
     p.slots = p.own_pass.splits;
     if (shared) {
         AttendDev &b = p.pre;
@@ -145,7 +150,7 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
         b = a;
         b.c = pc;
         b.shared = 1;
-        p.pre_pass = plan_pass((uint64_t)a.n_tokens * a.group, a.c.heads, (uint64_t)pc.limit, 48);
+        p.pre_pass = plan_pass((uint64_t)a.n_tokens * a.group, a.c.heads, (uint64_t)pc.limit, 48, false);
         b.splits = p.pre_pass.splits;
         b.row_blocks = p.pre_pass.row_blocks;
         b.first_slot = 0;

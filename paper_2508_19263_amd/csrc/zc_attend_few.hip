@@ -15,7 +15,7 @@ namespace zc {
 
 namespace {
 
-constexpr uint32_t kWaves = 4;    // wavefronts per workgroup
+constexpr uint32_t kWaves = 4;                 // wavefronts per workgroup (with eight, batches were 1 us slower and single sequences 0.6 us faster)
 
 template <int FMT, int D> struct BlockRegs {
     static constexpr int ES = PageElem<FMT>::BYTES;
@@ -25,11 +25,17 @@ template <int FMT, int D> struct BlockRegs {
     uint32_t v[8][VW];
 };
 
-template <int N> __device__ __forceinline__ void load_words(uint32_t (&to)[N], const uint8_t *p)
+template <int N> __device__ __forceinline__ void load_words(uint32_t (&to)[N], __amdgpu_buffer_rsrc_t from, uint32_t at)
 {
-    if constexpr (N == 1) to[0] = *reinterpret_cast<const uint32_t *>(p);
-    else if constexpr (N == 2) { const u32x2 x = *reinterpret_cast<const u32x2 *>(p); to[0] = x[0]; to[1] = x[1]; }
-    else { const u32x4_t x = *reinterpret_cast<const u32x4_t *>(p); to[0] = x[0]; to[1] = x[1]; to[2] = x[2]; to[3] = x[3]; }
+    if constexpr (N == 1) to[0] = __builtin_amdgcn_raw_buffer_load_b32(from, (int)at, 0, 0);
+    else if constexpr (N == 2) { const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(from, (int)at, 0, 0); to[0] = x[0]; to[1] = x[1]; }
+    else { const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(from, (int)at, 0, 0); to[0] = x[0]; to[1] = x[1]; to[2] = x[2]; to[3] = x[3]; }
+}
+
+// 16 tokens of a page
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t half_page(const uint8_t *p, int bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, bytes, 0x00020000);
 }
 
 // The operand for dimension i of a lane's DL: 8 tokens' elements of it.
@@ -49,7 +55,7 @@ template <int FMT, int VW> __device__ __forceinline__ u32x4_t value_operand(cons
 }
 
 template <int FMT, int D, int QT, bool LOGITS>
-__global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_few(AttendDev a)
+__global__ __launch_bounds__(kWaves * 64, 2) void k_attend_few(AttendDev a)
 {
     using Regs = BlockRegs<FMT, D>;
     constexpr int ES = Regs::ES, NK = Regs::NK, DL = Regs::DL, KS = D / 32;
@@ -82,7 +88,7 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
         from_max = max_over_wave(from_max);
     }
     const Blocks blocks = seen_blocks(32, last_max, from_min, sinks);
-    // this workgroup's part, in steps that all four wavefronts take part in
+    // this workgroup's part, in steps that all wavefronts take part in
     const int32_t per_split = ((blocks.count + (int32_t)a.splits - 1) / (int32_t)a.splits + (int32_t)kWaves - 1) / (int32_t)kWaves * (int32_t)kWaves;
     const int32_t begin = min((int32_t)split * per_split, blocks.count), end = min(begin + per_split, blocks.count);
 
@@ -135,14 +141,15 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
         for (int i = 0; i < DL; i++) o[t][i] = f32x4{0, 0, 0, 0};
     }
 
-    // the two halves' places of a step: byte offsets into the pools, and which of their pages are present
+    // The two halves of a step: what of the pools they are (nothing where a page is absent or the step is none: such loads give 0
+    // without going to memory), and which are present.
     struct Place { uint64_t at[2]; int32_t t0; uint32_t there; };
     auto place_of = [&](int32_t b) {
+        Place x = {{0, 0}, 0, 0};
+        if (b >= end) return x;
         if (b - ids_from >= 32 * (int32_t)kWaves) fetch_ids(b);
         const int32_t i = (b - ids_from) / (int32_t)kWaves * 2;
-        Place x;
         x.t0 = blocks.at(b) * 32;
-        x.there = 0;
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             const int32_t page = __builtin_amdgcn_readlane(ids, i + h);
@@ -151,33 +158,33 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
         }
         return x;
     };
-    Regs r;
-    auto load_keys = [&](const Place &x) {
+    auto load_keys = [&](const Place &x, Regs &r) {
 #pragma unroll
-        for (int h = 0; h < 2; h++)
+        for (int h = 0; h < 2; h++) {
+            const __amdgpu_buffer_rsrc_t from = half_page(a.c.k + x.at[h], x.there >> h & 1 ? 16 * D * ES : 0);
 #pragma unroll
-            for (int u = 0; u < NK; u++) r.k[h][u] = *reinterpret_cast<const u32x4_t *>(a.c.k + x.at[h] + k_lane + u * 64);
+            for (int u = 0; u < NK; u++) r.k[h][u] = __builtin_amdgcn_raw_buffer_load_b128(from, (int)(k_lane + u * 64), 0, 0);
+        }
     };
-    auto load_values = [&](const Place &x) {
+    auto load_values = [&](const Place &x, Regs &r) {
 #pragma unroll
-        for (int h = 0; h < 2; h++)
+        for (int h = 0; h < 2; h++) {
+            const __amdgpu_buffer_rsrc_t from = half_page(a.c.v + x.at[h], x.there >> h & 1 ? 16 * D * ES : 0);
 #pragma unroll
-            for (int j = 0; j < 4; j++) load_words(r.v[h * 4 + j], a.c.v + x.at[h] + v_lane + j * (D * ES));
+            for (int j = 0; j < 4; j++) load_words(r.v[h * 4 + j], from, v_lane + j * (D * ES));
+        }
     };
 
-    // Keys of the next step are asked for when this step's products are on their way, values when this step's are used up.
-    Place now = {};
-    if (b < end) {
-        now = place_of(b);
-        load_keys(now);
-        load_values(now);
-    }
+    // Keys of the next step are asked for when this step's products are on their way, values when this step's are used up.  (Three
+    // steps ahead in as many sets of registers was slower: three copies of the loop to fetch, and a step or two is what a wavefront has.)
+    Regs r;
+    Place place = place_of(b);
+    load_keys(place, r);
+    load_values(place, r);
     for (; b < end; b += (int32_t)kWaves) {
-        const int32_t t0 = now.t0;
-        const uint32_t there = now.there;
-        const bool more = b + (int32_t)kWaves < end;
-        Place next = now;
-        if (more) next = place_of(b + (int32_t)kWaves);
+        const int32_t t0 = place.t0;
+        const uint32_t there = place.there;
+        place = place_of(b + (int32_t)kWaves);
         f32x4 s[QT][2];
 #pragma unroll
         for (int t = 0; t < QT; t++) s[t][0] = s[t][1] = f32x4{0, 0, 0, 0};
@@ -192,10 +199,10 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
                 for (int t = 0; t < QT; t++) s[t][h] = mma16_keys(key, q[t][u], s[t][h]);
             }
         }
-        if (more) load_keys(next);
+        load_keys(place, r);
         const bool whole = there == 3 && t0 + 31 <= last_min && (t0 >= from_max || t0 + 32 <= sinks);
         uint32_t bad = 0;                                // bit j: token j of this lane's 8 has an element that is not finite
-        if (!whole) {
+        if (__builtin_expect(!whole, 0)) {
             // Tokens that no row sees are zeroed (what they hold is not to be multiplied, not even with 0); of those that only some
             // rows see, elements that are not finite are zeroed too and added to the rows that do see them below.
             const uint32_t halves = (there & 1 ? 0x0Fu : 0u) | (there & 2 ? 0xF0u : 0u);
@@ -215,7 +222,7 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
         u32x4_t p[QT];
 #pragma unroll
         for (int t = 0; t < QT; t++) {
-            if (!whole) {
+            if (__builtin_expect(!whole, 0)) {
                 const uint32_t mask = seen_of_eight(rows[t].sight, t0 + (int32_t)g * 4) & ((there & 1 ? 0x0Fu : 0u) | (there & 2 ? 0xF0u : 0u));
 #pragma unroll
                 for (int j = 0; j < 8; j++) {
@@ -247,7 +254,7 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
             l[t] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
 #pragma unroll
             for (int j = 0; j < 4; j++) p[t][j] = pack_weights<FMT>(e[2 * j], e[2 * j + 1]);
-            if (__any(bad != 0)) {
+            if (__builtin_expect(__any(bad != 0), 0)) {
 #pragma unroll 1
                 for (uint32_t n = 0; n < 32; n++) {      // token 4 gg + (j & 3) of half j / 4
                     const uint32_t j = n & 7, gg = n >> 3;
@@ -277,11 +284,10 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
 #pragma unroll
             for (int t = 0; t < QT; t++) o[t][i] = mma16_values<FMT>(val, p[t], o[t][i]);
         }
-        if (more) load_values(next);
-        now = next;
+        load_values(place, r);
     }
 
-    // ---- the four wavefronts' results, 16 rows at a time
+    // ---- the wavefronts' results, 16 rows at a time
     __shared__ float ml[kWaves][QT * 16][2];
     __shared__ __align__(16) float ob[kWaves][16][D + 4];
 #pragma unroll
@@ -290,21 +296,22 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
         if (g == 0) { ml[wave][t * 16 + n16][0] = m[t] == kNegInf ? kNegInf : m[t] * c; ml[wave][t * 16 + n16][1] = l[t]; }
     }
     __syncthreads();
-    const uint32_t row16 = threadIdx.x >> 4, piece = threadIdx.x & 15;
+    constexpr uint32_t kPerRow = kWaves * 4, DP = D / kPerRow;     // threads per row, dimensions per thread
+    const uint32_t row16 = threadIdx.x / kPerRow, piece = threadIdx.x % kPerRow;
 #pragma unroll
     for (int t = 0; t < QT; t++) {
         const float mine = ml[wave][t * 16 + n16][0];
         float top = kNegInf;
 #pragma unroll
         for (uint32_t w = 0; w < kWaves; w++) top = fmaxf(top, ml[w][t * 16 + n16][0]);
-        const float f = mine == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(mine - top);
+        const float f = __builtin_amdgcn_exp2f(mine - (top == kNegInf ? 0.0f : top));
 #pragma unroll
         for (int cc = 0; cc < 4; cc++)
 #pragma unroll
             for (int i = 0; i < DL; i += 4) {
                 f32x4 x;
 #pragma unroll
-                for (int j = 0; j < 4; j++) x[j] = mine == kNegInf ? 0.0f : o[t][i + j][cc] * f;
+                for (int j = 0; j < 4; j++) x[j] = o[t][i + j][cc] * f;
                 *reinterpret_cast<f32x4 *>(&ob[wave][n16][((int)g * 4 + cc) * DL + i]) = x;
             }
         __syncthreads();
@@ -316,33 +323,27 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
 #pragma unroll
             for (uint32_t w = 0; w < kWaves; w++) big = fmaxf(big, ml[w][t * 16 + row16][0]);
 #pragma unroll
-            for (uint32_t w = 0; w < kWaves; w++) {
-                const float mw = ml[w][t * 16 + row16][0];
-                sum += mw == kNegInf ? 0.0f : ml[w][t * 16 + row16][1] * __builtin_amdgcn_exp2f(mw - big);
-            }
-            float x[DL];
+            for (uint32_t w = 0; w < kWaves; w++) sum += ml[w][t * 16 + row16][1] * __builtin_amdgcn_exp2f(ml[w][t * 16 + row16][0] - (big == kNegInf ? 0.0f : big));
+            float x[DP];
 #pragma unroll
-            for (int d = 0; d < DL; d++) x[d] = 0.0f;
+            for (uint32_t d = 0; d < DP; d++) x[d] = 0.0f;
 #pragma unroll
             for (uint32_t w = 0; w < kWaves; w++)
 #pragma unroll
-                for (int d = 0; d < DL; d++) x[d] += ob[w][row16][piece * DL + d];
+                for (uint32_t d = 0; d < DP; d++) x[d] += ob[w][row16][piece * DP + d];
             if (tok >= 0) {
                 const uint64_t row = (uint64_t)tok * a.q_heads + head * a.group + r % a.group;
                 if (a.direct) {
                     const float inv = big == kNegInf ? 0.0f : v_scale / sum;
-                    uint16_t *to = a.out + (uint64_t)tok * a.out_token_stride + (uint64_t)(head * a.group + r % a.group) * a.out_head_stride + piece * DL;
+                    uint16_t *to = a.out + (uint64_t)tok * a.out_token_stride + (uint64_t)(head * a.group + r % a.group) * a.out_head_stride + piece * DP;
 #pragma unroll
-                    for (int d = 0; d < DL; d += 4) {
-                        u32x2 w = {pack_bf16(x[d] * inv, x[d + 1] * inv), pack_bf16(x[d + 2] * inv, x[d + 3] * inv)};
-                        *reinterpret_cast<u32x2 *>(to + d) = w;
-                    }
+                    for (uint32_t d = 0; d < DP; d += 2) *reinterpret_cast<uint32_t *>(to + d) = pack_bf16(x[d] * inv, x[d + 1] * inv);
                     if (a.lse && piece == 0) a.lse[row] = big == kNegInf ? kNegInf : (big + __builtin_amdgcn_logf(sum)) * kLn2;
                 } else {
                     const uint64_t slot = (uint64_t)(a.first_slot + split) * a.n_tokens * a.q_heads + row;
-                    float *to = a.part_o + slot * D + piece * DL;
+                    float *to = a.part_o + slot * D + piece * DP;
 #pragma unroll
-                    for (int d = 0; d < DL; d += 4) *reinterpret_cast<f32x4 *>(to + d) = f32x4{x[d] * v_scale, x[d + 1] * v_scale, x[d + 2] * v_scale, x[d + 3] * v_scale};
+                    for (uint32_t d = 0; d < DP; d++) to[d] = x[d] * v_scale;
                     if (piece == 0) { a.part_ml[slot * 2] = big; a.part_ml[slot * 2 + 1] = sum; }
                 }
             }
@@ -353,9 +354,9 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : D == 64 ? 4 : 3) void k_attend_f
 
 template <int FMT, int D> int launch(const AttendDev &a, uint32_t tiles, dim3 blocks, hipStream_t s)
 {
-    if (a.logits) hipLaunchKernelGGL((k_attend_few<FMT, D, 1, true>), blocks, dim3(256), 0, s, a);
-    else if (tiles == 1) hipLaunchKernelGGL((k_attend_few<FMT, D, 1, false>), blocks, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_attend_few<FMT, D, 2, false>), blocks, dim3(256), 0, s, a);
+    if (a.logits) hipLaunchKernelGGL((k_attend_few<FMT, D, 1, true>), blocks, dim3(kWaves * 64), 0, s, a);
+    else if (tiles == 1) hipLaunchKernelGGL((k_attend_few<FMT, D, 1, false>), blocks, dim3(kWaves * 64), 0, s, a);
+    else hipLaunchKernelGGL((k_attend_few<FMT, D, 2, false>), blocks, dim3(kWaves * 64), 0, s, a);
     return (int)hipGetLastError();
 }
 template <int FMT> int launch(const AttendDev &a, uint32_t head_dim, uint32_t tiles, dim3 blocks, hipStream_t s)

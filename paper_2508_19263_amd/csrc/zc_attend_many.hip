@@ -221,7 +221,7 @@ __global__ __launch_bounds__(256, QN == 1 ? 2 : 1) void k_attend_many(AttendDev 
         u32x4_t p[QN][4];
 #pragma unroll
         for (int t = 0; t < QN; t++) {
-            if (!all) {
+            if (__builtin_expect(!all, 0)) {
                 uint32_t mask = 0;                             // bit h * 16 + i: product i of half h is of a token that the row sees
 #pragma unroll
                 for (int n = 0; n < 8; n++) {
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(256, QN == 1 ? 2 : 1) void k_attend_many(AttendDev 
 #pragma unroll
             for (int i = 0; i < 32; i++) sum[i & 3] += s[t][i / 16][i & 15];
             l[t] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            if (bad) {
+            if (__builtin_expect(bad != 0, 0)) {
 #pragma unroll 1
                 for (uint32_t n = 0; n < 64; n++) {
                     if (!(bad >> n & 1)) continue;
@@ -306,7 +306,7 @@ __global__ __launch_bounds__(256, QN == 1 ? 2 : 1) void k_attend_many(AttendDev 
         fetch(begin);
         store(begin, 0, 0);
         uint32_t there = fetched_there;
-        if (begin + 1 < end) fetch(begin + 1);
+        fetch(min(begin + 1, end - 1));
         __syncthreads();
         uint32_t mod3 = 0;
         for (int32_t b = begin; b < end; b++) {
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(256, QN == 1 ? 2 : 1) void k_attend_many(AttendDev 
                 store(b + 1, buf ^ 1, next3);
                 there = fetched_there;
                 if (tid < 2) bad_tokens[next3 == 2 ? 0 : next3 + 1][tid] = 0;     // last read before the barrier that began this step
-                if (b + 2 < end) fetch(b + 2);
+                fetch(min(b + 2, end - 1));                            // (the last one is asked for again: no branch, no wait)
             }
             __syncthreads();
             mod3 = next3;

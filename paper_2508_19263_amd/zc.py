@@ -86,6 +86,9 @@ class AttendArgs(C.Structure):
                 ("d_q_start", C.c_void_p), ("d_lse", C.c_void_p), ("d_weights_in", C.c_void_p), ("d_weights_out", C.c_void_p)]
 
 
+_ATTEND_ARGS_BYTES = C.sizeof(AttendArgs)
+
+
 class ZcError(RuntimeError):
     def __init__(self, status, what):
         self.status = status
@@ -505,7 +508,7 @@ def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, ma
         raise ValueError("%s: q has to be [n_tokens, n_q_heads, head_dim] in BF16 with contiguous rows" % what)
     n, heads, dim = q.shape
     if out is None:
-        out = torch.empty((n, heads, dim), dtype=q.dtype, device=q.device)
+        out = q.new_empty((n, heads, dim))
     elif out.shape != q.shape or out.stride(2) != 1 or out.element_size() != 2:
         raise ValueError("%s: out has to have q's shape and type, with contiguous rows" % what)
     if lse is None:
@@ -514,30 +517,22 @@ def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, ma
         raise ValueError("%s: lse has to be contiguous float32 [n_tokens, n_q_heads]" % what)
     if q_start is not None and (q_start.dtype != torch.int32 or q_start.numel() != cache.n_seqs + 1 or not q_start.is_contiguous()):
         raise ValueError("%s: q_start has to be contiguous int32 of n_seqs + 1 entries" % what)
-    a = AttendArgs()
-    a.struct_size = C.sizeof(AttendArgs)
-    a.n_tokens, a.n_q_heads, a.max_q_len, a.window, a.sinks = n, heads, max_q_len, window, sinks
-    a.max_kv_len, a.max_prefix_len = max_kv_len, max_prefix_len
-    a.scale = dim ** -0.5 if scale is None else scale
-    a.d_q, a.d_out, a.d_lse = q.data_ptr(), out.data_ptr(), lse.data_ptr()
-    a.q_token_stride, a.q_head_stride = q.stride(0), q.stride(1)
-    a.out_token_stride, a.out_head_stride = out.stride(0), out.stride(1)
-    if q_start is not None:
-        a.d_q_start = q_start.data_ptr()
-    for name, t in (("d_weights_in", weights), ("d_weights_out", weights_out)):
-        if t is not None:
-            if t.dtype != torch.float32 or tuple(t.shape) != (cache.n_seqs, cache.n_heads, cache.capacity) or not t.is_contiguous():
-                raise ValueError("%s: weights have to be contiguous float32 [n_seqs, n_heads, table_pages * page_tokens]" % what)
-            setattr(a, name, t.data_ptr())
-    L, ref, pre = lib(), C.byref(a), None if prefix is None else prefix.ref
-    need = L.zc_attend_workspace_bytes(ref, pre, cache.ref)
-    if ws is None and need:
-        ws = torch.empty(need, dtype=torch.uint8, device=q.device)
-    at, size = (ws.data_ptr(), ws.numel()) if ws is not None else (None, 0)
-    if prefix is None:
-        st = L.zc_attend(ref, cache.ref, at, size, _stream())
-    else:
-        st = L.zc_attend_shared(ref, pre, cache.ref, at, size, _stream())
+    for t in (weights, weights_out):
+        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (cache.n_seqs, cache.n_heads, cache.capacity) or not t.is_contiguous()):
+            raise ValueError("%s: weights have to be contiguous float32 [n_seqs, n_heads, table_pages * page_tokens]" % what)
+    a = AttendArgs(_ATTEND_ARGS_BYTES, n, heads, max_q_len, window, sinks, max_kv_len, max_prefix_len, dim ** -0.5 if scale is None else scale, 0,
+                   q.data_ptr(), out.data_ptr(), q.stride(0), q.stride(1), out.stride(0), out.stride(1),
+                   None if q_start is None else q_start.data_ptr(), lse.data_ptr(),
+                   None if weights is None else weights.data_ptr(), None if weights_out is None else weights_out.data_ptr())
+    L, ref = lib(), C.byref(a)
+    at, size = (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+    if ws is None:
+        size = L.zc_attend_workspace_bytes(ref, None if prefix is None else prefix.ref, cache.ref)
+        if size:
+            ws = torch.empty(size, dtype=torch.uint8, device=q.device)
+            at = ws.data_ptr()
+    stream = torch._C._cuda_getCurrentRawStream(q.device.index)
+    st = L.zc_attend(ref, cache.ref, at, size, stream) if prefix is None else L.zc_attend_shared(ref, prefix.ref, cache.ref, at, size, stream)
     if st != OK:
         raise ZcError(st, what)
     return out, lse
