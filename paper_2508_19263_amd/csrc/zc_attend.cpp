@@ -79,7 +79,7 @@ Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_sp
 
 int launch_pass(const AttendDev &a, const Pass &p, const zc_kv_cache &c, void *stream)
 {
-    return p.many ? launch_attend_many(a, c.format, c.head_dim, p.tiles, stream) : launch_attend_few(a, c.format, c.head_dim, p.tiles, stream);
+    return p.many ? launch_attend_many(a, c.format, c.head_dim, stream) : launch_attend_few(a, c.format, c.head_dim, p.tiles, stream);
 }
 
 // a call's passes and workspace, from its arguments

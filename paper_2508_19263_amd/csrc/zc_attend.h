@@ -56,7 +56,7 @@ struct EvictDev {
 
 // tiles: of 16 rows in k_attend_few, of 128 in k_attend_many
 int launch_attend_few(const AttendDev &a, uint32_t format, uint32_t head_dim, uint32_t tiles, void *stream);
-int launch_attend_many(const AttendDev &a, uint32_t format, uint32_t head_dim, uint32_t tiles, void *stream);
+int launch_attend_many(const AttendDev &a, uint32_t format, uint32_t head_dim, void *stream);
 // slots > 1: joins them; a.logits: adds up the weights from them
 int launch_attend_join(const AttendDev &a, const WeightsDev &w, uint32_t head_dim, uint32_t slots, void *stream);
 int launch_attend_weights(const AttendDev &a, const WeightsDev &w, uint32_t format, uint32_t head_dim, int32_t longest, void *stream);

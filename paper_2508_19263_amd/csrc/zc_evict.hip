@@ -65,10 +65,19 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(EvictDev e)
                     f(i, keys[j], i >= begin && i < end);
                 }
         } else {
-            for (uint32_t j = 0; j < rounds; j++) {
-                const uint32_t i = from + j * 64 + lane;
-                const bool middle = i >= begin && i < end;
-                f(i, middle ? weight_key(w[i]) : 0u, middle);
+            for (uint32_t j0 = 0; j0 < rounds; j0 += 8) {          // eight reads on their way at a time
+                float x[8];
+#pragma unroll
+                for (uint32_t j = 0; j < 8; j++) {
+                    const uint32_t i = from + (j0 + j) * 64 + lane;
+                    x[j] = j0 + j < rounds && i >= begin && i < end ? w[i] : 0.0f;
+                }
+#pragma unroll
+                for (uint32_t j = 0; j < 8; j++)
+                    if (j0 + j < rounds) {
+                        const uint32_t i = from + (j0 + j) * 64 + lane;
+                        f(i, weight_key(x[j]), i >= begin && i < end);
+                    }
             }
         }
     };
@@ -181,7 +190,7 @@ int launch_evict(const EvictDev &e, void *stream)
     const uint32_t units = e.n_seqs * e.from.heads;
     const uint32_t rounds = ((uint32_t)e.from.capacity + kThreads - 1) / kThreads;
     if (rounds <= 8) hipLaunchKernelGGL(k_evict_select<8>, dim3(units), dim3(kThreads), 0, s, e);
-    else if (rounds <= 64) hipLaunchKernelGGL(k_evict_select<64>, dim3(units), dim3(kThreads), 0, s, e);
+    else if (rounds <= 16) hipLaunchKernelGGL(k_evict_select<16>, dim3(units), dim3(kThreads), 0, s, e);
     else hipLaunchKernelGGL(k_evict_select<0>, dim3(units), dim3(kThreads), 0, s, e);
     int rc = (int)hipGetLastError();
     if (rc) return rc;
