@@ -8,7 +8,10 @@ namespace zc {
 
 namespace {
 
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+
 constexpr uint32_t kThreads = 1024, kGroupWaves = kThreads / 64;
+constexpr uint32_t kBins = 2048, kCopies = 8, kRoom = 1024;      // bins of the histogram, its copies, keys of the threshold's bin per wavefront
 
 // Order of the weights as unsigned integers: NaN lowest, -0 equal to +0.
 __device__ __forceinline__ uint32_t weight_key(float w)
@@ -18,19 +21,49 @@ __device__ __forceinline__ uint32_t weight_key(float w)
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
+// The tokens of four consecutive ones from `first` on that are in [begin, end), as bits.
+__device__ __forceinline__ uint32_t bits_in(uint32_t first, uint32_t begin, uint32_t end)
+{
+    const int32_t lo = min(max((int32_t)(begin - first), 0), 4), hi = min(max((int32_t)(end - first), 0), 4);
+    return ((1u << hi) - 1) & ~((1u << lo) - 1);
+}
+
+// Inclusive sums over the lanes of a wavefront.
+__device__ __forceinline__ uint32_t scan_wave(uint32_t x)
+{
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xF, 0xF, false);      // from one, two, four, eight lanes before, in rows of 16
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xA, 0xF, false);      // the row's sum before, the half's
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false);
+    return x;
+}
+
+// Sum of the 16 numbers before the n-th; every lane of the wavefront gets it.
+__device__ __forceinline__ uint32_t sum_before(const uint32_t *x, uint32_t n, uint32_t lane)
+{
+    const uint32_t v = scan_wave(lane < n ? x[lane & (kGroupWaves - 1)] : 0u);
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
 // One workgroup per (sequence, head).  The keep - sinks - recent largest weights of the middle are those above a threshold and
-// the first of those equal to it.  A wavefront has a stretch of tokens of its own, up to N of them per lane held as keys in
-// registers (N = 0: read anew each time).  Four passes over the keys, 8 bits at a time from the top, find the threshold: a histogram in
-// LDS has 32 copies, one per lane of half a wavefront, side by side in the banks, so that the few exponents that weights have cost
-// no waits (with one copy of 2,048 bins the passes over 65,536 tokens took 100 us).  Then every wavefront counts its stretch, and
-// once it knows what lies before it writes its tokens in order.  Bound by latency.
-template <int N>
+// the first of those equal to it.  Every wavefront has a stretch of tokens, four consecutive ones to a lane:
+//   a histogram of the keys' top 11 bits (sign, exponent and two bits of the mantissa) says which bin the threshold is in;
+//   the keys of that bin, some percent, are collected in LDS, where 11 and 10 bits more of them are counted;
+//   every wavefront knows how many of its tokens stay, so how many stay in front of its own, and writes them in order.
+// Three passes over the weights (six, with 8 bits of all keys at a time, took 82 instead of 31 us for 65,536 tokens; the instructions
+// are what bounds it, on one compute unit per sequence and head).  Where a bin has more keys than there is room for, they are
+// taken from memory again each time.  HELD: the keys of up to so many times 256 tokens of a wavefront stay in registers instead (0: none;
+// 8,192 tokens 15.9 -> 12 us).  The histogram has eight copies for eight neighbouring lanes: weights have few exponents.
+template <int HELD>
 __global__ __launch_bounds__(kThreads) void k_evict_select(EvictDev e)
 {
-    __shared__ __align__(16) uint32_t hist[256 * 32];
-    __shared__ __align__(16) uint32_t total[256];
+    __shared__ __align__(16) uint32_t hist[kBins * kCopies];
+    __shared__ uint32_t some[kGroupWaves][kRoom];
     __shared__ uint32_t wave_sum[kGroupWaves], wave_more[kGroupWaves];
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ uint32_t found[2], crowded;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t unit = blockIdx.x, head = unit % e.from.heads, seq = unit / e.from.heads;
     const uint32_t length = (uint32_t)min(max(e.from.lengths[seq], 0), e.from.capacity);
     int32_t *kept = e.kept + (uint64_t)unit * e.keep;
@@ -43,110 +76,151 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(EvictDev e)
     }
     const float *w = e.weights + (uint64_t)unit * (uint64_t)e.from.capacity;
     const uint32_t begin = e.sinks, end = length - e.recent, need = e.keep - e.sinks - e.recent;   // the middle, of which `need` stay
-    const uint32_t rounds = (length + kThreads - 1) / kThreads, from = wave * rounds * 64;         // the stretch: `rounds` times 64 tokens
+    const uint32_t rounds = (length + kGroupWaves * 256 - 1) / (kGroupWaves * 256), from = wave * rounds * 256;    // the stretch: `rounds` times 256 tokens
+    const uint64_t below = (1ull << lane) - 1;
 
-    uint32_t keys[N ? N : 1];
-    if constexpr (N > 0) {
+    // f(first token of this lane's four, their keys) for the stretch, four reads on their way at a time; a table's tokens are a
+    // multiple of 16, so four from a multiple of 4 that is below the length are inside
+    auto key_of = [&](uint32_t r, uint32_t (&key)[4]) {
+        const f32x4u v = *reinterpret_cast<const f32x4u *>(w + min(from + r * 256 + lane * 4, (length - 1) & ~3u));
 #pragma unroll
-        for (int j = 0; j < N; j++) {
-            const uint32_t i = from + (uint32_t)j * 64 + lane;
-            float x = 0.0f;
-            if ((uint32_t)j < rounds && i >= begin && i < end) x = w[i];
-            keys[j] = weight_key(x);
-        }
+        for (int j = 0; j < 4; j++) key[j] = weight_key(v[j]);
+    };
+    uint32_t held[HELD ? HELD : 1][4];
+    if constexpr (HELD > 0) {
+#pragma unroll
+        for (int r = 0; r < HELD; r++) key_of((uint32_t)r, held[r]);
     }
-    // f(token, its key, whether it is of the middle) for the stretch, 64 tokens at a time
     auto over_stretch = [&](auto f) {
-        if constexpr (N > 0) {
+        if constexpr (HELD > 0) {
 #pragma unroll
-            for (int j = 0; j < N; j++)
-                if ((uint32_t)j < rounds) {
-                    const uint32_t i = from + (uint32_t)j * 64 + lane;
-                    f(i, keys[j], i >= begin && i < end);
-                }
+            for (uint32_t r = 0; r < HELD; r++)
+                if (r < rounds) f(from + r * 256 + lane * 4, held[r]);
         } else {
-            for (uint32_t j0 = 0; j0 < rounds; j0 += 8) {          // eight reads on their way at a time
-                float x[8];
+            for (uint32_t r0 = 0; r0 < rounds; r0 += 4) {
+                uint32_t key[4][4];
 #pragma unroll
-                for (uint32_t j = 0; j < 8; j++) {
-                    const uint32_t i = from + (j0 + j) * 64 + lane;
-                    x[j] = j0 + j < rounds && i >= begin && i < end ? w[i] : 0.0f;
-                }
+                for (uint32_t k = 0; k < 4; k++) key_of(r0 + k, key[k]);
 #pragma unroll
-                for (uint32_t j = 0; j < 8; j++)
-                    if (j0 + j < rounds) {
-                        const uint32_t i = from + (j0 + j) * 64 + lane;
-                        f(i, weight_key(x[j]), i >= begin && i < end);
-                    }
+                for (uint32_t k = 0; k < 4; k++)
+                    if (r0 + k < rounds) f(from + (r0 + k) * 256 + lane * 4, key[k]);
             }
         }
     };
-
-    // ---- the threshold: `above` keys of the middle are larger, and need - above of those equal to it stay
-    uint32_t threshold = 0, above = 0;
-    if (need) {
-        uint32_t mask = 0;
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (uint32_t i = tid; i < 256 * 32 / 4; i += kThreads) reinterpret_cast<uint4 *>(hist)[i] = make_uint4(0, 0, 0, 0);
-            __syncthreads();
-            over_stretch([&](uint32_t, uint32_t key, bool middle) {
-                if (middle && (key & mask) == threshold) atomicAdd(&hist[(key >> shift & 255) * 32 + (lane & 31)], 1u);
-            });
-            __syncthreads();
-            {
-                const uint4 x = reinterpret_cast<const uint4 *>(hist)[tid * 2], y = reinterpret_cast<const uint4 *>(hist)[tid * 2 + 1];
-                uint32_t sum = x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;        // a quarter of bin tid / 4
-                sum += __shfl_xor(sum, 1);
-                sum += __shfl_xor(sum, 2);
-                if ((tid & 3) == 0) total[tid / 4] = sum;
-            }
-            __syncthreads();
-            // every wavefront for itself: lane n has bins 255 - 4 n and the three below
-            const uint4 bins = reinterpret_cast<const uint4 *>(total)[63 - lane];
-            const uint32_t four = bins.x + bins.y + bins.z + bins.w;
-            uint32_t upto = four;
-            for (uint32_t d = 1; d < 64; d *= 2) {
-                const uint32_t x = __shfl_up(upto, d);
-                if (lane >= d) upto += x;
-            }
-            const uint64_t reached = __ballot(above + upto >= need);                 // not 0: the middle has more than `need` keys
-            const int who = __ffsll((unsigned long long)reached) - 1;
-            uint32_t before = above + upto - four, bin = 255 - 4 * lane;
-            if (before + bins.w < need) {
-                before += bins.w; bin--;
-                if (before + bins.z < need) {
-                    before += bins.z; bin--;
-                    if (before + bins.y < need) { before += bins.y; bin--; }
-                }
-            }
-            above = __shfl(before, who);
-            threshold |= (uint32_t)__shfl(bin, who) << shift;
-            mask |= 255u << shift;
+    auto clear = [&]() {
+        for (uint32_t i = tid; i < kBins * kCopies / 4; i += kThreads) reinterpret_cast<uint4 *>(hist)[i] = make_uint4(0, 0, 0, 0);
+    };
+    // The bin that the need-th largest key is in, given `above` larger keys elsewhere, which becomes how many are larger than that bin.
+    auto find = [&](uint32_t &above) {
+        uint32_t two[2];                                       // bins 2047 - 2 tid and the one below
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const uint4 *x = reinterpret_cast<const uint4 *>(hist + (kBins - 1 - 2 * tid - k) * kCopies);
+            two[k] = (x[0].x + x[0].y + x[0].z + x[0].w) + (x[1].x + x[1].y + x[1].z + x[1].w);
         }
+        const uint32_t upto = scan_wave(two[0] + two[1]);
+        if (lane == 63) wave_sum[wave] = upto;
+        __syncthreads();
+        const uint32_t before = above + upto - two[0] - two[1] + sum_before(wave_sum, wave, lane);
+        if (before < need && before + two[0] + two[1] >= need) {
+            const bool first = before + two[0] >= need;
+            found[0] = kBins - 1 - 2 * tid - (first ? 0 : 1);
+            found[1] = before + (first ? 0 : two[0]);
+        }
+        __syncthreads();
+        above = found[1];
+        return found[0];
+    };
+
+    uint32_t top = 0xFFFFFFFFu, threshold = 0xFFFFFFFFu, above = 0, n_some = 0, n_sure = 0;    // need == 0: no key is large enough
+    bool in_lds = true;
+    if (need) {
+        clear();
+        if (tid == 0) crowded = 0;
+        __syncthreads();
+        over_stretch([&](uint32_t first, const uint32_t (&key)[4]) {
+            const uint32_t in = bits_in(first, begin, end);
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                if (in >> j & 1) atomicAdd(&hist[(key[j] >> 21) * kCopies + (lane & (kCopies - 1))], 1u);
+        });
+        __syncthreads();
+        top = find(above);                                     // (the middle has more than `need` keys)
+        clear();
+    }
+    // what of the stretch stays for sure, and the keys of the threshold's bin
+    over_stretch([&](uint32_t first, const uint32_t (&key)[4]) {
+        const uint32_t in = bits_in(first, begin, end);
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const bool middle = in >> j & 1;
+            n_sure += (uint32_t)__popcll(__ballot(middle ? need && key[j] >> 21 > top : first + j < length));
+            const uint64_t q = __ballot(middle && key[j] >> 21 == top);
+            if (q) {
+                const uint32_t at = n_some + (uint32_t)__popcll(q & below);
+                if ((q >> lane & 1) && at < kRoom) some[wave][at] = key[j];
+                n_some += (uint32_t)__popcll(q);
+            }
+        }
+    });
+    uint32_t n_equal = 0;
+    if (need) {
+        if (n_some > kRoom && lane == 0) crowded = 1;
+        __syncthreads();
+        in_lds = !crowded;
+        // f(key) for the stretch's keys of that bin
+        auto over_some = [&](auto f) {
+            if (in_lds) {
+                for (uint32_t i = lane; i < n_some; i += 64) f(some[wave][i]);
+            } else {
+                over_stretch([&](uint32_t first, const uint32_t (&key)[4]) {
+                    const uint32_t in = bits_in(first, begin, end);
+#pragma unroll
+                    for (int j = 0; j < 4; j++)
+                        if ((in >> j & 1) && key[j] >> 21 == top) f(key[j]);
+                });
+            }
+        };
+        over_some([&](uint32_t key) { atomicAdd(&hist[(key >> 10 & 2047) * kCopies + (lane & (kCopies - 1))], 1u); });
+        __syncthreads();
+        threshold = top << 11 | find(above);
+        clear();
+        __syncthreads();
+        over_some([&](uint32_t key) { if (key >> 10 == threshold) atomicAdd(&hist[(key & 1023) * kCopies + (lane & (kCopies - 1))], 1u); });
+        __syncthreads();
+        threshold = threshold << 10 | find(above);
+        uint32_t more = 0;
+        over_some([&](uint32_t key) { more += key > threshold; n_equal += key == threshold; });
+        for (uint32_t d = 1; d < 64; d *= 2) { more += __shfl_xor(more, d); n_equal += __shfl_xor(n_equal, d); }
+        n_sure += more;
+        __syncthreads();                                       // wave_sum is free again
     }
     const uint32_t ties = need - above;
-    auto sure = [&](uint32_t i, uint32_t key, bool middle) { return i < length && (!middle || (need && key > threshold)); };
-    auto equal = [&](uint32_t key, bool middle) { return middle && need && key == threshold; };
-
-    uint32_t n_sure = 0, n_equal = 0;
-    over_stretch([&](uint32_t i, uint32_t key, bool middle) {
-        n_sure += sure(i, key, middle);
-        n_equal += equal(key, middle);
-    });
-    for (uint32_t d = 1; d < 64; d *= 2) { n_sure += __shfl_xor(n_sure, d); n_equal += __shfl_xor(n_equal, d); }
     if (lane == 0) { wave_sum[wave] = n_sure; wave_more[wave] = n_equal; }
     __syncthreads();
-    uint32_t sure_before = 0, equal_before = 0;
-    for (uint32_t i = 0; i < wave; i++) { sure_before += wave_sum[i]; equal_before += wave_more[i]; }
-    const uint64_t below = (1ull << lane) - 1;
-    over_stretch([&](uint32_t i, uint32_t key, bool middle) {
-        const bool is_sure = sure(i, key, middle), is_equal = equal(key, middle);
-        const uint64_t s = __ballot(is_sure), q = __ballot(is_equal);
-        const uint32_t rank = equal_before + (uint32_t)__popcll(q & below);
-        const uint32_t at = sure_before + (uint32_t)__popcll(s & below) + min(rank, ties);
-        if ((is_sure || (is_equal && rank < ties)) && at < e.keep) kept[at] = (int32_t)i;
-        sure_before += (uint32_t)__popcll(s);
-        equal_before += (uint32_t)__popcll(q);
+    uint32_t sure_before = sum_before(wave_sum, wave, lane), equal_before = sum_before(wave_more, wave, lane);
+    over_stretch([&](uint32_t first, const uint32_t (&key)[4]) {
+        const uint32_t in = bits_in(first, begin, end);
+        bool sure[4], equal[4];
+        uint32_t s_in = sure_before, q_in = equal_before;      // of those before this lane's first token
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const bool middle = in >> j & 1;
+            sure[j] = middle ? need && key[j] > threshold : first + j < length;
+            equal[j] = middle && need && key[j] == threshold;
+            const uint64_t s = __ballot(sure[j]), q = __ballot(equal[j]);
+            s_in += (uint32_t)__popcll(s & below);
+            q_in += (uint32_t)__popcll(q & below);
+            sure_before += (uint32_t)__popcll(s);
+            equal_before += (uint32_t)__popcll(q);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const uint32_t at = s_in + min(q_in, ties);
+            if ((sure[j] || (equal[j] && q_in < ties)) && at < e.keep) kept[at] = (int32_t)(first + j);
+            s_in += sure[j];
+            q_in += equal[j];
+        }
     });
 }
 
@@ -188,9 +262,7 @@ int launch_evict(const EvictDev &e, void *stream)
 {
     const hipStream_t s = (hipStream_t)stream;
     const uint32_t units = e.n_seqs * e.from.heads;
-    const uint32_t rounds = ((uint32_t)e.from.capacity + kThreads - 1) / kThreads;
-    if (rounds <= 8) hipLaunchKernelGGL(k_evict_select<8>, dim3(units), dim3(kThreads), 0, s, e);
-    else if (rounds <= 16) hipLaunchKernelGGL(k_evict_select<16>, dim3(units), dim3(kThreads), 0, s, e);
+    if ((uint32_t)e.from.capacity <= 2 * kGroupWaves * 256) hipLaunchKernelGGL(k_evict_select<2>, dim3(units), dim3(kThreads), 0, s, e);
     else hipLaunchKernelGGL(k_evict_select<0>, dim3(units), dim3(kThreads), 0, s, e);
     int rc = (int)hipGetLastError();
     if (rc) return rc;
