@@ -88,7 +88,8 @@ struct AttendPlan {
     AttendDev pre;
     Pass own_pass, pre_pass;
     uint32_t slots;                            // 1: the only pass writes the result itself
-    uint64_t part_o_bytes, logits_at, ws_bytes;
+    uint64_t part_o_bytes, logits_at, weights_at, ws_bytes;
+    uint32_t weight_parts;
     bool logits;                               // weights come from the logits that the pass leaves, else from the keys again
 };
 
@@ -175,6 +176,20 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
         p.logits_at = p.ws_bytes = align256(p.ws_bytes);
         p.ws_bytes += (uint64_t)a.n_seqs * a.c.heads * a.logit_rows * a.logit_stride * 4;
     }
+    p.weight_parts = 1;
+    if (x->d_weights_out && !p.logits) {
+        // about 1,024 workgroups, of two that share a compute unit: a prompt's first tokens have the most rows, and the last ones fill up
+        const uint64_t units = (uint64_t)a.n_seqs * a.c.heads, groups = units * ((uint64_t)(a.c.limit + 255) / 256);
+        uint64_t parts = (1024 + groups - 1) / groups;
+        if (parts > rows_per_head / 64) parts = rows_per_head / 64;
+        if (parts > kMostParts) parts = kMostParts;
+        p.weight_parts = parts ? (uint32_t)parts : 1;
+        if (groups * p.weight_parts > 0x7FFFFFFFu) return ZC_ERR_INVALID_ARG;
+        if (p.weight_parts > 1) {
+            p.weights_at = align256(p.ws_bytes);
+            p.ws_bytes = p.weights_at + units * p.weight_parts * (uint64_t)a.c.capacity * 4;
+        }
+    }
     *out = p;
     return ZC_OK;
 }
@@ -191,13 +206,13 @@ zc_status attend(const zc_attend_args *x, const zc_kv_cache *prefix, const zc_kv
         p.own.part_ml = p.pre.part_ml = (float *)((uint8_t *)d_ws + p.part_o_bytes);
         p.own.logits = p.logits ? (float *)((uint8_t *)d_ws + p.logits_at) : nullptr;
     }
-    const WeightsDev w = {x->d_weights_in, x->d_weights_out};
+    const WeightsDev w = {x->d_weights_in, x->d_weights_out, p.weight_parts > 1 ? (float *)((uint8_t *)d_ws + p.weights_at) : nullptr, p.weight_parts};
     if (x->n_tokens) {
         if (shared) LAUNCH_TRY(launch_pass(p.pre, p.pre_pass, *cache, stream));
         LAUNCH_TRY(launch_pass(p.own, p.own_pass, *cache, stream));
         if (p.slots > 1 || p.logits) LAUNCH_TRY(launch_attend_join(p.own, w, cache->head_dim, p.slots, stream));
     }
-    if (x->d_weights_out && !p.logits) LAUNCH_TRY(launch_attend_weights(p.own, w, cache->format, cache->head_dim, p.own.c.limit, stream));
+    if (x->d_weights_out && !p.logits) LAUNCH_TRY(launch_attend_weights(p.own, w, cache->format, cache->head_dim, stream));
     return ZC_OK;
 }
 

@@ -39,9 +39,13 @@ struct AttendDev {
     uint32_t direct;                   // 1: one slot in all, the pass writes out and lse itself
 };
 
+constexpr uint32_t kMostParts = 16;
+
 struct WeightsDev {
     const float *in;                   // or null
     float *out;                        // [seqs][heads][capacity]
+    float *part;                       // workspace: [parts][seqs][heads][capacity] where parts > 1
+    uint32_t parts;                    // workgroups of k_attend_weights that share tokens, at most kMostParts
 };
 
 struct EvictDev {
@@ -59,7 +63,7 @@ int launch_attend_few(const AttendDev &a, uint32_t format, uint32_t head_dim, ui
 int launch_attend_many(const AttendDev &a, uint32_t format, uint32_t head_dim, void *stream);
 // slots > 1: joins them; a.logits: adds up the weights from them
 int launch_attend_join(const AttendDev &a, const WeightsDev &w, uint32_t head_dim, uint32_t slots, void *stream);
-int launch_attend_weights(const AttendDev &a, const WeightsDev &w, uint32_t format, uint32_t head_dim, int32_t longest, void *stream);
+int launch_attend_weights(const AttendDev &a, const WeightsDev &w, uint32_t format, uint32_t head_dim, void *stream);
 int launch_evict(const EvictDev &e, void *stream);
 
 }  // namespace zc

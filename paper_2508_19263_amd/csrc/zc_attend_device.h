@@ -127,6 +127,12 @@ template <int FMT> __device__ __forceinline__ float element(const uint8_t *p)
     else return __uint_as_float(two_to_bf16<FMT, false>(*p) << 16);
 }
 
+// Byte offset in LDS of 16-byte piece c of row n, rows of D two-byte elements: 16 rows' pieces of one number lie in as many banks.
+template <int D> __device__ __forceinline__ uint32_t key_place(uint32_t n, uint32_t c)
+{
+    return D == 128 ? n * 256 + ((c ^ (n & 15)) << 4) : n * 128 + ((c ^ ((n >> 1) & 7)) << 4);
+}
+
 // ---- sequences, rows, positions ----------------------------------------------------------------
 struct Span { int32_t first, count; };         // a sequence's query tokens
 

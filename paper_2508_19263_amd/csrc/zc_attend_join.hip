@@ -120,25 +120,31 @@ __global__ __launch_bounds__(256, 4) void k_attend_join(AttendDev a, WeightsDev 
     }
 }
 
-// weights_out[t] = weights_in[t] + sum over the rows that see t of exp(s - lse).  A wavefront keeps the keys of 64 tokens in
-// registers and goes over the rows 32 at a time, straight from memory: S^T = K Q^T leaves a lane one row's products with 32 of
-// the tokens, whose exponentials it adds up token by token; the 32 lanes of a token are added at the end.  With many rows (a prompt)
-// the eight wavefronts of a workgroup share the tokens and take every eighth 32 rows, and their sums are joined in LDS; else every
-// wavefront has tokens of its own.  The sums have one order, whatever the launch.  Bound by the matrix instructions and the
-// exponentials with many rows, by the read of the keys with few.
+// weights_out[t] = weights_in[t] + sum over the rows that see t of exp(s - lse).  A workgroup takes 256 tokens of a (sequence, K/V
+// head), 64 to a wavefront, whose keys it keeps in registers, and goes over the rows that may see them 64 at a time; these come to
+// LDS once for its four wavefronts, into one of two buffers while the other is worked on.  S^T = K Q^T leaves a lane one row's
+// products with 32 of the tokens, whose exponentials it adds up token by token; the 32 lanes of a token are added at the end.  Where
+// there are fewer workgroups than fill the GPU, `parts` of them share the tokens, each with every so many-th 64 rows, and k_weights_sum adds
+// up what they leave.  The sums have one order, whatever the launch.  Bound by the matrix instructions and the exponentials.
+// (Rows straight from memory to a wavefront's registers, each 32 bytes of 32 rows at a time, took 160 us for 4,099 tokens and 32 heads.)
 template <int FMT, int D>
-__global__ __launch_bounds__(512) void k_attend_weights(AttendDev a, WeightsDev wt, uint32_t by_rows)
+__global__ __launch_bounds__(256, 2) void k_attend_weights(AttendDev a, WeightsDev wt)
 {
     constexpr int ES = PageElem<FMT>::BYTES, KS = D / 16;
-    __shared__ float sums[8][64];
-    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n32 = lane & 31, g = lane >> 5;
+    constexpr uint32_t kRows = 64, kPieces = D / 8, kRowsPerPass = 256 / kPieces, kPasses = kRows / kRowsPerPass;
+    __shared__ __align__(1024) uint8_t lds[2][kRows * D * 2];
+    __shared__ float minus_lse[2][kRows];                      // in base 2; minus infinity: the row gives nothing
+    __shared__ int32_t positions[2][kRows];
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n32 = lane & 31, g = lane >> 5;
     const uint32_t units = a.n_seqs * a.c.heads, unit = blockIdx.x % units, head = unit % a.c.heads, seq = unit / a.c.heads;
-    const uint32_t tile = by_rows ? blockIdx.x / units : blockIdx.x / units * (blockDim.x / 64) + wave;
-    const int32_t t0 = (int32_t)(tile * 64);
+    const uint32_t part = blockIdx.x / units % wt.parts;
+    const int32_t block0 = (int32_t)(blockIdx.x / units / wt.parts * 256), t0 = block0 + (int32_t)wave * 64;
     const int32_t length = clamped_length(a.c.lengths, seq, a.c.limit);
-    if (t0 >= length) return;                                  // by rows: the whole workgroup
+    if (block0 >= length) return;                              // the whole workgroup
     const Span span = query_span(a, seq);
-    const float c = a.scale * (a.c.k_scales ? a.c.k_scales[unit] : 1.0f) * kLog2e;
+    const float signed_c = a.scale * (a.c.k_scales ? a.c.k_scales[unit] : 1.0f) * kLog2e;
+    const float c = fmaxf(fabsf(signed_c), 1e-30f);            // as in the passes: products of what is hidden are minus infinity, and stay it
+    const uint32_t flip = signed_c < 0 ? 0x80008000u : 0u;
 
     const int32_t *table = a.c.table + (uint64_t)unit * a.c.table_pages;
     const uint32_t page_log = a.c.page_shift + (D == 128 ? 7 : 6) + (ES - 1), page_mask = (1u << a.c.page_shift) - 1;
@@ -167,57 +173,93 @@ __global__ __launch_bounds__(512) void k_attend_weights(AttendDev a, WeightsDev 
             }
         }
     }
-    // rows that may see one of these tokens: query tokens from position t0 on, up to the window's end unless they are sinks
-    const int32_t before = length - span.count, first = max(0, t0 - before);
+    // rows that may see one of the 256 tokens: query tokens from position block0 on, up to the window's end unless some are sinks
+    const int32_t before = length - span.count, first = max(0, block0 - before);
     int32_t end = span.count;
-    if (a.window && t0 >= (int32_t)a.sinks) end = min(end, t0 + 63 + (int32_t)a.window - before);
-    const uint32_t step = by_rows ? 32 * 8 : 32, first_row = (uint32_t)first * a.group + (by_rows ? wave * 32 : 0), n_rows = (uint32_t)max(end, 0) * a.group;
+    if (a.window && block0 >= (int32_t)a.sinks) end = min(end, block0 + 255 + (int32_t)a.window - before);
+    const uint32_t n_rows = (uint32_t)max(end, 0) * a.group;
+    const uint32_t first_row = (uint32_t)first * a.group / kRows * kRows + part * kRows, step = kRows * wt.parts;
     float acc[32];
 #pragma unroll
     for (int i = 0; i < 32; i++) acc[i] = 0.0f;
 
-    // this lane's row of the next step: query token `i` of the sequence, head `h` of the group
-    uint32_t i = (first_row + n32) / a.group, h = (first_row + n32) % a.group;
-    const uint32_t step_i = step / a.group, step_h = step % a.group;
-    u32x4_t q[KS];
-    float lse;
-    int32_t position;
-    auto fetch = [&](bool valid) {
-        const uint32_t tok = (uint32_t)span.first + (valid ? i : (uint32_t)first), q_head = head * a.group + h;
-        const uint16_t *row = a.q + (uint64_t)tok * a.q_token_stride + (uint64_t)q_head * a.q_head_stride;
+    // this thread's rows of the next step: query token `i` of the sequence, head `h` of the group; it takes a 16-byte piece of each
+    const uint32_t piece = tid % kPieces, row0 = tid / kPieces, step_i = step / a.group, step_h = step % a.group;
+    uint32_t i[kPasses], h[kPasses];
 #pragma unroll
-        for (int u = 0; u < KS; u++) q[u] = *reinterpret_cast<const u32x4_t *>(row + (FMT == ZC_FMT_BF16 ? u * 16 + g * 8 : (u & ~1) * 16 + g * 16 + (u & 1) * 8));
-        lse = valid ? a.lse[(uint64_t)tok * a.q_heads + q_head] * kLog2e : kNegInf;
-        position = before + (int32_t)i;
-    };
-    if (first_row < n_rows) fetch(first_row + n32 < n_rows);
-    for (uint32_t r0 = first_row; r0 < n_rows; r0 += step) {
-        f32x16 s[2];
+    for (uint32_t p = 0; p < kPasses; p++) {
+        const uint32_t r = first_row + p * kRowsPerPass + row0;
+        i[p] = r / a.group;
+        h[p] = r % a.group;
+    }
+    u32x4_t x[kPasses];
+    float lse[kPasses];
+    int32_t position[kPasses];
+    auto fetch = [&]() {
 #pragma unroll
-        for (int k = 0; k < 16; k++) s[0][k] = s[1][k] = 0.0f;
-#pragma unroll
-        for (int u = 0; u < KS; u++) {
-            s[0] = mma32_keys(key[0][u], q[u], s[0]);
-            s[1] = mma32_keys(key[1][u], q[u], s[1]);
+        for (uint32_t p = 0; p < kPasses; p++) {
+            const bool valid = (int32_t)i[p] < end;
+            const uint32_t tok = (uint32_t)span.first + (valid ? i[p] : (uint32_t)first), q_head = head * a.group + h[p];
+            x[p] = *reinterpret_cast<const u32x4_t *>(a.q + (uint64_t)tok * a.q_token_stride + (uint64_t)q_head * a.q_head_stride + piece * 8);
+            const float v = a.lse[(uint64_t)tok * a.q_heads + q_head];
+            lse[p] = valid && v != kNegInf ? v * -kLog2e : kNegInf;
+            position[p] = before + (int32_t)i[p];
+            i[p] += step_i;
+            h[p] += step_h;
+            if (h[p] >= a.group) { h[p] -= a.group; i[p]++; }
         }
-        const Sight sg = sight(a, position, 0, length);
-        const float minus = lse == kNegInf ? kNegInf : -lse;   // a row that sees nothing gives nothing
-        i += step_i;
-        h += step_h;
-        if (h >= a.group) { h -= a.group; i++; }
-        if (r0 + step < n_rows) fetch(r0 + step + n32 < n_rows);
-        // all of these rows see all of these tokens
-        const bool whole = there == 15 && !__any(!(t0 + 63 <= sg.last && (t0 >= sg.from || t0 + 64 <= sg.sinks)) || minus == kNegInf);
-        if (whole) {
+    };
+    auto store = [&](uint32_t buf) {
+#pragma unroll
+        for (uint32_t p = 0; p < kPasses; p++) {
+            const uint32_t r = p * kRowsPerPass + row0;
+            *reinterpret_cast<u32x4_t *>(lds[buf] + key_place<D>(r, piece)) = x[p] ^ flip;
+            if (piece == 0) { minus_lse[buf][r] = lse[p]; positions[buf][r] = position[p]; }
+        }
+    };
+    auto add_up = [&](uint32_t buf) {
+#pragma unroll
+        for (uint32_t half = 0; half < kRows / 32; half++) {
+            const uint32_t r = half * 32 + n32;
+            f32x16 s[2];
+            const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+            for (int u = 0; u < KS; u++) {
+                const u32x4_t q = *reinterpret_cast<const u32x4_t *>(lds[buf] + key_place<D>(r, FMT == ZC_FMT_BF16 ? u * 2 + g : (u & ~1) * 2 + g * 2 + (u & 1)));
+                s[0] = mma32_keys(key[0][u], q, u ? s[0] : zero);
+                s[1] = mma32_keys(key[1][u], q, u ? s[1] : zero);
+            }
+            const float minus = minus_lse[buf][r];
+            const Sight sg = sight(a, positions[buf][r], 0, length);
+            // all of these rows see all of these tokens
+            const bool whole = there == 15 && !__any(!(t0 + 63 <= sg.last && (t0 >= sg.from || t0 + 64 <= sg.sinks)) || minus == kNegInf);
+            if (__builtin_expect(!whole, 0)) {
+                uint32_t mask = 0;
+#pragma unroll
+                for (int n = 0; n < 8; n++) mask |= (seen_of_four(sg, t0 + n * 8 + (int32_t)g * 4) & (there >> (n / 2) & 1 ? 15u : 0u)) << (n * 4);
+                mask = minus == kNegInf ? 0u : mask;
+#pragma unroll
+                for (int k = 0; k < 32; k++) {
+                    const uint32_t keep = bit_as_mask(mask, k);
+                    s[k / 16][k & 15] = __uint_as_float((bits(s[k / 16][k & 15]) & keep) | (bits(kNegInf) & ~keep));
+                }
+            }
 #pragma unroll
             for (int k = 0; k < 32; k++) acc[k] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[k / 16][k & 15], c, minus));
-        } else {
-            uint32_t mask = 0;
-#pragma unroll
-            for (int n = 0; n < 8; n++) mask |= (seen_of_four(sg, t0 + n * 8 + (int32_t)g * 4) & (there >> (n / 2) & 1 ? 15u : 0u)) << (n * 4);
-            mask = minus == kNegInf ? 0u : mask;
-#pragma unroll
-            for (int k = 0; k < 32; k++) acc[k] += __uint_as_float(bits(__builtin_amdgcn_exp2f(__builtin_fmaf(s[k / 16][k & 15], c, minus))) & bit_as_mask(mask, k));
+        }
+    };
+    if (first_row < n_rows) {
+        fetch();
+        store(0);
+        fetch();
+        __syncthreads();
+        uint32_t buf = 0;
+        for (uint32_t r0 = first_row; r0 < n_rows; r0 += step) {
+            add_up(buf);
+            store(buf ^ 1);                                    // (behind the last rows: of none)
+            fetch();
+            __syncthreads();
+            buf ^= 1;
         }
     }
     // the sum over 32 lanes of each of 32 numbers: halves are exchanged until lane n has number n
@@ -229,29 +271,35 @@ __global__ __launch_bounds__(512) void k_attend_weights(AttendDev a, WeightsDev 
             const float give = upper ? acc[k] : acc[k + width], keep = upper ? acc[k + width] : acc[k];
             acc[k] = keep + __shfl_xor(give, width);
         }
-    // number n is token (n / 16) * 32 + (n / 4 % 4) * 8 + g * 4 + n % 4 of the tile
-    const uint32_t token = n32 / 16 * 32 + (n32 / 4 & 3) * 8 + g * 4 + (n32 & 3);
-    float sum = acc[0];
-    if (by_rows) {
-        sums[wave][token] = sum;
-        __syncthreads();
-        if (wave) return;
-        sum = 0.0f;
-        for (int w = 0; w < 8; w++) sum += sums[w][token];
-    }
-    const int32_t t = t0 + (int32_t)token;
+    // number n is token (n / 16) * 32 + (n / 4 % 4) * 8 + g * 4 + n % 4 of the wavefront's
+    const int32_t t = t0 + (int32_t)(n32 / 16 * 32 + (n32 / 4 & 3) * 8 + g * 4 + (n32 & 3));
     if (t < length) {
         const uint64_t at = (uint64_t)unit * (uint64_t)a.c.capacity + (uint64_t)t;
-        wt.out[at] = (wt.in ? wt.in[at] : 0.0f) + sum;
+        if (wt.parts > 1) wt.part[(uint64_t)part * units * (uint64_t)a.c.capacity + at] = acc[0];
+        else wt.out[at] = (wt.in ? wt.in[at] : 0.0f) + acc[0];
     }
 }
 
-template <int FMT> void launch_weights(const AttendDev &a, const WeightsDev &w, uint32_t head_dim, uint32_t tiles, hipStream_t s)
+// A token to a thread, 256 of a (sequence, K/V head) to a workgroup: the parts' sums, one after the other.
+__global__ __launch_bounds__(256) void k_weights_sum(AttendDev a, WeightsDev wt)
 {
-    const uint32_t by_rows = (uint64_t)a.max_q_len * a.group > 64, per_group = by_rows ? 1 : 4, threads = by_rows ? 512 : 256;
-    const uint32_t per_head = (tiles + per_group - 1) / per_group, blocks = a.n_seqs * a.c.heads * per_head;
-    if (head_dim == 64) hipLaunchKernelGGL((k_attend_weights<FMT, 64>), dim3(blocks), dim3(threads), 0, s, a, w, by_rows);
-    else hipLaunchKernelGGL((k_attend_weights<FMT, 128>), dim3(blocks), dim3(threads), 0, s, a, w, by_rows);
+    const uint32_t units = a.n_seqs * a.c.heads, unit = blockIdx.x % units;
+    const int32_t length = clamped_length(a.c.lengths, unit / a.c.heads, a.c.limit), t = (int32_t)(blockIdx.x / units * 256 + threadIdx.x);
+    if (t >= length) return;
+    const uint64_t at = (uint64_t)unit * (uint64_t)a.c.capacity + (uint32_t)t, apart = (uint64_t)units * (uint64_t)a.c.capacity;
+    float x[kMostParts];
+#pragma unroll
+    for (uint32_t p = 0; p < kMostParts; p++) x[p] = wt.part[min(p, wt.parts - 1) * apart + at];
+    float sum = 0.0f;
+#pragma unroll
+    for (uint32_t p = 0; p < kMostParts; p++) sum += p < wt.parts ? x[p] : 0.0f;
+    wt.out[at] = (wt.in ? wt.in[at] : 0.0f) + sum;
+}
+
+template <int FMT> void launch_weights(const AttendDev &a, const WeightsDev &w, uint32_t head_dim, uint32_t blocks, hipStream_t s)
+{
+    if (head_dim == 64) hipLaunchKernelGGL((k_attend_weights<FMT, 64>), dim3(blocks), dim3(256), 0, s, a, w);
+    else hipLaunchKernelGGL((k_attend_weights<FMT, 128>), dim3(blocks), dim3(256), 0, s, a, w);
 }
 
 }  // namespace
@@ -265,13 +313,14 @@ int launch_attend_join(const AttendDev &a, const WeightsDev &w, uint32_t head_di
     return (int)hipGetLastError();
 }
 
-int launch_attend_weights(const AttendDev &a, const WeightsDev &w, uint32_t format, uint32_t head_dim, int32_t longest, void *stream)
+int launch_attend_weights(const AttendDev &a, const WeightsDev &w, uint32_t format, uint32_t head_dim, void *stream)
 {
-    const uint32_t tiles = (uint32_t)(longest + 63) / 64;
+    const uint32_t units = a.n_seqs * a.c.heads, blocks = units * w.parts * ((uint32_t)(a.c.limit + 255) / 256);
     const hipStream_t s = (hipStream_t)stream;
-    if (format == ZC_FMT_BF16) launch_weights<ZC_FMT_BF16>(a, w, head_dim, tiles, s);
-    else if (format == ZC_FMT_FP8_E4M3) launch_weights<ZC_FMT_FP8_E4M3>(a, w, head_dim, tiles, s);
-    else launch_weights<ZC_FMT_FP8_E5M2>(a, w, head_dim, tiles, s);
+    if (format == ZC_FMT_BF16) launch_weights<ZC_FMT_BF16>(a, w, head_dim, blocks, s);
+    else if (format == ZC_FMT_FP8_E4M3) launch_weights<ZC_FMT_FP8_E4M3>(a, w, head_dim, blocks, s);
+    else launch_weights<ZC_FMT_FP8_E5M2>(a, w, head_dim, blocks, s);
+    if (w.parts > 1) hipLaunchKernelGGL(k_weights_sum, dim3(units * ((uint32_t)(a.c.limit + 255) / 256)), dim3(256), 0, s, a, w);
     return (int)hipGetLastError();
 }
 

@@ -31,12 +31,7 @@ template <int FMT> __device__ __forceinline__ u32x4_t eight_to_half(uint32_t lo,
     return u32x4_t{two_to_half<FMT, false>(lo), two_to_half<FMT, true>(lo), two_to_half<FMT, false>(hi), two_to_half<FMT, true>(hi)};
 }
 
-// Byte offsets in a tile of 64 tokens x D two-byte elements.  Keys: 16-byte piece c of a token.
-template <int D> __device__ __forceinline__ uint32_t key_place(uint32_t token, uint32_t c)
-{
-    return D == 128 ? token * 256 + ((c ^ (token & 15)) << 4) : token * 128 + ((c ^ ((token >> 1) & 7)) << 4);
-}
-// Values: byte offset x inside a token's row, moved in pieces of 64 bytes.
+// Byte offset in a tile of 64 tokens x D two-byte elements of values: byte x of a token's row, moved in pieces of 64 bytes.
 template <int D> __device__ __forceinline__ uint32_t value_place(uint32_t token, uint32_t x)
 {
     return D == 128 ? token * 256 + (x ^ ((token & 3) << 6)) : token * 128 + (x ^ ((token >> 1 & 1) << 6));
