@@ -10,6 +10,8 @@
 // 16 tokens' pieces nor the transposing ones meet in a bank.  Bound by the matrix instructions and the exponentials.
 #include "zc_attend_device.h"
 
+#include <type_traits>
+
 namespace zc {
 
 namespace {
@@ -19,6 +21,7 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr uint32_t kWaves = 4;
 constexpr int kTile = 64;                      // tokens per step
+constexpr int kSchedMatrix = 0x8, kSchedLdsRead = 0x100, kReadsAhead = 6;   // kinds of instructions for __builtin_amdgcn_sched_group_barrier
 constexpr int kHalves = kTile / 32, kStretches = kTile / 16;
 
 template <int FMT> __device__ __forceinline__ f32x16 mma32_values(u32x4_t a, u32x4_t b, f32x16 c)
@@ -113,32 +116,33 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendDev a)
     const uint32_t page_log = a.c.page_shift + (D == 128 ? 7 : 6) + (ES - 1);   // of a page's bytes
     const uint32_t page_mask = (1u << a.c.page_shift) - 1;
     const uint32_t piece = tid % kPieces, row0 = tid / kPieces;
-    int32_t ids = -1, ids_from = begin;                        // lane kStretches * i + h: page of tokens 16 h .. of tile ids_from + i (-1: absent)
+    // lane kStretches * i + h: page of tokens 16 h .. of tile ids_from + i (0 where it is absent), and the bit that says it is there
+    int32_t ids = 0, ids_from = begin;
+    uint64_t present = 0;
     auto fetch_ids = [&](int32_t b) {
         const int32_t mine = b + (int32_t)(lane / kStretches);
         const uint32_t page = ((uint32_t)blocks.at(mine) * kTile + (lane % kStretches) * 16) >> a.c.page_shift;
-        ids = -1;
-        if (mine < end && page < a.c.table_pages) ids = table[page];
-        if ((uint32_t)ids >= a.c.n_pages) ids = -1;
+        int32_t id = -1;
+        if (mine < end && page < a.c.table_pages) id = table[page];
+        const bool there = (uint32_t)id < a.c.n_pages;
+        present = __ballot(there);
+        ids = there ? id : 0;
         ids_from = b;
     };
-    auto there_of = [&](int32_t b) {                           // which of a tile's stretches of 16 tokens are present
-        const int32_t at = (b - ids_from) * kStretches;
-        uint32_t there = 0;
-#pragma unroll
-        for (int h = 0; h < kStretches; h++) there |= __builtin_amdgcn_readlane(ids, at + h) >= 0 ? 1u << h : 0u;
-        return there;
-    };
+    // which of a tile's stretches of 16 tokens are present
+    auto there_of = [&](int32_t b) { return (uint32_t)(present >> ((b - ids_from) * kStretches)) & ((1u << kStretches) - 1); };
     u32x4_t kx[kPasses], vx[kPasses];
-    auto fetch = [&](const uint8_t *pool, int32_t b, u32x4_t (&to)[kPasses]) {
+    const uint32_t mine = (row0 & 15) * (D * ES) + piece * 16;
+    auto fetch = [&](int32_t b) {
         const int32_t at = (b - ids_from) * kStretches;
         const uint32_t t0 = (uint32_t)blocks.at(b) * kTile;
 #pragma unroll
         for (uint32_t p = 0; p < kPasses; p++) {
             const uint32_t first = p * kRowsPerPass + wave * (64 / kPieces);   // the wavefront's first row: its rows lie in one stretch of 16
-            const int32_t page = __builtin_amdgcn_readlane(ids, at + (int32_t)(first / 16));
-            const uint64_t where = ((uint64_t)(uint32_t)max(page, 0) << page_log) + ((t0 + (first & ~15u)) & page_mask) * (D * ES);
-            to[p] = *reinterpret_cast<const u32x4_t *>(pool + where + ((p * kRowsPerPass + row0) & 15) * (D * ES) + piece * 16);
+            const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(ids, at + (int32_t)(first / 16));
+            const uint64_t where = ((uint64_t)page << page_log) + ((t0 + (first & ~15u)) & page_mask) * (D * ES);
+            kx[p] = *reinterpret_cast<const u32x4_t *>(a.c.k + where + mine);
+            vx[p] = *reinterpret_cast<const u32x4_t *>(a.c.v + where + mine);
         }
     };
     // whether every row of the workgroup (of the wavefront) sees every token of a tile
@@ -155,9 +159,8 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendDev a)
             }
         }
     };
-    auto store_values = [&](int32_t b, uint32_t there, uint32_t buf, uint32_t mod3) {
-        const int32_t t0 = blocks.at(b) * kTile;
-        if (__builtin_expect(!whole(t0, there, all_last_min, all_from_max), 0)) {
+    auto store_values = [&](int32_t t0, uint32_t there, bool edge, uint32_t buf, uint32_t mod3) {
+        if (__builtin_expect(edge, 0)) {
             // Tokens that no row sees are zeroed (what they hold is not to be multiplied, not even with 0); of those that only
             // some rows see, elements that are not finite are zeroed too and noted: they are added to the rows that do see them.
 #pragma unroll
@@ -229,15 +232,21 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendDev a)
         }
     };
 
-    auto step = [&](int32_t b, uint32_t there, uint32_t buf, uint32_t mod3) {
-        const int32_t t0 = blocks.at(b) * kTile;
-        // nothing of the tile is for this wavefront's rows
-        if (t0 > last_max || (t0 + kTile <= from_min && t0 >= sinks)) return;
-        const uint8_t *kt = lds[buf][0], *vt = lds[buf][1];
-        Products s;
+    auto multiply = [&](uint32_t buf, Products &s) {
+        const uint8_t *kt = lds[buf][0];
 #pragma unroll
         for (int u = 0; u < KS; u++) multiply_keys(kt, u, s);
-        hide(t0, there, s);
+        // reads of keys run ahead of their products
+        __builtin_amdgcn_sched_group_barrier(kSchedLdsRead, kReadsAhead, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * KS; i++) {
+            __builtin_amdgcn_sched_group_barrier(kSchedMatrix, 1, 0);
+            if (i + kReadsAhead < 2 * KS) __builtin_amdgcn_sched_group_barrier(kSchedLdsRead, 1, 0);
+        }
+    };
+    auto rest = [&](int32_t t0, uint32_t there, bool edge, uint32_t buf, uint32_t mod3, Products &s) {
+        const uint8_t *vt = lds[buf][1];
+        if (__builtin_expect(edge, 0)) hide(t0, there, s);
         raise(top_of(s));
         const float mc = m == kNegInf ? 0.0f : m * c;
         float sum[4] = {0, 0, 0, 0};
@@ -250,7 +259,8 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendDev a)
             if (i & 1) p[i / 8][i / 2 & 3] = pack_weights<FMT>(s.half[i / 16][(i & 15) - 1], e);
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        const uint64_t bad = (uint64_t)uniform(bad_tokens[mod3][0]) | (uint64_t)uniform(bad_tokens[mod3][1]) << 32;
+        uint64_t bad = 0;
+        if (__builtin_expect(edge, 0)) bad = (uint64_t)uniform(bad_tokens[mod3][0]) | (uint64_t)uniform(bad_tokens[mod3][1]) << 32;
         if (__builtin_expect(bad != 0, 0)) {
 #pragma unroll 1
             for (uint32_t n = 0; n < kTile; n++) {
@@ -289,37 +299,44 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendDev a)
             }
     };
 
-    // Two buffers: while a tile is worked on, the next one waits in registers, goes to the other buffer behind the work, and the one
-    // after it is asked for.  (A tile's products made beside the exponentials of the one before it, in 32 or 64 tokens, was slower:
-    // 940 and 966 us for two prompts of 8,192 and 7,001 tokens against 905.  Their registers leave none to read LDS ahead with.)
+    // Two buffers: the next tile is asked for when a tile's products have been made, waits in registers while their weights are
+    // worked out and the values multiplied, and goes to the other buffer.  (Asked for a whole step ahead it took the registers that
+    // reading keys ahead needs: 905 - 920 us for two prompts of 8,192 and 7,001 tokens.  A tile's products made beside the
+    // exponentials of the one before it, in 32 or 64 tokens: 940 and 966 us, for the same reason.)
     if (begin < end) {
         fetch_ids(begin);
         uint32_t there = there_of(begin), mod3 = 0;
-        fetch(a.c.k, begin, kx);
-        fetch(a.c.v, begin, vx);
+        int32_t t0 = blocks.at(begin) * kTile;
+        bool edge = !whole(t0, there, all_last_min, all_from_max);             // some row of the workgroup does not see all of the tile
+        fetch(begin);
         store_keys(0);
-        store_values(begin, there, 0, 0);
-        const int32_t second = min(begin + 1, end - 1);
-        uint32_t there_next = there_of(second);
-        fetch(a.c.k, second, kx);
-        fetch(a.c.v, second, vx);
+        store_values(t0, there, edge, 0, 0);
         __syncthreads();
-        for (int32_t b = begin; b < end; b++) {
-            const uint32_t buf = (uint32_t)(b - begin) & 1, next3 = mod3 == 2 ? 0 : mod3 + 1;
-            step(b, there, buf, mod3);
-            if (b + 1 < end) {
-                store_keys(buf ^ 1);
-                store_values(b + 1, there_next, buf ^ 1, next3);
-                if (tid < kHalves) bad_tokens[next3 == 2 ? 0 : next3 + 1][tid] = 0;    // last read before the barrier that began this step
-                there = there_next;
-                const int32_t later = min(b + 2, end - 1);                             // (the last one is asked for again: no branch, no wait)
-                if (later - ids_from >= 64 / kStretches) fetch_ids(later);
-                there_next = there_of(later);
-                fetch(a.c.k, later, kx);
-                fetch(a.c.v, later, vx);
-            }
+        auto step = [&](int32_t b, auto buffer) {
+            constexpr uint32_t buf = decltype(buffer)::value;
+            const uint32_t next3 = mod3 == 2 ? 0 : mod3 + 1;
+            const int32_t later = min(b + 1, end - 1);                         // (the last one is asked for again: no branch, no wait)
+            const bool ours = t0 <= last_max && (t0 + kTile > from_min || t0 < sinks);  // else nothing of the tile is for this wavefront's rows
+            if (later - ids_from >= 64 / kStretches) fetch_ids(later);
+            const uint32_t there_next = there_of(later);
+            const int32_t t0_next = blocks.at(later) * kTile;
+            const bool edge_next = !whole(t0_next, there_next, all_last_min, all_from_max);
+            Products s;
+            if (ours) multiply(buf, s);
+            fetch(later);
+            if (ours) rest(t0, there, edge, buf, mod3, s);
+            store_keys(buf ^ 1);
+            store_values(t0_next, there_next, edge_next, buf ^ 1, next3);
+            if (tid < kHalves) bad_tokens[next3 == 2 ? 0 : next3 + 1][tid] = 0;        // last read before the barrier that began this step
+            there = there_next;
+            t0 = t0_next;
+            edge = edge_next;
             __syncthreads();
             mod3 = next3;
+        };
+        for (int32_t b = begin; b < end; b += 2) {
+            step(b, std::integral_constant<uint32_t, 0>());
+            if (b + 1 < end) step(b + 1, std::integral_constant<uint32_t, 1>());
         }
     }
 
