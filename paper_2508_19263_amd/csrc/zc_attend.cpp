@@ -59,7 +59,8 @@ struct Pass {
 Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_splits, bool only)
 {
     Pass p;
-    p.many = rows > 32;
+    // up to 64 rows k_attend_few reads a cache twice: 35 rows of six caches with a window of 2,048, 17.0 against 18.6 us in k_attend_many
+    p.many = rows > 64;
     p.tiles = p.many || rows <= 16 ? 1 : 2;
     const uint64_t per_block = p.tiles * (p.many ? 128 : 16);
     p.row_blocks = (uint32_t)((rows + per_block - 1) / per_block);
@@ -161,7 +162,7 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
     a.splits = p.own_pass.splits;
     a.row_blocks = p.own_pass.row_blocks;
     a.direct = p.slots == 1;
-    if (p.own_pass.blocks > 0x7FFFFFFFu || p.pre_pass.blocks > 0x7FFFFFFFu) return ZC_ERR_INVALID_ARG;
+    if (p.own_pass.blocks + p.pre_pass.blocks > 0x7FFFFFFFu) return ZC_ERR_INVALID_ARG;
     if (p.slots > 1) {
         const uint64_t rows = (uint64_t)a.n_tokens * a.q_heads * p.slots;
         p.part_o_bytes = rows * cache->head_dim * 4;
@@ -208,8 +209,13 @@ zc_status attend(const zc_attend_args *x, const zc_kv_cache *prefix, const zc_kv
     }
     const WeightsDev w = {x->d_weights_in, x->d_weights_out, p.weight_parts > 1 ? (float *)((uint8_t *)d_ws + p.weights_at) : nullptr, p.weight_parts};
     if (x->n_tokens) {
-        if (shared) LAUNCH_TRY(launch_pass(p.pre, p.pre_pass, *cache, stream));
-        LAUNCH_TRY(launch_pass(p.own, p.own_pass, *cache, stream));
+        if (shared && !p.own_pass.many && p.own_pass.row_blocks == 1) {
+            const uint32_t tiles = p.pre_pass.many || p.own_pass.tiles > p.pre_pass.tiles ? p.own_pass.tiles : p.pre_pass.tiles;
+            LAUNCH_TRY(launch_attend_shared(p.pre, p.own, cache->format, cache->head_dim, p.pre_pass.many, tiles, stream));
+        } else {
+            if (shared) LAUNCH_TRY(launch_pass(p.pre, p.pre_pass, *cache, stream));
+            LAUNCH_TRY(launch_pass(p.own, p.own_pass, *cache, stream));
+        }
         if (p.slots > 1 || p.logits) LAUNCH_TRY(launch_attend_join(p.own, w, cache->head_dim, p.slots, stream));
     }
     if (x->d_weights_out && !p.logits) LAUNCH_TRY(launch_attend_weights(p.own, w, cache->format, cache->head_dim, stream));

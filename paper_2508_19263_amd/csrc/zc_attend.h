@@ -61,6 +61,8 @@ struct EvictDev {
 // tiles: of 16 rows in k_attend_few, of 128 in k_attend_many
 int launch_attend_few(const AttendDev &a, uint32_t format, uint32_t head_dim, uint32_t tiles, void *stream);
 int launch_attend_many(const AttendDev &a, uint32_t format, uint32_t head_dim, void *stream);
+// both passes of a shared prefix; tiles: of 16 rows, of the own pass and of the prefix where that is not pre_many
+int launch_attend_shared(const AttendDev &pre, const AttendDev &own, uint32_t format, uint32_t head_dim, bool pre_many, uint32_t tiles, void *stream);
 // slots > 1: joins them; a.logits: adds up the weights from them
 int launch_attend_join(const AttendDev &a, const WeightsDev &w, uint32_t head_dim, uint32_t slots, void *stream);
 int launch_attend_weights(const AttendDev &a, const WeightsDev &w, uint32_t format, uint32_t head_dim, void *stream);

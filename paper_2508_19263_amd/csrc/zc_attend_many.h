@@ -1,0 +1,381 @@
+// Attention over K/V pages for many query rows (prompts, batches under one prefix): the body of k_attend_many, and of
+// the part of k_attend_shared that is like it.
+//
+// A workgroup of four wavefronts takes 128 rows of one K/V head, 32 to a wavefront, and goes over the tokens
+// they see 64 at a time.  A tile of keys and values is brought to LDS once for all of them, in the type it is multiplied in (FP8
+// is converted on the way: keys to BF16, values to half precision), into one of two buffers while the other is worked on:
+//   S^T = K Q^T     32 tokens x 32 rows per instruction; a lane holds one row's products with half of the tile's tokens
+//   O^T += V^T P^T  a lane's weights are its operand as they stand; V comes from LDS through transposing reads, four tokens
+//                   of a dimension at a time, which are exactly the runs of four tokens that S^T leaves in a lane
+// The bank a 16-byte piece of a key (64-byte piece of a value) lies in depends on its token too, so that neither the reads of
+// 16 tokens' pieces nor the transposing ones meet in a bank.  Bound by the matrix instructions and the exponentials.
+#pragma once
+#include "zc_attend_device.h"
+
+#include <type_traits>
+
+namespace zc {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr uint32_t kManyWaves = 4;
+constexpr int kTile = 64;                      // tokens per step
+constexpr int kSchedMatrix = 0x8, kSchedLdsRead = 0x100, kReadsAhead = 6;   // kinds of instructions for __builtin_amdgcn_sched_group_barrier
+constexpr int kHalves = kTile / 32, kStretches = kTile / 16;
+
+template <int FMT> __device__ __forceinline__ f32x16 mma32_values(u32x4_t a, u32x4_t b, f32x16 c)
+{
+    if constexpr (FMT == ZC_FMT_BF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, a), __builtin_bit_cast(halfx8, b), c, 0, 0, 0);
+}
+template <int FMT> __device__ __forceinline__ u32x4_t eight_to_half(uint32_t lo, uint32_t hi)
+{
+    return u32x4_t{two_to_half<FMT, false>(lo), two_to_half<FMT, true>(lo), two_to_half<FMT, false>(hi), two_to_half<FMT, true>(hi)};
+}
+
+// Byte offset in a tile of 64 tokens x D two-byte elements of values: byte x of a token's row, moved in pieces of 64 bytes.
+template <int D> __device__ __forceinline__ uint32_t value_place(uint32_t token, uint32_t x)
+{
+    return D == 128 ? token * 256 + (x ^ ((token & 3) << 6)) : token * 128 + (x ^ ((token >> 1 & 1) << 6));
+}
+
+template <int D> struct ManyShared {
+    alignas(1024) uint8_t lds[2][2][kTile * D * 2];            // [buffer][keys, values]
+    uint32_t bad_tokens[3][kHalves];                           // [tile modulo 3]: tokens with an element that is not finite
+    int32_t limits[kManyWaves][4];
+};
+
+template <int FMT, int D>
+__device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, ManyShared<D> &shared)
+{
+    constexpr int ES = PageElem<FMT>::BYTES, KS = D / 16, DT = D / 32;
+    constexpr uint32_t kPieces = D * ES / 16;                  // 16-byte pieces of a stored row
+    constexpr uint32_t kRowsPerPass = 256 / kPieces, kPasses = kTile / kRowsPerPass;
+    auto &lds = shared.lds;
+    auto &bad_tokens = shared.bad_tokens;
+    auto &limits = shared.limits;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n32 = lane & 31, g = lane >> 5;
+    const uint32_t units = (a.shared ? 1 : a.n_seqs) * a.c.heads;
+    const uint32_t unit = id % units;                          // neighbours on an XCD work on the same few heads
+    id /= units;
+    const uint32_t split = id % a.splits, row_block = a.row_blocks - 1 - id / a.splits;    // the long rows of a prompt first
+    const uint32_t head = unit % a.c.heads, seq = unit / a.c.heads;
+
+    const int32_t prefix = prefix_tokens(a), offset = a.shared ? 0 : prefix;
+    const int32_t length = clamped_length(a.c.lengths, seq, a.c.limit);
+    const Span span = rows_span(a, seq);
+    const uint32_t first_row = row_block * (kManyWaves * 32);
+    if ((uint64_t)first_row >= (uint64_t)span.count * a.group) return;         // the whole workgroup
+    const Row row = row_of(a, span, head, first_row + wave * 32 + n32, prefix, offset, length);
+    int32_t last_min = INT32_MAX, last_max = -1, from_min = INT32_MAX, from_max = INT32_MIN;
+    if (row.token >= 0) {
+        last_min = last_max = row.sight.last;
+        from_min = from_max = row.sight.from;
+    }
+    last_min = min_over_wave(last_min);
+    last_max = max_over_wave(last_max);
+    from_min = min_over_wave(from_min);
+    from_max = max_over_wave(from_max);
+    if (lane == 0) { limits[wave][0] = last_min; limits[wave][1] = last_max; limits[wave][2] = from_min; limits[wave][3] = from_max; }
+    if (tid < 3 * kHalves) (&bad_tokens[0][0])[tid] = 0;
+    __syncthreads();
+    // the same of the whole workgroup
+    int32_t all_last_min = INT32_MAX, all_last_max = -1, all_from_min = INT32_MAX, all_from_max = INT32_MIN;
+    for (uint32_t w = 0; w < kManyWaves; w++) {
+        all_last_min = min(all_last_min, uniform(limits[w][0]));
+        all_last_max = max(all_last_max, uniform(limits[w][1]));
+        all_from_min = min(all_from_min, uniform(limits[w][2]));
+        all_from_max = max(all_from_max, uniform(limits[w][3]));
+    }
+    const int32_t sinks = (int32_t)a.sinks - offset;
+    const Blocks blocks = seen_blocks(kTile, all_last_max, all_from_min, sinks);
+    const int32_t per_split = (blocks.count + (int32_t)a.splits - 1) / (int32_t)a.splits;
+    const int32_t begin = min((int32_t)split * per_split, blocks.count), end = min(begin + per_split, blocks.count);
+
+    const float k_scale = a.c.k_scales ? a.c.k_scales[unit] : 1.0f, v_scale = a.c.v_scales ? a.c.v_scales[unit] : 1.0f;
+    const float signed_c = a.scale * k_scale * kLog2e;
+    // logits in base 2; a negative factor goes to the queries' signs, and 0 is made one that takes any product to 0 but minus infinity
+    const float c = fmaxf(fabsf(signed_c), 1e-30f);
+    const uint32_t flip = signed_c < 0 ? 0x80008000u : 0u;
+    u32x4_t q[KS];
+    {
+        const uint16_t *from = a.q + (uint64_t)max(row.token, 0) * a.q_token_stride + (uint64_t)row.q_head * a.q_head_stride;
+#pragma unroll
+        for (int u = 0; u < KS; u++) {
+            u32x4_t x = {0, 0, 0, 0};
+            if (row.token >= 0) x = *reinterpret_cast<const u32x4_t *>(from + u * 16 + g * 8);
+            q[u] = x ^ flip;
+        }
+    }
+    float m = kNegInf, l = 0.0f;                               // maximum of the bare products; sum over this lane's tokens
+    f32x16 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; d++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) o[d][i] = 0.0f;
+
+    // ---- bringing tiles: a thread takes piece `piece` of rows row0 + pass * kRowsPerPass of keys and values
+    const int32_t *table = a.c.table + (uint64_t)unit * a.c.table_pages;
+    const uint32_t page_log = a.c.page_shift + (D == 128 ? 7 : 6) + (ES - 1);   // of a page's bytes
+    const uint32_t page_mask = (1u << a.c.page_shift) - 1;
+    const uint32_t piece = tid % kPieces, row0 = tid / kPieces;
+    // lane kStretches * i + h: page of tokens 16 h .. of tile ids_from + i (0 where it is absent), and the bit that says it is there
+    int32_t ids = 0, ids_from = begin;
+    uint64_t present = 0;
+    auto fetch_ids = [&](int32_t b) {
+        const int32_t mine = b + (int32_t)(lane / kStretches);
+        const uint32_t page = ((uint32_t)blocks.at(mine) * kTile + (lane % kStretches) * 16) >> a.c.page_shift;
+        int32_t id = -1;
+        if (mine < end && page < a.c.table_pages) id = table[page];
+        const bool there = (uint32_t)id < a.c.n_pages;
+        present = __ballot(there);
+        ids = there ? id : 0;
+        ids_from = b;
+    };
+    // which of a tile's stretches of 16 tokens are present
+    auto there_of = [&](int32_t b) { return (uint32_t)(present >> ((b - ids_from) * kStretches)) & ((1u << kStretches) - 1); };
+    u32x4_t kx[kPasses], vx[kPasses];
+    const uint32_t mine = (row0 & 15) * (D * ES) + piece * 16;
+    auto fetch = [&](int32_t b) {
+        const int32_t at = (b - ids_from) * kStretches;
+        const uint32_t t0 = (uint32_t)blocks.at(b) * kTile;
+#pragma unroll
+        for (uint32_t p = 0; p < kPasses; p++) {
+            const uint32_t first = p * kRowsPerPass + wave * (64 / kPieces);   // the wavefront's first row: its rows lie in one stretch of 16
+            const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(ids, at + (int32_t)(first / 16));
+            const uint64_t where = ((uint64_t)page << page_log) + ((t0 + (first & ~15u)) & page_mask) * (D * ES);
+            kx[p] = *reinterpret_cast<const u32x4_t *>(a.c.k + where + mine);
+            vx[p] = *reinterpret_cast<const u32x4_t *>(a.c.v + where + mine);
+        }
+    };
+    // whether every row of the workgroup (of the wavefront) sees every token of a tile
+    auto whole = [&](int32_t t0, uint32_t there, int32_t lmin, int32_t fmax) { return there == (1u << kStretches) - 1 && t0 + kTile - 1 <= lmin && (t0 >= fmax || t0 + kTile <= sinks); };
+    auto store_keys = [&](uint32_t buf) {
+        uint8_t *kt = lds[buf][0];
+#pragma unroll
+        for (uint32_t p = 0; p < kPasses; p++) {
+            const uint32_t r = p * kRowsPerPass + row0;
+            if constexpr (FMT == ZC_FMT_BF16) *reinterpret_cast<u32x4_t *>(kt + key_place<D>(r, piece)) = kx[p];
+            else {
+                *reinterpret_cast<u32x4_t *>(kt + key_place<D>(r, piece * 2)) = eight_to_bf16<FMT>(kx[p][0], kx[p][1]);
+                *reinterpret_cast<u32x4_t *>(kt + key_place<D>(r, piece * 2 + 1)) = eight_to_bf16<FMT>(kx[p][2], kx[p][3]);
+            }
+        }
+    };
+    auto store_values = [&](int32_t t0, uint32_t there, bool edge, uint32_t buf, uint32_t mod3) {
+        if (__builtin_expect(edge, 0)) {
+            // Tokens that no row sees are zeroed (what they hold is not to be multiplied, not even with 0); of those that only
+            // some rows see, elements that are not finite are zeroed too and noted: they are added to the rows that do see them.
+#pragma unroll
+            for (uint32_t p = 0; p < kPasses; p++) {
+                const uint32_t r = p * kRowsPerPass + row0;
+                const int32_t t = t0 + (int32_t)r;
+                const bool used = (there >> (r / 16) & 1) && seen(Sight{all_last_max, all_from_min, sinks}, t);
+                const bool by_all = seen(Sight{all_last_min, all_from_max, sinks}, t);
+                uint32_t wild = 0;
+#pragma unroll
+                for (int w = 0; w < 4; w++) {
+                    vx[p][w] = used ? vx[p][w] : 0u;
+                    const uint32_t x = by_all ? 0u : nonfinite_mask<FMT>(vx[p][w]);
+                    wild |= x;
+                    vx[p][w] &= ~x;
+                }
+                if (wild) atomicOr(&bad_tokens[mod3][r / 32], 1u << (r & 31));
+            }
+        }
+        uint8_t *vt = lds[buf][1];
+#pragma unroll
+        for (uint32_t p = 0; p < kPasses; p++) {
+            const uint32_t r = p * kRowsPerPass + row0;
+            if constexpr (FMT == ZC_FMT_BF16) *reinterpret_cast<u32x4_t *>(vt + value_place<D>(r, piece * 16)) = vx[p];
+            else {
+                *reinterpret_cast<u32x4_t *>(vt + value_place<D>(r, piece * 32)) = eight_to_half<FMT>(vx[p][0], vx[p][1]);
+                *reinterpret_cast<u32x4_t *>(vt + value_place<D>(r, piece * 32 + 16)) = eight_to_half<FMT>(vx[p][2], vx[p][3]);
+            }
+        }
+    };
+
+    // Product 16 h + i of a tile is the lane's row with token 32 h + (i / 4) * 8 + g * 4 + i % 4.
+    struct Products { f32x16 half[kHalves]; };
+    // one of the steps of S^T = K Q^T: 16 dimensions
+    auto multiply_keys = [&](const uint8_t *kt, int u, Products &s) {
+#pragma unroll
+        for (int h = 0; h < kHalves; h++) {
+            const u32x4_t key = *reinterpret_cast<const u32x4_t *>(kt + key_place<D>(h * 32 + n32, u * 2 + g));
+            const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+            s.half[h] = mma32_keys(key, q[u], u ? s.half[h] : zero);
+        }
+    };
+    auto hide = [&](int32_t t0, uint32_t there, Products &s) {      // what the row does not see
+        if (__builtin_expect(!whole(t0, there, last_min, from_max), 0)) {
+            uint32_t mask = 0;
+#pragma unroll
+            for (int n = 0; n < kTile / 8; n++) mask |= (seen_of_four(row.sight, t0 + n * 8 + (int32_t)g * 4) & (there >> (n / 2) & 1 ? 15u : 0u)) << (n * 4);
+#pragma unroll
+            for (int i = 0; i < kTile / 2; i++) {
+                const uint32_t keep = bit_as_mask(mask, i);
+                s.half[i / 16][i & 15] = __uint_as_float((bits(s.half[i / 16][i & 15]) & keep) | (bits(kNegInf) & ~keep));
+            }
+        }
+    };
+    auto top_of = [&](const Products &s) {
+        float top = s.half[0][0];
+#pragma unroll
+        for (int i = 1; i < kTile / 2; i++) top = fmaxf(top, s.half[i / 16][i & 15]);
+        return max_over_32(top);
+    };
+    auto raise = [&](float top) {                              // the maximum, where a product has left it far behind
+        if (__builtin_expect(__any((top - m) * c > kSlack), 0)) {
+            const float now = fmaxf(m, top);
+            const float f = m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f((m - now) * c);
+            m = now;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DT; d++) o[d] *= f;
+        }
+    };
+
+    auto multiply = [&](uint32_t buf, Products &s) {
+        const uint8_t *kt = lds[buf][0];
+        // Of the two wavefronts of a SIMD the one at its matrix instructions goes first, and the other one's arithmetic fills in: two
+        // prompts 885 -> 870 us, pieces of prompts 158 -> 149 us (the other way round 898 and 162 us).
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int u = 0; u < KS; u++) multiply_keys(kt, u, s);
+        // reads of keys run ahead of their products
+        __builtin_amdgcn_sched_group_barrier(kSchedLdsRead, kReadsAhead, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * KS; i++) {
+            __builtin_amdgcn_sched_group_barrier(kSchedMatrix, 1, 0);
+            if (i + kReadsAhead < 2 * KS) __builtin_amdgcn_sched_group_barrier(kSchedLdsRead, 1, 0);
+        }
+    };
+    auto rest = [&](int32_t t0, uint32_t there, bool edge, uint32_t buf, uint32_t mod3, Products &s) {
+        const uint8_t *vt = lds[buf][1];
+        if (__builtin_expect(edge, 0)) hide(t0, there, s);
+        raise(top_of(s));
+        const float mc = m == kNegInf ? 0.0f : m * c;
+        float sum[4] = {0, 0, 0, 0};
+        u32x4_t p[kStretches];
+#pragma unroll
+        for (int i = 0; i < kTile / 2; i++) {
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s.half[i / 16][i & 15], c, -mc));        // (0 for the products hidden above)
+            s.half[i / 16][i & 15] = e;
+            sum[i & 3] += e;
+            if (i & 1) p[i / 8][i / 2 & 3] = pack_weights<FMT>(s.half[i / 16][(i & 15) - 1], e);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        uint64_t bad = 0;
+        if (__builtin_expect(edge, 0)) bad = (uint64_t)uniform(bad_tokens[mod3][0]) | (uint64_t)uniform(bad_tokens[mod3][1]) << 32;
+        if (__builtin_expect(bad != 0, 0)) {
+#pragma unroll 1
+            for (uint32_t n = 0; n < kTile; n++) {
+                if (!(bad >> n & 1)) continue;
+                const uint32_t i = (n >> 5) * 16 + (n & 3) + (n >> 3 & 3) * 4, gg = n >> 2 & 1;        // product i, in the lanes of group gg
+                uint32_t word = p[0][0];
+#pragma unroll
+                for (uint32_t k = 1; k < kTile / 4; k++) word = i / 2 == k ? p[k / 4][k & 3] : word;
+                word = (uint32_t)__shfl((int)word, (int)(n32 + gg * 32)) >> (i & 1) * 16 & 0xFFFFu;
+                const float weight = FMT == ZC_FMT_BF16 ? __uint_as_float(word << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)word);
+                const int32_t tok = t0 + (int32_t)n;
+                const bool mine = seen(row.sight, tok);
+                const uint8_t *from = a.c.v + ((uint64_t)(uint32_t)max(table[(uint32_t)tok >> a.c.page_shift], 0) << page_log) + ((uint32_t)tok & page_mask) * (D * ES);
+#pragma unroll
+                for (int d = 0; d < DT; d++)
+#pragma unroll
+                    for (int kk = 0; kk < 16; kk += 4) {
+#pragma unroll
+                        for (int k = kk; k < kk + 4; k++) {
+                            const float x = element<FMT>(from + (d * 32 + (k / 4) * 8 + (int)g * 4 + (k & 3)) * ES);
+                            o[d][k] += mine && !(fabsf(x) < __builtin_inff()) ? weight * x : 0.0f;
+                        }
+                        __builtin_amdgcn_sched_barrier(0);       // a few at a time: this hardly ever runs and is to cost no registers
+                    }
+            }
+        }
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int k = 0; k < kStretches; k++)
+#pragma unroll
+            for (int d = 0; d < DT; d++) {
+                // lanes of a group of 16: four tokens, four 8-byte pieces of 16 dimensions
+                const uint32_t tok = k * 16 + g * 4 + (lane >> 2 & 3), x = d * 64 + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+                const u32x2 lw = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + value_place<D>(tok, x))));
+                const u32x2 hw = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + value_place<D>(tok + 8, x))));
+                o[d] = mma32_values<FMT>(u32x4_t{lw[0], lw[1], hw[0], hw[1]}, p[k], o[d]);
+            }
+    };
+
+    // Two buffers: the next tile is asked for when a tile's products have been made, waits in registers while their weights are
+    // worked out and the values multiplied, and goes to the other buffer.  (Asked for a whole step ahead it took the registers that
+    // reading keys ahead needs: 905 - 920 us for two prompts of 8,192 and 7,001 tokens.  A tile's products made beside the
+    // exponentials of the one before it, in 32 or 64 tokens: 940 and 966 us, for the same reason.)
+    if (begin < end) {
+        fetch_ids(begin);
+        uint32_t there = there_of(begin), mod3 = 0;
+        int32_t t0 = blocks.at(begin) * kTile;
+        bool edge = !whole(t0, there, all_last_min, all_from_max);             // some row of the workgroup does not see all of the tile
+        fetch(begin);
+        store_keys(0);
+        store_values(t0, there, edge, 0, 0);
+        __syncthreads();
+        auto step = [&](int32_t b, auto buffer) {
+            constexpr uint32_t buf = decltype(buffer)::value;
+            const uint32_t next3 = mod3 == 2 ? 0 : mod3 + 1;
+            const int32_t later = min(b + 1, end - 1);                         // (the last one is asked for again: no branch, no wait)
+            const bool ours = t0 <= last_max && (t0 + kTile > from_min || t0 < sinks);  // else nothing of the tile is for this wavefront's rows
+            if (later - ids_from >= 64 / kStretches) fetch_ids(later);
+            const uint32_t there_next = there_of(later);
+            const int32_t t0_next = blocks.at(later) * kTile;
+            const bool edge_next = !whole(t0_next, there_next, all_last_min, all_from_max);
+            Products s;
+            if (ours) multiply(buf, s);
+            __builtin_amdgcn_s_setprio(0);
+            fetch(later);
+            if (ours) rest(t0, there, edge, buf, mod3, s);
+            __builtin_amdgcn_s_setprio(0);
+            store_keys(buf ^ 1);
+            store_values(t0_next, there_next, edge_next, buf ^ 1, next3);
+            if (tid < kHalves) bad_tokens[next3 == 2 ? 0 : next3 + 1][tid] = 0;        // last read before the barrier that began this step
+            there = there_next;
+            t0 = t0_next;
+            edge = edge_next;
+            __syncthreads();
+            mod3 = next3;
+        };
+        for (int32_t b = begin; b < end; b += 2) {
+            step(b, std::integral_constant<uint32_t, 0>());
+            if (b + 1 < end) step(b + 1, std::integral_constant<uint32_t, 1>());
+        }
+    }
+
+    // ---- results: a lane has 4 consecutive dimensions at a time
+    if (row.token < 0) return;
+    const float sum = sum_over_32(l);
+    const float top = m == kNegInf ? kNegInf : m * c;
+    const uint64_t at = (uint64_t)row.token * a.q_heads + row.q_head;
+    if (a.direct) {
+        const float inv = m == kNegInf ? 0.0f : v_scale / sum;
+        uint16_t *to = a.out + (uint64_t)row.token * a.out_token_stride + (uint64_t)row.q_head * a.out_head_stride + g * 4;
+#pragma unroll
+        for (int d = 0; d < DT; d++)
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const u32x2 w = {pack_bf16(o[d][k * 4] * inv, o[d][k * 4 + 1] * inv), pack_bf16(o[d][k * 4 + 2] * inv, o[d][k * 4 + 3] * inv)};
+                *reinterpret_cast<u32x2 *>(to + d * 32 + k * 8) = w;
+            }
+        if (a.lse && g == 0) a.lse[at] = m == kNegInf ? kNegInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    } else {
+        const uint64_t slot = (uint64_t)(a.first_slot + split) * a.n_tokens * a.q_heads + at;
+        float *to = a.part_o + slot * D + g * 4;
+#pragma unroll
+        for (int d = 0; d < DT; d++)
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                *reinterpret_cast<f32x4 *>(to + d * 32 + k * 8) = f32x4{o[d][k * 4] * v_scale, o[d][k * 4 + 1] * v_scale, o[d][k * 4 + 2] * v_scale, o[d][k * 4 + 3] * v_scale};
+        if (g == 0) { a.part_ml[slot * 2] = top; a.part_ml[slot * 2 + 1] = sum; }
+    }
+}
+
+}  // namespace zc
