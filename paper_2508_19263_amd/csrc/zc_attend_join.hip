@@ -183,39 +183,48 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendDev a, WeightsD
 #pragma unroll
     for (int i = 0; i < 32; i++) acc[i] = 0.0f;
 
-    // this thread's rows of the next step: query token `i` of the sequence, head `h` of the group; it takes a 16-byte piece of each
+    // This thread takes a 16-byte piece of some rows of each step, and (the first 64) what goes with one of them.  A row is query token
+    // `i` of the sequence, head `h` of the group; both and the place of the row are carried from step to step.
     const uint32_t piece = tid % kPieces, row0 = tid / kPieces, step_i = step / a.group, step_h = step % a.group;
-    uint32_t i[kPasses], h[kPasses];
+    const int64_t q_token = (int64_t)a.q_token_stride, q_head = (int64_t)a.q_head_stride, back = q_token - (int64_t)a.group * q_head;
+    const uint16_t *const q0 = a.q + (int64_t)span.first * q_token + (int64_t)(head * a.group) * q_head;        // the first row of all
+    uint32_t i[kPasses], h[kPasses], my_i = (first_row + tid) / a.group, my_h = (first_row + tid) % a.group;
+    const uint16_t *from[kPasses];
 #pragma unroll
     for (uint32_t p = 0; p < kPasses; p++) {
         const uint32_t r = first_row + p * kRowsPerPass + row0;
         i[p] = r / a.group;
         h[p] = r % a.group;
+        from[p] = q0 + (int64_t)i[p] * q_token + (int64_t)h[p] * q_head;
     }
+    const int64_t step_q = (int64_t)step_i * q_token + (int64_t)step_h * q_head;
     u32x4_t x[kPasses];
-    float lse[kPasses];
-    int32_t position[kPasses];
+    float my_lse = kNegInf;
+    int32_t my_position = 0;
     auto fetch = [&]() {
 #pragma unroll
         for (uint32_t p = 0; p < kPasses; p++) {
-            const bool valid = (int32_t)i[p] < end;
-            const uint32_t tok = (uint32_t)span.first + (valid ? i[p] : (uint32_t)first), q_head = head * a.group + h[p];
-            x[p] = *reinterpret_cast<const u32x4_t *>(a.q + (uint64_t)tok * a.q_token_stride + (uint64_t)q_head * a.q_head_stride + piece * 8);
-            const float v = a.lse[(uint64_t)tok * a.q_heads + q_head];
-            lse[p] = valid && v != kNegInf ? v * -kLog2e : kNegInf;
-            position[p] = before + (int32_t)i[p];
+            const uint16_t *row = (int32_t)i[p] < end ? from[p] : q0;          // (behind the last row: some row, which gives nothing)
+            x[p] = *reinterpret_cast<const u32x4_t *>(row + piece * 8);
             i[p] += step_i;
             h[p] += step_h;
-            if (h[p] >= a.group) { h[p] -= a.group; i[p]++; }
+            from[p] += step_q;
+            if (h[p] >= a.group) { h[p] -= a.group; i[p]++; from[p] += back; }
+        }
+        if (tid < kRows) {
+            const bool valid = (int32_t)my_i < end;
+            const float v = valid ? a.lse[(uint64_t)((uint32_t)span.first + my_i) * a.q_heads + head * a.group + my_h] : kNegInf;
+            my_lse = v != kNegInf ? v * -kLog2e : kNegInf;
+            my_position = before + (int32_t)my_i;
+            my_i += step_i;
+            my_h += step_h;
+            if (my_h >= a.group) { my_h -= a.group; my_i++; }
         }
     };
     auto store = [&](uint32_t buf) {
 #pragma unroll
-        for (uint32_t p = 0; p < kPasses; p++) {
-            const uint32_t r = p * kRowsPerPass + row0;
-            *reinterpret_cast<u32x4_t *>(lds[buf] + key_place<D>(r, piece)) = x[p] ^ flip;
-            if (piece == 0) { minus_lse[buf][r] = lse[p]; positions[buf][r] = position[p]; }
-        }
+        for (uint32_t p = 0; p < kPasses; p++) *reinterpret_cast<u32x4_t *>(lds[buf] + key_place<D>(p * kRowsPerPass + row0, piece)) = x[p] ^ flip;
+        if (tid < kRows) { minus_lse[buf][tid] = my_lse; positions[buf][tid] = my_position; }
     };
     auto add_up = [&](uint32_t buf) {
 #pragma unroll
