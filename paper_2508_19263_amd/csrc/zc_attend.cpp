@@ -12,6 +12,7 @@ namespace zc {
 namespace {
 
 constexpr uint32_t kMaxTokens = 1u << 30;      // positions are signed 32-bit numbers in the kernels, sums of two included
+constexpr uint64_t kMaxBlocks = (1u << 24) - 1;   // of 256 threads: HIP launches fewer than 2^32
 constexpr uint32_t kMaxSlots = 64;             // parts of one row: k_attend_join holds one per lane
 
 bool aligned4(const void *p) { return ((uintptr_t)p & 3) == 0; }
@@ -25,7 +26,7 @@ zc_status check_cache(const zc_kv_cache *c, PagesDev *out)
     if (c->page_tokens < 16 || c->page_tokens > 65536 || (c->page_tokens & (c->page_tokens - 1))) return ZC_ERR_INVALID_ARG;
     if (!c->n_seqs || !c->n_heads || !c->table_pages || !c->n_pages || c->n_pages > 0x7FFFFFFFu) return ZC_ERR_INVALID_ARG;
     const uint64_t capacity = (uint64_t)c->table_pages * c->page_tokens;
-    if (capacity >= kMaxTokens || (uint64_t)c->n_seqs * c->n_heads > 0x3FFFFFFu) return ZC_ERR_INVALID_ARG;
+    if (capacity >= kMaxTokens || (uint64_t)c->n_seqs * c->n_heads > (kMaxBlocks >> 2)) return ZC_ERR_INVALID_ARG;     // (k_evict_select has 1,024 threads for each)
     if (!c->d_k_pages || !c->d_v_pages || !c->d_table || !c->d_lengths) return ZC_ERR_INVALID_ARG;
     if (!aligned16(c->d_k_pages) || !aligned16(c->d_v_pages) || !aligned4(c->d_table) || !aligned4(c->d_lengths) ||
         !aligned4(c->d_k_scales) || !aligned4(c->d_v_scales)) return ZC_ERR_INVALID_ARG;
@@ -162,7 +163,7 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
     a.splits = p.own_pass.splits;
     a.row_blocks = p.own_pass.row_blocks;
     a.direct = p.slots == 1;
-    if (p.own_pass.blocks + p.pre_pass.blocks > 0x7FFFFFFFu) return ZC_ERR_INVALID_ARG;
+    if (p.own_pass.blocks + p.pre_pass.blocks > kMaxBlocks) return ZC_ERR_INVALID_ARG;
     if (p.slots > 1) {
         const uint64_t rows = (uint64_t)a.n_tokens * a.q_heads * p.slots;
         p.part_o_bytes = rows * cache->head_dim * 4;
@@ -177,6 +178,8 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
         p.logits_at = p.ws_bytes = align256(p.ws_bytes);
         p.ws_bytes += (uint64_t)a.n_seqs * a.c.heads * a.logit_rows * a.logit_stride * 4;
     }
+    const uint64_t join_blocks = (p.slots > 1 ? (uint64_t)a.n_tokens * a.q_heads : 0) + (p.logits ? (uint64_t)a.n_seqs * a.c.heads * (((uint64_t)a.c.limit + 1023) / 1024) : 0);
+    if (join_blocks > kMaxBlocks) return ZC_ERR_INVALID_ARG;
     p.weight_parts = 1;
     if (x->d_weights_out && !p.logits) {
         // about 1,024 workgroups, of two that share a compute unit: a prompt's first tokens have the most rows, and the last ones fill up
@@ -185,7 +188,7 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
         if (parts > rows_per_head / 64) parts = rows_per_head / 64;
         if (parts > kMostParts) parts = kMostParts;
         p.weight_parts = parts ? (uint32_t)parts : 1;
-        if (groups * p.weight_parts > 0x7FFFFFFFu) return ZC_ERR_INVALID_ARG;
+        if (groups * p.weight_parts > kMaxBlocks) return ZC_ERR_INVALID_ARG;
         if (p.weight_parts > 1) {
             p.weights_at = align256(p.ws_bytes);
             p.ws_bytes = p.weights_at + units * p.weight_parts * (uint64_t)a.c.capacity * 4;
@@ -252,7 +255,9 @@ extern "C" zc_status zc_evict(const zc_kv_cache *from, const float *d_weights, u
     if (!zc::same_shape(*from, *to) || from->n_seqs != to->n_seqs || from->d_lengths == to->d_lengths) return ZC_ERR_INVALID_ARG;
     if (!d_weights || (keep && !d_kept) || !zc::aligned4(d_weights) || !zc::aligned4(d_weights_to) || !zc::aligned4(d_kept)) return ZC_ERR_INVALID_ARG;
     if (d_weights_to == d_weights || (uint64_t)sinks + recent > keep || keep >= zc::kMaxTokens) return ZC_ERR_INVALID_ARG;
-    if (to->table_pages * (uint64_t)to->page_tokens < (keep < (uint32_t)e.from.capacity ? keep : (uint32_t)e.from.capacity)) return ZC_ERR_BUFFER_TOO_SMALL;
+    const uint64_t most = keep < (uint32_t)e.from.capacity ? keep : (uint32_t)e.from.capacity;     // rows per sequence and head
+    if (to->table_pages * (uint64_t)to->page_tokens < most) return ZC_ERR_BUFFER_TOO_SMALL;
+    if ((uint64_t)from->n_seqs * from->n_heads * ((most + 63) / 64) > zc::kMaxBlocks) return ZC_ERR_INVALID_ARG;
     e.k_to = (uint8_t *)to->d_k_pages;
     e.v_to = (uint8_t *)to->d_v_pages;
     e.weights = d_weights;

@@ -133,6 +133,10 @@ template <int D> __device__ __forceinline__ uint32_t key_place(uint32_t n, uint3
     return D == 128 ? n * 256 + ((c ^ (n & 15)) << 4) : n * 128 + ((c ^ ((n >> 1) & 7)) << 4);
 }
 
+// A part's maximum in base 2: minus infinity where it has seen nothing (its sum is 0), not a number where its sum is not one, though all
+// its products were not numbers either and have left the maximum where it was.
+__device__ __forceinline__ float log2_top(float m, float c, float sum) { return sum != sum ? sum : m == kNegInf ? kNegInf : m * c; }
+
 // ---- sequences, rows, positions ----------------------------------------------------------------
 struct Span { int32_t first, count; };         // a sequence's query tokens
 

@@ -303,7 +303,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
 #pragma unroll
     for (int t = 0; t < QT; t++) {
         l[t] = sum_over_16(sum_over_32(l[t]));
-        if (g == 0) { ml[wave][t * 16 + n16][0] = m[t] == kNegInf ? kNegInf : m[t] * c; ml[wave][t * 16 + n16][1] = l[t]; }
+        if (g == 0) { ml[wave][t * 16 + n16][0] = log2_top(m[t], c, l[t]); ml[wave][t * 16 + n16][1] = l[t]; }
     }
     __syncthreads();
     constexpr uint32_t kPerRow = kWaves * 4, DP = D / kPerRow;     // threads per row, dimensions per thread
@@ -344,17 +344,17 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
             if (tok >= 0) {
                 const uint64_t row = (uint64_t)tok * a.q_heads + head * a.group + r % a.group;
                 if (a.direct) {
-                    const float inv = big == kNegInf ? 0.0f : v_scale / sum;
+                    const float inv = sum == 0.0f ? 0.0f : v_scale / sum;
                     uint16_t *to = a.out + (uint64_t)tok * a.out_token_stride + (uint64_t)(head * a.group + r % a.group) * a.out_head_stride + piece * DP;
 #pragma unroll
                     for (uint32_t d = 0; d < DP; d += 2) *reinterpret_cast<uint32_t *>(to + d) = pack_bf16(x[d] * inv, x[d + 1] * inv);
-                    if (a.lse && piece == 0) a.lse[row] = big == kNegInf ? kNegInf : (big + __builtin_amdgcn_logf(sum)) * kLn2;
+                    if (a.lse && piece == 0) a.lse[row] = sum == 0.0f ? kNegInf : (big + __builtin_amdgcn_logf(sum)) * kLn2;
                 } else {
                     const uint64_t slot = (uint64_t)(a.first_slot + split) * a.n_tokens * a.q_heads + row;
                     float *to = a.part_o + slot * D + piece * DP;
 #pragma unroll
                     for (uint32_t d = 0; d < DP; d++) to[d] = x[d] * v_scale;
-                    if (piece == 0) { a.part_ml[slot * 2] = big; a.part_ml[slot * 2 + 1] = sum; }
+                    if (piece == 0) { a.part_ml[slot * 2] = sum != sum ? sum : big; a.part_ml[slot * 2 + 1] = sum; }
                 }
             }
         }

@@ -57,10 +57,10 @@ __global__ __launch_bounds__(256, 4) void k_attend_join(AttendDev a, WeightsDev 
         __syncthreads();
         if (tid >= LD) return;
         x = (joined[0][tid] + joined[1][tid]) + (joined[2][tid] + joined[3][tid]);
-        const float inv = top == kNegInf ? 0.0f : 1.0f / sum;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
         const u32x2 w = {pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv)};
         *reinterpret_cast<u32x2 *>(a.out + (uint64_t)token * a.out_token_stride + row % a.q_heads * a.out_head_stride + dim) = w;
-        if (a.lse && tid == 0) a.lse[row] = top == kNegInf ? kNegInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+        if (a.lse && tid == 0) a.lse[row] = sum == 0.0f ? kNegInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
         return;
     }
 
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256, 4) void k_attend_join(AttendDev a, WeightsDev 
                 for (int d = 1; d < 16; d *= 2) l += __shfl_xor(l, d);
             }
         }
-        if ((tid & 15) == 0) lse[r] = m == kNegInf ? kNegInf : m + __builtin_amdgcn_logf(l);
+        if ((tid & 15) == 0) lse[r] = l == 0.0f ? kNegInf : m + __builtin_amdgcn_logf(l);
         __syncthreads();
     }
     if (t >= length) return;
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(256, 4) void k_attend_join(AttendDev a, WeightsDev 
             const f32x4 x = *reinterpret_cast<const f32x4 *>(from + (uint64_t)r * a.logit_stride);
             const float minus = lse[r];
 #pragma unroll
-            for (int j = 0; j < 4; j++) sum[j] += minus == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(x[j] - minus);
+            for (int j = 0; j < 4; j++) sum[j] += minus == kNegInf || x[j] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(x[j] - minus);     // (hidden: minus infinity)
         }
     }
     const uint64_t at = (uint64_t)unit * (uint64_t)a.c.capacity + (uint64_t)t;
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendDev a, WeightsD
                 s[0] = mma32_keys(key[0][u], q, u ? s[0] : zero);
                 s[1] = mma32_keys(key[1][u], q, u ? s[1] : zero);
             }
-            const float minus = minus_lse[buf][r];
+            float minus = minus_lse[buf][r];
             const Sight sg = sight(a, positions[buf][r], 0, length);
             // all of these rows see all of these tokens
             const bool whole = there == 15 && !__any(!(t0 + 63 <= sg.last && (t0 >= sg.from || t0 + 64 <= sg.sinks)) || minus == kNegInf);
@@ -247,6 +247,11 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendDev a, WeightsD
 #pragma unroll
                 for (int n = 0; n < 8; n++) mask |= (seen_of_four(sg, t0 + n * 8 + (int32_t)g * 4) & (there >> (n / 2) & 1 ? 15u : 0u)) << (n * 4);
                 mask = minus == kNegInf ? 0u : mask;
+                if (__builtin_expect(__any(minus != minus), 0)) {          // a row whose softmax is not a number gives that to what it sees, and to nothing else
+#pragma unroll
+                    for (int k = 0; k < 32; k++) acc[k] += minus != minus && (mask >> k & 1) ? minus : 0.0f;
+                    minus = minus != minus ? kNegInf : minus;
+                }
 #pragma unroll
                 for (int k = 0; k < 32; k++) {
                     const uint32_t keep = bit_as_mask(mask, k);

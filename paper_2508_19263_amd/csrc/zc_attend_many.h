@@ -353,10 +353,10 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
     // ---- results: a lane has 4 consecutive dimensions at a time
     if (row.token < 0) return;
     const float sum = sum_over_32(l);
-    const float top = m == kNegInf ? kNegInf : m * c;
+    const float top = log2_top(m, c, sum);
     const uint64_t at = (uint64_t)row.token * a.q_heads + row.q_head;
     if (a.direct) {
-        const float inv = m == kNegInf ? 0.0f : v_scale / sum;
+        const float inv = sum == 0.0f ? 0.0f : v_scale / sum;
         uint16_t *to = a.out + (uint64_t)row.token * a.out_token_stride + (uint64_t)row.q_head * a.out_head_stride + g * 4;
 #pragma unroll
         for (int d = 0; d < DT; d++)
@@ -365,7 +365,7 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
                 const u32x2 w = {pack_bf16(o[d][k * 4] * inv, o[d][k * 4 + 1] * inv), pack_bf16(o[d][k * 4 + 2] * inv, o[d][k * 4 + 3] * inv)};
                 *reinterpret_cast<u32x2 *>(to + d * 32 + k * 8) = w;
             }
-        if (a.lse && g == 0) a.lse[at] = m == kNegInf ? kNegInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+        if (a.lse && g == 0) a.lse[at] = sum == 0.0f ? kNegInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
     } else {
         const uint64_t slot = (uint64_t)(a.first_slot + split) * a.n_tokens * a.q_heads + at;
         float *to = a.part_o + slot * D + g * 4;

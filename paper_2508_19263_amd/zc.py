@@ -465,11 +465,16 @@ class Batch:
         return self.out
 
 
+_PAGE_TYPES = {FMT_BF16: (torch.bfloat16, torch.int16, torch.uint16), FMT_FP8_E4M3: (torch.uint8, torch.int8, torch.float8_e4m3fn),
+               FMT_FP8_E5M2: (torch.uint8, torch.int8, torch.float8_e5m2)}
+_ROW_TYPES = (torch.bfloat16, torch.int16, torch.uint16)
+
+
 class PagedCache:
     """K and V of a batch of sequences in pages, as the attention and eviction calls take them.
 
-    k_pages, v_pages: [n_pages, page_tokens, head_dim], contiguous, as stored (any one-byte type for FP8, any two-byte type
-    for BF16); table: int32 [n_seqs, n_heads, table_pages] of page numbers (one that is no page's: absent); lengths: int32
+    k_pages, v_pages: [n_pages, page_tokens, head_dim], contiguous, as stored (of the format's type, or as plain integers of
+    its size); table: int32 [n_seqs, n_heads, table_pages] of page numbers (one that is no page's: absent); lengths: int32
     [n_seqs], tokens in the cache; k_scales, v_scales: float32 [n_seqs, n_heads] or None.  The object holds the tensors
     and the descriptor; the lengths and the table are read on the device when a call runs, so they may change between calls."""
 
@@ -477,17 +482,20 @@ class PagedCache:
         for name, t, dtype, dims in (("table", table, torch.int32, 3), ("lengths", lengths, torch.int32, 1)):
             if t.dtype != dtype or t.dim() != dims or not t.is_contiguous():
                 raise ValueError("PagedCache: %s has to be a contiguous %s tensor of %d dimensions" % (name, dtype, dims))
-        size = {FMT_BF16: 2, FMT_FP8_E4M3: 1, FMT_FP8_E5M2: 1}.get(fmt)
-        if size is None:
+        types = _PAGE_TYPES.get(fmt)
+        if types is None:
             raise ZcError(ERR_UNSUPPORTED, "PagedCache")
         for t in (k_pages, v_pages):
-            if t.dim() != 3 or t.element_size() != size or not t.is_contiguous() or t.shape != k_pages.shape:
-                raise ValueError("PagedCache: pages have to be contiguous [n_pages, page_tokens, head_dim] of %d bytes an element" % size)
+            if t.dim() != 3 or t.dtype not in types or not t.is_contiguous() or t.shape != k_pages.shape:
+                raise ValueError("PagedCache: pages have to be contiguous [n_pages, page_tokens, head_dim] tensors of the format's type")
         if lengths.shape[0] != table.shape[0]:
             raise ValueError("PagedCache: table and lengths are of different numbers of sequences")
         for t in (k_scales, v_scales):
             if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != tuple(table.shape[:2]) or not t.is_contiguous()):
                 raise ValueError("PagedCache: scales have to be contiguous float32 [n_seqs, n_heads]")
+        self.device = k_pages.device
+        if any(t is not None and t.device != self.device for t in (v_pages, table, lengths, k_scales, v_scales)):
+            raise ValueError("PagedCache: tensors are on different devices")
         self.k_pages, self.v_pages, self.table, self.lengths = k_pages, v_pages, table, lengths
         self.k_scales, self.v_scales, self.fmt = k_scales, v_scales, fmt
         self.n_seqs, self.n_heads, self.table_pages = table.shape
@@ -504,12 +512,12 @@ class PagedCache:
 
 
 def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, max_kv_len, max_prefix_len, out, lse, weights, weights_out, ws):
-    if q.dim() != 3 or q.shape[2] != cache.head_dim or q.stride(2) != 1 or q.element_size() != 2:
+    if q.dim() != 3 or q.shape[2] != cache.head_dim or q.stride(2) != 1 or q.dtype not in _ROW_TYPES:
         raise ValueError("%s: q has to be [n_tokens, n_q_heads, head_dim] in BF16 with contiguous rows" % what)
     n, heads, dim = q.shape
     if out is None:
         out = q.new_empty((n, heads, dim))
-    elif out.shape != q.shape or out.stride(2) != 1 or out.element_size() != 2:
+    elif out.shape != q.shape or out.stride(2) != 1 or out.dtype not in _ROW_TYPES:
         raise ValueError("%s: out has to have q's shape and type, with contiguous rows" % what)
     if lse is None:
         lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
@@ -520,6 +528,10 @@ def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, ma
     for t in (weights, weights_out):
         if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (cache.n_seqs, cache.n_heads, cache.capacity) or not t.is_contiguous()):
             raise ValueError("%s: weights have to be contiguous float32 [n_seqs, n_heads, table_pages * page_tokens]" % what)
+    device = q.device
+    if device.type != "cuda" or cache.device != device or any(t is not None and t.device != device for t in (out, lse, q_start, weights, weights_out, ws)) or \
+            (prefix is not None and prefix.device != device):
+        raise ValueError("%s: tensors have to be on one GPU" % what)
     a = AttendArgs(_ATTEND_ARGS_BYTES, n, heads, max_q_len, window, sinks, max_kv_len, max_prefix_len, dim ** -0.5 if scale is None else scale, 0,
                    q.data_ptr(), out.data_ptr(), q.stride(0), q.stride(1), out.stride(0), out.stride(1),
                    None if q_start is None else q_start.data_ptr(), lse.data_ptr(),
@@ -531,7 +543,7 @@ def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, ma
         if size:
             ws = torch.empty(size, dtype=torch.uint8, device=q.device)
             at = ws.data_ptr()
-    stream = torch._C._cuda_getCurrentRawStream(q.device.index)
+    stream = torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     st = L.zc_attend(ref, cache.ref, at, size, stream) if prefix is None else L.zc_attend_shared(ref, prefix.ref, cache.ref, at, size, stream)
     if st != OK:
         raise ZcError(st, what)
@@ -565,6 +577,8 @@ def evict(cache, weights, keep, into, into_weights=None, sinks=0, recent=0, kept
     for t, c in ((weights, cache), (into_weights, into)):
         if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (c.n_seqs, c.n_heads, c.capacity) or not t.is_contiguous()):
             raise ValueError("zc_evict: weights have to be contiguous float32 [n_seqs, n_heads, table_pages * page_tokens]")
+    if weights.device.type != "cuda" or any(t is not None and t.device != weights.device for t in (cache, into, into_weights, kept)):
+        raise ValueError("zc_evict: tensors have to be on one GPU")
     st = lib().zc_evict(cache.ref, weights.data_ptr(), keep, sinks, recent, into.ref, into_weights.data_ptr() if into_weights is not None else None,
                         kept.data_ptr(), _stream())
     _check(st, "zc_evict")

@@ -118,7 +118,7 @@ def attention(q, q_lens, cache, prefix=None, window=0, sinks=0, scale=None, weig
                 e = torch.where(on, torch.exp(logits - top), torch.zeros_like(logits))
                 total = e.sum(dim=1, keepdim=True)
                 empty = (total == 0)
-                p = e / torch.where(empty, torch.ones_like(total), total)
+                p = torch.where(on, e / torch.where(empty, torch.ones_like(total), total), torch.zeros_like(e))
                 fine = v.isfinite()
                 o = p @ torch.where(fine, v, torch.zeros_like(v))
                 for t in torch.nonzero((~fine).any(dim=1)).flatten().tolist():
@@ -126,7 +126,7 @@ def attention(q, q_lens, cache, prefix=None, window=0, sinks=0, scale=None, weig
                 out[first:first + count, j] = torch.where(empty, torch.zeros_like(o), o)
                 lse[first:first + count, j] = (top + torch.log(total)).squeeze(1)
                 size = (x.abs() @ torch.where(k.isfinite(), k, torch.zeros_like(k)).abs().t()) * abs(scale)
-                d = (dim * 2.0 ** -24 * size.amax(dim=1) + 2.0 ** -22 * (1 + size.amax(dim=1))).view(-1, 1)
+                d = (dim * 2.0 ** -24 * size.amax(dim=1) + 2.0 ** -22 * (1 + size.amax(dim=1))).nan_to_num(0, 0, 0).view(-1, 1)      # (a row that is not a number has nothing to be near)
                 sums = (P + length) * 2.0 ** -24
                 a = p @ torch.where(fine, v, torch.zeros_like(v)).abs()
                 tol_out[first:first + count, j] = 2 * (2.0 ** -8 * o.abs() + (bits + 2 * d + sums) * a + 2.0 ** -24)

@@ -123,6 +123,34 @@ def test_what_is_not_finite_stays_with_those_who_see_it(fmt, name, q_len):
         assert bool(out[:40].isfinite().all()) and not bool(out.isfinite().all())
 
 
+@pytest.mark.parametrize("fmt", [BF16, E4M3])
+@pytest.mark.parametrize("q_len,before", [(3, 0), (100, 0), (2, 3000), (100, 3000)])
+def test_a_query_that_is_not_a_number(fmt, q_len, before):
+    """It is the business of its own row, and of the weights of what it sees; also where a cache is split."""
+    cache = Cache([300, 200 + before], 1, 128, fmt)
+    if before:
+        q = queries(2 * q_len, 4, 128)
+        q[q_len:, 2] = float("nan")
+        out, lse = zc.attend(q, cache.paged, q_start=starts([q_len, q_len]), max_q_len=q_len)
+        shared, shared_lse = zc.attend_shared(q, Cache([3000], 1, 128, fmt, seed=3).paged, cache.paged, q_start=starts([q_len, q_len]), max_q_len=q_len)
+        for o, z in ((out, lse), (shared, shared_lse)):
+            assert bool(o[q_len:, 2].isnan().all()) and bool(z[q_len:, 2].isnan().all())
+            assert int(o.isnan().any(dim=2).sum()) == q_len and int(z.isfinite().sum()) == z.numel() - q_len
+        return
+    q = queries(q_len + 1, 4, 128)
+    bad = q_len - 2                                              # the last but one of the first sequence
+    q[bad, 1, 7] = float("nan")
+    w_out = torch.zeros((2, 1, cache.paged.capacity), device="cuda")
+    out, lse = zc.attend(q, cache.paged, q_start=starts([q_len, 1]), max_q_len=q_len, window=50, sinks=3, weights_out=w_out)
+    want, want_lse, want_w, tol, tol_lse, tol_w = attention(q, [q_len, 1], cache, None, 50, 3, None, torch.zeros_like(w_out))
+    agree(out, want, tol.nan_to_num(0), "out")
+    agree(lse, want_lse, tol_lse.nan_to_num(0), "lse")
+    for s, n in enumerate(cache.lens):
+        agree(w_out[s, :, :n], want_w[s, :, :n], tol_w[s, :, :n].nan_to_num(0), "weights")
+    assert bool(out[bad, 1].isnan().all()) and int(out.isnan().any(dim=2).sum()) == 1
+    assert bool(w_out[0, 0, 299].isfinite()) and bool(w_out[0, 0, 298].isnan()) and bool(w_out[0, 0, 100].isfinite())
+
+
 def test_strided_queries_and_results():
     cache = Cache([200, 50, 17], 2, 128, E4M3)
     q_lens = [3, 1, 40]

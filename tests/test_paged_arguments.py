@@ -139,5 +139,20 @@ def test_the_binding_checks_the_calls_tensors():
         zc.evict(c, torch.zeros((2, 1, 31)), 4, paged())
     with pytest.raises(ValueError):
         zc.evict(c, torch.zeros((2, 1, 32)), 4, paged(), kept=torch.zeros((2, 1, 5), dtype=torch.int32))
+    with pytest.raises(ValueError):
+        zc.attend(q.to(torch.float16), c)
+    with pytest.raises(ValueError):
+        zc.attend(q, c)                                          # not on a GPU
+    with pytest.raises(ValueError):
+        zc.evict(c, torch.zeros((2, 1, 32)), 4, paged())
+    for other in (torch.float8_e5m2, torch.float8_e4m3fnuz):
+        with pytest.raises(ValueError):
+            paged(k_pages=torch.zeros((5, 16, 64), dtype=other))
     with pytest.raises(zc.ZcError):
         paged(fmt=zc.FMT_FP4_E2M1_MX)
+
+
+def test_calls_too_large_for_a_launch():
+    wide = dict(n_seqs=1 << 20, n_heads=2)
+    assert attend(args(n_tokens=1 << 20, n_q_heads=64, max_q_len=1), cache(n_seqs=1 << 20, n_heads=64)) == zc.ERR_INVALID_ARG
+    assert evict(cache(table_pages=1 << 20, **wide), cache(d_lengths=2 * SOME, table_pages=1 << 20, **wide), keep=1 << 24) == zc.ERR_INVALID_ARG
