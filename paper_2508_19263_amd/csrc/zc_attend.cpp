@@ -212,7 +212,7 @@ zc_status attend(const zc_attend_args *x, const zc_kv_cache *prefix, const zc_kv
     }
     const WeightsDev w = {x->d_weights_in, x->d_weights_out, p.weight_parts > 1 ? (float *)((uint8_t *)d_ws + p.weights_at) : nullptr, p.weight_parts};
     if (x->n_tokens) {
-        if (shared && !p.own_pass.many && p.own_pass.row_blocks == 1) {
+        if (shared && !p.own_pass.many) {
             const uint32_t tiles = p.pre_pass.many || p.own_pass.tiles > p.pre_pass.tiles ? p.own_pass.tiles : p.pre_pass.tiles;
             LAUNCH_TRY(launch_attend_shared(p.pre, p.own, cache->format, cache->head_dim, p.pre_pass.many, tiles, stream));
         } else {

@@ -15,12 +15,14 @@ __global__ __launch_bounds__(256, 2) void k_attend_shared(AttendDev pre, AttendD
 {
     constexpr size_t kBytes = PRE_MANY && sizeof(ManyShared<D>) > sizeof(FewShared<D, QT>) ? sizeof(ManyShared<D>) : sizeof(FewShared<D, QT>);
     __shared__ __align__(1024) uint8_t room[kBytes];
+    // (A reference to one of the two arguments, chosen here, would have the compiler copy both to scratch memory.)
     if (blockIdx.x < pre_blocks) {
+        const uint32_t units = pre.c.heads, id = blockIdx.x / units;
         if constexpr (PRE_MANY) attend_many<FMT, D>(pre, blockIdx.x, *reinterpret_cast<ManyShared<D> *>(room));
-        else attend_few<FMT, D, QT, false>(pre, blockIdx.x % pre.c.heads, blockIdx.x / pre.c.heads, 0, *reinterpret_cast<FewShared<D, QT> *>(room));
+        else attend_few<FMT, D, QT, false>(pre, blockIdx.x % units, id % pre.splits, id / pre.splits, *reinterpret_cast<FewShared<D, QT> *>(room));
     } else {
-        const uint32_t id = blockIdx.x - pre_blocks, units = own.n_seqs * own.c.heads;
-        attend_few<FMT, D, QT, false>(own, id % units, id / units, 0, *reinterpret_cast<FewShared<D, QT> *>(room));
+        const uint32_t units = own.n_seqs * own.c.heads, id = (blockIdx.x - pre_blocks) / units;
+        attend_few<FMT, D, QT, false>(own, (blockIdx.x - pre_blocks) % units, id % own.splits, id / own.splits, *reinterpret_cast<FewShared<D, QT> *>(room));
     }
 }
 
@@ -41,7 +43,7 @@ template <int FMT> int launch(const AttendDev &pre, const AttendDev &own, uint32
 
 int launch_attend_shared(const AttendDev &pre, const AttendDev &own, uint32_t format, uint32_t head_dim, bool pre_many, uint32_t tiles, void *stream)
 {
-    const uint32_t pre_blocks = pre.c.heads * pre.row_blocks * pre.splits, blocks = pre_blocks + own.n_seqs * own.c.heads * own.splits;
+    const uint32_t pre_blocks = pre.c.heads * pre.row_blocks * pre.splits, blocks = pre_blocks + own.n_seqs * own.c.heads * own.row_blocks * own.splits;
     const hipStream_t s = (hipStream_t)stream;
     if (format == ZC_FMT_BF16) return launch<ZC_FMT_BF16>(pre, own, head_dim, pre_blocks, blocks, pre_many, tiles, s);
     if (format == ZC_FMT_FP8_E4M3) return launch<ZC_FMT_FP8_E4M3>(pre, own, head_dim, pre_blocks, blocks, pre_many, tiles, s);

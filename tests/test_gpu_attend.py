@@ -63,6 +63,17 @@ def test_many_query_tokens(fmt, dim, q_lens, lens, window, sinks):
     check(Cache(lens, 2, dim, fmt), q_lens, 4, window, sinks, weights=True)
 
 
+@pytest.mark.parametrize("rows", [1, 15, 16, 17, 31, 32, 33, 48, 63, 64, 65, 127, 128, 129])
+@pytest.mark.parametrize("window", [0, 200])
+def test_numbers_of_rows(rows, window):
+    """Rows per K/V head on both sides of what a tile, a wavefront and a workgroup take, in one sequence, in many, over a prefix."""
+    for fmt in (BF16, E4M3):
+        check(Cache([900], 2, 128, fmt), [rows], 1, window, 3, weights=True)
+        check(Cache([900], 2, 64, fmt), [1], rows, window, 3)
+        check(Cache([40 + i for i in range(rows)], 2, 64, fmt), [1] * rows, 1, window, 3, prefix=Cache([700], 2, 64, fmt, seed=4))
+        check(Cache([300, 200], 2, 128, fmt), [rows, 1], 1, window, 3, prefix=Cache([333], 2, 128, fmt, seed=4))
+
+
 @pytest.mark.parametrize("fmt", [BF16, E4M3])
 @pytest.mark.parametrize("group,heads", [(1, 1), (2, 5), (8, 1), (64, 1)])
 def test_head_layouts(fmt, group, heads):
@@ -78,7 +89,8 @@ def test_long_cache(fmt):
 @pytest.mark.parametrize("fmt", [BF16, E4M3, E5M2])
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("prefix,lens,q_lens", [(1, [1], [1]), (17, [0, 5, 40], [1, 1, 1]), (3000, [1, 100, 33, 257], [1, 1, 4, 2]), (5000, [20] * 40, [1] * 40),
-                                                (257, [300, 10], [300, 3]), (0, [9, 4], [1, 1]), (100, [2, 0], [5, 3])])
+                                                (257, [300, 10], [300, 3]), (0, [9, 4], [1, 1]), (100, [2, 0], [5, 3]),
+                                                (3000, [30] * 10, [1] * 10), (900, [64, 70], [15, 9]), (40, [700, 20, 0, 5], [1, 9, 1, 4])])
 @pytest.mark.parametrize("window,sinks", [(0, 0), (64, 8), (2000, 130)])
 def test_shared_prefix(fmt, dim, prefix, lens, q_lens, window, sinks):
     """A query whose sequence has fewer tokens of its own than it has queries is positioned in the prefix."""
