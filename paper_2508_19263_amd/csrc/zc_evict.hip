@@ -14,19 +14,12 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr uint32_t kThreads = 1024, kGroupWaves = kThreads / 64;
 constexpr uint32_t kBins = 2048, kCopies = 8, kRoom = 1024;      // bins of the histogram, its copies, keys of the threshold's bin per wavefront
 
-// Order of the weights as unsigned integers: NaN lowest, -0 equal to +0.
+// Order of the weights as unsigned integers: NaN lowest, -0 equal to +0.  0 is no weight's.
 __device__ __forceinline__ uint32_t weight_key(float w)
 {
-    if (!(w == w)) return 0;
+    if (!(w == w)) return 1;
     const uint32_t b = __float_as_uint(w + 0.0f);
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;
-}
-
-// The tokens of four consecutive ones from `first` on that are in [begin, end), as bits.
-__device__ __forceinline__ uint32_t bits_in(uint32_t first, uint32_t begin, uint32_t end)
-{
-    const int32_t lo = min(max((int32_t)(begin - first), 0), 4), hi = min(max((int32_t)(end - first), 0), 4);
-    return ((1u << hi) - 1) & ~((1u << lo) - 1);
 }
 
 // Inclusive sums over the lanes of a wavefront.
@@ -53,7 +46,7 @@ __device__ __forceinline__ uint32_t sum_before(const uint32_t *x, uint32_t n, ui
 //   a histogram of the keys' top 11 bits (sign, exponent and two bits of the mantissa) says which bin the threshold is in;
 //   the keys of that bin, some percent, are collected in LDS, where 11 and 10 bits more of them are counted;
 //   every wavefront knows how many of its tokens stay, so how many stay in front of its own, and writes them in order.
-// Three passes over the weights (six, with 8 bits of all keys at a time, took 82 instead of 31 us for 65,536 tokens; the instructions
+// Three passes over the weights (six, with 8 bits of all keys at a time, took 82 instead of 44 us for 65,536 tokens; the instructions
 // are what bounds it, on one compute unit per sequence and head).  Where a bin has more keys than there is room for, they are
 // taken from memory again each time.  HELD: the keys of up to so many times 256 tokens of a wavefront stay in registers instead (0: none;
 // 8,192 tokens 15.9 -> 12 us).  The histogram has eight copies for eight neighbouring lanes: weights have few exponents.
@@ -77,15 +70,19 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(EvictDev e)
     }
     const float *w = e.weights + (uint64_t)unit * (uint64_t)e.from.capacity;
     const uint32_t begin = e.sinks, end = length - e.recent, need = e.keep - e.sinks - e.recent;   // the middle, of which `need` stay
+    for (uint32_t i = tid; i < e.sinks; i += kThreads) kept[i] = (int32_t)i;
+    for (uint32_t i = tid; i < e.recent; i += kThreads) kept[e.keep - e.recent + i] = (int32_t)(end + i);
+    if (!need) return;
     const uint32_t rounds = (length + kGroupWaves * 256 - 1) / (kGroupWaves * 256), from = wave * rounds * 256;    // the stretch: `rounds` times 256 tokens
     const uint64_t below = (1ull << lane) - 1;
 
     // f(first token of this lane's four, their keys) for the stretch, four reads on their way at a time; a table's tokens are a
     // multiple of 16, so four from a multiple of 4 that is below the length are inside
-    auto key_of = [&](uint32_t r, uint32_t (&key)[4]) {
-        const f32x4u v = *reinterpret_cast<const f32x4u *>(w + min(from + r * 256 + lane * 4, (length - 1) & ~3u));
+    auto key_of = [&](uint32_t r, uint32_t (&key)[4]) {        // 0: not of the middle
+        const uint32_t first = from + r * 256 + lane * 4;
+        const f32x4u v = *reinterpret_cast<const f32x4u *>(w + min(first, (length - 1) & ~3u));
 #pragma unroll
-        for (int j = 0; j < 4; j++) key[j] = weight_key(v[j]);
+        for (int j = 0; j < 4; j++) key[j] = first + j - begin < end - begin ? weight_key(v[j]) : 0u;
     };
     uint32_t held[HELD ? HELD : 1][4];
     if constexpr (HELD > 0) {
@@ -133,30 +130,24 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(EvictDev e)
         return found[0];
     };
 
-    uint32_t top = 0xFFFFFFFFu, threshold = 0xFFFFFFFFu, above = 0, n_some = 0, n_sure = 0;    // need == 0: no key is large enough
-    bool in_lds = true;
-    if (need) {
-        clear();
-        if (tid == 0) crowded = 0;
-        __syncthreads();
-        over_stretch([&](uint32_t first, const uint32_t (&key)[4]) {
-            const uint32_t in = bits_in(first, begin, end);
+    uint32_t above = 0, n_some = 0, n_sure = 0, n_equal = 0;
+    clear();
+    if (tid == 0) crowded = 0;
+    __syncthreads();
+    over_stretch([&](uint32_t, const uint32_t (&key)[4]) {
 #pragma unroll
-            for (int j = 0; j < 4; j++)
-                if (in >> j & 1) atomicAdd(&hist[(key[j] >> 21) * kCopies + (lane & (kCopies - 1))], 1u);
-        });
-        __syncthreads();
-        top = find(above);                                     // (the middle has more than `need` keys)
-        clear();
-    }
-    // what of the stretch stays for sure, and the keys of the threshold's bin
-    over_stretch([&](uint32_t first, const uint32_t (&key)[4]) {
-        const uint32_t in = bits_in(first, begin, end);
+        for (int j = 0; j < 4; j++)
+            if (key[j]) atomicAdd(&hist[(key[j] >> 21) * kCopies + (lane & (kCopies - 1))], 1u);
+    });
+    __syncthreads();
+    const uint32_t top = find(above);                          // (the middle has more than `need` keys)
+    clear();
+    // what of the stretch is above the threshold's bin, and the keys of that bin
+    over_stretch([&](uint32_t, const uint32_t (&key)[4]) {
 #pragma unroll
         for (int j = 0; j < 4; j++) {
-            const bool middle = in >> j & 1;
-            n_sure += (uint32_t)__popcll(__ballot(middle ? need && key[j] >> 21 > top : first + j < length));
-            const uint64_t q = __ballot(middle && key[j] >> 21 == top);
+            n_sure += key[j] > (top << 21 | 0x1FFFFFu);
+            const uint64_t q = __ballot(key[j] >> 21 == top && key[j]);
             if (q) {
                 const uint32_t at = n_some + (uint32_t)__popcll(q & below);
                 if ((q >> lane & 1) && at < kRoom) some[wave][at] = key[j];
@@ -164,63 +155,60 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(EvictDev e)
             }
         }
     });
-    uint32_t n_equal = 0;
-    if (need) {
-        if (n_some > kRoom && lane == 0) crowded = 1;
-        __syncthreads();
-        in_lds = !crowded;
-        // f(key) for the stretch's keys of that bin
-        auto over_some = [&](auto f) {
-            if (in_lds) {
-                for (uint32_t i = lane; i < n_some; i += 64) f(some[wave][i]);
-            } else {
-                over_stretch([&](uint32_t first, const uint32_t (&key)[4]) {
-                    const uint32_t in = bits_in(first, begin, end);
+    if (n_some > kRoom && lane == 0) crowded = 1;
+    __syncthreads();
+    const bool in_lds = !crowded;
+    // f(key) for the stretch's keys of that bin
+    auto over_some = [&](auto f) {
+        if (in_lds) {
+            for (uint32_t i = lane; i < n_some; i += 64) f(some[wave][i]);
+        } else {
+            over_stretch([&](uint32_t, const uint32_t (&key)[4]) {
 #pragma unroll
-                    for (int j = 0; j < 4; j++)
-                        if ((in >> j & 1) && key[j] >> 21 == top) f(key[j]);
-                });
-            }
-        };
-        over_some([&](uint32_t key) { atomicAdd(&hist[(key >> 10 & 2047) * kCopies + (lane & (kCopies - 1))], 1u); });
-        __syncthreads();
-        threshold = top << 11 | find(above);
-        clear();
-        __syncthreads();
-        over_some([&](uint32_t key) { if (key >> 10 == threshold) atomicAdd(&hist[(key & 1023) * kCopies + (lane & (kCopies - 1))], 1u); });
-        __syncthreads();
-        threshold = threshold << 10 | find(above);
-        uint32_t more = 0;
-        over_some([&](uint32_t key) { more += key > threshold; n_equal += key == threshold; });
-        for (uint32_t d = 1; d < 64; d *= 2) { more += __shfl_xor(more, d); n_equal += __shfl_xor(n_equal, d); }
-        n_sure += more;
-        __syncthreads();                                       // wave_sum is free again
-    }
+                for (int j = 0; j < 4; j++)
+                    if (key[j] >> 21 == top && key[j]) f(key[j]);
+            });
+        }
+    };
+    over_some([&](uint32_t key) { atomicAdd(&hist[(key >> 10 & 2047) * kCopies + (lane & (kCopies - 1))], 1u); });
+    __syncthreads();
+    uint32_t threshold = top << 11 | find(above);
+    clear();
+    __syncthreads();
+    over_some([&](uint32_t key) { if (key >> 10 == threshold) atomicAdd(&hist[(key & 1023) * kCopies + (lane & (kCopies - 1))], 1u); });
+    __syncthreads();
+    threshold = threshold << 10 | find(above);
+    over_some([&](uint32_t key) { n_sure += key > threshold; n_equal += key == threshold; });
+    n_sure = (uint32_t)__builtin_amdgcn_readlane((int)scan_wave(n_sure), 63);
+    n_equal = (uint32_t)__builtin_amdgcn_readlane((int)scan_wave(n_equal), 63);
+    __syncthreads();                                       // wave_sum is free again
     const uint32_t ties = need - above;
     if (lane == 0) { wave_sum[wave] = n_sure; wave_more[wave] = n_equal; }
     __syncthreads();
     uint32_t sure_before = sum_before(wave_sum, wave, lane), equal_before = sum_before(wave_more, wave, lane);
     over_stretch([&](uint32_t first, const uint32_t (&key)[4]) {
-        const uint32_t in = bits_in(first, begin, end);
-        bool sure[4], equal[4];
         uint32_t s_in = sure_before, q_in = equal_before;      // of those before this lane's first token
 #pragma unroll
         for (int j = 0; j < 4; j++) {
-            const bool middle = in >> j & 1;
-            sure[j] = middle ? need && key[j] > threshold : first + j < length;
-            equal[j] = middle && need && key[j] == threshold;
-            const uint64_t s = __ballot(sure[j]), q = __ballot(equal[j]);
+            const uint64_t s = __ballot(key[j] > threshold);
             s_in += (uint32_t)__popcll(s & below);
-            q_in += (uint32_t)__popcll(q & below);
             sure_before += (uint32_t)__popcll(s);
-            equal_before += (uint32_t)__popcll(q);
+        }
+        if (__any(key[0] == threshold || key[1] == threshold || key[2] == threshold || key[3] == threshold)) {
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const uint64_t q = __ballot(key[j] == threshold);
+                q_in += (uint32_t)__popcll(q & below);
+                equal_before += (uint32_t)__popcll(q);
+            }
         }
 #pragma unroll
         for (int j = 0; j < 4; j++) {
-            const uint32_t at = s_in + min(q_in, ties);
-            if ((sure[j] || (equal[j] && q_in < ties)) && at < e.keep) kept[at] = (int32_t)(first + j);
-            s_in += sure[j];
-            q_in += equal[j];
+            const bool equal = key[j] == threshold;
+            const uint32_t at = e.sinks + s_in + min(q_in, ties);
+            if ((key[j] > threshold || (equal && q_in < ties)) && at < e.keep) kept[at] = (int32_t)(first + j);
+            s_in += key[j] > threshold;
+            q_in += equal;
         }
     });
 }
