@@ -53,16 +53,23 @@ __device__ __forceinline__ float sum_over_16(float x)
     const u32x2 r = __builtin_amdgcn_permlane16_swap(bits(x), bits(x), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-__device__ __forceinline__ int32_t min_over_wave(int32_t x)
+// f over all lanes of a wavefront: within rows of 16 by rotation, then over the rows
+template <int N> __device__ __forceinline__ uint32_t rotated(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x120 + N, 0xF, 0xF, false); }
+template <typename F> __device__ __forceinline__ uint32_t over_wave(uint32_t x, F f)
 {
-    for (int d = 1; d < 64; d *= 2) x = min(x, __shfl_xor(x, d));
-    return uniform(x);
+    x = f(x, rotated<8>(x));
+    x = f(x, rotated<4>(x));
+    x = f(x, rotated<2>(x));
+    x = f(x, rotated<1>(x));
+    u32x2 r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = f(r[0], r[1]);
+    r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return f(r[0], r[1]);
 }
-__device__ __forceinline__ int32_t max_over_wave(int32_t x)
-{
-    for (int d = 1; d < 64; d *= 2) x = max(x, __shfl_xor(x, d));
-    return uniform(x);
-}
+__device__ __forceinline__ int32_t min_over_wave(int32_t x) { return uniform((int32_t)over_wave((uint32_t)x, [](uint32_t p, uint32_t q) { return (uint32_t)min((int32_t)p, (int32_t)q); })); }
+__device__ __forceinline__ int32_t max_over_wave(int32_t x) { return uniform((int32_t)over_wave((uint32_t)x, [](uint32_t p, uint32_t q) { return (uint32_t)max((int32_t)p, (int32_t)q); })); }
+__device__ __forceinline__ float max_over_wave(float x) { return __uint_as_float(over_wave(bits(x), [](uint32_t p, uint32_t q) { return bits(fmaxf(__uint_as_float(p), __uint_as_float(q))); })); }
+__device__ __forceinline__ float sum_over_wave(float x) { return __uint_as_float(over_wave(bits(x), [](uint32_t p, uint32_t q) { return bits(__uint_as_float(p) + __uint_as_float(q)); })); }
 
 // FP8 elements are exact in BF16 and in half precision, so keys go to the type of the queries, and values to the type with
 // more mantissa: the weights they are multiplied with lie in [0, 1] and are rounded to that type too.

@@ -22,7 +22,7 @@ __global__ __launch_bounds__(256, 4) void k_attend_join(AttendDev a, WeightsDev 
     if (blockIdx.x < join_blocks) {
         constexpr uint32_t LD = D / 4, SUBS = 256 / LD;        // lanes per slot, slots at a time
         __shared__ f32x4 joined[4][LD];
-        const uint64_t row = blockIdx.x;
+        const uint32_t row = blockIdx.x;
         const int32_t token = (int32_t)(row / a.q_heads);
         if (sequence_of(a, token) < 0) return;
         float m = kNegInf, l = 0.0f;
@@ -38,11 +38,9 @@ __global__ __launch_bounds__(256, 4) void k_attend_join(AttendDev a, WeightsDev 
             part[k] = f32x4{0, 0, 0, 0};
             if (s < slots) part[k] = *reinterpret_cast<const f32x4 *>(a.part_o + (s * n_rows + row) * D + dim);
         }
-        float top = m;
-        for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+        const float top = max_over_wave(m);
         const float f = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m - top);
-        float sum = m == kNegInf ? 0.0f : l * f;
-        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+        const float sum = sum_over_wave(m == kNegInf ? 0.0f : l * f);
         f32x4 x = {0, 0, 0, 0};
 #pragma unroll
         for (uint32_t k = 0; k < 64 / SUBS; k++) {
