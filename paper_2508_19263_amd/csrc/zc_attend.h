@@ -35,11 +35,13 @@ struct AttendDev {
     uint32_t n_seqs, n_tokens, q_heads, group, max_q_len, window, sinks;
     uint32_t shared;                   // 1: `c` is the prefix, and a row block takes rows of all sequences
     uint32_t splits, first_slot;       // this pass's slots are first_slot .. first_slot + splits
+    uint32_t even;                     // k_attend_few: parts that what a sequence sees is divided into if these are no longer than kLongPart
     uint32_t row_blocks;               // row blocks per (sequence, head), or per head of the prefix
     uint32_t direct;                   // 1: one slot in all, the pass writes out and lse itself
 };
 
 constexpr uint32_t kMostParts = 16;
+constexpr uint32_t kLongPart = 8192;   // tokens
 
 struct WeightsDev {
     const float *in;                   // or null

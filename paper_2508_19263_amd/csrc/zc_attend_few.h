@@ -99,8 +99,18 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
     }
     const Blocks blocks = seen_blocks(32, last_max, from_min, sinks);
     // this workgroup's part, in steps that all wavefronts take part in
-    const int32_t per_split = ((blocks.count + (int32_t)a.splits - 1) / (int32_t)a.splits + (int32_t)kWaves - 1) / (int32_t)kWaves * (int32_t)kWaves;
+    const int32_t even = min((blocks.count + (int32_t)a.even - 1) / (int32_t)a.even, (int32_t)kLongPart / 32), least = (blocks.count + (int32_t)a.splits - 1) / (int32_t)a.splits;
+    const int32_t per_split = (max(even, least) + (int32_t)kWaves - 1) / (int32_t)kWaves * (int32_t)kWaves;
     const int32_t begin = min((int32_t)split * per_split, blocks.count), end = min(begin + per_split, blocks.count);
+    if (begin == end && !a.direct) {                     // nothing left for this part (k_attend_join does not look at what its rows would be)
+        const uint32_t r = first_row + threadIdx.x, i = r / a.group;
+        if (threadIdx.x < QT * 16 && (int32_t)i < span.count) {
+            const uint64_t slot = (uint64_t)(a.first_slot + split) * a.n_tokens * a.q_heads + (uint64_t)(span.first + (int32_t)i) * a.q_heads + head * a.group + r % a.group;
+            a.part_ml[slot * 2] = kNegInf;
+            a.part_ml[slot * 2 + 1] = 0.0f;
+        }
+        return;
+    }
 
     const int32_t *table = a.c.table + (uint64_t)(unit) * a.c.table_pages;
     const uint32_t page_log = a.c.page_shift + (D == 128 ? 7 : 6) + (ES - 1);   // of a page's bytes

@@ -369,6 +369,7 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
     } else {
         const uint64_t slot = (uint64_t)(a.first_slot + split) * a.n_tokens * a.q_heads + at;
         float *to = a.part_o + slot * D + g * 4;
+        if (begin < end)                                       // (else k_attend_join does not look at it)
 #pragma unroll
         for (int d = 0; d < DT; d++)
 #pragma unroll

@@ -86,6 +86,14 @@ def test_long_cache(fmt):
     check(Cache([40007, 100, 12345], 1, 64, fmt), [1, 5, 3], 4, 30000, 100)
 
 
+@pytest.mark.parametrize("fmt", [BF16, E4M3])
+@pytest.mark.parametrize("group,window,weights", [(1, 0, False), (4, 9000, True), (20, 0, False)])
+def test_one_long_cache_among_short_ones(fmt, group, window, weights):
+    # more (sequence, head) pairs than compute units, and parts that only the long cache fills
+    lens = [300, 8192, 0, 17001, 8193, 1, 8191] + [33 * i for i in range(10)]
+    check(Cache(lens, 16, 64, fmt), [1] * 17, group, window, 4 if window else 0, weights=weights, single=True)
+
+
 @pytest.mark.parametrize("fmt", [BF16, E4M3, E5M2])
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("prefix,lens,q_lens", [(1, [1], [1]), (17, [0, 5, 40], [1, 1, 1]), (3000, [1, 100, 33, 257], [1, 1, 4, 2]), (5000, [20] * 40, [1] * 40),
