@@ -73,8 +73,8 @@ Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_sp
     const uint64_t groups = units * p.row_blocks, part = 256, possible = only && longest <= 640 ? 1 : (longest + part - 1) / part;
     // Lengths are not known here, only the longest.  So that one long cache among short ones does not keep everyone waiting, parts are at
     // most kLongPart tokens, and what is left over of a shorter cache's parts ends at once: 31 FP8 caches of 1,000 tokens and one of 131,072
-    // 1,077 -> 168 us, 64 of 0 to 32,768 448 -> 420 us; 64 of 8,192 188 us as before, 16 of 32,768 189 -> 197 us.  (At most 4,096: 146, 397,
-    // 197 and 200 us.)  k_attend_many has row blocks enough where rows are many, and its parts would take their number times as much room.
+    // 1,077 -> 128 us, 64 of 0 to 32,768 444 -> 408 us; 64 of 8,192 188 us as before, 16 of 32,768 190 -> 198 us.  (At most 4,096: 109, 391,
+    // 202 and 209 us.)  k_attend_many has row blocks enough where rows are many, and its parts would take their number times as much room.
     const uint64_t enough = p.many ? 512 : 256;
     uint64_t even = groups ? (enough + groups - 1) / groups : 1;
     if (even > possible) even = possible;

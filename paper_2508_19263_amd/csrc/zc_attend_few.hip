@@ -9,7 +9,9 @@ template <int FMT, int D, int QT, bool LOGITS>
 __global__ __launch_bounds__(kWaves * 64, 2) void k_attend_few(AttendDev a)
 {
     __shared__ FewShared<D, QT> shared;
-    attend_few<FMT, D, QT, LOGITS>(a, blockIdx.x, blockIdx.y, blockIdx.z, shared);
+    // Each part begins with another unit: workgroups that lie a round apart go to the same compute unit, where the parts of a long
+    // cache would meet (one FP8 cache of 131,072 tokens and 31 of 1,000: 168 -> 128 us, six of 100 to 3,001 13.6 -> 12.4 us).
+    attend_few<FMT, D, QT, LOGITS>(a, (blockIdx.x + blockIdx.y * 13) % gridDim.x, blockIdx.y, blockIdx.z, shared);
 }
 
 template <int FMT, int D> int launch(const AttendDev &a, uint32_t tiles, dim3 blocks, hipStream_t s)
