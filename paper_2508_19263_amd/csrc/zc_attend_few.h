@@ -9,6 +9,10 @@
 // Neither K, V nor the weights pass through LDS; V is transposed by byte permutes inside a lane, which holds 8 tokens x
 // head_dim / 16 consecutive dimensions.  At the end the wavefronts' (m, l, O) are joined in LDS; parts of a cache that went
 // to different workgroups are joined by k_attend_join.
+//
+// Measured with 8 K/V heads of 128 in random pages of 16 tokens, one query token, joins included (a kernel that only reads reaches
+// 6.1 TB/s): 64 FP8 caches of 8,192 tokens 188 us, 5.7 TB/s; 48 BF16 ones of 12,000 416 us, 5.7 TB/s; 4 FP8 ones of 8,192 17.4 us,
+// 3.9 TB/s (14.7 us are this kernel's); one with 512 tokens in sight 8.5 us, all latency.
 #pragma once
 #include "zc_attend_device.h"
 

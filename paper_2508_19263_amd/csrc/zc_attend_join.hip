@@ -9,11 +9,13 @@ namespace {
 // One workgroup per (query token, query head).  With (m_s, l_s, O_s) of the slots, M = max m_s:
 //   out = sum O_s 2^(m_s - M) / sum l_s 2^(m_s - M),   lse = (M + log2 of that sum) ln 2.
 // A lane first holds one slot's pair (at most 64 slots), then four dimensions of every eighth (head_dim 128) or sixteenth slot.
-// Bound by latency: the parts are in the L2 or the memory-side cache.
+// Bound by latency: the parts are in the L2 or the memory-side cache (128 rows of 8 slots 4 us, launch included; 2,048 rows of
+// 33 slots, 35 MB, 9 us).
 //
 // Workgroups behind those take 1,024 tokens of a (sequence, K/V head) each and add up their weights from the logits that
 // k_attend_few has left (`logits`, where rereading these costs less than rereading the keys): four tokens to a thread, the
-// rows one after the other.
+// rows one after the other.  (4 FP8 caches of 8,192 tokens, 8 K/V heads, 4 rows each: 4.6 us with the join, 0.6 more than the join
+// alone; the whole call 19.8 us against 17.4 without weights.)
 template <int D>
 __global__ __launch_bounds__(256, 4) void k_attend_join(AttendDev a, WeightsDev wt, uint32_t slots, uint32_t join_blocks, uint32_t blocks_per_unit)
 {
@@ -123,8 +125,9 @@ __global__ __launch_bounds__(256, 4) void k_attend_join(AttendDev a, WeightsDev 
 // LDS once for its four wavefronts, into one of two buffers while the other is worked on.  S^T = K Q^T leaves a lane one row's
 // products with 32 of the tokens, whose exponentials it adds up token by token; the 32 lanes of a token are added at the end.  Where
 // there are fewer workgroups than fill the GPU, `parts` of them share the tokens, each with every so many-th 64 rows, and k_weights_sum adds
-// up what they leave.  The sums have one order, whatever the launch.  Bound by the matrix instructions and the exponentials.
-// (Rows straight from memory to a wavefront's registers, each 32 bytes of 32 rows at a time, took 160 us for 4,099 tokens and 32 heads.)
+// up what they leave.  The sums have one order, whatever the launch.  Bound by the matrix instructions and the exponentials: a prompt of
+// 4,099 tokens, 8 K/V heads of 128 and 4 query heads to each, takes 110 us, 625 TFLOP/s, and 5 for the sums.  (Rows straight from memory to a
+// wavefront's registers, each 32 bytes of 32 rows at a time: 160 us.)
 template <int FMT, int D>
 __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendDev a, WeightsDev wt)
 {

@@ -8,7 +8,12 @@
 //   O^T += V^T P^T  a lane's weights are its operand as they stand; V comes from LDS through transposing reads, four tokens
 //                   of a dimension at a time, which are exactly the runs of four tokens that S^T leaves in a lane
 // The bank a 16-byte piece of a key (64-byte piece of a value) lies in depends on its token too, so that neither the reads of
-// 16 tokens' pieces nor the transposing ones meet in a bank.  Bound by the matrix instructions and the exponentials.
+// 16 tokens' pieces nor the transposing ones meet in a bank.  Bound by the matrix instructions and the exponentials, which share
+// a SIMD between two wavefronts (registers and LDS have room for two): the matrix unit is busy 37 % of the time.
+//
+// Measured with 8 K/V heads of 128 and 4 query heads to each: two BF16 prompts of 8,192 and 7,001 tokens with a window of 4,096 and 16
+// sinks 873 us, 856 TFLOP/s; pieces of 1,024 and 511 tokens behind 7,977 and 7,680 FP8 ones 139 us, 741 TFLOP/s.  (Counted are the products
+// of tokens that are seen; a library product of 8,192^3 reaches 1,136 on this card, whose clock goes down under it.)
 #pragma once
 #include "zc_attend_device.h"
 
