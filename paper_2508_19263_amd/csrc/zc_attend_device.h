@@ -134,6 +134,12 @@ template <int FMT> __device__ __forceinline__ float element(const uint8_t *p)
     else return __uint_as_float(two_to_bf16<FMT, false>(*p) << 16);
 }
 
+// 16 tokens of a page (bytes 0: none, what is asked for is 0)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t sixteen_tokens(const uint8_t *p, int bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, bytes, 0x00020000);
+}
+
 // Byte offset in LDS of 16-byte piece c of row n, rows of D two-byte elements: 16 rows' pieces of one number lie in as many banks.
 template <int D> __device__ __forceinline__ uint32_t key_place(uint32_t n, uint32_t c)
 {

@@ -35,12 +35,6 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&to)[N], _
     else { const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(from, (int)at, 0, 0); to[0] = x[0]; to[1] = x[1]; to[2] = x[2]; to[3] = x[3]; }
 }
 
-// 16 tokens of a page
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t half_page(const uint8_t *p, int bytes)
-{
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, bytes, 0x00020000);
-}
-
 // The operand for dimension i of a lane's DL: 8 tokens' elements of it.
 template <int FMT, int VW> __device__ __forceinline__ u32x4_t value_operand(const uint32_t (&v)[8][VW], int i)
 {
@@ -185,7 +179,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
     auto load_keys = [&](const Place &x, Regs &r) {
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            const __amdgpu_buffer_rsrc_t from = half_page(a.c.k + x.at[h], x.there >> h & 1 ? 16 * D * ES : 0);
+            const __amdgpu_buffer_rsrc_t from = sixteen_tokens(a.c.k + x.at[h], x.there >> h & 1 ? 16 * D * ES : 0);
 #pragma unroll
             for (int u = 0; u < NK; u++) r.k[h][u] = __builtin_amdgcn_raw_buffer_load_b128(from, (int)(k_lane + u * 64), 0, 0);
         }
@@ -193,7 +187,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
     auto load_values = [&](const Place &x, Regs &r) {
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            const __amdgpu_buffer_rsrc_t from = half_page(a.c.v + x.at[h], x.there >> h & 1 ? 16 * D * ES : 0);
+            const __amdgpu_buffer_rsrc_t from = sixteen_tokens(a.c.v + x.at[h], x.there >> h & 1 ? 16 * D * ES : 0);
 #pragma unroll
             for (int j = 0; j < 4; j++) load_words(r.v[h * 4 + j], from, v_lane + j * (D * ES));
         }

@@ -17,8 +17,6 @@
 #pragma once
 #include "zc_attend_device.h"
 
-#include <type_traits>
-
 namespace zc {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -45,21 +43,32 @@ template <int D> __device__ __forceinline__ uint32_t value_place(uint32_t token,
     return D == 128 ? token * 256 + (x ^ ((token & 3) << 6)) : token * 128 + (x ^ ((token >> 1 & 1) << 6));
 }
 
-template <int D> struct ManyShared {
-    alignas(1024) uint8_t lds[2][2][kTile * D * 2];            // [buffer][keys, values]
+// A workgroup's LDS.  The two buffers are variables of their own, so that the compiler knows what is brought to one of them does not
+// lie in the other, and reads of the other need not wait for it.
+template <int D> struct ManyTile {
+    alignas(1024) uint8_t keys[kTile * D * 2], values[kTile * D * 2];
+};
+struct ManyNotes {
     uint32_t bad_tokens[3][kHalves];                           // [tile modulo 3]: tokens with an element that is not finite
     int32_t limits[kManyWaves][4];
 };
 
-template <int FMT, int D>
-__device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, ManyShared<D> &shared)
+// 16 bytes at a lane's own offset to the lane's place in a wavefront's 1,024 consecutive bytes of LDS
+__device__ __forceinline__ void bring(__amdgpu_buffer_rsrc_t from, uint32_t at, uint8_t *to)
 {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, (int)at, 0, 0, 0);
+}
+__device__ __forceinline__ void wait_for_brought() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+template <int FMT, int D>
+__device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, ManyTile<D> &tile0, ManyTile<D> &tile1, ManyNotes &notes)
+{
+    constexpr bool kBring = FMT == ZC_FMT_BF16;                // tiles go to LDS as they are, past the registers
     constexpr int ES = PageElem<FMT>::BYTES, KS = D / 16, DT = D / 32;
     constexpr uint32_t kPieces = D * ES / 16;                  // 16-byte pieces of a stored row
-    constexpr uint32_t kRowsPerPass = 256 / kPieces, kPasses = kTile / kRowsPerPass;
-    auto &lds = shared.lds;
-    auto &bad_tokens = shared.bad_tokens;
-    auto &limits = shared.limits;
+    constexpr uint32_t kRowsPerPass = 64 / kPieces, kPasses = 16 / kRowsPerPass;
+    auto &bad_tokens = notes.bad_tokens;
+    auto &limits = notes.limits;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n32 = lane & 31, g = lane >> 5;
     const uint32_t units = (a.shared ? 1 : a.n_seqs) * a.c.heads;
     const uint32_t unit = id % units;                          // neighbours on an XCD work on the same few heads
@@ -120,11 +129,11 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
 #pragma unroll
         for (int i = 0; i < 16; i++) o[d][i] = 0.0f;
 
-    // ---- bringing tiles: a thread takes piece `piece` of rows row0 + pass * kRowsPerPass of keys and values
+    // ---- bringing tiles: a wavefront takes 16 tokens, which lie in one page, some rows at a time; a lane has piece `piece` of each
     const int32_t *table = a.c.table + (uint64_t)unit * a.c.table_pages;
     const uint32_t page_log = a.c.page_shift + (D == 128 ? 7 : 6) + (ES - 1);   // of a page's bytes
     const uint32_t page_mask = (1u << a.c.page_shift) - 1;
-    const uint32_t piece = tid % kPieces, row0 = tid / kPieces;
+    const uint32_t piece = lane % kPieces, row0 = wave * 16 + lane / kPieces;       // (the row of pass 0)
     // lane kStretches * i + h: page of tokens 16 h .. of tile ids_from + i (0 where it is absent), and the bit that says it is there
     int32_t ids = 0, ids_from = begin;
     uint64_t present = 0;
@@ -141,62 +150,81 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
     // which of a tile's stretches of 16 tokens are present
     auto there_of = [&](int32_t b) { return (uint32_t)(present >> ((b - ids_from) * kStretches)) & ((1u << kStretches) - 1); };
     u32x4_t kx[kPasses], vx[kPasses];
-    const uint32_t mine = (row0 & 15) * (D * ES) + piece * 16;
-    auto fetch = [&](int32_t b) {
-        const int32_t at = (b - ids_from) * kStretches;
-        const uint32_t t0 = (uint32_t)blocks.at(b) * kTile;
+    // Where a lane's piece of a pass lies from the first of the 16 tokens.  kBring: place `piece` of a row of LDS holds another piece of
+    // it, by key_place and value_place, whose exchange of pieces is its own inverse.
+    auto mine_k = [&](uint32_t p) {
+        const uint32_t r = row0 + p * kRowsPerPass;
+        return (r & 15) * (D * ES) + (kBring ? key_place<D>(r, piece) & (D * 2 - 1) : piece * 16);
+    };
+    auto mine_v = [&](uint32_t p) {
+        const uint32_t r = row0 + p * kRowsPerPass;
+        return (r & 15) * (D * ES) + (kBring ? value_place<D>(r, piece * 16) & (D * 2 - 1) : piece * 16);
+    };
+    auto fetch = [&](int32_t b, ManyTile<D> &to) {
+        const uint32_t t0 = (uint32_t)blocks.at(b) * kTile + wave * 16, page = (uint32_t)__builtin_amdgcn_readlane(ids, (b - ids_from) * kStretches + (int32_t)wave);
+        const uint64_t where = ((uint64_t)page << page_log) + (t0 & page_mask) * (D * ES);
+        const __amdgpu_buffer_rsrc_t k = sixteen_tokens(a.c.k + where, 16 * D * ES), v = sixteen_tokens(a.c.v + where, 16 * D * ES);
 #pragma unroll
         for (uint32_t p = 0; p < kPasses; p++) {
-            const uint32_t first = p * kRowsPerPass + wave * (64 / kPieces);   // the wavefront's first row: its rows lie in one stretch of 16
-            const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(ids, at + (int32_t)(first / 16));
-            const uint64_t where = ((uint64_t)page << page_log) + ((t0 + (first & ~15u)) & page_mask) * (D * ES);
-            kx[p] = *reinterpret_cast<const u32x4_t *>(a.c.k + where + mine);
-            vx[p] = *reinterpret_cast<const u32x4_t *>(a.c.v + where + mine);
+            if constexpr (kBring) {
+                bring(k, mine_k(p), to.keys + wave * (16 * D * 2) + p * 1024);
+                bring(v, mine_v(p), to.values + wave * (16 * D * 2) + p * 1024);
+            } else {
+                kx[p] = __builtin_amdgcn_raw_buffer_load_b128(k, (int)mine_k(p), 0, 0);
+                vx[p] = __builtin_amdgcn_raw_buffer_load_b128(v, (int)mine_v(p), 0, 0);
+            }
         }
     };
     // whether every row of the workgroup (of the wavefront) sees every token of a tile
     auto whole = [&](int32_t t0, uint32_t there, int32_t lmin, int32_t fmax) { return there == (1u << kStretches) - 1 && t0 + kTile - 1 <= lmin && (t0 >= fmax || t0 + kTile <= sinks); };
-    auto store_keys = [&](uint32_t buf) {
-        uint8_t *kt = lds[buf][0];
-#pragma unroll
-        for (uint32_t p = 0; p < kPasses; p++) {
-            const uint32_t r = p * kRowsPerPass + row0;
-            if constexpr (FMT == ZC_FMT_BF16) *reinterpret_cast<u32x4_t *>(kt + key_place<D>(r, piece)) = kx[p];
-            else {
-                *reinterpret_cast<u32x4_t *>(kt + key_place<D>(r, piece * 2)) = eight_to_bf16<FMT>(kx[p][0], kx[p][1]);
-                *reinterpret_cast<u32x4_t *>(kt + key_place<D>(r, piece * 2 + 1)) = eight_to_bf16<FMT>(kx[p][2], kx[p][3]);
-            }
-        }
-    };
-    auto store_values = [&](int32_t t0, uint32_t there, bool edge, uint32_t buf, uint32_t mod3) {
-        if (__builtin_expect(edge, 0)) {
-            // Tokens that no row sees are zeroed (what they hold is not to be multiplied, not even with 0); of those that only
-            // some rows see, elements that are not finite are zeroed too and noted: they are added to the rows that do see them.
+    auto store_keys = [&](ManyTile<D> &to) {
+        if constexpr (!kBring) {
 #pragma unroll
             for (uint32_t p = 0; p < kPasses; p++) {
                 const uint32_t r = p * kRowsPerPass + row0;
-                const int32_t t = t0 + (int32_t)r;
-                const bool used = (there >> (r / 16) & 1) && seen(Sight{all_last_max, all_from_min, sinks}, t);
-                const bool by_all = seen(Sight{all_last_min, all_from_max, sinks}, t);
-                uint32_t wild = 0;
-#pragma unroll
-                for (int w = 0; w < 4; w++) {
-                    vx[p][w] = used ? vx[p][w] : 0u;
-                    const uint32_t x = by_all ? 0u : nonfinite_mask<FMT>(vx[p][w]);
-                    wild |= x;
-                    vx[p][w] &= ~x;
-                }
-                if (wild) atomicOr(&bad_tokens[mod3][r / 32], 1u << (r & 31));
+                *reinterpret_cast<u32x4_t *>(to.keys + key_place<D>(r, piece * 2)) = eight_to_bf16<FMT>(kx[p][0], kx[p][1]);
+                *reinterpret_cast<u32x4_t *>(to.keys + key_place<D>(r, piece * 2 + 1)) = eight_to_bf16<FMT>(kx[p][2], kx[p][3]);
             }
         }
-        uint8_t *vt = lds[buf][1];
+    };
+    // Tokens that no row sees are zeroed (what they hold is not to be multiplied, not even with 0); of those that only some rows see,
+    // elements that are not finite are zeroed too and noted: they are added to the rows that do see them.
+    auto clean = [&](u32x4_t &x, uint32_t r, int32_t t0, uint32_t there, uint32_t mod3) {
+        const int32_t t = t0 + (int32_t)r;
+        const bool used = (there >> wave & 1) && seen(Sight{all_last_max, all_from_min, sinks}, t);
+        const bool by_all = seen(Sight{all_last_min, all_from_max, sinks}, t);
+        uint32_t wild = 0;
 #pragma unroll
-        for (uint32_t p = 0; p < kPasses; p++) {
-            const uint32_t r = p * kRowsPerPass + row0;
-            if constexpr (FMT == ZC_FMT_BF16) *reinterpret_cast<u32x4_t *>(vt + value_place<D>(r, piece * 16)) = vx[p];
-            else {
-                *reinterpret_cast<u32x4_t *>(vt + value_place<D>(r, piece * 32)) = eight_to_half<FMT>(vx[p][0], vx[p][1]);
-                *reinterpret_cast<u32x4_t *>(vt + value_place<D>(r, piece * 32 + 16)) = eight_to_half<FMT>(vx[p][2], vx[p][3]);
+        for (int w = 0; w < 4; w++) {
+            x[w] = used ? x[w] : 0u;
+            const uint32_t y = by_all ? 0u : nonfinite_mask<FMT>(x[w]);
+            wild |= y;
+            x[w] &= ~y;
+        }
+        if (wild) atomicOr(&bad_tokens[mod3][r / 32], 1u << (r & 31));
+    };
+    auto store_values = [&](int32_t t0, uint32_t there, bool edge, ManyTile<D> &to, uint32_t mod3) {
+        if constexpr (kBring) {
+            wait_for_brought();
+            if (__builtin_expect(edge, 0)) {
+#pragma unroll
+                for (uint32_t p = 0; p < kPasses; p++) {
+                    u32x4_t *place = reinterpret_cast<u32x4_t *>(to.values + wave * (16 * D * 2) + p * 1024 + lane * 16);
+                    u32x4_t x = *place;
+                    clean(x, p * kRowsPerPass + row0, t0, there, mod3);
+                    *place = x;
+                }
+            }
+        } else {
+            if (__builtin_expect(edge, 0)) {
+#pragma unroll
+                for (uint32_t p = 0; p < kPasses; p++) clean(vx[p], p * kRowsPerPass + row0, t0, there, mod3);
+            }
+#pragma unroll
+            for (uint32_t p = 0; p < kPasses; p++) {
+                const uint32_t r = p * kRowsPerPass + row0;
+                *reinterpret_cast<u32x4_t *>(to.values + value_place<D>(r, piece * 32)) = eight_to_half<FMT>(vx[p][0], vx[p][1]);
+                *reinterpret_cast<u32x4_t *>(to.values + value_place<D>(r, piece * 32 + 16)) = eight_to_half<FMT>(vx[p][2], vx[p][3]);
             }
         }
     };
@@ -241,8 +269,8 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
         }
     };
 
-    auto multiply = [&](uint32_t buf, Products &s) {
-        const uint8_t *kt = lds[buf][0];
+    auto multiply = [&](const ManyTile<D> &tile, Products &s) {
+        const uint8_t *kt = tile.keys;
         // Of the two wavefronts of a SIMD the one at its matrix instructions goes first, and the other one's arithmetic fills in: two
         // prompts 885 -> 870 us, pieces of prompts 158 -> 149 us (the other way round 898 and 162 us).
         __builtin_amdgcn_s_setprio(1);
@@ -256,8 +284,8 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
             if (i + kReadsAhead < 2 * KS) __builtin_amdgcn_sched_group_barrier(kSchedLdsRead, 1, 0);
         }
     };
-    auto rest = [&](int32_t t0, uint32_t there, bool edge, uint32_t buf, uint32_t mod3, Products &s) {
-        const uint8_t *vt = lds[buf][1];
+    auto rest = [&](int32_t t0, uint32_t there, bool edge, const ManyTile<D> &tile, uint32_t mod3, Products &s) {
+        const uint8_t *vt = tile.values;
         if (__builtin_expect(edge, 0)) hide(t0, there, s);
         raise(top_of(s));
         const float mc = m == kNegInf ? 0.0f : m * c;
@@ -321,12 +349,11 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
         uint32_t there = there_of(begin), mod3 = 0;
         int32_t t0 = blocks.at(begin) * kTile;
         bool edge = !whole(t0, there, all_last_min, all_from_max);             // some row of the workgroup does not see all of the tile
-        fetch(begin);
-        store_keys(0);
-        store_values(t0, there, edge, 0, 0);
+        fetch(begin, tile0);
+        store_keys(tile0);
+        store_values(t0, there, edge, tile0, 0);
         __syncthreads();
-        auto step = [&](int32_t b, auto buffer) {
-            constexpr uint32_t buf = decltype(buffer)::value;
+        auto step = [&](int32_t b, ManyTile<D> &tile, ManyTile<D> &next) {
             const uint32_t next3 = mod3 == 2 ? 0 : mod3 + 1;
             const int32_t later = min(b + 1, end - 1);                         // (the last one is asked for again: no branch, no wait)
             const bool ours = t0 <= last_max && (t0 + kTile > from_min || t0 < sinks);  // else nothing of the tile is for this wavefront's rows
@@ -335,13 +362,14 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
             const int32_t t0_next = blocks.at(later) * kTile;
             const bool edge_next = !whole(t0_next, there_next, all_last_min, all_from_max);
             Products s;
-            if (ours) multiply(buf, s);
+            if constexpr (kBring) fetch(later, next);
+            if (ours) multiply(tile, s);
             __builtin_amdgcn_s_setprio(0);
-            fetch(later);
-            if (ours) rest(t0, there, edge, buf, mod3, s);
+            if constexpr (!kBring) fetch(later, next);
+            if (ours) rest(t0, there, edge, tile, mod3, s);
             __builtin_amdgcn_s_setprio(0);
-            store_keys(buf ^ 1);
-            store_values(t0_next, there_next, edge_next, buf ^ 1, next3);
+            store_keys(next);
+            store_values(t0_next, there_next, edge_next, next, next3);
             if (tid < kHalves) bad_tokens[next3 == 2 ? 0 : next3 + 1][tid] = 0;        // last read before the barrier that began this step
             there = there_next;
             t0 = t0_next;
@@ -350,8 +378,8 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
             mod3 = next3;
         };
         for (int32_t b = begin; b < end; b += 2) {
-            step(b, std::integral_constant<uint32_t, 0>());
-            if (b + 1 < end) step(b + 1, std::integral_constant<uint32_t, 1>());
+            step(b, tile0, tile1);
+            if (b + 1 < end) step(b + 1, tile1, tile0);
         }
     }
 

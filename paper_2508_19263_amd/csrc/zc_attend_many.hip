@@ -8,8 +8,9 @@ namespace {
 template <int FMT, int D>
 __global__ __launch_bounds__(kManyWaves * 64, 2) void k_attend_many(AttendDev a)
 {
-    __shared__ ManyShared<D> shared;
-    attend_many<FMT, D>(a, blockIdx.x, shared);
+    __shared__ ManyTile<D> tile0, tile1;
+    __shared__ ManyNotes notes;
+    attend_many<FMT, D>(a, blockIdx.x, tile0, tile1, notes);
 }
 
 template <int FMT, int D> int launch(const AttendDev &a, uint32_t blocks, hipStream_t s)

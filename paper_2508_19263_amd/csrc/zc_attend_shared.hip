@@ -15,12 +15,16 @@ namespace {
 template <int FMT, int D, bool PRE_MANY, int QT>
 __global__ __launch_bounds__(256, 2) void k_attend_shared(AttendDev pre, AttendDev own, uint32_t pre_blocks)
 {
-    constexpr size_t kBytes = PRE_MANY && sizeof(ManyShared<D>) > sizeof(FewShared<D, QT>) ? sizeof(ManyShared<D>) : sizeof(FewShared<D, QT>);
+    constexpr size_t kBytes = PRE_MANY && sizeof(ManyTile<D>) > sizeof(FewShared<D, QT>) ? sizeof(ManyTile<D>) : sizeof(FewShared<D, QT>);
     __shared__ __align__(1024) uint8_t room[kBytes];
     // (A reference to one of the two arguments, chosen here, would have the compiler copy both to scratch memory.)
     if (blockIdx.x < pre_blocks) {
         const uint32_t units = pre.c.heads, id = blockIdx.x / units;
-        if constexpr (PRE_MANY) attend_many<FMT, D>(pre, blockIdx.x, *reinterpret_cast<ManyShared<D> *>(room));
+        if constexpr (PRE_MANY) {
+            __shared__ ManyTile<D> tile1;
+            __shared__ ManyNotes notes;
+            attend_many<FMT, D>(pre, blockIdx.x, *reinterpret_cast<ManyTile<D> *>(room), tile1, notes);
+        }
         else attend_few<FMT, D, QT, false>(pre, blockIdx.x % units, id % pre.splits, id / pre.splits, *reinterpret_cast<FewShared<D, QT> *>(room));
     } else {
         const uint32_t units = own.n_seqs * own.c.heads, id = (blockIdx.x - pre_blocks) / units;
