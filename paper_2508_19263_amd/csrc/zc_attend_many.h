@@ -2,18 +2,20 @@
 // the part of k_attend_shared that is like it.
 //
 // A workgroup of four wavefronts takes 128 rows of one K/V head, 32 to a wavefront, and goes over the tokens
-// they see 64 at a time.  A tile of keys and values is brought to LDS once for all of them, in the type it is multiplied in (FP8
-// is converted on the way: keys to BF16, values to half precision), into one of two buffers while the other is worked on:
+// they see 64 at a time.  A tile of keys and values is brought to LDS once for all of them, in the type it is multiplied in (BF16 goes
+// there past the registers; FP8 is converted on the way: keys to BF16, values to half precision), into one of two buffers while the
+// other is worked on:
 //   S^T = K Q^T     32 tokens x 32 rows per instruction; a lane holds one row's products with half of the tile's tokens
 //   O^T += V^T P^T  a lane's weights are its operand as they stand; V comes from LDS through transposing reads, four tokens
 //                   of a dimension at a time, which are exactly the runs of four tokens that S^T leaves in a lane
 // The bank a 16-byte piece of a key (64-byte piece of a value) lies in depends on its token too, so that neither the reads of
-// 16 tokens' pieces nor the transposing ones meet in a bank.  Bound by the matrix instructions and the exponentials, which share
-// a SIMD between two wavefronts (registers and LDS have room for two): the matrix unit is busy 37 % of the time.
+// 16 tokens' pieces nor the transposing ones meet in a bank.
 //
 // Measured with 8 K/V heads of 128 and 4 query heads to each: two BF16 prompts of 8,192 and 7,001 tokens with a window of 4,096 and 16
-// sinks 873 us, 856 TFLOP/s; pieces of 1,024 and 511 tokens behind 7,977 and 7,680 FP8 ones 139 us, 741 TFLOP/s.  (Counted are the products
-// of tokens that are seen; a library product of 8,192^3 reaches 1,136 on this card, whose clock goes down under it.)
+// sinks 790 - 850 us, 880 - 945 TFLOP/s (counted are the products of tokens that are seen); pieces of 1,024 and 511 tokens behind 7,977
+// and 7,680 FP8 ones 140 us, 735 TFLOP/s.  A library product of 8,192^3 reaches 1,136 on this card, and its clock goes down to 1.5 GHz
+// under it; here it goes from 2.2 to 1.9.  The matrix unit is busy 40 % of the cycles and the exponentials and what belongs to them take
+// as many (two wavefronts to a SIMD; registers and LDS have room for no more); other orders of the same instructions give the same time.
 #pragma once
 #include "zc_attend_device.h"
 
@@ -340,10 +342,11 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
             }
     };
 
-    // Two buffers: the next tile is asked for when a tile's products have been made, waits in registers while their weights are
-    // worked out and the values multiplied, and goes to the other buffer.  (Asked for a whole step ahead it took the registers that
-    // reading keys ahead needs: 905 - 920 us for two prompts of 8,192 and 7,001 tokens.  A tile's products made beside the
-    // exponentials of the one before it, in 32 or 64 tokens: 940 and 966 us, for the same reason.)
+    // Two buffers.  The next tile goes straight to the other buffer while a tile is worked on (BF16: two prompts of 8,192 and 7,001 tokens
+    // 916 -> 847 us against the way through registers), or, where it is converted, is asked for when the tile's products have been made,
+    // waits in registers while their weights are worked out and the values multiplied, and is stored then.  (Asked for a whole step ahead, it
+    // takes the registers that reading keys ahead needs.  So does making a tile's products beside the exponentials of the one before
+    // it, in 32 or 64 tokens: 6 to 12 % slower.)
     if (begin < end) {
         fetch_ids(begin);
         uint32_t there = there_of(begin), mod3 = 0;
