@@ -6,6 +6,9 @@ namespace zc {
 
 namespace {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+constexpr uint32_t kFewSlots = 8;
+
 // One workgroup per (query token, query head).  With (m_s, l_s, O_s) of the slots, M = max m_s:
 //   out = sum O_s 2^(m_s - M) / sum l_s 2^(m_s - M),   lse = (M + log2 of that sum) ln 2.
 // A lane first holds one slot's pair (at most 64 slots), then four dimensions of every eighth (head_dim 128) or sixteenth slot.
@@ -16,13 +19,46 @@ namespace {
 // k_attend_few has left (`logits`, where rereading these costs less than rereading the keys): four tokens to a thread, the
 // rows one after the other.  (4 FP8 caches of 8,192 tokens, 8 K/V heads, 4 rows each: 4.6 us with the join, 0.6 more than the join
 // alone; the whole call 19.8 us against 17.4 without weights.)
-template <int D>
+//
+// FEW: at most kFewSlots of them.  A row is D / 4 threads then, each with four dimensions of every slot, 8 or 16 rows to a workgroup, and
+// nothing is exchanged: 1,680 rows of 64 and six slots 5.2 -> 3.5 us, 43,000 of 64 and two slots 50 -> 7 us.
+template <int D, bool FEW>
 __global__ __launch_bounds__(256, 4) void k_attend_join(AttendDev a, WeightsDev wt, uint32_t slots, uint32_t join_blocks, uint32_t blocks_per_unit)
 {
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const uint64_t n_rows = (uint64_t)a.n_tokens * a.q_heads;
     if (blockIdx.x < join_blocks) {
         constexpr uint32_t LD = D / 4, SUBS = 256 / LD;        // lanes per slot, slots at a time
+        if constexpr (FEW) {
+            const uint32_t row = blockIdx.x * SUBS + tid / LD, dim = tid % LD * 4;
+            if (row >= n_rows) return;
+            const int32_t token = (int32_t)(row / a.q_heads);
+            if (sequence_of(a, token) < 0) return;
+            f32x2 ml[kFewSlots];
+            f32x4 part[kFewSlots];
+#pragma unroll
+            for (uint32_t s = 0; s < kFewSlots; s++) {
+                ml[s] = f32x2{kNegInf, 0.0f};
+                if (s < slots) ml[s] = *reinterpret_cast<const f32x2 *>(a.part_ml + (s * n_rows + row) * 2);
+                part[s] = f32x4{0, 0, 0, 0};
+                if (s < slots) part[s] = *reinterpret_cast<const f32x4 *>(a.part_o + (s * n_rows + row) * D + dim);
+            }
+            float top = kNegInf, sum = 0.0f;
+#pragma unroll
+            for (uint32_t s = 0; s < kFewSlots; s++) top = fmaxf(top, ml[s][0]);
+            f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+            for (uint32_t s = 0; s < kFewSlots; s++) {
+                const float f = ml[s][0] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(ml[s][0] - top);
+                sum += ml[s][0] == kNegInf ? 0.0f : ml[s][1] * f;
+                x += f == 0.0f ? f32x4{0, 0, 0, 0} : part[s] * f;
+            }
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const u32x2 w = {pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv)};
+            *reinterpret_cast<u32x2 *>(a.out + (uint64_t)token * a.out_token_stride + row % a.q_heads * a.out_head_stride + dim) = w;
+            if (a.lse && dim == 0) a.lse[row] = sum == 0.0f ? kNegInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+            return;
+        }
         __shared__ f32x4 joined[4][LD];
         const uint32_t row = blockIdx.x;
         const int32_t token = (int32_t)(row / a.q_heads);
@@ -321,10 +357,15 @@ template <int FMT> void launch_weights(const AttendDev &a, const WeightsDev &w, 
 
 int launch_attend_join(const AttendDev &a, const WeightsDev &w, uint32_t head_dim, uint32_t slots, void *stream)
 {
-    const uint32_t join_blocks = slots > 1 ? (uint32_t)((uint64_t)a.n_tokens * a.q_heads) : 0;
+    const uint32_t rows = (uint32_t)((uint64_t)a.n_tokens * a.q_heads), per_block = slots <= kFewSlots ? 1024 / head_dim : 1;
+    const uint32_t join_blocks = slots > 1 ? (rows + per_block - 1) / per_block : 0;
     const uint32_t per_unit = a.logits ? (uint32_t)(a.c.limit + 1023) / 1024 : 1, blocks = join_blocks + (a.logits ? a.n_seqs * a.c.heads * per_unit : 0);
-    if (head_dim == 64) hipLaunchKernelGGL((k_attend_join<64>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, a, w, slots, join_blocks, per_unit);
-    else hipLaunchKernelGGL((k_attend_join<128>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, a, w, slots, join_blocks, per_unit);
+    const hipStream_t s = (hipStream_t)stream;
+    if (slots <= kFewSlots) {
+        if (head_dim == 64) hipLaunchKernelGGL((k_attend_join<64, true>), dim3(blocks), dim3(256), 0, s, a, w, slots, join_blocks, per_unit);
+        else hipLaunchKernelGGL((k_attend_join<128, true>), dim3(blocks), dim3(256), 0, s, a, w, slots, join_blocks, per_unit);
+    } else if (head_dim == 64) hipLaunchKernelGGL((k_attend_join<64, false>), dim3(blocks), dim3(256), 0, s, a, w, slots, join_blocks, per_unit);
+    else hipLaunchKernelGGL((k_attend_join<128, false>), dim3(blocks), dim3(256), 0, s, a, w, slots, join_blocks, per_unit);
     return (int)hipGetLastError();
 }
 
