@@ -28,7 +28,7 @@ struct AttendDev {
     const int32_t *prefix_length;      // length of the shared prefix or null
     float *part_o, *part_ml;           // workspace: [slot][row][dim] and [slot][row][2], rows in the order of lse
     uint64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;   // elements
-    float *logits;                     // k_attend_few with at most 16 rows, or null: [seq][head][logit_rows][logit_stride], in base 2
+    float *logits;                     // k_attend_few with at most kLogitRows rows, or null: [seq][head][logit_rows][logit_stride], in base 2
     uint32_t logit_rows, logit_stride;
     float scale;
     int32_t own_limit, prefix_limit;
@@ -41,6 +41,7 @@ struct AttendDev {
 };
 
 constexpr uint32_t kMostParts = 16;
+constexpr uint32_t kLogitRows = 24;    // rows whose logits k_attend_few leaves
 constexpr uint32_t kLongPart = 8192;   // tokens
 
 struct WeightsDev {

@@ -249,7 +249,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
                 }
             }
             if (LOGITS && rows[t].token >= 0) {
-                float *to = a.logits + ((uint64_t)unit * a.logit_rows + n16) * a.logit_stride + (uint32_t)t0 + g * 4;
+                float *to = a.logits + ((uint64_t)unit * a.logit_rows + t * 16 + n16) * a.logit_stride + (uint32_t)t0 + g * 4;
 #pragma unroll
                 for (int h = 0; h < 2; h++) *reinterpret_cast<f32x4 *>(to + h * 16) = s[t][h] * c;
             }

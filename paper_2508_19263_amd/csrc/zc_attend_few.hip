@@ -16,7 +16,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_attend_few(AttendDev a)
 
 template <int FMT, int D> int launch(const AttendDev &a, uint32_t tiles, dim3 blocks, hipStream_t s)
 {
-    if (a.logits) hipLaunchKernelGGL((k_attend_few<FMT, D, 1, true>), blocks, dim3(kWaves * 64), 0, s, a);
+    if (a.logits && tiles == 1) hipLaunchKernelGGL((k_attend_few<FMT, D, 1, true>), blocks, dim3(kWaves * 64), 0, s, a);
+    else if (a.logits) hipLaunchKernelGGL((k_attend_few<FMT, D, 2, true>), blocks, dim3(kWaves * 64), 0, s, a);
     else if (tiles == 1) hipLaunchKernelGGL((k_attend_few<FMT, D, 1, false>), blocks, dim3(kWaves * 64), 0, s, a);
     else hipLaunchKernelGGL((k_attend_few<FMT, D, 2, false>), blocks, dim3(kWaves * 64), 0, s, a);
     return (int)hipGetLastError();

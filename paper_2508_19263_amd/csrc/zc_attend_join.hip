@@ -100,39 +100,36 @@ __global__ __launch_bounds__(256, 4) void k_attend_join(AttendDev a, WeightsDev 
         return;
     }
 
-    __shared__ float lse[16];
+    __shared__ float lse[kLogitRows];
     const uint32_t unit = (blockIdx.x - join_blocks) / blocks_per_unit, head = unit % a.c.heads, seq = unit / a.c.heads;
     const int32_t t = (int32_t)((blockIdx.x - join_blocks) % blocks_per_unit * 1024 + tid * 4);
     const int32_t length = clamped_length(a.c.lengths, seq, a.c.limit);
     const Span span = query_span(a, seq);
-    const uint32_t rows = (uint32_t)span.count * a.group;      // at most 16
-    {
-        // the rows' lse in base 2: 16 lanes for each row's slots
-        const uint32_t r = tid / 16;
+    const uint32_t rows = (uint32_t)span.count * a.group;      // at most kLogitRows
+    // the rows' lse in base 2: 16 lanes for each row's slots
+    for (uint32_t r = tid / 16; r < rows; r += 16) {
         float m = kNegInf, l = 0.0f;
-        if (r < rows) {
-            const uint64_t row = (uint64_t)(span.first + (int32_t)(r / a.group)) * a.q_heads + head * a.group + r % a.group;
-            if (slots == 1) {
-                m = a.lse[row] * kLog2e;
-                l = 1.0f;
-            } else {
-                float ms[4], ls[4];
+        const uint64_t row = (uint64_t)(span.first + (int32_t)(r / a.group)) * a.q_heads + head * a.group + r % a.group;
+        if (slots == 1) {
+            m = a.lse[row] * kLog2e;
+            l = 1.0f;
+        } else {
+            float ms[4], ls[4];
 #pragma unroll
-                for (uint32_t k = 0; k < 4; k++) {
-                    const uint32_t s = k * 16 + (tid & 15);
-                    ms[k] = s < slots ? a.part_ml[(s * n_rows + row) * 2] : kNegInf;
-                    ls[k] = s < slots ? a.part_ml[(s * n_rows + row) * 2 + 1] : 0.0f;
-                    m = fmaxf(m, ms[k]);
-                }
-                for (int d = 1; d < 16; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-#pragma unroll
-                for (uint32_t k = 0; k < 4; k++) l += ms[k] == kNegInf ? 0.0f : ls[k] * __builtin_amdgcn_exp2f(ms[k] - m);
-                for (int d = 1; d < 16; d *= 2) l += __shfl_xor(l, d);
+            for (uint32_t k = 0; k < 4; k++) {
+                const uint32_t s = k * 16 + (tid & 15);
+                ms[k] = s < slots ? a.part_ml[(s * n_rows + row) * 2] : kNegInf;
+                ls[k] = s < slots ? a.part_ml[(s * n_rows + row) * 2 + 1] : 0.0f;
+                m = fmaxf(m, ms[k]);
             }
+            for (int d = 1; d < 16; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+#pragma unroll
+            for (uint32_t k = 0; k < 4; k++) l += ms[k] == kNegInf ? 0.0f : ls[k] * __builtin_amdgcn_exp2f(ms[k] - m);
+            for (int d = 1; d < 16; d *= 2) l += __shfl_xor(l, d);
         }
         if ((tid & 15) == 0) lse[r] = l == 0.0f ? kNegInf : m + __builtin_amdgcn_logf(l);
-        __syncthreads();
     }
+    __syncthreads();
     if (t >= length) return;
     const Sight any = sight(a, length - 1, 0, length), first = sight(a, length - span.count, 0, length);
     // the four tokens lie in one block of those the pass has gone over, or in none
@@ -140,11 +137,16 @@ __global__ __launch_bounds__(256, 4) void k_attend_join(AttendDev a, WeightsDev 
     f32x4 sum = {0, 0, 0, 0};
     if (gone_over) {
         const float *from = a.logits + (uint64_t)unit * a.logit_rows * a.logit_stride + (uint32_t)t;
-        for (uint32_t r = 0; r < rows; r++) {
-            const f32x4 x = *reinterpret_cast<const f32x4 *>(from + (uint64_t)r * a.logit_stride);
-            const float minus = lse[r];
+        for (uint32_t r0 = 0; r0 < rows; r0 += 8) {            // eight rows on their way at a time
+            f32x4 x[8];
 #pragma unroll
-            for (int j = 0; j < 4; j++) sum[j] += minus == kNegInf || x[j] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(x[j] - minus);     // (hidden: minus infinity)
+            for (uint32_t k = 0; k < 8; k++) x[k] = *reinterpret_cast<const f32x4 *>(from + (uint64_t)min(r0 + k, rows - 1) * a.logit_stride);
+#pragma unroll
+            for (uint32_t k = 0; k < 8; k++) {
+                const float minus = r0 + k < rows ? lse[r0 + k] : kNegInf;
+#pragma unroll
+                for (int j = 0; j < 4; j++) sum[j] += minus == kNegInf || x[k][j] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(x[k][j] - minus);     // (hidden: minus infinity)
+            }
         }
     }
     const uint64_t at = (uint64_t)unit * (uint64_t)a.c.capacity + (uint64_t)t;

@@ -74,6 +74,15 @@ def test_numbers_of_rows(rows, window):
         check(Cache([300, 200], 2, 128, fmt), [rows, 1], 1, window, 3, prefix=Cache([333], 2, 128, fmt, seed=4))
 
 
+@pytest.mark.parametrize("rows", [1, 15, 16, 17, 23, 24, 25, 33])
+@pytest.mark.parametrize("fmt,dim", [(BF16, 128), (E4M3, 64)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (200, 5)])
+def test_weights_of_numbers_of_rows(rows, fmt, dim, window, sinks):
+    check(Cache([700, 37, 2500], 3, dim, fmt), [rows, 1, max(1, rows - 1)], 1, window, sinks, weights=True)
+    if rows % 4 == 0:
+        check(Cache([700, 37, 2500], 3, dim, fmt), [4, 0, 3], rows // 4, window, sinks, weights=True)
+
+
 @pytest.mark.parametrize("fmt", [BF16, E4M3])
 @pytest.mark.parametrize("group,heads", [(1, 1), (2, 5), (8, 1), (64, 1)])
 def test_head_layouts(fmt, group, heads):
