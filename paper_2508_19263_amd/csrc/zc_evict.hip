@@ -46,10 +46,11 @@ __device__ __forceinline__ uint32_t sum_before(const uint32_t *x, uint32_t n, ui
 //   a histogram of the keys' top 11 bits (sign, exponent and two bits of the mantissa) says which bin the threshold is in;
 //   the keys of that bin, some percent, are collected in LDS, where 11 and 10 bits more of them are counted;
 //   every wavefront knows how many of its tokens stay, so how many stay in front of its own, and writes them in order.
-// Three passes over the weights (six, with 8 bits of all keys at a time, took 82 instead of 43 us for 16 x 8 times 20,011 to 65,536 tokens;
-// the instructions are what bounds it, on one compute unit per sequence and head).  Where a bin has more keys than there is room for, they are
-// taken from memory again each time.  HELD: the keys of up to so many times 256 tokens of a wavefront stay in registers instead (0: none;
-// 4 x 8 times 8,192 tokens 15.9 -> 11.6 us).  The histogram has eight copies for eight neighbouring lanes: weights have few exponents.
+// Three passes over the weights; their instructions are what bounds it, on one compute unit per sequence and head (16 x 8 times 20,011
+// to 65,536 tokens 36 us; six passes, with 8 bits of all keys at a time, took 82 instead of 43 us when it was made of three).  Where a
+// bin has more keys than there is room for, they are taken from memory again each time.  HELD: the keys of up to so many times 256
+// tokens of a wavefront stay in registers instead (0: none): 4 x 8 times 8,192 tokens 15.9 -> 11.6 us, 4 times 17,062 with their
+// move 31.8 -> 28.5, 8 times 53,013 80 -> 73.  The histogram has eight copies for eight neighbouring lanes: weights have few exponents.
 template <int HELD>
 __global__ __launch_bounds__(kThreads) void k_evict_select(EvictDev e)
 {
@@ -289,7 +290,10 @@ int launch_evict(const EvictDev &e, void *stream)
 {
     const hipStream_t s = (hipStream_t)stream;
     const uint32_t units = e.n_seqs * e.from.heads;
-    if ((uint32_t)e.from.capacity <= 2 * kGroupWaves * 256) hipLaunchKernelGGL(k_evict_select<2>, dim3(units), dim3(kThreads), 0, s, e);
+    const uint32_t rounds = ((uint32_t)e.from.capacity + kGroupWaves * 256 - 1) / (kGroupWaves * 256);
+    if (rounds <= 2) hipLaunchKernelGGL(k_evict_select<2>, dim3(units), dim3(kThreads), 0, s, e);
+    else if (rounds <= 8) hipLaunchKernelGGL(k_evict_select<8>, dim3(units), dim3(kThreads), 0, s, e);
+    else if (rounds <= 16) hipLaunchKernelGGL(k_evict_select<16>, dim3(units), dim3(kThreads), 0, s, e);
     else hipLaunchKernelGGL(k_evict_select<0>, dim3(units), dim3(kThreads), 0, s, e);
     int rc = (int)hipGetLastError();
     if (rc) return rc;

@@ -70,6 +70,13 @@ def test_long_caches(kind):
     check(cache, weights_of(kind, cache), 30000, 4, 1000)
 
 
+@pytest.mark.parametrize("kind", ["random", "ties", "same", "wild"])
+@pytest.mark.parametrize("lens", [[8193, 5000], [32768, 4097], [32769, 100], [65536, 65535], [65537, 16385]])
+def test_lengths_that_registers_hold_or_not(kind, lens):
+    cache = Cache(lens, 1, 64, E4M3)
+    check(cache, weights_of(kind, cache), 4000, 4, 1000)
+
+
 def test_nothing_kept_and_no_weights_moved():
     cache = Cache([50, 20], 2, 64, E4M3)
     into = Cache([5, 5], 2, 64, E4M3, seed=8)
