@@ -528,10 +528,10 @@ def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, ma
     for t in (weights, weights_out):
         if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (cache.n_seqs, cache.n_heads, cache.capacity) or not t.is_contiguous()):
             raise ValueError("%s: weights have to be contiguous float32 [n_seqs, n_heads, table_pages * page_tokens]" % what)
-    device = q.device
-    if device.type != "cuda" or cache.device != device or any(t is not None and t.device != device for t in (out, lse, q_start, weights, weights_out, ws)) or \
+    device, current = q.device, torch._C._cuda_getDevice() if q.is_cuda else -1       # (the kernels go to the current GPU's stream)
+    if device.index != current or cache.device != device or any(t is not None and t.device != device for t in (out, lse, q_start, weights, weights_out, ws)) or \
             (prefix is not None and prefix.device != device):
-        raise ValueError("%s: tensors have to be on one GPU" % what)
+        raise ValueError("%s: tensors have to be on one GPU, the current one" % what)
     a = AttendArgs(_ATTEND_ARGS_BYTES, n, heads, max_q_len, window, sinks, max_kv_len, max_prefix_len, dim ** -0.5 if scale is None else scale, 0,
                    q.data_ptr(), out.data_ptr(), q.stride(0), q.stride(1), out.stride(0), out.stride(1),
                    None if q_start is None else q_start.data_ptr(), lse.data_ptr(),
@@ -543,7 +543,7 @@ def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, ma
         if size:
             ws = torch.empty(size, dtype=torch.uint8, device=q.device)
             at = ws.data_ptr()
-    stream = torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    stream = torch._C._cuda_getCurrentRawStream(current)
     st = L.zc_attend(ref, cache.ref, at, size, stream) if prefix is None else L.zc_attend_shared(ref, prefix.ref, cache.ref, at, size, stream)
     if st != OK:
         raise ZcError(st, what)
@@ -577,8 +577,8 @@ def evict(cache, weights, keep, into, into_weights=None, sinks=0, recent=0, kept
     for t, c in ((weights, cache), (into_weights, into)):
         if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (c.n_seqs, c.n_heads, c.capacity) or not t.is_contiguous()):
             raise ValueError("zc_evict: weights have to be contiguous float32 [n_seqs, n_heads, table_pages * page_tokens]")
-    if weights.device.type != "cuda" or any(t is not None and t.device != weights.device for t in (cache, into, into_weights, kept)):
-        raise ValueError("zc_evict: tensors have to be on one GPU")
+    if not weights.is_cuda or weights.device.index != torch._C._cuda_getDevice() or any(t is not None and t.device != weights.device for t in (cache, into, into_weights, kept)):
+        raise ValueError("zc_evict: tensors have to be on one GPU, the current one")
     st = lib().zc_evict(cache.ref, weights.data_ptr(), keep, sinks, recent, into.ref, into_weights.data_ptr() if into_weights is not None else None,
                         kept.data_ptr(), _stream())
     _check(st, "zc_evict")
