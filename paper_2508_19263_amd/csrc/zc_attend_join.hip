@@ -17,8 +17,8 @@ constexpr uint32_t kFewSlots = 8;
 //
 // Workgroups behind those take 1,024 tokens of a (sequence, K/V head) each and add up their weights from the logits that
 // k_attend_few has left (`logits`, where rereading these costs less than rereading the keys): four tokens to a thread, the
-// rows one after the other.  (4 FP8 caches of 8,192 tokens, 8 K/V heads, 4 rows each: 4.6 us with the join, 0.6 more than the join
-// alone; the whole call 19.8 us against 17.4 without weights.)
+// rows one after the other.  (4 FP8 caches of 8,192 tokens, 8 K/V heads, 4 rows each: 5.0 us with the join, 1.1 more than the join
+// alone; the whole call 19.7 us against 17.5 without weights.)
 //
 // FEW: at most kFewSlots of them.  A row is D / 4 threads then, each with four dimensions of every slot, 8 or 16 rows to a workgroup, and
 // nothing is exchanged: 1,680 rows of 64 and six slots 5.2 -> 3.5 us, 43,000 of 64 and two slots 50 -> 7 us.
