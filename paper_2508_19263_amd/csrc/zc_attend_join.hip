@@ -16,12 +16,13 @@ constexpr uint32_t kFewSlots = 8;
 // 33 slots, 35 MB, 9 us).
 //
 // Workgroups behind those take 1,024 tokens of a (sequence, K/V head) each and add up their weights from the logits that
-// k_attend_few has left (`logits`, where rereading these costs less than rereading the keys): four tokens to a thread, the
-// rows one after the other.  (4 FP8 caches of 8,192 tokens, 8 K/V heads, 4 rows each: 5.0 us with the join, 1.1 more than the join
+// k_attend_few has left (`logits`, where rereading these costs less than rereading the keys): four tokens to a thread, eight
+// rows on their way at a time.  (4 FP8 caches of 8,192 tokens, 8 K/V heads, 4 rows each: 5.0 us with the join, 1.1 more than the join
 // alone; the whole call 19.7 us against 17.5 without weights.)
 //
 // FEW: at most kFewSlots of them.  A row is D / 4 threads then, each with four dimensions of every slot, 8 or 16 rows to a workgroup, and
-// nothing is exchanged: 1,680 rows of 64 and six slots 5.2 -> 3.5 us, 43,000 of 64 and two slots 50 -> 7 us.
+// nothing is exchanged: a call with 1,680 rows of 64 and three slots took 16.9 us without it and takes 15.2, one with 43,000 and two 81
+// and 38.  (With the 33 slots above, 8 of them at a time would be several rounds of loads one after the other.)
 template <int D, bool FEW>
 __global__ __launch_bounds__(256, 4) void k_attend_join(AttendDev a, WeightsDev wt, uint32_t slots, uint32_t join_blocks, uint32_t blocks_per_unit)
 {
