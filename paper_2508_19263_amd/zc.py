@@ -528,6 +528,8 @@ def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, ma
     for t in (weights, weights_out):
         if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (cache.n_seqs, cache.n_heads, cache.capacity) or not t.is_contiguous()):
             raise ValueError("%s: weights have to be contiguous float32 [n_seqs, n_heads, table_pages * page_tokens]" % what)
+    if ws is not None and not ws.is_contiguous():
+        raise ValueError("%s: ws has to be contiguous" % what)
     device, current = q.device, torch._C._cuda_getDevice() if q.is_cuda else -1       # (the kernels go to the current GPU's stream)
     if device.index != current or cache.device != device or any(t is not None and t.device != device for t in (out, lse, q_start, weights, weights_out, ws)) or \
             (prefix is not None and prefix.device != device):
