@@ -530,6 +530,8 @@ def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, ma
             raise ValueError("%s: weights have to be contiguous float32 [n_seqs, n_heads, table_pages * page_tokens]" % what)
     if ws is not None and not ws.is_contiguous():
         raise ValueError("%s: ws has to be contiguous" % what)
+    if max_q_len is None:
+        max_q_len = 1 if q_start is None else max(n, 1)
     device, current = q.device, torch._C._cuda_getDevice() if q.is_cuda else -1       # (the kernels go to the current GPU's stream)
     if device.index != current or cache.device != device or any(t is not None and t.device != device for t in (out, lse, q_start, weights, weights_out, ws)) or \
             (prefix is not None and prefix.device != device):
@@ -552,17 +554,19 @@ def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, ma
     return out, lse
 
 
-def attend(q, cache, q_start=None, max_q_len=1, window=0, sinks=0, scale=None, max_kv_len=0, out=None, lse=None, weights=None, weights_out=None, ws=None):
+def attend(q, cache, q_start=None, max_q_len=None, window=0, sinks=0, scale=None, max_kv_len=0, out=None, lse=None, weights=None, weights_out=None, ws=None):
     """Attention of BF16 queries [n_tokens, n_q_heads, head_dim] over a PagedCache; returns (out, lse).
 
-    q_start: int32 [n_seqs + 1], where each sequence's query tokens begin (None: one token per sequence); at most max_q_len
-    each.  window: how many of the latest tokens a query sees, itself included (0: all); sinks: how many of the first ones
-    it always sees.  scale: of the logits (None: head_dim ** -0.5).  max_kv_len: no length is above it (0: the table's room).
-    weights_out: also leaves weights (None: zeros) plus the attention weight given to each token there."""
+    q_start: int32 [n_seqs + 1], where each sequence's query tokens begin (None: one token per sequence).  max_q_len: no sequence
+    has more of them (None: any number); kernels are chosen by it, so it is worth giving where all sequences go on by a token or a
+    few, and those that bring a prompt are best given a call of their own.  window: how many of the latest tokens a query sees,
+    itself included (0: all); sinks: how many of the first ones it always sees.  scale: of the logits (None: head_dim ** -0.5).
+    max_kv_len: no length is above it (0: the table's room).  weights_out: also leaves weights (None: zeros) plus the attention
+    weight given to each token there."""
     return _attend("zc_attend", q, None, cache, q_start, max_q_len, window, sinks, scale, max_kv_len, 0, out, lse, weights, weights_out, ws)
 
 
-def attend_shared(q, prefix, cache, q_start=None, max_q_len=1, window=0, sinks=0, scale=None, max_kv_len=0, max_prefix_len=0, out=None, lse=None, ws=None):
+def attend_shared(q, prefix, cache, q_start=None, max_q_len=None, window=0, sinks=0, scale=None, max_kv_len=0, max_prefix_len=0, out=None, lse=None, ws=None):
     """attend() for sequences whose first tokens are those of `prefix` (a PagedCache of one sequence), read once for all of
     them; `cache` holds what follows in each."""
     return _attend("zc_attend_shared", q, prefix, cache, q_start, max_q_len, window, sinks, scale, max_kv_len, max_prefix_len, out, lse, None, None, ws)
