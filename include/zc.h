@@ -420,7 +420,8 @@ typedef struct {
  *   out = v_scale * sum exp(s_t) v_t / sum exp(s_t),   lse = ln sum exp(s_t);
  * a query that sees nothing (or nothing with a logit above minus infinity) has out = 0 and lse = -infinity.  Products are
  * accumulated, and the softmax is held, in 32 bits; its weights are rounded to the type the values are multiplied in (BF16 for
- * BF16 pages, half precision for FP8 pages), the result once to BF16.  Query tokens of no sequence are left untouched. */
+ * BF16 pages; half precision for FP8 pages, to within 2^-32 of a row's largest weight where they are below 2^-21 of it), the result
+ * once to BF16.  Query tokens of no sequence are left untouched. */
 typedef struct {
     uint32_t struct_size;       /* = sizeof(zc_attend_args) */
     uint32_t n_tokens, n_q_heads, max_q_len;

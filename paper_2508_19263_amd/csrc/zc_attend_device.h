@@ -22,6 +22,10 @@ constexpr float kNegInf = -__builtin_inff();
 // A row's running maximum is replaced, and what has been added up scaled, only where a logit is more than 2^kSlack above it: weights
 // then reach 2^kSlack, which the 32-bit sums and the operands' types (half precision to 2^16) hold with the same relative error.
 constexpr float kSlack = 8.0f;
+// Weights in half precision (FP8 values) are all 2^kLift of what they are, and the sum that they are divided by is too.  Half
+// precision ends at 2^-24, but the sum counts what is below: many light tokens beside a heavy one would lose their share.  With both
+// powers weights reach 2^15 of half precision's 2^16, and end at 2^-31 of a row's heaviest.
+template <int FMT> constexpr float kLift = FMT == ZC_FMT_BF16 ? 0.0f : 7.0f;
 
 template <int FMT> struct PageElem;
 template <> struct PageElem<ZC_FMT_BF16> { static constexpr int BYTES = 2; };
@@ -72,7 +76,7 @@ __device__ __forceinline__ float max_over_wave(float x) { return __uint_as_float
 __device__ __forceinline__ float sum_over_wave(float x) { return __uint_as_float(over_wave(bits(x), [](uint32_t p, uint32_t q) { return bits(__uint_as_float(p) + __uint_as_float(q)); })); }
 
 // FP8 elements are exact in BF16 and in half precision, so keys go to the type of the queries, and values to the type with
-// more mantissa: the weights they are multiplied with lie in [0, 1] and are rounded to that type too.
+// more mantissa: the weights they are multiplied with (at most 2^(kSlack + kLift)) are rounded to that type too.
 // two bytes (the low or the high ones of a word)
 template <int FMT, bool HIGH> __device__ __forceinline__ uint32_t two_to_bf16(uint32_t w)
 {
@@ -146,9 +150,11 @@ template <int D> __device__ __forceinline__ uint32_t key_place(uint32_t n, uint3
     return D == 128 ? n * 256 + ((c ^ (n & 15)) << 4) : n * 128 + ((c ^ ((n >> 1) & 7)) << 4);
 }
 
-// A part's maximum in base 2: minus infinity where it has seen nothing (its sum is 0), not a number where its sum is not one, though all
+// What a row's logits in base 2 are taken relative to: its weights are 2 to the power of the difference.
+template <int FMT> __device__ __forceinline__ float log2_base(float m, float c) { return m == kNegInf ? 0.0f : m * c - kLift<FMT>; }
+// A part's base: minus infinity where it has seen nothing (its sum is 0), not a number where its sum is not one, though all
 // its products were not numbers either and have left the maximum where it was.
-__device__ __forceinline__ float log2_top(float m, float c, float sum) { return sum != sum ? sum : m == kNegInf ? kNegInf : m * c; }
+template <int FMT> __device__ __forceinline__ float log2_top(float m, float c, float sum) { return sum != sum ? sum : m == kNegInf ? kNegInf : log2_base<FMT>(m, c); }
 
 // ---- sequences, rows, positions ----------------------------------------------------------------
 struct Span { int32_t first, count; };         // a sequence's query tokens

@@ -263,11 +263,11 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
 #pragma unroll
                 for (int i = 0; i < DL; i++) o[t][i] *= f;
             }
-            const float mc = m[t] == kNegInf ? 0.0f : m[t] * c;
+            const float base = log2_base<FMT>(m[t], c);
             float e[8];
 #pragma unroll
             for (int j = 0; j < 8; j++) {
-                e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][j / 4][j & 3], c, -mc));
+                e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][j / 4][j & 3], c, -base));
             }
             l[t] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
 #pragma unroll
@@ -311,7 +311,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
 #pragma unroll
     for (int t = 0; t < QT; t++) {
         l[t] = sum_over_16(sum_over_32(l[t]));
-        if (g == 0) { ml[wave][t * 16 + n16][0] = log2_top(m[t], c, l[t]); ml[wave][t * 16 + n16][1] = l[t]; }
+        if (g == 0) { ml[wave][t * 16 + n16][0] = log2_top<FMT>(m[t], c, l[t]); ml[wave][t * 16 + n16][1] = l[t]; }
     }
     __syncthreads();
     constexpr uint32_t kPerRow = kWaves * 4, DP = D / kPerRow;     // threads per row, dimensions per thread

@@ -291,12 +291,12 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
         const uint8_t *vt = tile.values;
         if (__builtin_expect(edge, 0)) hide(t0, there, s);
         raise(top_of(s));
-        const float mc = m == kNegInf ? 0.0f : m * c;
+        const float base = log2_base<FMT>(m, c);
         float sum[4] = {0, 0, 0, 0};
         u32x4_t p[kStretches];
 #pragma unroll
         for (int i = 0; i < kTile / 2; i++) {
-            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s.half[i / 16][i & 15], c, -mc));        // (0 for the products hidden above)
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s.half[i / 16][i & 15], c, -base));        // (0 for the products hidden above)
             s.half[i / 16][i & 15] = e;
             sum[i & 3] += e;
             if (i & 1) p[i / 8][i / 2 & 3] = pack_weights<FMT>(s.half[i / 16][(i & 15) - 1], e);
@@ -390,7 +390,7 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
     // ---- results: a lane has 4 consecutive dimensions at a time
     if (row.token < 0) return;
     const float sum = sum_over_32(l);
-    const float top = log2_top(m, c, sum);
+    const float top = log2_top<FMT>(m, c, sum);
     const uint64_t at = (uint64_t)row.token * a.q_heads + row.q_head;
     if (a.direct) {
         const float inv = sum == 0.0f ? 0.0f : v_scale / sum;
