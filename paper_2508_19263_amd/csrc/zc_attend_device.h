@@ -156,6 +156,14 @@ template <int FMT> __device__ __forceinline__ float log2_base(float m, float c) 
 // its products were not numbers either and have left the maximum where it was.
 template <int FMT> __device__ __forceinline__ float log2_top(float m, float c, float sum) { return sum != sum ? sum : m == kNegInf ? kNegInf : log2_base<FMT>(m, c); }
 
+// Eight elements of a query as they are multiplied: a negative factor of the logits goes to their signs, and one that is not a number takes
+// their place, so that what a row sees is not a number and what is hidden from it (minus infinity, put there after the product) stays that.
+__device__ __forceinline__ u32x4_t query_operand(u32x4_t x, float factor)
+{
+    const uint32_t flip = factor < 0 ? 0x80008000u : 0u;
+    return factor != factor ? u32x4_t{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u} : x ^ flip;
+}
+
 // ---- sequences, rows, positions ----------------------------------------------------------------
 struct Span { int32_t first, count; };         // a sequence's query tokens
 

@@ -131,9 +131,8 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
     const float k_scale = a.c.k_scales ? a.c.k_scales[unit] : 1.0f;
     const float v_scale = a.c.v_scales ? a.c.v_scales[unit] : 1.0f;
     const float signed_c = a.scale * k_scale * kLog2e;
-    // logits in base 2; a negative factor goes to the queries' signs, and 0 is made one that takes any product to 0 but minus infinity
+    // logits in base 2; 0 is made a factor that takes any product to 0 but minus infinity (for signs and NaN see query_operand)
     const float c = fmaxf(fabsf(signed_c), 1e-30f);
-    const uint32_t flip = signed_c < 0 ? 0x80008000u : 0u;
 
     u32x4_t q[QT][KS];
 #pragma unroll
@@ -145,7 +144,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
             const int dim = FMT == ZC_FMT_BF16 ? s * 32 + (int)g * 8 : (s / 2) * 64 + (int)g * 16 + (s & 1) * 8;
             u32x4_t x = {0, 0, 0, 0};
             if (rows[t].token >= 0) x = *reinterpret_cast<const u32x4_t *>(row + dim);
-            q[t][s] = x ^ flip;
+            q[t][s] = query_operand(x, signed_c);
         }
     }
 

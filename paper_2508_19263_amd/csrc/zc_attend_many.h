@@ -112,9 +112,8 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
 
     const float k_scale = a.c.k_scales ? a.c.k_scales[unit] : 1.0f, v_scale = a.c.v_scales ? a.c.v_scales[unit] : 1.0f;
     const float signed_c = a.scale * k_scale * kLog2e;
-    // logits in base 2; a negative factor goes to the queries' signs, and 0 is made one that takes any product to 0 but minus infinity
+    // logits in base 2; 0 is made a factor that takes any product to 0 but minus infinity (for signs and NaN see query_operand)
     const float c = fmaxf(fabsf(signed_c), 1e-30f);
-    const uint32_t flip = signed_c < 0 ? 0x80008000u : 0u;
     u32x4_t q[KS];
     {
         const uint16_t *from = a.q + (uint64_t)max(row.token, 0) * a.q_token_stride + (uint64_t)row.q_head * a.q_head_stride;
@@ -122,7 +121,7 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
         for (int u = 0; u < KS; u++) {
             u32x4_t x = {0, 0, 0, 0};
             if (row.token >= 0) x = *reinterpret_cast<const u32x4_t *>(from + u * 16 + g * 8);
-            q[u] = x ^ flip;
+            q[u] = query_operand(x, signed_c);
         }
     }
     float m = kNegInf, l = 0.0f;                               // maximum of the bare products; sum over this lane's tokens

@@ -37,3 +37,39 @@ def test_many_light_tokens_beside_a_heavy_one(fmt, dim, nats, q_len, length):
     floor = 2 * 2.0 ** -32 * cache.rows("v", 0, 0).abs().sum(dim=0) if fmt != BF16 else 0.0
     agree(out, want, tol + floor, "out")
     agree(lse, want_lse, tol_lse, "lse")
+
+
+@pytest.mark.parametrize("lens,q_lens", [([300, 2], [1, 5]), ([300, 20], [1, 40]), ([3000, 2], [1, 5]), ([3000, 900], [1, 1])])
+@pytest.mark.parametrize("fmt", [BF16, E4M3])
+def test_a_scale_that_is_not_a_number(fmt, lens, q_lens):
+    """It is seen in its head's results and weights, and nowhere else; queries that see nothing have nothing to do with it."""
+    cache = Cache(lens, 2, 128, fmt, scales=True)
+    q, w = queries(sum(q_lens), 8, 128), torch.zeros((2, 2, cache.paged.capacity), device="cuda")
+    more = dict(q_start=starts(q_lens), max_q_len=max(q_lens))
+    want, want_lse = zc.attend(q, cache.paged, weights_out=w, **more)
+    cache.ks[1, 0] = float("nan")
+    w_nan = torch.zeros_like(w)
+    out, lse = zc.attend(q, cache.paged, weights_out=w_nan, **more)
+    blind, first = max(0, q_lens[1] - lens[1]), q_lens[0]        # query tokens of the second sequence that see nothing
+    hit = torch.zeros((sum(q_lens), 8), dtype=torch.bool, device="cuda")
+    hit[first + blind:, :4] = True
+    assert bool(out[hit].isnan().all()) and bool(lse[hit].isnan().all())
+    assert torch.equal(out[~hit], want[~hit]) and torch.equal(lse[~hit], want_lse[~hit])
+    assert blind == 0 or (not bool(out[first:first + blind].any()) and bool((lse[first:first + blind] == -math.inf).all()))
+    assert bool(w_nan[1, 0, :lens[1]].isnan().all())
+    w_nan[1, 0], w[1, 0] = 0, 0
+    assert torch.equal(w_nan, w)
+
+
+@pytest.mark.parametrize("answers", [2, 40])
+def test_a_prefixs_scale_that_is_not_a_number(answers):
+    """Answers that the window has led away from the prefix do not see it."""
+    cache = Cache([50] + [3] * (answers - 1), 2, 128, E4M3)
+    prefix = Cache([300], 2, 128, E4M3, seed=3)
+    q = queries(answers, 8, 128)
+    want, want_lse = zc.attend_shared(q, prefix.paged, cache.paged, window=10)
+    prefix.ks[0, 0] = float("nan")
+    out, lse = zc.attend_shared(q, prefix.paged, cache.paged, window=10)
+    assert bool(out[1:, :4].isnan().all()) and bool(lse[1:, :4].isnan().all())
+    for got, there in ((out, want), (lse, want_lse)):
+        assert torch.equal(got[0], there[0]) and torch.equal(got[:, 4:], there[:, 4:])
