@@ -427,7 +427,7 @@ typedef struct {
     uint32_t n_tokens, n_q_heads, max_q_len;
     uint32_t window, sinks;
     uint32_t max_kv_len, max_prefix_len;    /* no length is above them (greater ones are taken as these); 0: what the tables have room for */
-    float scale;
+    float scale;                /* of the logits; |scale * k_scale| log2 e is taken as 2^-126 where it is less */
     uint32_t reserved;
     const void *d_q;            /* BF16, 16-byte aligned; token t, head j at element t * q_token_stride + j * q_head_stride */
     void *d_out;                /* BF16, likewise */

@@ -19,6 +19,9 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNegInf = -__builtin_inff();
+// A factor of the logits of 0 would take minus infinity, which stands for what is hidden, to NaN: the smallest normal number in its place
+// takes any product to less than 4, and those below 2^100 to nothing.
+constexpr float kLeastFactor = 0x1p-126f;
 // A row's running maximum is replaced, and what has been added up scaled, only where a logit is more than 2^kSlack above it: weights
 // then reach 2^kSlack, which the 32-bit sums and the operands' types (half precision to 2^16) hold with the same relative error.
 constexpr float kSlack = 8.0f;

@@ -183,7 +183,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendDev a, WeightsD
     if (block0 >= length) return;                              // the whole workgroup
     const Span span = query_span(a, seq);
     const float signed_c = a.scale * (a.c.k_scales ? a.c.k_scales[unit] : 1.0f) * kLog2e;
-    const float c = fmaxf(fabsf(signed_c), 1e-30f);            // as in the passes: products of what is hidden are minus infinity, and stay it
+    const float c = fmaxf(fabsf(signed_c), kLeastFactor);      // as in the passes
     const uint32_t flip = signed_c < 0 ? 0x80008000u : 0u;     // (a factor that is not a number is in every lse already)
 
     const int32_t *table = a.c.table + (uint64_t)unit * a.c.table_pages;

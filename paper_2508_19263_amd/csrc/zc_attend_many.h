@@ -112,8 +112,8 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
 
     const float k_scale = a.c.k_scales ? a.c.k_scales[unit] : 1.0f, v_scale = a.c.v_scales ? a.c.v_scales[unit] : 1.0f;
     const float signed_c = a.scale * k_scale * kLog2e;
-    // logits in base 2; 0 is made a factor that takes any product to 0 but minus infinity (for signs and NaN see query_operand)
-    const float c = fmaxf(fabsf(signed_c), 1e-30f);
+    // logits in base 2 (for signs and NaN see query_operand)
+    const float c = fmaxf(fabsf(signed_c), kLeastFactor);
     u32x4_t q[KS];
     {
         const uint16_t *from = a.q + (uint64_t)max(row.token, 0) * a.q_token_stride + (uint64_t)row.q_head * a.q_head_stride;

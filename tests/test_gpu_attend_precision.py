@@ -73,3 +73,11 @@ def test_a_prefixs_scale_that_is_not_a_number(answers):
     assert bool(out[1:, :4].isnan().all()) and bool(lse[1:, :4].isnan().all())
     for got, there in ((out, want), (lse, want_lse)):
         assert torch.equal(got[0], there[0]) and torch.equal(got[:, 4:], there[:, 4:])
+
+
+@pytest.mark.parametrize("q_lens", [[1, 7], [1, 70]])
+def test_a_scale_of_zero_with_large_keys(q_lens):
+    """Products around 1e32 and a factor of 0: every token has the same weight."""
+    def edit(c):
+        c.k[:] = stored(c.k.view(torch.bfloat16).float() * 1e30, BF16)
+    check(Cache([300, 41], 2, 128, BF16, edit=edit), q_lens, 4, scale=0.0, weights=True)
