@@ -511,6 +511,16 @@ class PagedCache:
         self.ref = C.byref(c)
 
 
+_MOST = 0xFFFFFFFF
+
+
+def _check_numbers(what, **numbers):
+    """The library takes 32 bits, and ctypes cuts what has more: -1 would be the largest number there is."""
+    for name, x in numbers.items():
+        if not 0 <= x <= _MOST:
+            raise ValueError("%s: %s has to be in 0 .. 2^32 - 1, not %d" % (what, name, x))
+
+
 def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, max_kv_len, max_prefix_len, out, lse, weights, weights_out, ws):
     if q.dim() != 3 or q.shape[2] != cache.head_dim or q.stride(2) != 1 or q.dtype not in _ROW_TYPES:
         raise ValueError("%s: q has to be [n_tokens, n_q_heads, head_dim] in BF16 with contiguous rows" % what)
@@ -532,6 +542,8 @@ def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, ma
         raise ValueError("%s: ws has to be contiguous" % what)
     if max_q_len is None:
         max_q_len = 1 if q_start is None else max(n, 1)
+    if not (0 <= max_q_len <= _MOST and 0 <= window <= _MOST and 0 <= sinks <= _MOST and 0 <= max_kv_len <= _MOST and 0 <= max_prefix_len <= _MOST):
+        _check_numbers(what, max_q_len=max_q_len, window=window, sinks=sinks, max_kv_len=max_kv_len, max_prefix_len=max_prefix_len)
     device, current = q.device, torch._C._cuda_getDevice() if q.is_cuda else -1       # (the kernels go to the current GPU's stream)
     if device.index != current or cache.device != device or any(t is not None and t.device != device for t in (out, lse, q_start, weights, weights_out, ws)) or \
             (prefix is not None and prefix.device != device):
@@ -576,6 +588,7 @@ def evict(cache, weights, keep, into, into_weights=None, sinks=0, recent=0, kept
     """Leaves `keep` tokens per sequence and head: the first `sinks`, the last `recent`, and of the others those with the largest
     weights (float32 [n_seqs, n_heads, table_pages * page_tokens]); they go to the pages of `into` (another PagedCache),
     whose lengths are set.  Returns their numbers, int32 [n_seqs, n_heads, keep], ascending, -1 behind the last."""
+    _check_numbers("zc_evict", keep=keep, sinks=sinks, recent=recent)
     if kept is None:
         kept = torch.empty((cache.n_seqs, cache.n_heads, keep), dtype=torch.int32, device=weights.device)
     elif kept.dtype != torch.int32 or tuple(kept.shape) != (cache.n_seqs, cache.n_heads, keep) or not kept.is_contiguous():

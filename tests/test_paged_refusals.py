@@ -26,3 +26,21 @@ def test_scratch_with_holes(ws):
     """Its size is taken from the number of elements, so these have to lie one behind the other."""
     with pytest.raises(ValueError, match="ws"):
         call(ws=ws)
+
+
+@pytest.mark.parametrize("name", ["max_q_len", "window", "sinks", "max_kv_len"])
+@pytest.mark.parametrize("value", [-1, 1 << 32, (1 << 32) + 5])
+def test_numbers_that_the_call_has_no_room_for(name, value):
+    """ctypes would cut them to 32 bits: sinks=-1 would make every token a sink."""
+    with pytest.raises(ValueError, match=name):
+        call(**{name: value})
+    with pytest.raises(ValueError, match=name):
+        zc.attend_shared(torch.zeros((2, 4, 64), dtype=torch.bfloat16), paged(table=torch.zeros((1, 1, 2), dtype=torch.int32), lengths=torch.zeros(1, dtype=torch.int32)),
+                         paged(), **{name: value})
+
+
+@pytest.mark.parametrize("name", ["keep", "sinks", "recent"])
+@pytest.mark.parametrize("value", [-1, 1 << 32])
+def test_numbers_that_eviction_has_no_room_for(name, value):
+    with pytest.raises(ValueError, match=name):
+        evict(**{name: value})
