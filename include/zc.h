@@ -430,7 +430,7 @@ typedef struct {
     float scale;                /* of the logits; |scale * k_scale| log2 e is taken as 2^-126 where it is less */
     uint32_t reserved;
     const void *d_q;            /* BF16, 16-byte aligned; token t, head j at element t * q_token_stride + j * q_head_stride */
-    void *d_out;                /* BF16, likewise */
+    void *d_out;                /* BF16, likewise; with d_weights_out not on top of d_q, which is read again then */
     uint64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;  /* multiples of 8 */
     const int32_t *d_q_start;
     float *d_lse;               /* [n_tokens][n_q_heads], or NULL */

@@ -121,6 +121,7 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
     if (!std::isfinite(x->scale) || x->reserved) return ZC_ERR_INVALID_ARG;
     if (x->d_weights_out && (shared || (x->n_tokens && !x->d_lse))) return ZC_ERR_INVALID_ARG;
     if (x->d_weights_in && !x->d_weights_out) return ZC_ERR_INVALID_ARG;
+    if (x->d_weights_out && x->n_tokens && x->d_out == x->d_q) return ZC_ERR_INVALID_ARG;       // (k_attend_weights reads the queries when the results are there)
     if (x->max_kv_len && x->max_kv_len < (uint32_t)a.c.limit) a.c.limit = (int32_t)x->max_kv_len;
 
     a.q = (const uint16_t *)x->d_q;

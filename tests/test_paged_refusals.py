@@ -44,3 +44,14 @@ def test_numbers_that_the_call_has_no_room_for(name, value):
 def test_numbers_that_eviction_has_no_room_for(name, value):
     with pytest.raises(ValueError, match=name):
         evict(**{name: value})
+
+
+def test_queries_that_are_read_again():
+    """Weights of many rows come from the queries once more, when the results have been written."""
+    for rows in (1, 100):
+        x = args(n_tokens=100, max_q_len=rows, d_q_start=SOME, d_weights_out=4 * SOME, d_out=2 * SOME)
+        c = cache(table_pages=4096)
+        need = zc.lib().zc_attend_workspace_bytes(C.byref(x), None, C.byref(c))
+        assert zc.lib().zc_attend(C.byref(x), C.byref(c), 8 * SOME, max(need, 1) - 1, None) == zc.ERR_BUFFER_TOO_SMALL       # nothing but that is wrong
+        x.d_out = x.d_q
+        assert zc.lib().zc_attend(C.byref(x), C.byref(c), 8 * SOME, 1 << 40, None) == zc.ERR_INVALID_ARG
