@@ -529,6 +529,8 @@ def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, ma
         out = q.new_empty((n, heads, dim))
     elif out.shape != q.shape or out.stride(2) != 1 or out.dtype not in _ROW_TYPES:
         raise ValueError("%s: out has to have q's shape and type, with contiguous rows" % what)
+    elif (n > 1 and out.stride(0) < dim) or (heads > 1 and out.stride(1) < dim):
+        raise ValueError("%s: rows of out overlap" % what)
     if lse is None:
         lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
     elif lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous():

@@ -46,6 +46,13 @@ def test_numbers_that_eviction_has_no_room_for(name, value):
         evict(**{name: value})
 
 
+@pytest.mark.parametrize("out", [torch.zeros((1, 4, 64), dtype=torch.bfloat16).expand(2, 4, 64), torch.zeros((2, 1, 64), dtype=torch.bfloat16).expand(2, 4, 64),
+                                 torch.zeros(1000, dtype=torch.bfloat16).as_strided((2, 4, 64), (256, 32, 1))])
+def test_results_on_top_of_each_other(out):
+    with pytest.raises(ValueError, match="overlap"):
+        call(out=out)
+
+
 def test_queries_that_are_read_again():
     """Weights of many rows come from the queries once more, when the results have been written."""
     for rows in (1, 100):
