@@ -546,6 +546,8 @@ def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, ma
         max_q_len = 1 if q_start is None else max(n, 1)
     if not (0 <= max_q_len <= _MOST and 0 <= window <= _MOST and 0 <= sinks <= _MOST and 0 <= max_kv_len <= _MOST and 0 <= max_prefix_len <= _MOST):
         _check_numbers(what, max_q_len=max_q_len, window=window, sinks=sinks, max_kv_len=max_kv_len, max_prefix_len=max_prefix_len)
+    if (q.requires_grad or (weights is not None and weights.requires_grad)) and torch.is_grad_enabled():
+        raise ValueError("%s: there is no gradient through a stored cache: detach q and weights, or call it under torch.no_grad()" % what)
     device, current = q.device, torch._C._cuda_getDevice() if q.is_cuda else -1       # (the kernels go to the current GPU's stream)
     if device.index != current or cache.device != device or any(t is not None and t.device != device for t in (out, lse, q_start, weights, weights_out, ws)) or \
             (prefix is not None and prefix.device != device):
@@ -598,6 +600,8 @@ def evict(cache, weights, keep, into, into_weights=None, sinks=0, recent=0, kept
     for t, c in ((weights, cache), (into_weights, into)):
         if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (c.n_seqs, c.n_heads, c.capacity) or not t.is_contiguous()):
             raise ValueError("zc_evict: weights have to be contiguous float32 [n_seqs, n_heads, table_pages * page_tokens]")
+    if into_weights is not None and weights.requires_grad and torch.is_grad_enabled():
+        raise ValueError("zc_evict: no gradient goes to into_weights: detach weights, or call it under torch.no_grad()")
     if not weights.is_cuda or weights.device.index != torch._C._cuda_getDevice() or any(t is not None and t.device != weights.device for t in (cache, into, into_weights, kept)):
         raise ValueError("zc_evict: tensors have to be on one GPU, the current one")
     st = lib().zc_evict(cache.ref, weights.data_ptr(), keep, sinks, recent, into.ref, into_weights.data_ptr() if into_weights is not None else None,

@@ -46,6 +46,21 @@ def test_numbers_that_eviction_has_no_room_for(name, value):
         evict(**{name: value})
 
 
+def test_gradients_are_not_dropped():
+    q, w = torch.zeros((2, 4, 64), dtype=torch.bfloat16, requires_grad=True), torch.zeros((2, 1, 32), requires_grad=True)
+    with pytest.raises(ValueError, match="gradient"):
+        call(q=q)
+    with pytest.raises(ValueError, match="gradient"):
+        call(weights=w, weights_out=torch.zeros((2, 1, 32)))
+    with pytest.raises(ValueError, match="gradient"):
+        evict(weights=w, into_weights=torch.zeros((2, 1, 32)))
+    with torch.no_grad():
+        with pytest.raises(ValueError, match="GPU"):             # nothing but that is wrong
+            call(q=q)
+        with pytest.raises(ValueError, match="GPU"):
+            evict(weights=w)
+
+
 @pytest.mark.parametrize("out", [torch.zeros((1, 4, 64), dtype=torch.bfloat16).expand(2, 4, 64), torch.zeros((2, 1, 64), dtype=torch.bfloat16).expand(2, 4, 64),
                                  torch.zeros(1000, dtype=torch.bfloat16).as_strided((2, 4, 64), (256, 32, 1))])
 def test_results_on_top_of_each_other(out):
