@@ -552,8 +552,11 @@ def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, ma
     if device.index != current or cache.device != device or any(t is not None and t.device != device for t in (out, lse, q_start, weights, weights_out, ws)) or \
             (prefix is not None and prefix.device != device):
         raise ValueError("%s: tensors have to be on one GPU, the current one" % what)
+    strides = q.stride()[:2] + out.stride()[:2]
+    if n == 1 or heads == 1:                                     # the stride of a dimension of one element is any number
+        strides = [0 if size == 1 else stride for size, stride in zip((n, heads, n, heads), strides)]
     a = AttendArgs(_ATTEND_ARGS_BYTES, n, heads, max_q_len, window, sinks, max_kv_len, max_prefix_len, dim ** -0.5 if scale is None else scale, 0,
-                   q.data_ptr(), out.data_ptr(), q.stride(0), q.stride(1), out.stride(0), out.stride(1),
+                   q.data_ptr(), out.data_ptr(), *strides,
                    None if q_start is None else q_start.data_ptr(), lse.data_ptr(),
                    None if weights is None else weights.data_ptr(), None if weights_out is None else weights_out.data_ptr())
     L, ref = lib(), C.byref(a)

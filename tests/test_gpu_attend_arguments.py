@@ -24,3 +24,17 @@ def test_all_query_tokens_are_answered_whatever_their_number(q_lens, shared):
     want, want_lse, _, tol, tol_lse, _ = attention(q, q_lens, cache, prefix)
     agree(out, want, tol, "out")
     agree(lse, want_lse, tol_lse, "lse")
+
+
+@pytest.mark.parametrize("n,heads", [(1, 8), (3, 1), (1, 1)])
+def test_strides_of_single_tokens_and_heads(n, heads):
+    """Where there is only one token, or one query head, its stride is any number, and no element is found by it."""
+    cache = Cache([200] * n, min(heads, 2), 64, zc.FMT_BF16)
+    flat = queries(n, heads, 64)
+    want, want_lse = zc.attend(flat, cache.paged)
+    order = (2, 0, 1) if n == 1 else (0, 2, 1)                   # a last dimension of one element goes where there is only one token or head
+    q, out = (torch.zeros((heads, 64, 1) if n == 1 else (n, 64, 1), dtype=torch.bfloat16, device="cuda").permute(order) for _ in range(2))
+    q.copy_(flat)
+    assert q.shape == flat.shape and (q.stride(0) % 8 or q.stride(1) % 8) and q.stride(2) == 1
+    got, lse = zc.attend(q, cache.paged, out=out)
+    assert torch.equal(got, want) and torch.equal(lse, want_lse) and got is out
