@@ -205,7 +205,7 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
         if (groups * p.weight_parts > kMaxBlocks) return ZC_ERR_INVALID_ARG;
         if (p.weight_parts > 1) {
             p.weights_at = align256(p.ws_bytes);
-            p.ws_bytes = p.weights_at + units * p.weight_parts * (uint64_t)a.c.capacity * 4;
+            p.ws_bytes = p.weights_at + units * p.weight_parts * (uint64_t)a.c.limit * 4;
         }
     }
     *out = p;

@@ -47,7 +47,7 @@ constexpr uint32_t kLongPart = 8192;   // tokens
 struct WeightsDev {
     const float *in;                   // or null
     float *out;                        // [seqs][heads][capacity]
-    float *part;                       // workspace: [parts][seqs][heads][capacity] where parts > 1
+    float *part;                       // workspace: [parts][seqs][heads][limit] where parts > 1
     uint32_t parts;                    // workgroups of k_attend_weights that share tokens, at most kMostParts
 };
 

@@ -329,7 +329,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendDev a, WeightsD
     const int32_t t = t0 + (int32_t)(n32 / 16 * 32 + (n32 / 4 & 3) * 8 + g * 4 + (n32 & 3));
     if (t < length) {
         const uint64_t at = (uint64_t)unit * (uint64_t)a.c.capacity + (uint64_t)t;
-        if (wt.parts > 1) wt.part[(uint64_t)part * units * (uint64_t)a.c.capacity + at] = acc[0];
+        if (wt.parts > 1) wt.part[((uint64_t)part * units + unit) * (uint64_t)a.c.limit + (uint64_t)t] = acc[0];
         else wt.out[at] = (wt.in ? wt.in[at] : 0.0f) + acc[0];
     }
 }
@@ -340,10 +340,11 @@ __global__ __launch_bounds__(256) void k_weights_sum(AttendDev a, WeightsDev wt)
     const uint32_t units = a.n_seqs * a.c.heads, unit = blockIdx.x % units;
     const int32_t length = clamped_length(a.c.lengths, unit / a.c.heads, a.c.limit), t = (int32_t)(blockIdx.x / units * 256 + threadIdx.x);
     if (t >= length) return;
-    const uint64_t at = (uint64_t)unit * (uint64_t)a.c.capacity + (uint32_t)t, apart = (uint64_t)units * (uint64_t)a.c.capacity;
+    const uint64_t at = (uint64_t)unit * (uint64_t)a.c.capacity + (uint32_t)t;
+    const uint64_t from = (uint64_t)unit * (uint64_t)a.c.limit + (uint32_t)t, apart = (uint64_t)units * (uint64_t)a.c.limit;
     float x[kMostParts];
 #pragma unroll
-    for (uint32_t p = 0; p < kMostParts; p++) x[p] = wt.part[min(p, wt.parts - 1) * apart + at];
+    for (uint32_t p = 0; p < kMostParts; p++) x[p] = wt.part[min(p, wt.parts - 1) * apart + from];
     float sum = 0.0f;
 #pragma unroll
     for (uint32_t p = 0; p < kMostParts; p++) sum += p < wt.parts ? x[p] : 0.0f;

@@ -1,0 +1,46 @@
+"""Limits below the table's room, scratch of the caller's, mixed batches, pages far apart: against the definition in 64 bits (tests/paged.py)."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2508_19263_amd import zc
+from tests.paged import JUNK, Cache, agree, attention, gen, starts
+from tests.test_gpu_attend import check, queries
+
+pytestmark = pytest.mark.gpu
+
+BF16, E4M3 = zc.FMT_BF16, zc.FMT_FP8_E4M3
+
+
+@pytest.mark.parametrize("fmt,dim", [(BF16, 64), (E4M3, 128)])
+@pytest.mark.parametrize("q_lens,lens", [([1, 1, 1], [999, 40, 0]), ([3, 1, 2], [999, 40, 17]), ([40, 3, 9], [999, 40, 17]), ([700, 3, 9], [1337, 40, 17]),
+                                         ([1, 1, 1], [2999, 40, 1])])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (300, 5)])
+def test_the_longest_length_below_the_tables_room(fmt, dim, q_lens, lens, window, sinks):
+    """Few rows and many, weights from the logits and from the keys, and from parts of the rows: the weights lie by the table's room."""
+    cache = Cache(lens, 2, dim, fmt, room=5000)
+    check(cache, q_lens, 4, window, sinks, weights=True, max_kv_len=max(lens))
+    check(cache, q_lens, 4, window, sinks, max_kv_len=max(lens))
+
+
+@pytest.mark.parametrize("fmt,dim", [(BF16, 128), (E4M3, 64)])
+@pytest.mark.parametrize("q_lens,lens", [([1, 1, 1], [199, 40, 0]), ([3, 1, 2], [199, 1, 17]), ([1] * 40, [7 + i for i in range(40)]), ([100, 3], [333, 9])])
+@pytest.mark.parametrize("prefix", [37, 2001])
+def test_limits_of_a_prefix_and_what_follows_it(fmt, dim, q_lens, lens, prefix):
+    pre, cache = Cache([prefix], 2, dim, fmt, room=4000, seed=9), Cache(lens, 2, dim, fmt, room=700)
+    for window, sinks in ((0, 0), (150, 5)):
+        check(cache, q_lens, 4, window, sinks, prefix=pre, max_kv_len=max(lens), max_prefix_len=prefix)
+
+
+@pytest.mark.parametrize("q_lens", [[2, 1], [90, 1]])
+def test_lengths_above_a_limit_are_taken_as_the_limit(q_lens):
+    cache, pre = Cache([900, 77], 2, 128, E4M3, room=2000), Cache([500], 2, 128, E4M3, room=1000, seed=4)
+    q, w = queries(sum(q_lens), 8, 128), [torch.full((2, 2, cache.paged.capacity), -7.0, device="cuda") for _ in range(2)]
+    more = dict(q_start=starts(q_lens), max_q_len=max(q_lens), window=400, sinks=3, max_kv_len=613)
+    results = []
+    for i, (own, prefix) in enumerate(((900, 500), (613, 301))):
+        cache.lengths[0], pre.lengths[0] = own, prefix
+        results.append(zc.attend(q, cache.paged, weights_out=w[i], **more) + zc.attend_shared(q, pre.paged, cache.paged, max_prefix_len=301, **more))
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and torch.equal(*w)
+    assert bool((w[0][0, :, 613:] == -7).all()) and bool((w[0][0, :, :613] >= 0).all())

@@ -77,3 +77,18 @@ def test_queries_that_are_read_again():
         assert zc.lib().zc_attend(C.byref(x), C.byref(c), 8 * SOME, max(need, 1) - 1, None) == zc.ERR_BUFFER_TOO_SMALL       # nothing but that is wrong
         x.d_out = x.d_q
         assert zc.lib().zc_attend(C.byref(x), C.byref(c), 8 * SOME, 1 << 40, None) == zc.ERR_INVALID_ARG
+
+
+def scratch(x, c):
+    return zc.lib().zc_attend_workspace_bytes(C.byref(x), None, C.byref(c))
+
+
+def weighed(**change):
+    return args(d_q_start=SOME, d_out=2 * SOME, d_weights_out=4 * SOME, **change)
+
+
+def test_scratch_follows_the_longest_length_and_not_the_tables_room():
+    """One prompt of 300 tokens: sums of parts of the rows, for 300 tokens each."""
+    x = weighed(n_tokens=300, n_q_heads=32, max_q_len=300, max_kv_len=300)
+    small, large = (scratch(x, cache(n_seqs=1, n_heads=8, table_pages=n)) for n in (19, 1 << 16))
+    assert 0 < small == large < 1 << 20
