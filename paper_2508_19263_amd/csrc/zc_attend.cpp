@@ -14,6 +14,7 @@ namespace {
 constexpr uint32_t kMaxTokens = 1u << 30;      // positions are signed 32-bit numbers in the kernels, sums of two included
 constexpr uint64_t kMaxBlocks = (1u << 24) - 1;   // of 256 threads: HIP launches fewer than 2^32
 constexpr uint32_t kMaxSlots = 64;             // parts of one row: k_attend_join holds one per lane
+constexpr uint64_t kMostLogits = 1u << 30;     // bytes of scratch
 
 bool aligned4(const void *p) { return ((uintptr_t)p & 3) == 0; }
 
@@ -184,11 +185,15 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
     // the keys again.  Microseconds from logits against keys, 32 caches of 8,000 tokens, 8 heads: 4 rows, FP8, 128 dimensions 134
     // against 233, 64 dimensions 79 against 153; 24 rows 190 against 235 and 145 against 164; 32 rows 216 against 229 and 176 against 161.
     // One cache of 4,000: 4 rows 11.8 against 17.6, 24 rows 20.1 against 20.8, 32 rows 22.5 against 20.8.
-    const uint64_t rows_per_head = (uint64_t)a.max_q_len * a.group;
-    p.logits = x->d_weights_out && x->n_tokens && rows_per_head <= kLogitRows;
+    // Logits have room for the longest length of every sequence, which large tables over few pages make much more than there are tokens, so
+    // where they would take more than kMostLogits the keys are read again too (64 caches of 8,000 tokens, 4 rows, 128 dimensions, with room for
+    // just 1 GiB of logits and for a step more: FP8 321 and 600 us, BF16 521 and 822; with max_kv_len = 8,000, 253 and 451).
+    const uint64_t rows_per_head = (uint64_t)a.max_q_len * a.group, logit_stride = ((uint64_t)a.c.limit + 31) / 32 * 32;
+    p.logits = x->d_weights_out && x->n_tokens && rows_per_head <= kLogitRows &&
+               (uint64_t)a.n_seqs * a.c.heads * rows_per_head * logit_stride * 4 <= kMostLogits;
     if (p.logits) {
         a.logit_rows = (uint32_t)rows_per_head;
-        a.logit_stride = ((uint32_t)a.c.limit + 31) / 32 * 32;
+        a.logit_stride = (uint32_t)logit_stride;
         p.logits_at = p.ws_bytes = align256(p.ws_bytes);
         p.ws_bytes += (uint64_t)a.n_seqs * a.c.heads * a.logit_rows * a.logit_stride * 4;
     }

@@ -44,3 +44,14 @@ def test_lengths_above_a_limit_are_taken_as_the_limit(q_lens):
         results.append(zc.attend(q, cache.paged, weights_out=w[i], **more) + zc.attend_shared(q, pre.paged, cache.paged, max_prefix_len=301, **more))
     assert all(torch.equal(a, b) for a, b in zip(*results)) and torch.equal(*w)
     assert bool((w[0][0, :, 613:] == -7).all()) and bool((w[0][0, :, :613] >= 0).all())
+
+
+@pytest.mark.parametrize("fmt,dim", [(BF16, 64), (E4M3, 128)])
+def test_weights_of_few_rows_with_room_for_more_logits_than_are_kept(fmt, dim):
+    """Eight tables with room for a million tokens, nearly all of whose pages are absent: logits of 24 rows would take 1.6 GB."""
+    cache = Cache([700, 37, 250, 0, 1, 64, 65, 333], 2, dim, fmt)
+    table = torch.full((8, 2, 1 << 16), -1, dtype=torch.int32, device="cuda")
+    table[:, :, :cache.table.shape[2]] = cache.table
+    cache.table = table
+    cache.paged = zc.PagedCache(cache.paged.k_pages, cache.paged.v_pages, table, cache.lengths, fmt, cache.ks, cache.vs)
+    check(cache, [2, 1, 2, 0, 1, 2, 1, 1], 12, 200, 5, weights=True)

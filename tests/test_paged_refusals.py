@@ -92,3 +92,21 @@ def test_scratch_follows_the_longest_length_and_not_the_tables_room():
     x = weighed(n_tokens=300, n_q_heads=32, max_q_len=300, max_kv_len=300)
     small, large = (scratch(x, cache(n_seqs=1, n_heads=8, table_pages=n)) for n in (19, 1 << 16))
     assert 0 < small == large < 1 << 20
+
+
+def test_scratch_of_weights_has_a_bound():
+    """Logits of few rows are kept for the weights where they take at most 1 GiB; else the keys are read again, with 32 bits for every token and
+    as many parts of the rows as make about 1,024 workgroups."""
+    large = cache(n_seqs=32, n_heads=8, table_pages=8192)                      # room for 131,072 tokens
+    parts = 32 * 8 * 24 * 16 * (128 * 4 + 8)                                   # of the attention: rows x parts of 8,192 tokens
+    x = weighed(n_tokens=96, n_q_heads=64, max_q_len=3)                        # 24 rows: 3 GiB of logits
+    assert scratch(x, large) <= parts + 1024
+    x.max_kv_len = 8000                                                        # 188 MiB
+    assert scratch(x, large) >= 32 * 8 * 24 * 8000 * 4
+    x = weighed(n_tokens=32, n_q_heads=8, max_q_len=1)                         # one row: 128 MiB
+    assert scratch(x, large) >= 32 * 8 * 131072 * 4
+    x = weighed(n_tokens=1, n_q_heads=24, max_q_len=1)                         # one cache, 24 rows, just 1 GiB and a step more
+    for tokens, fits in ((11184800, True), (11184832, False)):
+        c = cache(n_seqs=1, n_heads=1, table_pages=tokens // 16)
+        need, logits = scratch(x, c), 24 * tokens * 4
+        assert (need >= logits) == fits and need < logits + (1 << 25) and (fits or need < 1 << 30)
