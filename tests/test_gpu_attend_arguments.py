@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2508_19263_amd import zc
-from tests.paged import Cache, agree, attention, gen, starts
+from tests.paged import Cache, agree, attention, starts
 from tests.test_gpu_attend import queries
 
 pytestmark = pytest.mark.gpu

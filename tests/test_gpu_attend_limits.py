@@ -1,11 +1,11 @@
-"""Limits below the table's room, scratch of the caller's, mixed batches, pages far apart: against the definition in 64 bits (tests/paged.py)."""
+"""Limits below the table's room, scratch of the caller's, mixed batches: against the definition in 64 bits (tests/paged.py)."""
 import ctypes as C
 
 import pytest
 import torch
 
 from paper_2508_19263_amd import zc
-from tests.paged import JUNK, Cache, agree, attention, gen, starts
+from tests.paged import Cache, gen, starts
 from tests.test_gpu_attend import check, queries
 
 pytestmark = pytest.mark.gpu
@@ -55,3 +55,33 @@ def test_weights_of_few_rows_with_room_for_more_logits_than_are_kept(fmt, dim):
     cache.table = table
     cache.paged = zc.PagedCache(cache.paged.k_pages, cache.paged.v_pages, table, cache.lengths, fmt, cache.ks, cache.vs)
     check(cache, [2, 1, 2, 0, 1, 2, 1, 1], 12, 200, 5, weights=True)
+
+
+@pytest.mark.parametrize("q_lens,lens", [([1, 1], [9000, 40]), ([5, 1], [3000, 900]), ([300, 1], [700, 900])])
+@pytest.mark.parametrize("weights", [False, True])
+def test_scratch_of_the_callers(q_lens, lens, weights):
+    """Of exactly the size that is asked for, whatever it holds before, and nothing behind it is touched."""
+    cache = Cache(lens, 2, 128, E4M3)
+    q, w = queries(sum(q_lens), 8, 128), [torch.zeros((2, 2, cache.paged.capacity), device="cuda") for _ in range(2)]
+    more = dict(q_start=starts(q_lens), max_q_len=max(q_lens))
+    want, want_lse = zc.attend(q, cache.paged, weights_out=w[0] if weights else None, **more)
+    a = zc.AttendArgs()
+    a.struct_size, a.n_tokens, a.n_q_heads, a.max_q_len, a.scale = C.sizeof(zc.AttendArgs), sum(q_lens), 8, max(q_lens), 128 ** -0.5
+    a.d_q, a.d_q_start, a.d_out, a.d_lse = q.data_ptr(), more["q_start"].data_ptr(), want.data_ptr(), want_lse.data_ptr()
+    a.q_token_stride = a.out_token_stride = 1024
+    a.q_head_stride = a.out_head_stride = 128
+    a.d_weights_out = w[0].data_ptr() if weights else None
+    size = zc.lib().zc_attend_workspace_bytes(C.byref(a), None, cache.paged.ref)
+    room = torch.full((size + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+    out, lse = zc.attend(q, cache.paged, weights_out=w[1] if weights else None, ws=room[:size], **more)
+    assert size and torch.equal(out, want) and torch.equal(lse, want_lse) and torch.equal(w[0], w[1])
+    assert bool((room[size:] == 0xFF).all())
+    if size > 16:
+        with pytest.raises(zc.ZcError):
+            zc.attend(q, cache.paged, weights_out=w[1] if weights else None, ws=room[:size - 1], **more)
+
+
+@pytest.mark.parametrize("fmt", [BF16, E4M3])
+def test_a_prompt_beside_long_decodes(fmt):
+    check(Cache([300, 20011, 0, 5000, 1], 2, 64, fmt), [200, 1, 1, 3, 1], 4, weights=True)
+    check(Cache([300, 20011, 0, 5000, 1], 2, 64, fmt), [200, 1, 1, 3, 1], 4, 9000, 20)
