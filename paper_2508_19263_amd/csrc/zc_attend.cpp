@@ -61,7 +61,12 @@ struct Pass {
 Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_splits, bool only)
 {
     Pass p;
-    // up to 64 rows k_attend_few reads a cache twice: 35 rows of six caches with a window of 2,048, 17.0 against 18.6 us in k_attend_many
+    // k_attend_few goes over a cache once for every 32 rows, k_attend_many once for 128.  Microseconds of the former against the latter, rows to a
+    // K/V head in front, one query head each, 8 K/V heads: 64: 4 FP8 caches of 8,192 tokens 25.7 against 30.4, one 15.7 against 19.6, 4 BF16 ones
+    // of 4,000 21.3 against 27.0, six E5M2 ones with heads of 64 and a window of 2,048 15.8 against 19.8, 16 BF16 ones of 1,000 with heads of 64
+    // 13.6 against 18.2; 65 (a third row block): 39.1 against 31.7, 18.3 against 19.8, 34.6 against 28.0, 17.6 against 20.3, 18.2 against 18.6.
+    // Where caches alone fill the GPU the boundary lies lower, for BF16 below 33: 32 BF16 ones of 4,000 147 against 106 (33 rows) and 151 against 111
+    // (64), 32 FP8 ones of 8,192 141 against 136 (35) and 145 against 140 (64).
     p.many = rows > 64;
     p.tiles = p.many || rows <= 16 ? 1 : 2;
     const uint64_t per_block = p.tiles * (p.many ? 128 : 16);

@@ -100,7 +100,9 @@ template <int FMT> __device__ __forceinline__ u32x4_t eight_to_bf16(uint32_t lo,
 {
     return u32x4_t{two_to_bf16<FMT, false>(lo), two_to_bf16<FMT, true>(lo), two_to_bf16<FMT, false>(hi), two_to_bf16<FMT, true>(hi)};
 }
-// two weights to the type the values of the format are multiplied in
+// Two weights to the type the values of the format are multiplied in.  BF16 has 8 bits, and values of its range go to no other two-byte
+// type: results are off by 0.0019 - 0.0022 of their norm where 32-bit weights leave the 0.0016 - 0.0017 of rounding the result (FP8 values,
+// with half precision: the same 0.0017).  What is left of the weights could be multiplied too, for as many matrix instructions again.
 template <int FMT> __device__ __forceinline__ uint32_t pack_weights(float a, float b)
 {
     if constexpr (FMT == ZC_FMT_BF16) return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});

@@ -1,9 +1,9 @@
 // k_attend_shared: both passes of a batch under one prefix in one launch.  The first workgroups take parts of the prefix for rows of
-// all sequences (as k_attend_many, or k_attend_few where these are at most 32), those behind them the sequences' own caches (as
-// k_attend_few), which fill the places that the former leave: 64 answers (8 K/V heads of 128, 4 query heads to each, FP8) of 16 to 777
-// tokens under 32,768 took 77 us with one pass after the other and take 75 in one launch, five answers (BF16) under 1,531 19.1 and
-// 12.9.  Of the former 63 us are this kernel's, 550 TFLOP/s, bound like k_attend_many but with tiles converted for only two row blocks,
-// and 9 the join of 33 slots; of the latter, 10 and 3, bound by latency.
+// all sequences (as k_attend_many, or k_attend_few where these are at most 64), those behind them the sequences' own caches (as
+// k_attend_few), which fill the places that the former leave.  Replayed from a graph, one pass after the other against one launch: 64 answers
+// (8 K/V heads of 128, 4 query heads to each, FP8) of 16 to 777 tokens under 32,768, 76 against 72 - 75 us; five answers (BF16) under 1,531,
+// 19.2 against 12.9.  Under a kernel trace 59 us of the former are this kernel's, 590 TFLOP/s, bound like k_attend_many but with tiles
+// converted for only two row blocks, and 9 the join of 33 slots; of the latter, 11 and 4, bound by latency.
 #include "zc_attend_few.h"
 #include "zc_attend_many.h"
 
