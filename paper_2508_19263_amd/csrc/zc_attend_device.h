@@ -22,8 +22,8 @@ constexpr float kNegInf = -__builtin_inff();
 // A factor of the logits of 0 would take minus infinity, which stands for what is hidden, to NaN: the smallest normal number in its place
 // takes any product to less than 4, and those below 2^100 to nothing.
 constexpr float kLeastFactor = 0x1p-126f;
-// A row's running maximum is replaced, and what has been added up scaled, only where a logit is more than 2^kSlack above it: weights
-// then reach 2^kSlack, which the 32-bit sums and the operands' types (half precision to 2^16) hold with the same relative error.
+// A row's running maximum is replaced, and what has been added up scaled, only where a weight would be more than 2^kSlack times its: the
+// 32-bit sums and the operands' types (half precision to 2^16) hold what is below that with the same relative error.
 constexpr float kSlack = 8.0f;
 // Weights in half precision (FP8 values) are all 2^kLift of what they are, and the sum that they are divided by is too.  Half
 // precision ends at 2^-24, but the sum counts what is below: many light tokens beside a heavy one would lose their share.  With both
@@ -155,11 +155,17 @@ template <int D> __device__ __forceinline__ uint32_t key_place(uint32_t n, uint3
     return D == 128 ? n * 256 + ((c ^ (n & 15)) << 4) : n * 128 + ((c ^ ((n >> 1) & 7)) << 4);
 }
 
-// What a row's logits in base 2 are taken relative to: its weights are 2 to the power of the difference.
-template <int FMT> __device__ __forceinline__ float log2_base(float m, float c) { return m == kNegInf ? 0.0f : m * c - kLift<FMT>; }
+// What a row's logits in base 2 are taken relative to, its base, is kLift below its running maximum: its weights are 2 to the power of the
+// difference.  That is always taken of the base as it has been rounded, and a weight's exponent judged as it will be: of logits beyond 2^24,
+// where numbers lie 2 and more apart, weights are off by powers of 2, but none leaves its type's range for that.
+constexpr float kNoBase = -3e38f;              // nothing seen yet; minus infinity less it is minus infinity
+template <int FMT> __device__ __forceinline__ bool out_of_reach(float base, float top, float c) { return __builtin_fmaf(top, c, -base) > kSlack + kLift<FMT>; }
+// the base after a product `top`
+template <int FMT> __device__ __forceinline__ float raised(float base, float top, float c) { return fmaxf(base, __builtin_fmaf(top, c, -kLift<FMT>)); }
+__device__ __forceinline__ float weight_of(float product, float c, float base) { return __builtin_amdgcn_exp2f(__builtin_fmaf(product, c, -base)); }
 // A part's base: minus infinity where it has seen nothing (its sum is 0), not a number where its sum is not one, though all
-// its products were not numbers either and have left the maximum where it was.
-template <int FMT> __device__ __forceinline__ float log2_top(float m, float c, float sum) { return sum != sum ? sum : m == kNegInf ? kNegInf : log2_base<FMT>(m, c); }
+// its products were not numbers either and have left the base where it was.
+__device__ __forceinline__ float part_base(float base, float sum) { return sum != sum ? sum : base == kNoBase ? kNegInf : base; }
 
 // Eight elements of a query as they are multiplied: a negative factor of the logits goes to their signs, and one that is not a number takes
 // their place, so that what a row sees is not a number and what is hidden from it (minus infinity, put there after the product) stays that.

@@ -3,7 +3,7 @@
 // The rows of one (sequence, K/V head), its query tokens times the query heads that share the K/V head, are few, and the
 // cache is long: the kernel is bound by the read of the pages.  Each wavefront takes every fourth block of 32 tokens of its
 // workgroup's part of the cache and multiplies it with all rows, 16 at a time, straight from registers:
-//   S^T = K Q^T      a lane holds one query row's products with 2 x 4 tokens; their running maximum m and sum l go with it
+//   S^T = K Q^T      a lane holds one query row's products with 2 x 4 tokens; the base they are taken relative to and their sum l go with it
 //   O^T += V^T P^T   those 8 weights are the lane's operand as they stand: the order of the tokens in the sum is free, so the
 //                    lane that holds rows of V for the product takes those of the same 8 tokens
 // Neither K, V nor the weights pass through LDS; V is transposed by byte permutes inside a lane, which holds 8 tokens x
@@ -148,11 +148,11 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
         }
     }
 
-    float m[QT], l[QT];                                  // maximum of the bare products; sum over this lane's tokens
+    float base[QT], l[QT];                               // what the rows' logits are taken relative to; sum over this lane's tokens
     f32x4 o[QT][DL];
 #pragma unroll
     for (int t = 0; t < QT; t++) {
-        m[t] = kNegInf;
+        base[t] = kNoBase;
         l[t] = 0.0f;
 #pragma unroll
         for (int i = 0; i < DL; i++) o[t][i] = f32x4{0, 0, 0, 0};
@@ -254,20 +254,17 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
             }
             float top = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])), fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
             top = max_over_16(max_over_32(top));
-            if (__any((top - m[t]) * c > kSlack)) {
-                const float now = fmaxf(m[t], top);
-                const float f = m[t] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f((m[t] - now) * c);   // (nothing to scale yet)
-                m[t] = now;
+            if (__any(out_of_reach<FMT>(base[t], top, c))) {
+                const float now = raised<FMT>(base[t], top, c);
+                const float f = __builtin_amdgcn_exp2f(base[t] - now);
+                base[t] = now;
                 l[t] *= f;
 #pragma unroll
                 for (int i = 0; i < DL; i++) o[t][i] *= f;
             }
-            const float base = log2_base<FMT>(m[t], c);
             float e[8];
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][j / 4][j & 3], c, -base));
-            }
+            for (int j = 0; j < 8; j++) e[j] = weight_of(s[t][j / 4][j & 3], c, base[t]);
             l[t] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
 #pragma unroll
             for (int j = 0; j < 4; j++) p[t][j] = pack_weights<FMT>(e[2 * j], e[2 * j + 1]);
@@ -310,7 +307,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
 #pragma unroll
     for (int t = 0; t < QT; t++) {
         l[t] = sum_over_16(sum_over_32(l[t]));
-        if (g == 0) { ml[wave][t * 16 + n16][0] = log2_top<FMT>(m[t], c, l[t]); ml[wave][t * 16 + n16][1] = l[t]; }
+        if (g == 0) { ml[wave][t * 16 + n16][0] = part_base(base[t], l[t]); ml[wave][t * 16 + n16][1] = l[t]; }
     }
     __syncthreads();
     constexpr uint32_t kPerRow = kWaves * 4, DP = D / kPerRow;     // threads per row, dimensions per thread

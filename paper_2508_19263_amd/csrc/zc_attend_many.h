@@ -124,7 +124,7 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
             q[u] = query_operand(x, signed_c);
         }
     }
-    float m = kNegInf, l = 0.0f;                               // maximum of the bare products; sum over this lane's tokens
+    float base = kNoBase, l = 0.0f;                            // what the row's logits are taken relative to; sum over this lane's tokens
     f32x16 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; d++)
@@ -260,11 +260,11 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
         for (int i = 1; i < kTile / 2; i++) top = fmaxf(top, s.half[i / 16][i & 15]);
         return max_over_32(top);
     };
-    auto raise = [&](float top) {                              // the maximum, where a product has left it far behind
-        if (__builtin_expect(__any((top - m) * c > kSlack), 0)) {
-            const float now = fmaxf(m, top);
-            const float f = m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f((m - now) * c);
-            m = now;
+    auto raise = [&](float top) {                              // the base, where a product has left it far behind
+        if (__builtin_expect(__any(out_of_reach<FMT>(base, top, c)), 0)) {
+            const float now = raised<FMT>(base, top, c);
+            const float f = __builtin_amdgcn_exp2f(base - now);
+            base = now;
             l *= f;
 #pragma unroll
             for (int d = 0; d < DT; d++) o[d] *= f;
@@ -290,12 +290,11 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
         const uint8_t *vt = tile.values;
         if (__builtin_expect(edge, 0)) hide(t0, there, s);
         raise(top_of(s));
-        const float base = log2_base<FMT>(m, c);
         float sum[4] = {0, 0, 0, 0};
         u32x4_t p[kStretches];
 #pragma unroll
         for (int i = 0; i < kTile / 2; i++) {
-            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s.half[i / 16][i & 15], c, -base));        // (0 for the products hidden above)
+            const float e = weight_of(s.half[i / 16][i & 15], c, base);                       // (0 for the products hidden above)
             s.half[i / 16][i & 15] = e;
             sum[i & 3] += e;
             if (i & 1) p[i / 8][i / 2 & 3] = pack_weights<FMT>(s.half[i / 16][(i & 15) - 1], e);
@@ -389,7 +388,7 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
     // ---- results: a lane has 4 consecutive dimensions at a time
     if (row.token < 0) return;
     const float sum = sum_over_32(l);
-    const float top = log2_top<FMT>(m, c, sum);
+    const float top = part_base(base, sum);
     const uint64_t at = (uint64_t)row.token * a.q_heads + row.q_head;
     if (a.direct) {
         const float inv = sum == 0.0f ? 0.0f : v_scale / sum;

@@ -81,3 +81,23 @@ def test_a_scale_of_zero_with_large_keys(q_lens):
     def edit(c):
         c.k[:] = stored(c.k.view(torch.bfloat16).float() * 1e30, BF16)
     check(Cache([300, 41], 2, 128, BF16, edit=edit), q_lens, 4, scale=0.0, weights=True)
+
+
+@pytest.mark.parametrize("fmt", [BF16, E4M3, E5M2])
+@pytest.mark.parametrize("q_len,length", [(1, 600), (1, 9000), (150, 600)])
+def test_logits_whose_rounding_is_as_large_as_they_lie_apart(fmt, q_len, length):
+    """All logits lie around 2^25 in base 2, where numbers in 32 bits are 4 apart, and the later tokens' 8 above the first ones': the weights'
+    exponents are off by up to 2, and no weight may leave its type's range for it."""
+    def edit(c):
+        c.k[:] = 0
+        c.k[..., 0] = stored(torch.full(c.k.shape[:3], 16.0, device="cuda"), fmt)
+        c.k[:, :, 256:, 1] = stored(torch.ones(c.k.shape[:2] + (c.k.shape[2] - 256,), device="cuda"), fmt)
+    cache = Cache([length], 1, 128, fmt, edit=edit, scales=False)
+    q = torch.zeros((q_len, 2, 128), dtype=torch.bfloat16, device="cuda")
+    q[..., 0], q[..., 1] = 1.0, 2.0 ** -18
+    for scale in (1453600.0, 1453500.0, 1400000.0, 2907000.0):
+        out, lse = zc.attend(q, cache.paged, q_start=starts([q_len]), max_q_len=q_len, scale=scale)
+        want, want_lse, _, tol, tol_lse, _ = attention(q, [q_len], cache, scale=scale)
+        agree(out, want, tol, "out")
+        agree(lse, want_lse, tol_lse, "lse")
+        assert float(out.abs().max()) <= 1.01 * float(cache.rows("v", 0, 0).abs().max())
