@@ -11,7 +11,7 @@
 // to different workgroups are joined by k_attend_join.
 //
 // Measured with 8 K/V heads of 128 in random pages of 16 tokens, one query token, joins included (a kernel that only reads reaches
-// 6.1 TB/s): 64 FP8 caches of 8,192 tokens 189 us, 5.7 TB/s; 48 BF16 ones of 12,000 418 us, 5.6 TB/s; 4 FP8 ones of 8,192 16.8 us,
+// 6.1 TB/s): 64 FP8 caches of 8,192 tokens 189 us, 5.7 TB/s; 48 BF16 ones of 12,000 418 us, 5.6 TB/s; 4 FP8 ones of 8,192 16.7 us,
 // 4.0 TB/s, and 17.5 replayed from a graph; one with 512 tokens in sight 8.5 us, all latency.
 #pragma once
 #include "zc_attend_device.h"

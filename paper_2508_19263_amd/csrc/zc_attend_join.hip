@@ -17,8 +17,8 @@ constexpr uint32_t kFewSlots = 8;
 //
 // Workgroups behind those take 1,024 tokens of a (sequence, K/V head) each and add up their weights from the logits that
 // k_attend_few has left (`logits`, where rereading these costs less than rereading the keys): four tokens to a thread, eight
-// rows on their way at a time.  (4 FP8 caches of 8,192 tokens, 8 K/V heads, 4 rows each: 4.6 us with the join under a kernel trace, where the
-// join alone takes 4.0; the whole call 19.0 us against 16.8 without weights.)
+// rows on their way at a time.  (4 FP8 caches of 8,192 tokens, 8 K/V heads, 4 rows each: 4.5 us with the join under a kernel trace, where the
+// join alone takes 4.0; the whole call 19.0 us against 16.7 without weights.)
 //
 // FEW: at most kFewSlots of them.  A row is D / 4 threads then, each with four dimensions of every slot, 8 or 16 rows to a workgroup, and
 // nothing is exchanged: a call with 1,680 rows of 64 and three slots took 16.9 us without it and takes 15.2, one with 43,000 and two 81

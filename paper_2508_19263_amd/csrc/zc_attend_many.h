@@ -14,7 +14,7 @@
 // Measured with 8 K/V heads of 128 and 4 query heads to each: two BF16 prompts of 8,192 and 7,001 tokens with a window of 4,096 and 16
 // sinks 790 - 850 us, 880 - 945 TFLOP/s (counted are the products of tokens that are seen); pieces of 1,024 and 511 tokens behind 7,977
 // and 7,680 FP8 ones 137 - 147 us, 700 - 750 TFLOP/s.  A library product of 8,192^3 reaches 1,136 on this card, and its clock goes down to 1.5 GHz
-// under it; here it goes from 2.2 to 1.9.  The matrix unit is busy 50 % of the cycles (FP8: 37 %), the exponentials and what belongs to
+// under it; here it goes from 2.2 to 1.9.  The matrix unit is busy 51 % of the cycles (FP8: 38 %), the exponentials and what belongs to
 // them take about as many (two wavefronts to a SIMD; registers and LDS have room for no more); other orders of the same instructions
 // give the same time.
 #pragma once
