@@ -388,19 +388,21 @@ zc_status zc_build_code(const uint64_t *hist, uint32_t alphabet, uint32_t limit,
                         uint8_t *len_out, uint16_t *code_out);
 
 /* ---- Operators over K/V pages (Sec. 3.3, 5.2: a cache is kept, compressed and decoded in pages) -------------------------
- * What runs on the pages that the decode calls above leave in memory: attention, and the choice of the tokens that stay.
+ * What runs on the pages that the decode calls above leave in memory: new tokens are quantised into them and read back, attention, and
+ * the choice of the tokens that stay.
  * They are serving operators over a stored cache (there is no gradient).  All of them only launch kernels on `stream`:
  * they never copy, wait or allocate, and may be recorded by stream capture.  They read no host array but their arguments.
  *
  * A page holds page_tokens consecutive tokens of one K/V head of one sequence: [page_tokens][head_dim] elements, which is what
- * a chunk of chunk_bytes = page_tokens * head_dim * element size decodes to.  K and V have a pool of pages each, with the same
+ * a chunk of chunk_bytes = page_tokens * head_dim * element size decodes to.  The block scales of an FP4 page are [page_tokens][head_dim / 32]
+ * (MX) or [page_tokens][head_dim / 16] (NV) bytes of a pool of their own, as the chunk's d_scales.  K and V have a pool of pages each, with the same
  * page numbers.  Entry [s][h][i] of the table is the page of tokens i * page_tokens .. of sequence s and head h; a number that
  * is not below n_pages (a negative one, for instance) says that the page is absent: its tokens are not seen.  Pages that a
  * window has left behind can be given back that way.  What lies in a page behind a sequence's length has no influence,
  * whatever its bits. */
 typedef struct {
-    uint32_t struct_size;       /* = sizeof(zc_kv_cache) */
-    uint32_t format;            /* ZC_FMT_BF16, ZC_FMT_FP8_E4M3 or ZC_FMT_FP8_E5M2 */
+    uint32_t struct_size;       /* = sizeof(zc_kv_cache); without the last two members (formats that have no block scales) it is taken too */
+    uint32_t format;            /* ZC_FMT_BF16, ZC_FMT_FP8_E4M3, ZC_FMT_FP8_E5M2, ZC_FMT_FP4_E2M1_MX or ZC_FMT_FP4_E2M1_NV */
     uint32_t n_seqs, n_heads;   /* sequences, K/V heads */
     uint32_t head_dim;          /* 64 or 128 */
     uint32_t page_tokens;       /* a power of two, 16 to 65,536 */
@@ -410,7 +412,32 @@ typedef struct {
     const int32_t *d_table;     /* [n_seqs][n_heads][table_pages] */
     int32_t *d_lengths;         /* [n_seqs]: tokens in the cache (negative: 0; more than there is room for: that) */
     const float *d_k_scales, *d_v_scales;   /* [n_seqs][n_heads], what the stored elements are multiplied with, or NULL: 1 */
+    void *d_k_block_scales, *d_v_block_scales;  /* FP4: [n_pages][page_tokens][head_dim / 32 or 16], 16-byte aligned; else NULL */
 } zc_kv_cache;
+
+/* Rows of the last tokens of every sequence.  Sequence s has the tokens d_q_start[s] .. d_q_start[s + 1] (non-decreasing; NULL:
+ * n_tokens == n_seqs, token s is sequence s's); as in attention the i-th of n is at position length - n + i of the cache, so a length counts the
+ * tokens that are written already when they are. */
+typedef struct {
+    uint32_t struct_size;       /* = sizeof(zc_kv_rows) */
+    uint32_t n_tokens;
+    void *d_k, *d_v;            /* BF16, 16-byte aligned; token t, head h at element t * k_token_stride + h * k_head_stride */
+    uint64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;  /* multiples of 8 */
+    const int32_t *d_q_start;
+} zc_kv_rows;
+
+/* Quantises rows into the cache's pages.  With S the scale of the sequence and head (NULL: 1), y = x / S in 32 bits (0 where S is 0) is stored
+ *   BF16, FP8   rounded to the nearest number, ties to even;
+ *   FP4, MX     with e = floor(log2 m) - 2 (at least -127) of the block's largest magnitude m, E8M0 scale 2^e (m = 0: 2^-127), elements y / 2^e rounded likewise;
+ *   FP4, NV     with the block's E4M3 scale s = m / 6 in 32 bits, rounded likewise (at most 448), elements y / s (0 where s is 0).
+ * FP8 and FP4: what is beyond the largest number becomes that, infinities included.  NaN stays NaN; FP4: the block's scale is NaN and its
+ * elements 0.  Tokens of no sequence are skipped, and so is a row whose page is absent or whose position is negative or past the table's room.
+ * Nothing but the rows (and FP4 block scales) of these tokens is written; a page that tokens are written to is named once in the table. */
+zc_status zc_kv_write(const zc_kv_rows *rows, const zc_kv_cache *cache, void *stream);
+
+/* Reads rows back: element * block scale * S in 32 bits, rounded to BF16.  A row whose page is absent or whose position is negative or past the
+ * table's room is 0; rows of tokens of no sequence are left untouched. */
+zc_status zc_kv_read(const zc_kv_rows *rows, const zc_kv_cache *cache, void *stream);
 
 /* Attention of n_tokens query tokens.  Sequence s has the query tokens d_q_start[s] .. d_q_start[s + 1] (at most max_q_len of
  * them; d_q_start non-decreasing, or NULL: n_tokens == n_seqs, token s is sequence s's), whose keys and values are in the cache
@@ -420,7 +447,7 @@ typedef struct {
  *   out = v_scale * sum exp(s_t) v_t / sum exp(s_t),   lse = ln sum exp(s_t);
  * a query that sees nothing (or nothing with a logit above minus infinity) has out = 0 and lse = -infinity.  Products are
  * accumulated, and the softmax is held, in 32 bits; its weights are rounded to the type the values are multiplied in (BF16 for
- * BF16 pages; half precision for FP8 pages, to within 2^-32 of a row's largest weight where they are below 2^-21 of it), the result
+ * BF16 and MXFP4 pages; half precision for FP8 and NVFP4 pages, to within 2^-32 of a row's largest weight where they are below 2^-21 of it), the result
  * once to BF16.  Query tokens of no sequence are left untouched. */
 typedef struct {
     uint32_t struct_size;       /* = sizeof(zc_attend_args) */

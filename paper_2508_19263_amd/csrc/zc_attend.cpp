@@ -1,8 +1,9 @@
 // Host side of the operators over K/V pages: argument checks, the choice of kernels and splits, and the C entry points
-// zc_attend, zc_attend_shared, zc_attend_workspace_bytes and zc_evict.
+// zc_attend, zc_attend_shared, zc_attend_workspace_bytes, zc_kv_write, zc_kv_read and zc_evict.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <cstddef>
 
 #include "zc_attend.h"
 #include "zc_host.h"
@@ -18,22 +19,31 @@ constexpr uint64_t kMostLogits = 1u << 30;     // bytes of scratch
 
 bool aligned4(const void *p) { return ((uintptr_t)p & 3) == 0; }
 
+bool fp4(uint32_t format) { return format == ZC_FMT_FP4_E2M1_MX || format == ZC_FMT_FP4_E2M1_NV; }
+uint32_t row_bytes(const zc_kv_cache &c) { return c.format == ZC_FMT_BF16 ? c.head_dim * 2 : fp4(c.format) ? c.head_dim / 2 : c.head_dim; }
+uint32_t row_scales(const zc_kv_cache &c) { return !fp4(c.format) ? 0 : c.head_dim / (c.format == ZC_FMT_FP4_E2M1_MX ? 32 : 16); }
+
 zc_status check_cache(const zc_kv_cache *c, PagesDev *out)
 {
     if (!c) return ZC_ERR_INVALID_ARG;
-    if (c->struct_size != sizeof(zc_kv_cache)) return ZC_ERR_UNSUPPORTED;
-    if (c->format != ZC_FMT_BF16 && c->format != ZC_FMT_FP8_E4M3 && c->format != ZC_FMT_FP8_E5M2) return ZC_ERR_UNSUPPORTED;
+    constexpr uint32_t kFirstLayout = offsetof(zc_kv_cache, d_k_block_scales);
+    if (c->struct_size != sizeof(zc_kv_cache) && c->struct_size != kFirstLayout) return ZC_ERR_UNSUPPORTED;
+    if (c->format != ZC_FMT_BF16 && c->format != ZC_FMT_FP8_E4M3 && c->format != ZC_FMT_FP8_E5M2 && !fp4(c->format)) return ZC_ERR_UNSUPPORTED;
+    void *const k_blocks = c->struct_size == kFirstLayout ? nullptr : c->d_k_block_scales, *const v_blocks = c->struct_size == kFirstLayout ? nullptr : c->d_v_block_scales;
+    if (fp4(c->format) ? !k_blocks || !v_blocks : k_blocks || v_blocks) return ZC_ERR_UNSUPPORTED;
     if (c->head_dim != 64 && c->head_dim != 128) return ZC_ERR_UNSUPPORTED;
     if (c->page_tokens < 16 || c->page_tokens > 65536 || (c->page_tokens & (c->page_tokens - 1))) return ZC_ERR_INVALID_ARG;
     if (!c->n_seqs || !c->n_heads || !c->table_pages || !c->n_pages || c->n_pages > 0x7FFFFFFFu) return ZC_ERR_INVALID_ARG;
     const uint64_t capacity = (uint64_t)c->table_pages * c->page_tokens;
     if (capacity >= kMaxTokens || (uint64_t)c->n_seqs * c->n_heads > (kMaxBlocks >> 2)) return ZC_ERR_INVALID_ARG;     // (k_evict_select has 1,024 threads for each)
     if (!c->d_k_pages || !c->d_v_pages || !c->d_table || !c->d_lengths) return ZC_ERR_INVALID_ARG;
-    if (!aligned16(c->d_k_pages) || !aligned16(c->d_v_pages) || !aligned4(c->d_table) || !aligned4(c->d_lengths) ||
+    if (!aligned16(c->d_k_pages) || !aligned16(c->d_v_pages) || !aligned16(k_blocks) || !aligned16(v_blocks) || !aligned4(c->d_table) || !aligned4(c->d_lengths) ||
         !aligned4(c->d_k_scales) || !aligned4(c->d_v_scales)) return ZC_ERR_INVALID_ARG;
     PagesDev d = {};
     d.k = (const uint8_t *)c->d_k_pages;
     d.v = (const uint8_t *)c->d_v_pages;
+    d.k_blocks = (const uint8_t *)k_blocks;
+    d.v_blocks = (const uint8_t *)v_blocks;
     d.table = c->d_table;
     d.lengths = c->d_lengths;
     d.k_scales = c->d_k_scales;
@@ -222,6 +232,35 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
     return ZC_OK;
 }
 
+zc_status plan_rows(const zc_kv_rows *x, const zc_kv_cache *cache, RowsDev *out)
+{
+    if (!x || !cache) return ZC_ERR_INVALID_ARG;
+    if (x->struct_size != sizeof(zc_kv_rows)) return ZC_ERR_UNSUPPORTED;
+    RowsDev r = {};
+    const zc_status st = check_cache(cache, &r.c);
+    if (st) return st;
+    if (!x->d_q_start && x->n_tokens != cache->n_seqs) return ZC_ERR_INVALID_ARG;
+    if ((uint64_t)x->n_tokens * cache->n_heads > 0x3FFFFFFFu) return ZC_ERR_INVALID_ARG;
+    if (x->n_tokens && (!x->d_k || !x->d_v)) return ZC_ERR_INVALID_ARG;
+    if (!aligned16(x->d_k) || !aligned16(x->d_v) || !aligned4(x->d_q_start)) return ZC_ERR_INVALID_ARG;
+    if ((x->k_token_stride | x->k_head_stride | x->v_token_stride | x->v_head_stride) & 7) return ZC_ERR_INVALID_ARG;
+    r.k_pages = (uint8_t *)cache->d_k_pages;
+    r.v_pages = (uint8_t *)cache->d_v_pages;
+    r.k_scale_pages = const_cast<uint8_t *>(r.c.k_blocks);
+    r.v_scale_pages = const_cast<uint8_t *>(r.c.v_blocks);
+    r.k = (uint16_t *)x->d_k;
+    r.v = (uint16_t *)x->d_v;
+    r.k_token_stride = x->k_token_stride;
+    r.k_head_stride = x->k_head_stride;
+    r.v_token_stride = x->v_token_stride;
+    r.v_head_stride = x->v_head_stride;
+    r.q_start = x->d_q_start;
+    r.n_seqs = cache->n_seqs;
+    r.n_tokens = x->n_tokens;
+    *out = r;
+    return ZC_OK;
+}
+
 zc_status attend(const zc_attend_args *x, const zc_kv_cache *prefix, const zc_kv_cache *cache, bool shared, void *d_ws, uint64_t ws_bytes, void *stream)
 {
     AttendPlan p;
@@ -269,6 +308,25 @@ extern "C" zc_status zc_attend_shared(const zc_attend_args *args, const zc_kv_ca
     return zc::attend(args, prefix, cache, true, d_ws, ws_bytes, stream);
 }
 
+extern "C" zc_status zc_kv_write(const zc_kv_rows *rows, const zc_kv_cache *cache, void *stream)
+{
+    zc::RowsDev r;
+    const zc_status st = zc::plan_rows(rows, cache, &r);
+    if (st) return st;
+    if (r.n_tokens) LAUNCH_TRY(zc::launch_kv_write(r, cache->format, cache->head_dim, stream));
+    return ZC_OK;
+}
+
+extern "C" zc_status zc_kv_read(const zc_kv_rows *rows, const zc_kv_cache *cache, void *stream)
+{
+    zc::RowsDev r;
+    const zc_status st = zc::plan_rows(rows, cache, &r);
+    if (st) return st;
+    if (r.n_tokens && r.k == r.v) return ZC_ERR_INVALID_ARG;
+    if (r.n_tokens) LAUNCH_TRY(zc::launch_kv_read(r, cache->format, cache->head_dim, stream));
+    return ZC_OK;
+}
+
 extern "C" zc_status zc_evict(const zc_kv_cache *from, const float *d_weights, uint32_t keep, uint32_t sinks, uint32_t recent,
                               const zc_kv_cache *to, float *d_weights_to, int32_t *d_kept, void *stream)
 {
@@ -292,7 +350,12 @@ extern "C" zc_status zc_evict(const zc_kv_cache *from, const float *d_weights, u
     e.keep = keep;
     e.sinks = sinks;
     e.recent = recent;
-    e.row_bytes = from->head_dim * (from->format == ZC_FMT_BF16 ? 2 : 1);
+    e.row_bytes = zc::row_bytes(*from);
+    e.row_scales = zc::row_scales(*from);
+    if (e.row_scales) {
+        e.k_blocks_to = (uint8_t *)to->d_k_block_scales;
+        e.v_blocks_to = (uint8_t *)to->d_v_block_scales;
+    }
     LAUNCH_TRY(zc::launch_evict(e, stream));
     return ZC_OK;
 }

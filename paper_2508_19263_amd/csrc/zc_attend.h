@@ -13,6 +13,7 @@ struct PagesDev {
     const int32_t *table;              // [seqs][heads][table_pages]
     const int32_t *lengths;            // [seqs]
     const float *k_scales, *v_scales;  // [seqs][heads] or null
+    const uint8_t *k_blocks, *v_blocks;        // FP4: block scales of the pages' rows
     uint32_t heads, table_pages, n_pages, page_shift;
     int32_t capacity, limit;           // longer lengths are taken as `limit`
 };
@@ -58,7 +59,19 @@ struct EvictDev {
     float *weights_to;                 // [seqs][heads][to.capacity] or null
     int32_t *kept;                     // [seqs][heads][keep]
     int32_t *lengths_to;
+    uint8_t *k_blocks_to, *v_blocks_to;
     uint32_t n_seqs, keep, sinks, recent, row_bytes;
+    uint32_t row_scales;               // FP4: bytes of a row's block scales; else 0
+};
+
+// Rows of the last tokens of sequences, to be written to a cache or read back from it.
+struct RowsDev {
+    PagesDev c;
+    uint8_t *k_pages, *v_pages, *k_scale_pages, *v_scale_pages;       // what is written to
+    uint16_t *k, *v;                   // BF16 [tokens][heads][dim]
+    uint64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;       // elements
+    const int32_t *q_start;            // [seqs + 1] or null: one token per sequence
+    uint32_t n_seqs, n_tokens;
 };
 
 // tiles: of 16 rows in k_attend_few, of 128 in k_attend_many
@@ -70,5 +83,7 @@ int launch_attend_shared(const AttendDev &pre, const AttendDev &own, uint32_t fo
 int launch_attend_join(const AttendDev &a, const WeightsDev &w, uint32_t head_dim, uint32_t slots, void *stream);
 int launch_attend_weights(const AttendDev &a, const WeightsDev &w, uint32_t format, uint32_t head_dim, void *stream);
 int launch_evict(const EvictDev &e, void *stream);
+int launch_kv_write(const RowsDev &r, uint32_t format, uint32_t head_dim, void *stream);
+int launch_kv_read(const RowsDev &r, uint32_t format, uint32_t head_dim, void *stream);
 
 }  // namespace zc

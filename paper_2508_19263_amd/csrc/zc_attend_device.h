@@ -11,6 +11,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef f32x4 f32x4u __attribute__((aligned(4)));      // where only the elements are aligned
@@ -28,12 +29,15 @@ constexpr float kSlack = 8.0f;
 // Weights in half precision (FP8 values) are all 2^kLift of what they are, and the sum that they are divided by is too.  Half
 // precision ends at 2^-24, but the sum counts what is below: many light tokens beside a heavy one would lose their share.  With both
 // powers weights reach 2^15 of half precision's 2^16, and end at 2^-31 of a row's heaviest.
-template <int FMT> constexpr float kLift = FMT == ZC_FMT_BF16 ? 0.0f : 7.0f;
+template <int FMT> constexpr bool kFp4 = FMT == ZC_FMT_FP4_E2M1_MX || FMT == ZC_FMT_FP4_E2M1_NV;
+// Values are multiplied in BF16 where their range goes to no other two-byte type (BF16; MXFP4, whose scales are any power of two).
+template <int FMT> constexpr bool kValuesBf16 = FMT == ZC_FMT_BF16 || FMT == ZC_FMT_FP4_E2M1_MX;
+template <int FMT> constexpr float kLift = kValuesBf16<FMT> ? 0.0f : 7.0f;
 
-template <int FMT> struct PageElem;
-template <> struct PageElem<ZC_FMT_BF16> { static constexpr int BYTES = 2; };
-template <> struct PageElem<ZC_FMT_FP8_E4M3> { static constexpr int BYTES = 1; };
-template <> struct PageElem<ZC_FMT_FP8_E5M2> { static constexpr int BYTES = 1; };
+template <int FMT> constexpr int kElemBits = FMT == ZC_FMT_BF16 ? 16 : kFp4<FMT> ? 4 : 8;
+template <int FMT> constexpr int kBlock = FMT == ZC_FMT_FP4_E2M1_MX ? 32 : 16;             // FP4 elements that share a scale
+template <int FMT, int D> constexpr uint32_t kRowBytes = D * kElemBits<FMT> / 8;           // of a token's keys or values
+template <int FMT, int D> constexpr uint32_t kRowScales = D / kBlock<FMT>;                 // FP4: bytes of a token's block scales
 
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -105,7 +109,7 @@ template <int FMT> __device__ __forceinline__ u32x4_t eight_to_bf16(uint32_t lo,
 // with half precision: the same 0.0017).  What is left of the weights could be multiplied too, for as many matrix instructions again.
 template <int FMT> __device__ __forceinline__ uint32_t pack_weights(float a, float b)
 {
-    if constexpr (FMT == ZC_FMT_BF16) return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+    if constexpr (kValuesBf16<FMT>) return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
     else return __builtin_bit_cast(uint32_t, halfx2{(_Float16)a, (_Float16)b});
 }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b}); }
@@ -120,13 +124,64 @@ __device__ __forceinline__ f32x16 mma32_keys(u32x4_t a, u32x4_t b, f32x16 c)
 }
 template <int FMT> __device__ __forceinline__ f32x4 mma16_values(u32x4_t a, u32x4_t b, f32x4 c)
 {
-    if constexpr (FMT == ZC_FMT_BF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    if constexpr (kValuesBf16<FMT>) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8, a), __builtin_bit_cast(halfx8, b), c, 0, 0, 0);
+}
+
+// FP4 elements, two to a byte, the first in the low bits: numbers of 2 bits, times their block's scale.  MX: 2^(byte - 127), 255: NaN; the
+// conversions take it as the exponent of a float (0 in its place is 2^-127, and sign and mantissa do not count).  NV: an E4M3 number.
+template <int FMT> __device__ __forceinline__ float block_scale(uint32_t byte)
+{
+    if constexpr (FMT == ZC_FMT_FP4_E2M1_MX) return __uint_as_float(byte << 23);
+    else return __builtin_amdgcn_cvt_f32_fp8((int)byte, 0);
+}
+// whether elements of the block may be other than finite (MX: 6 times 2^126 is not)
+template <int FMT> __device__ __forceinline__ bool wild_scale(uint32_t byte)
+{
+    if constexpr (FMT == ZC_FMT_FP4_E2M1_MX) return byte >= 253;
+    else return (byte & 0x7F) == 0x7F;
+}
+// Elements 2 SEL and 2 SEL + 1 of a word.  To BF16 (exact: NV elements times their scale have 6 bits) and to the type that values are
+// multiplied in (NV: half precision, which holds 2^-10 to 6 times 448 exactly).
+template <int FMT, int SEL> __device__ __forceinline__ uint32_t two_fp4_to_bf16(uint32_t w, float scale)
+{
+    if constexpr (FMT == ZC_FMT_FP4_E2M1_MX) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, SEL));
+    else {
+        const f32x2 x = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, SEL));
+        return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(x[0] * scale), (__bf16)(x[1] * scale)});
+    }
+}
+template <int FMT, int SEL> __device__ __forceinline__ uint32_t two_fp4_to_values(uint32_t w, float scale)
+{
+    if constexpr (FMT == ZC_FMT_FP4_E2M1_MX) return two_fp4_to_bf16<FMT, SEL>(w, scale);
+    else {
+        const halfx2 x = __builtin_bit_cast(halfx2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, SEL));
+        return __builtin_bit_cast(uint32_t, x * halfx2{(_Float16)scale, (_Float16)scale});
+    }
+}
+template <int FMT> __device__ __forceinline__ u32x4_t eight_fp4_to_bf16(uint32_t w, float scale)
+{
+    return u32x4_t{two_fp4_to_bf16<FMT, 0>(w, scale), two_fp4_to_bf16<FMT, 1>(w, scale), two_fp4_to_bf16<FMT, 2>(w, scale), two_fp4_to_bf16<FMT, 3>(w, scale)};
+}
+template <int FMT> __device__ __forceinline__ u32x4_t eight_fp4_to_values(uint32_t w, float scale)
+{
+    return u32x4_t{two_fp4_to_values<FMT, 0>(w, scale), two_fp4_to_values<FMT, 1>(w, scale), two_fp4_to_values<FMT, 2>(w, scale), two_fp4_to_values<FMT, 3>(w, scale)};
+}
+// one element as a float, without its block's scale
+__device__ __forceinline__ float e2m1_element(uint32_t code)
+{
+    return __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 0))[0];
+}
+template <int FMT> __device__ __forceinline__ float block_factor(uint32_t byte)      // what the elements are multiplied with, as a float
+{
+    if constexpr (FMT == ZC_FMT_FP4_E2M1_MX) return byte == 0 ? 0x1p-127f : byte == 255 ? __builtin_nanf("") : __uint_as_float(byte << 23);
+    else return block_scale<FMT>(byte);
 }
 
 // ones over those of a word's elements that are infinities or NaN
 template <int FMT> __device__ __forceinline__ uint32_t nonfinite_mask(uint32_t w)
 {
+    static_assert(!kFp4<FMT>, "FP4 has none: see wild_scale");
     if constexpr (FMT == ZC_FMT_BF16) {
         const uint32_t t = ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;      // exponent of ones: carries into the sign's place
         return (t >> 15) * 0xFFFFu;
@@ -136,11 +191,21 @@ template <int FMT> __device__ __forceinline__ uint32_t nonfinite_mask(uint32_t w
         return (t >> 7) * 0xFFu;
     }
 }
-// one element as a float
-template <int FMT> __device__ __forceinline__ float element(const uint8_t *p)
+// One element of a row of values as a float, 0 where it is finite: what those rows that see its token add by themselves.  FP4: 0 only
+// where the block's scale is not wild (its finite elements have been left out with the others).
+template <int FMT, int D> __device__ __forceinline__ float wild_value(const PagesDev &c, uint64_t row, uint32_t dim)
 {
-    if constexpr (FMT == ZC_FMT_BF16) return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(p) << 16);
-    else return __uint_as_float(two_to_bf16<FMT, false>(*p) << 16);
+    if constexpr (kFp4<FMT>) {
+        const uint32_t byte = c.v_blocks[row * kRowScales<FMT, D> + dim / kBlock<FMT>];
+        const uint32_t code = c.v[row * kRowBytes<FMT, D> + dim / 2] >> (dim & 1) * 4;
+        return wild_scale<FMT>(byte) ? e2m1_element(code) * block_factor<FMT>(byte) : 0.0f;
+    } else {
+        const uint8_t *p = c.v + row * kRowBytes<FMT, D> + dim * (kElemBits<FMT> / 8);
+        float x;
+        if constexpr (FMT == ZC_FMT_BF16) x = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(p) << 16);
+        else x = __uint_as_float(two_to_bf16<FMT, false>(*p) << 16);
+        return fabsf(x) < __builtin_inff() ? 0.0f : x;
+    }
 }
 
 // 16 tokens of a page (bytes 0: none, what is asked for is 0)

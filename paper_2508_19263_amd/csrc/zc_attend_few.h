@@ -21,12 +21,20 @@ namespace zc {
 constexpr uint32_t kWaves = 4;                 // wavefronts per workgroup (k_attend_few: with eight, batches were 1 us slower and single sequences 0.6 us faster)
 
 template <int FMT, int D> struct BlockRegs {
-    static constexpr int ES = PageElem<FMT>::BYTES;
-    static constexpr int NK = D * ES / 64;               // 16-byte pieces of a key per lane
-    static constexpr int DL = D / 16, VW = DL * ES / 4;  // dimensions and words of a value per lane
+    static constexpr int NK = D * kElemBits<FMT> / 512;              // 16-byte pieces of a key per lane
+    static constexpr int DL = D / 16, VW = DL * kElemBits<FMT> / 32; // dimensions and words of a value per lane
     u32x4_t k[2][NK];
     uint32_t v[8][VW];
 };
+// FP4: a quarter of a key, in words of eight elements, and its one or two block scales; D / 16 consecutive dimensions (a word or half of one) of
+// a value and their block's scale.
+template <int FMT, int D> struct BlockRegs4 {
+    static constexpr int DL = D / 16, KW = D / 32;
+    uint32_t k[2][KW], k_scale[2];
+    uint32_t v[8], v_scale[8];
+};
+template <int FMT, int D, bool FP4 = kFp4<FMT>> struct FewRegs { typedef BlockRegs<FMT, D> Type; };
+template <int FMT, int D> struct FewRegs<FMT, D, true> { typedef BlockRegs4<FMT, D> Type; };
 
 template <int N> __device__ __forceinline__ void load_words(uint32_t (&to)[N], __amdgpu_buffer_rsrc_t from, uint32_t at)
 {
@@ -51,6 +59,17 @@ template <int FMT, int VW> __device__ __forceinline__ u32x4_t value_operand(cons
     return r;
 }
 
+// The same for FP4, dimensions 2 SEL and 2 SEL + 1: the tokens' pairs of them, converted, with the tokens in pairs instead.
+template <int FMT, int SEL> __device__ __forceinline__ void value_operands4(const uint32_t (&v)[8], const uint32_t (&scale)[8], u32x4_t &even, u32x4_t &odd)
+{
+#pragma unroll
+    for (int p = 0; p < 4; p++) {
+        const uint32_t a = two_fp4_to_values<FMT, SEL>(v[2 * p], block_scale<FMT>(scale[2 * p])), b = two_fp4_to_values<FMT, SEL>(v[2 * p + 1], block_scale<FMT>(scale[2 * p + 1]));
+        even[p] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+        odd[p] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    }
+}
+
 template <int D, int QT> struct FewShared {
     float ml[kWaves][QT * 16][2];
     alignas(16) float ob[kWaves][16][D + 4];
@@ -59,8 +78,9 @@ template <int D, int QT> struct FewShared {
 template <int FMT, int D, int QT, bool LOGITS>
 __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, uint32_t split, uint32_t row_block, FewShared<D, QT> &shared)
 {
-    using Regs = BlockRegs<FMT, D>;
-    constexpr int ES = Regs::ES, NK = Regs::NK, DL = Regs::DL, KS = D / 32;
+    using Regs = typename FewRegs<FMT, D>::Type;
+    constexpr int DL = Regs::DL, KS = D / 32;
+    constexpr uint32_t kRow = kRowBytes<FMT, D>;
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
     const uint32_t head = unit % a.c.heads, seq = unit / a.c.heads;              // a shared prefix's one "sequence" is 0
 
@@ -111,9 +131,8 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
     }
 
     const int32_t *table = a.c.table + (uint64_t)(unit) * a.c.table_pages;
-    const uint32_t page_log = a.c.page_shift + (D == 128 ? 7 : 6) + (ES - 1);   // of a page's bytes
     const uint32_t page_mask = (1u << a.c.page_shift) - 1;
-    const uint32_t k_lane = n16 * (D * ES) + g * 16, v_lane = g * 4 * (D * ES) + n16 * (DL * ES);
+    const uint32_t k_lane = n16 * kRow + g * (kFp4<FMT> ? kRow / 4 : 16), v_lane = g * 4 * kRow + n16 * (kRow / 16);
 
     // page ids of the wavefront's next 32 steps: lane 2i + h has that of half h of step i (-1: absent)
     int32_t ids = -1, ids_from = begin + (int32_t)wave;
@@ -141,7 +160,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
 #pragma unroll
         for (int s = 0; s < KS; s++) {
             // the dimensions that the lane's piece of a key has
-            const int dim = FMT == ZC_FMT_BF16 ? s * 32 + (int)g * 8 : (s / 2) * 64 + (int)g * 16 + (s & 1) * 8;
+            const int dim = FMT == ZC_FMT_BF16 ? s * 32 + (int)g * 8 : kFp4<FMT> ? (int)g * (D / 4) + s * 8 : (s / 2) * 64 + (int)g * 16 + (s & 1) * 8;
             u32x4_t x = {0, 0, 0, 0};
             if (rows[t].token >= 0) x = *reinterpret_cast<const u32x4_t *>(row + dim);
             q[t][s] = query_operand(x, signed_c);
@@ -160,7 +179,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
 
     // The two halves of a step: what of the pools they are (nothing where a page is absent or the step is none: such loads give 0
     // without going to memory), and which are present.
-    struct Place { uint64_t at[2]; int32_t t0; uint32_t there; };
+    struct Place { uint64_t at[2]; int32_t t0; uint32_t there; };          // at: rows of the pools
     auto place_of = [&](int32_t b) {
         Place x = {{0, 0}, 0, 0};
         if (b >= end) return x;
@@ -171,24 +190,44 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
         for (int h = 0; h < 2; h++) {
             const int32_t page = __builtin_amdgcn_readlane(ids, i + h);
             x.there |= page >= 0 ? 1u << h : 0u;
-            x.at[h] = ((uint64_t)(uint32_t)max(page, 0) << page_log) + (((uint32_t)x.t0 + h * 16) & page_mask) * (D * ES);
+            x.at[h] = ((uint64_t)(uint32_t)max(page, 0) << a.c.page_shift) + (((uint32_t)x.t0 + h * 16) & page_mask);
         }
         return x;
     };
     auto load_keys = [&](const Place &x, Regs &r) {
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            const __amdgpu_buffer_rsrc_t from = sixteen_tokens(a.c.k + x.at[h], x.there >> h & 1 ? 16 * D * ES : 0);
+            const __amdgpu_buffer_rsrc_t from = sixteen_tokens(a.c.k + x.at[h] * kRow, x.there >> h & 1 ? 16 * kRow : 0);
+            if constexpr (kFp4<FMT>) {
+                constexpr uint32_t kScales = kRowScales<FMT, D>;
+                const __amdgpu_buffer_rsrc_t scales = sixteen_tokens(a.c.k_blocks + x.at[h] * kScales, x.there >> h & 1 ? 16 * kScales : 0);
+                load_words(r.k[h], from, k_lane);
+                // a quarter of a key has two scales, one, or half of one
+                if constexpr (kScales == 8) r.k_scale[h] = __builtin_amdgcn_raw_buffer_load_b16(scales, (int)(n16 * 8 + g * 2), 0, 0);
+                else r.k_scale[h] = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)(n16 * kScales + g * kScales / 4), 0, 0);
+            } else {
 #pragma unroll
-            for (int u = 0; u < NK; u++) r.k[h][u] = __builtin_amdgcn_raw_buffer_load_b128(from, (int)(k_lane + u * 64), 0, 0);
+                for (int u = 0; u < Regs::NK; u++) r.k[h][u] = __builtin_amdgcn_raw_buffer_load_b128(from, (int)(k_lane + u * 64), 0, 0);
+            }
         }
     };
     auto load_values = [&](const Place &x, Regs &r) {
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            const __amdgpu_buffer_rsrc_t from = sixteen_tokens(a.c.v + x.at[h], x.there >> h & 1 ? 16 * D * ES : 0);
+            const __amdgpu_buffer_rsrc_t from = sixteen_tokens(a.c.v + x.at[h] * kRow, x.there >> h & 1 ? 16 * kRow : 0);
+            if constexpr (kFp4<FMT>) {
+                constexpr uint32_t kScales = kRowScales<FMT, D>;
+                const __amdgpu_buffer_rsrc_t scales = sixteen_tokens(a.c.v_blocks + x.at[h] * kScales, x.there >> h & 1 ? 16 * kScales : 0);
 #pragma unroll
-            for (int j = 0; j < 4; j++) load_words(r.v[h * 4 + j], from, v_lane + j * (D * ES));
+                for (int j = 0; j < 4; j++) {
+                    if constexpr (DL == 8) r.v[h * 4 + j] = __builtin_amdgcn_raw_buffer_load_b32(from, (int)(v_lane + j * kRow), 0, 0);
+                    else r.v[h * 4 + j] = __builtin_amdgcn_raw_buffer_load_b16(from, (int)(v_lane + j * kRow), 0, 0);
+                    r.v_scale[h * 4 + j] = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)((g * 4 + j) * kScales + n16 * kScales / 16), 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; j++) load_words(r.v[h * 4 + j], from, v_lane + j * kRow);
+            }
         }
     };
 
@@ -210,7 +249,8 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
 #pragma unroll
             for (int u = 0; u < KS; u++) {
                 u32x4_t key;
-                if constexpr (FMT == ZC_FMT_BF16) key = r.k[h][u];
+                if constexpr (kFp4<FMT>) key = eight_fp4_to_bf16<FMT>(r.k[h][u], block_scale<FMT>(kRowScales<FMT, D> == 8 && u >= 2 ? r.k_scale[h] >> 8 : r.k_scale[h] & 0xFFu));
+                else if constexpr (FMT == ZC_FMT_BF16) key = r.k[h][u];
                 else key = eight_to_bf16<FMT>(r.k[h][u / 2][(u & 1) * 2], r.k[h][u / 2][(u & 1) * 2 + 1]);
 #pragma unroll
                 for (int t = 0; t < QT; t++) s[t][h] = mma16_keys(key, q[t][u], s[t][h]);
@@ -228,11 +268,18 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
 #pragma unroll
             for (int j = 0; j < 8; j++) {
                 const uint32_t keep = bit_as_mask(used, j), some = ~bit_as_mask(by_all, j);
-#pragma unroll
-                for (int w = 0; w < Regs::VW; w++) {
-                    const uint32_t x = r.v[j][w] & keep, wild = nonfinite_mask<FMT>(x) & some;
+                if constexpr (kFp4<FMT>) {               // (a scale that is not finite takes its block's elements along)
+                    const uint32_t scale = r.v_scale[j] & keep, wild = wild_scale<FMT>(scale) ? some : 0u;
                     bad |= wild ? 1u << j : 0u;
-                    r.v[j][w] = x & ~wild;
+                    r.v_scale[j] = scale & ~wild;
+                    r.v[j] &= keep & ~wild;
+                } else {
+#pragma unroll
+                    for (int w = 0; w < Regs::VW; w++) {
+                        const uint32_t x = r.v[j][w] & keep, wild = nonfinite_mask<FMT>(x) & some;
+                        bad |= wild ? 1u << j : 0u;
+                        r.v[j][w] = x & ~wild;
+                    }
                 }
             }
         }
@@ -279,24 +326,40 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
                     for (uint32_t k = 1; k < 8; k++) weight = j == k ? e[k] : weight;
                     weight = __shfl(weight, (int)(n16 + gg * 16));
                     const bool mine = seen(rows[t].sight, tok);
-                    const uint8_t *row = a.c.v + ((uint64_t)(uint32_t)max(table[(uint32_t)tok >> a.c.page_shift], 0) << page_log) + (uint64_t)((uint32_t)tok & page_mask) * (D * ES) + g * 4 * DL * ES;
+                    const uint64_t stored = ((uint64_t)(uint32_t)max(table[(uint32_t)tok >> a.c.page_shift], 0) << a.c.page_shift) + ((uint32_t)tok & page_mask);
 #pragma unroll
                     for (int cc = 0; cc < 4; cc++) {
 #pragma unroll
                         for (int i = 0; i < DL; i++) {
-                            const float x = element<FMT>(row + (cc * DL + i) * ES);
-                            o[t][i][cc] += mine && !(fabsf(x) < __builtin_inff()) ? weight * x : 0.0f;
+                            const float x = wild_value<FMT, D>(a.c, stored, (g * 4 + cc) * DL + i);
+                            o[t][i][cc] += mine && x != 0.0f ? weight * x : 0.0f;
                         }
                         __builtin_amdgcn_sched_barrier(0);       // a few at a time: this hardly ever runs and is to cost no registers
                     }
                 }
             }
         }
+        if constexpr (kFp4<FMT>) {
 #pragma unroll
-        for (int i = 0; i < DL; i++) {
-            const u32x4_t val = value_operand<FMT>(r.v, i);
+            for (int i = 0; i < DL; i += 2) {
+                u32x4_t even, odd;
+                if (i == 0) value_operands4<FMT, 0>(r.v, r.v_scale, even, odd);
+                else if (i == 2) value_operands4<FMT, 1>(r.v, r.v_scale, even, odd);
+                else if (i == 4) value_operands4<FMT, 2>(r.v, r.v_scale, even, odd);
+                else value_operands4<FMT, 3>(r.v, r.v_scale, even, odd);
 #pragma unroll
-            for (int t = 0; t < QT; t++) o[t][i] = mma16_values<FMT>(val, p[t], o[t][i]);
+                for (int t = 0; t < QT; t++) {
+                    o[t][i] = mma16_values<FMT>(even, p[t], o[t][i]);
+                    o[t][i + 1] = mma16_values<FMT>(odd, p[t], o[t][i + 1]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < DL; i++) {
+                const u32x4_t val = value_operand<FMT>(r.v, i);
+#pragma unroll
+                for (int t = 0; t < QT; t++) o[t][i] = mma16_values<FMT>(val, p[t], o[t][i]);
+            }
         }
         load_values(place, r);
     }

@@ -6,7 +6,6 @@ namespace zc {
 
 namespace {
 
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 constexpr uint32_t kFewSlots = 8;
 
 // One workgroup per (query token, query head).  With (m_s, l_s, O_s) of the slots, M = max m_s:
@@ -170,7 +169,7 @@ __global__ __launch_bounds__(256, 4) void k_attend_join(AttendDev a, WeightsDev 
 template <int FMT, int D>
 __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendDev a, WeightsDev wt)
 {
-    constexpr int ES = PageElem<FMT>::BYTES, KS = D / 16;
+    constexpr int KS = D / 16;
     constexpr uint32_t kRows = 64, kPieces = D / 8, kRowsPerPass = 256 / kPieces, kPasses = kRows / kRowsPerPass;
     __shared__ __align__(1024) uint8_t lds[2][kRows * D * 2];
     __shared__ float minus_lse[2][kRows];                      // in base 2; minus infinity: the row gives nothing
@@ -187,7 +186,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendDev a, WeightsD
     const uint32_t flip = signed_c < 0 ? 0x80008000u : 0u;     // (a factor that is not a number is in every lse already)
 
     const int32_t *table = a.c.table + (uint64_t)unit * a.c.table_pages;
-    const uint32_t page_log = a.c.page_shift + (D == 128 ? 7 : 6) + (ES - 1), page_mask = (1u << a.c.page_shift) - 1;
+    const uint32_t page_mask = (1u << a.c.page_shift) - 1;
     u32x4_t key[2][KS];
     uint32_t there = 0;
 #pragma unroll
@@ -199,9 +198,19 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendDev a, WeightsD
     for (int h = 0; h < 2; h++) {
         const uint32_t t = (uint32_t)t0 + h * 32 + n32, page = t >> a.c.page_shift;
         const int32_t id = page < a.c.table_pages ? table[page] : -1;
-        const uint8_t *row = a.c.k + ((uint64_t)((uint32_t)id < a.c.n_pages ? id : 0) << page_log) + (t & page_mask) * (D * ES);
-        // the order of the dimensions in the sums is free: FP8 keys come in pieces of 16
-        if constexpr (FMT == ZC_FMT_BF16) {
+        const uint64_t stored = ((uint64_t)((uint32_t)id < a.c.n_pages ? id : 0) << a.c.page_shift) + (t & page_mask);
+        const uint8_t *row = a.c.k + stored * kRowBytes<FMT, D>;
+        // the order of the dimensions in the sums is free: FP8 keys come in pieces of 16, FP4 ones in pieces of 32
+        if constexpr (kFp4<FMT>) {
+#pragma unroll
+            for (int u = 0; u < KS; u += 4) {
+                const u32x4_t x = *reinterpret_cast<const u32x4_t *>(row + u * 8 + g * 16);
+                const uint8_t *blocks = a.c.k_blocks + stored * kRowScales<FMT, D> + (u * 16 + (int)g * 32) / kBlock<FMT>;
+                const float s0 = block_scale<FMT>(blocks[0]), s1 = kBlock<FMT> == 16 ? block_scale<FMT>(blocks[kBlock<FMT> == 16]) : s0;
+#pragma unroll
+                for (int w = 0; w < 4; w++) key[h][u + w] = eight_fp4_to_bf16<FMT>(x[w], w < 2 ? s0 : s1);
+            }
+        } else if constexpr (FMT == ZC_FMT_BF16) {
 #pragma unroll
             for (int u = 0; u < KS; u++) key[h][u] = *reinterpret_cast<const u32x4_t *>(row + u * 32 + g * 16);
         } else {
@@ -274,7 +283,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendDev a, WeightsD
             const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
             for (int u = 0; u < KS; u++) {
-                const u32x4_t q = *reinterpret_cast<const u32x4_t *>(lds[buf] + key_place<D>(r, FMT == ZC_FMT_BF16 ? u * 2 + g : (u & ~1) * 2 + g * 2 + (u & 1)));
+                const u32x4_t q = *reinterpret_cast<const u32x4_t *>(lds[buf] + key_place<D>(r, FMT == ZC_FMT_BF16 ? u * 2 + g : kFp4<FMT> ? (u & ~3) * 2 + g * 4 + (u & 3) : (u & ~1) * 2 + g * 2 + (u & 1)));
                 s[0] = mma32_keys(key[0][u], q, u ? s[0] : zero);
                 s[1] = mma32_keys(key[1][u], q, u ? s[1] : zero);
             }
@@ -379,7 +388,9 @@ int launch_attend_weights(const AttendDev &a, const WeightsDev &w, uint32_t form
     const hipStream_t s = (hipStream_t)stream;
     if (format == ZC_FMT_BF16) launch_weights<ZC_FMT_BF16>(a, w, head_dim, blocks, s);
     else if (format == ZC_FMT_FP8_E4M3) launch_weights<ZC_FMT_FP8_E4M3>(a, w, head_dim, blocks, s);
-    else launch_weights<ZC_FMT_FP8_E5M2>(a, w, head_dim, blocks, s);
+    else if (format == ZC_FMT_FP8_E5M2) launch_weights<ZC_FMT_FP8_E5M2>(a, w, head_dim, blocks, s);
+    else if (format == ZC_FMT_FP4_E2M1_MX) launch_weights<ZC_FMT_FP4_E2M1_MX>(a, w, head_dim, blocks, s);
+    else launch_weights<ZC_FMT_FP4_E2M1_NV>(a, w, head_dim, blocks, s);
     if (w.parts > 1) hipLaunchKernelGGL(k_weights_sum, dim3(units * ((uint32_t)(a.c.limit + 255) / 256)), dim3(256), 0, s, a, w);
     return (int)hipGetLastError();
 }

@@ -32,7 +32,7 @@ constexpr int kHalves = kTile / 32, kStretches = kTile / 16;
 
 template <int FMT> __device__ __forceinline__ f32x16 mma32_values(u32x4_t a, u32x4_t b, f32x16 c)
 {
-    if constexpr (FMT == ZC_FMT_BF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    if constexpr (kValuesBf16<FMT>) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, a), __builtin_bit_cast(halfx8, b), c, 0, 0, 0);
 }
 template <int FMT> __device__ __forceinline__ u32x4_t eight_to_half(uint32_t lo, uint32_t hi)
@@ -67,8 +67,9 @@ template <int FMT, int D>
 __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, ManyTile<D> &tile0, ManyTile<D> &tile1, ManyNotes &notes)
 {
     constexpr bool kBring = FMT == ZC_FMT_BF16;                // tiles go to LDS as they are, past the registers
-    constexpr int ES = PageElem<FMT>::BYTES, KS = D / 16, DT = D / 32;
-    constexpr uint32_t kPieces = D * ES / 16;                  // 16-byte pieces of a stored row
+    constexpr int KS = D / 16, DT = D / 32;
+    constexpr uint32_t kRow = kRowBytes<FMT, D>, kPieceBytes = kFp4<FMT> ? kRow / 4 : 16;
+    constexpr uint32_t kPieces = kRow / kPieceBytes;           // pieces of a stored row
     constexpr uint32_t kRowsPerPass = 64 / kPieces, kPasses = 16 / kRowsPerPass;
     auto &bad_tokens = notes.bad_tokens;
     auto &limits = notes.limits;
@@ -133,7 +134,6 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
 
     // ---- bringing tiles: a wavefront takes 16 tokens, which lie in one page, some rows at a time; a lane has piece `piece` of each
     const int32_t *table = a.c.table + (uint64_t)unit * a.c.table_pages;
-    const uint32_t page_log = a.c.page_shift + (D == 128 ? 7 : 6) + (ES - 1);   // of a page's bytes
     const uint32_t page_mask = (1u << a.c.page_shift) - 1;
     const uint32_t piece = lane % kPieces, row0 = wave * 16 + lane / kPieces;       // (the row of pass 0)
     // lane kStretches * i + h: page of tokens 16 h .. of tile ids_from + i (0 where it is absent), and the bit that says it is there
@@ -152,25 +152,42 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
     // which of a tile's stretches of 16 tokens are present
     auto there_of = [&](int32_t b) { return (uint32_t)(present >> ((b - ids_from) * kStretches)) & ((1u << kStretches) - 1); };
     u32x4_t kx[kPasses], vx[kPasses];
+    uint32_t k_blocks = 0, v_blocks = 0;                       // FP4: the block scales of the lane's piece: one, two, or one of two pieces
     // Where a lane's piece of a pass lies from the first of the 16 tokens.  kBring: place `piece` of a row of LDS holds another piece of
     // it, by key_place and value_place, whose exchange of pieces is its own inverse.
     auto mine_k = [&](uint32_t p) {
         const uint32_t r = row0 + p * kRowsPerPass;
-        return (r & 15) * (D * ES) + (kBring ? key_place<D>(r, piece) & (D * 2 - 1) : piece * 16);
+        return (r & 15) * kRow + (kBring ? key_place<D>(r, piece) & (D * 2 - 1) : piece * kPieceBytes);
     };
     auto mine_v = [&](uint32_t p) {
         const uint32_t r = row0 + p * kRowsPerPass;
-        return (r & 15) * (D * ES) + (kBring ? value_place<D>(r, piece * 16) & (D * 2 - 1) : piece * 16);
+        return (r & 15) * kRow + (kBring ? value_place<D>(r, piece * 16) & (D * 2 - 1) : piece * kPieceBytes);
     };
     auto fetch = [&](int32_t b, ManyTile<D> &to) {
         const uint32_t t0 = (uint32_t)blocks.at(b) * kTile + wave * 16, page = (uint32_t)__builtin_amdgcn_readlane(ids, (b - ids_from) * kStretches + (int32_t)wave);
-        const uint64_t where = ((uint64_t)page << page_log) + (t0 & page_mask) * (D * ES);
-        const __amdgpu_buffer_rsrc_t k = sixteen_tokens(a.c.k + where, 16 * D * ES), v = sixteen_tokens(a.c.v + where, 16 * D * ES);
+        const uint64_t where = ((uint64_t)page << a.c.page_shift) + (t0 & page_mask);
+        const __amdgpu_buffer_rsrc_t k = sixteen_tokens(a.c.k + where * kRow, 16 * kRow), v = sixteen_tokens(a.c.v + where * kRow, 16 * kRow);
+        if constexpr (kFp4<FMT>) {
+            constexpr uint32_t kScales = kRowScales<FMT, D>;
+            const __amdgpu_buffer_rsrc_t ks = sixteen_tokens(a.c.k_blocks + where * kScales, 16 * kScales), vs = sixteen_tokens(a.c.v_blocks + where * kScales, 16 * kScales);
+            const int at = (int)((row0 & 15) * kScales + piece * kScales / 4);
+            if constexpr (kScales == 8) {
+                k_blocks = __builtin_amdgcn_raw_buffer_load_b16(ks, at, 0, 0);
+                v_blocks = __builtin_amdgcn_raw_buffer_load_b16(vs, at, 0, 0);
+            } else {
+                k_blocks = __builtin_amdgcn_raw_buffer_load_b8(ks, at, 0, 0);
+                v_blocks = __builtin_amdgcn_raw_buffer_load_b8(vs, at, 0, 0);
+            }
+        }
 #pragma unroll
         for (uint32_t p = 0; p < kPasses; p++) {
             if constexpr (kBring) {
                 bring(k, mine_k(p), to.keys + wave * (16 * D * 2) + p * 1024);
                 bring(v, mine_v(p), to.values + wave * (16 * D * 2) + p * 1024);
+            } else if constexpr (kPieceBytes == 8) {
+                const u32x2 kw = __builtin_amdgcn_raw_buffer_load_b64(k, (int)mine_k(p), 0, 0), vw = __builtin_amdgcn_raw_buffer_load_b64(v, (int)mine_v(p), 0, 0);
+                kx[p] = u32x4_t{kw[0], kw[1], 0, 0};
+                vx[p] = u32x4_t{vw[0], vw[1], 0, 0};
             } else {
                 kx[p] = __builtin_amdgcn_raw_buffer_load_b128(k, (int)mine_k(p), 0, 0);
                 vx[p] = __builtin_amdgcn_raw_buffer_load_b128(v, (int)mine_v(p), 0, 0);
@@ -179,8 +196,14 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
     };
     // whether every row of the workgroup (of the wavefront) sees every token of a tile
     auto whole = [&](int32_t t0, uint32_t there, int32_t lmin, int32_t fmax) { return there == (1u << kStretches) - 1 && t0 + kTile - 1 <= lmin && (t0 >= fmax || t0 + kTile <= sinks); };
+    // FP4: the scale of the eight elements in word w of the piece
+    auto scale_of = [&](uint32_t blocks, uint32_t w) { return block_scale<FMT>(kRowScales<FMT, D> == 8 && w >= 2 ? blocks >> 8 : blocks & 0xFFu); };
     auto store_keys = [&](ManyTile<D> &to) {
-        if constexpr (!kBring) {
+        if constexpr (kFp4<FMT>) {
+#pragma unroll
+            for (uint32_t w = 0; w < kPieceBytes / 4; w++)
+                *reinterpret_cast<u32x4_t *>(to.keys + key_place<D>(row0, piece * (kPieceBytes / 4) + w)) = eight_fp4_to_bf16<FMT>(kx[0][w], scale_of(k_blocks, w));
+        } else if constexpr (!kBring) {
 #pragma unroll
             for (uint32_t p = 0; p < kPasses; p++) {
                 const uint32_t r = p * kRowsPerPass + row0;
@@ -196,12 +219,21 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
         const bool used = (there >> wave & 1) && seen(Sight{all_last_max, all_from_min, sinks}, t);
         const bool by_all = seen(Sight{all_last_min, all_from_max, sinks}, t);
         uint32_t wild = 0;
+        if constexpr (kFp4<FMT>) {                             // (a scale that is not finite takes its block's elements along)
+            const bool two = kRowScales<FMT, D> == 8;
+            const bool wild0 = !by_all && wild_scale<FMT>(v_blocks & 0xFFu), wild1 = two ? !by_all && wild_scale<FMT>(v_blocks >> 8) : wild0;
+            wild = used && (wild0 || wild1);
+            v_blocks &= (used && !wild0 ? 0xFFu : 0u) | (used && !wild1 ? 0xFF00u : 0u);
 #pragma unroll
-        for (int w = 0; w < 4; w++) {
-            x[w] = used ? x[w] : 0u;
-            const uint32_t y = by_all ? 0u : nonfinite_mask<FMT>(x[w]);
-            wild |= y;
-            x[w] &= ~y;
+            for (int w = 0; w < 4; w++) x[w] = used && !(w < 2 ? wild0 : wild1) ? x[w] : 0u;
+        } else {
+#pragma unroll
+            for (int w = 0; w < 4; w++) {
+                x[w] = used ? x[w] : 0u;
+                const uint32_t y = by_all ? 0u : nonfinite_mask<FMT>(x[w]);
+                wild |= y;
+                x[w] &= ~y;
+            }
         }
         if (wild) atomicOr(&bad_tokens[mod3][r / 32], 1u << (r & 31));
     };
@@ -222,6 +254,11 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
 #pragma unroll
                 for (uint32_t p = 0; p < kPasses; p++) clean(vx[p], p * kRowsPerPass + row0, t0, there, mod3);
             }
+            if constexpr (kFp4<FMT>) {
+#pragma unroll
+                for (uint32_t w = 0; w < kPieceBytes / 4; w++)
+                    *reinterpret_cast<u32x4_t *>(to.values + value_place<D>(row0, piece * (kPieceBytes * 4) + w * 16)) = eight_fp4_to_values<FMT>(vx[0][w], scale_of(v_blocks, w));
+            } else
 #pragma unroll
             for (uint32_t p = 0; p < kPasses; p++) {
                 const uint32_t r = p * kRowsPerPass + row0;
@@ -311,18 +348,18 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
 #pragma unroll
                 for (uint32_t k = 1; k < kTile / 4; k++) word = i / 2 == k ? p[k / 4][k & 3] : word;
                 word = (uint32_t)__shfl((int)word, (int)(n32 + gg * 32)) >> (i & 1) * 16 & 0xFFFFu;
-                const float weight = FMT == ZC_FMT_BF16 ? __uint_as_float(word << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)word);
+                const float weight = kValuesBf16<FMT> ? __uint_as_float(word << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)word);
                 const int32_t tok = t0 + (int32_t)n;
                 const bool mine = seen(row.sight, tok);
-                const uint8_t *from = a.c.v + ((uint64_t)(uint32_t)max(table[(uint32_t)tok >> a.c.page_shift], 0) << page_log) + ((uint32_t)tok & page_mask) * (D * ES);
+                const uint64_t stored = ((uint64_t)(uint32_t)max(table[(uint32_t)tok >> a.c.page_shift], 0) << a.c.page_shift) + ((uint32_t)tok & page_mask);
 #pragma unroll
                 for (int d = 0; d < DT; d++)
 #pragma unroll
                     for (int kk = 0; kk < 16; kk += 4) {
 #pragma unroll
                         for (int k = kk; k < kk + 4; k++) {
-                            const float x = element<FMT>(from + (d * 32 + (k / 4) * 8 + (int)g * 4 + (k & 3)) * ES);
-                            o[d][k] += mine && !(fabsf(x) < __builtin_inff()) ? weight * x : 0.0f;
+                            const float x = wild_value<FMT, D>(a.c, stored, d * 32 + (k / 4) * 8 + g * 4 + (k & 3));
+                            o[d][k] += mine && x != 0.0f ? weight * x : 0.0f;
                         }
                         __builtin_amdgcn_sched_barrier(0);       // a few at a time: this hardly ever runs and is to cost no registers
                     }

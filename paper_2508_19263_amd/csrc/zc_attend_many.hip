@@ -31,7 +31,9 @@ int launch_attend_many(const AttendDev &a, uint32_t format, uint32_t head_dim, v
     const hipStream_t s = (hipStream_t)stream;
     if (format == ZC_FMT_BF16) return launch<ZC_FMT_BF16>(a, head_dim, blocks, s);
     if (format == ZC_FMT_FP8_E4M3) return launch<ZC_FMT_FP8_E4M3>(a, head_dim, blocks, s);
-    return launch<ZC_FMT_FP8_E5M2>(a, head_dim, blocks, s);
+    if (format == ZC_FMT_FP8_E5M2) return launch<ZC_FMT_FP8_E5M2>(a, head_dim, blocks, s);
+    if (format == ZC_FMT_FP4_E2M1_MX) return launch<ZC_FMT_FP4_E2M1_MX>(a, head_dim, blocks, s);
+    return launch<ZC_FMT_FP4_E2M1_NV>(a, head_dim, blocks, s);
 }
 
 }  // namespace zc

@@ -53,7 +53,9 @@ int launch_attend_shared(const AttendDev &pre, const AttendDev &own, uint32_t fo
     const hipStream_t s = (hipStream_t)stream;
     if (format == ZC_FMT_BF16) return launch<ZC_FMT_BF16>(pre, own, head_dim, pre_blocks, blocks, pre_many, tiles, s);
     if (format == ZC_FMT_FP8_E4M3) return launch<ZC_FMT_FP8_E4M3>(pre, own, head_dim, pre_blocks, blocks, pre_many, tiles, s);
-    return launch<ZC_FMT_FP8_E5M2>(pre, own, head_dim, pre_blocks, blocks, pre_many, tiles, s);
+    if (format == ZC_FMT_FP8_E5M2) return launch<ZC_FMT_FP8_E5M2>(pre, own, head_dim, pre_blocks, blocks, pre_many, tiles, s);
+    if (format == ZC_FMT_FP4_E2M1_MX) return launch<ZC_FMT_FP4_E2M1_MX>(pre, own, head_dim, pre_blocks, blocks, pre_many, tiles, s);
+    return launch<ZC_FMT_FP4_E2M1_NV>(pre, own, head_dim, pre_blocks, blocks, pre_many, tiles, s);
 }
 
 }  // namespace zc

@@ -227,6 +227,21 @@ template <bool STREAM> __device__ __forceinline__ void store_piece(uint8_t *p, c
     else *x = v;
 }
 
+// FP4: a row's block scales, which lie at its number in pools of their own (0 from an absent page)
+template <typename T> __device__ __forceinline__ void move_scales_as(const EvictDev &e, bool from_there, uint64_t from, bool to_there, uint64_t to)
+{
+    const T k = from_there ? reinterpret_cast<const T *>(e.from.k_blocks)[from] : T(0), v = from_there ? reinterpret_cast<const T *>(e.from.v_blocks)[from] : T(0);
+    if (!to_there) return;
+    reinterpret_cast<T *>(e.k_blocks_to)[to] = k;
+    reinterpret_cast<T *>(e.v_blocks_to)[to] = v;
+}
+__device__ __forceinline__ void move_scales(const EvictDev &e, bool from_there, uint64_t from, bool to_there, uint64_t to)
+{
+    if (e.row_scales == 8) move_scales_as<uint64_t>(e, from_there, from, to_there, to);
+    else if (e.row_scales == 4) move_scales_as<uint32_t>(e, from_there, from, to_there, to);
+    else move_scales_as<uint16_t>(e, from_there, from, to_there, to);
+}
+
 // 64 rows of keys and of values of one (sequence, head) to a workgroup: where each comes from and goes to is worked out once, then
 // every thread has all of its 16-byte pieces (PIECES to a row) on their way before it stores them.  STREAM: past the caches, where a call moves more
 // than the memory-side cache holds (1.07 GB: 192 us, 5.6 TB/s, against 215; 67 MB: 13.4 against 11.7 us, 5.7 TB/s).  Bound by reading
@@ -234,7 +249,7 @@ template <bool STREAM> __device__ __forceinline__ void store_piece(uint8_t *p, c
 template <uint32_t PIECES, bool STREAM>
 __global__ __launch_bounds__(256) void k_evict_move(EvictDev e, uint32_t blocks_per_head)
 {
-    constexpr uint32_t kEach = 64 * PIECES / 256;              // pieces per thread
+    constexpr uint32_t kEach = 64 * PIECES < 256 ? 1 : 64 * PIECES / 256;      // pieces per thread (two to a row: of every other thread)
     constexpr uint64_t kNone = ~0ull;
     __shared__ uint64_t src_at[64], dst_at[64];
     const uint32_t unit = blockIdx.x / blocks_per_head, seq = unit / e.from.heads, tid = threadIdx.x;
@@ -247,6 +262,8 @@ __global__ __launch_bounds__(256) void k_evict_move(EvictDev e, uint32_t blocks_
             const int32_t sp = e.from.table[(uint64_t)unit * e.from.table_pages + (src >> e.from.page_shift)];
             const int32_t dp = e.to.table[(uint64_t)unit * e.to.table_pages + (dst >> e.to.page_shift)];
             if ((uint32_t)sp < e.from.n_pages) from = (((uint64_t)sp << e.from.page_shift) + (src & ((1u << e.from.page_shift) - 1))) * (PIECES * 16);
+            if (e.row_scales) move_scales(e, (uint32_t)sp < e.from.n_pages, ((uint64_t)(uint32_t)sp << e.from.page_shift) + (src & ((1u << e.from.page_shift) - 1)),
+                                          (uint32_t)dp < e.to.n_pages, ((uint64_t)(uint32_t)dp << e.to.page_shift) + (dst & ((1u << e.to.page_shift) - 1)));
             if ((uint32_t)dp < e.to.n_pages) to = (((uint64_t)dp << e.to.page_shift) + (dst & ((1u << e.to.page_shift) - 1))) * (PIECES * 16);
             if (e.weights_to) e.weights_to[(uint64_t)unit * (uint64_t)e.to.capacity + dst] = e.weights[(uint64_t)unit * (uint64_t)e.from.capacity + src];
         }
@@ -254,6 +271,7 @@ __global__ __launch_bounds__(256) void k_evict_move(EvictDev e, uint32_t blocks_
         dst_at[tid] = to;
     }
     __syncthreads();
+    if (PIECES * 64 < 256 && tid >= PIECES * 64) return;
     u32x4 k[kEach], v[kEach];
 #pragma unroll
     for (uint32_t i = 0; i < kEach; i++) {
@@ -300,7 +318,8 @@ int launch_evict(const EvictDev &e, void *stream)
     const uint32_t per_head = ((e.keep < (uint32_t)e.from.capacity ? e.keep : (uint32_t)e.from.capacity) + 63) / 64;
     if (!per_head) return 0;
     const bool stream_past = (uint64_t)units * per_head * 64 * e.row_bytes * 4 > kMemorySideCache;       // keys and values, read and written
-    if (e.row_bytes == 64) launch_move<4>(e, units * per_head, per_head, stream_past, s);
+    if (e.row_bytes == 32) launch_move<2>(e, units * per_head, per_head, stream_past, s);
+    else if (e.row_bytes == 64) launch_move<4>(e, units * per_head, per_head, stream_past, s);
     else if (e.row_bytes == 128) launch_move<8>(e, units * per_head, per_head, stream_past, s);
     else launch_move<16>(e, units * per_head, per_head, stream_past, s);
     return (int)hipGetLastError();

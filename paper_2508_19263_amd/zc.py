@@ -26,7 +26,7 @@ EXPORTS = ["zc_compress_bound", "zc_workspace_bytes", "zc_compress", "zc_compres
            "zc_decompress_batch_run", "zc_stats", "zc_build_code", "zc_train_code", "zc_compress_with_code",
            "zc_compress_batch_with_code", "zc_compress_batch_with_code_async", "zc_compress_batch_async", "zc_code_stale",
            "zc_validate_container", "zc_release_host_buffers", "zc_compress_noalloc", "zc_copy_reference", "zc_status_string",
-           "zc_attend", "zc_attend_shared", "zc_attend_workspace_bytes", "zc_evict"]
+           "zc_attend", "zc_attend_shared", "zc_attend_workspace_bytes", "zc_evict", "zc_kv_write", "zc_kv_read"]
 
 
 class Params(C.Structure):
@@ -75,7 +75,13 @@ class KvCache(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("format", C.c_uint32), ("n_seqs", C.c_uint32), ("n_heads", C.c_uint32),
                 ("head_dim", C.c_uint32), ("page_tokens", C.c_uint32), ("table_pages", C.c_uint32), ("n_pages", C.c_uint32),
                 ("d_k_pages", C.c_void_p), ("d_v_pages", C.c_void_p), ("d_table", C.c_void_p), ("d_lengths", C.c_void_p),
-                ("d_k_scales", C.c_void_p), ("d_v_scales", C.c_void_p)]
+                ("d_k_scales", C.c_void_p), ("d_v_scales", C.c_void_p), ("d_k_block_scales", C.c_void_p), ("d_v_block_scales", C.c_void_p)]
+
+
+class KvRows(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_tokens", C.c_uint32), ("d_k", C.c_void_p), ("d_v", C.c_void_p),
+                ("k_token_stride", C.c_uint64), ("k_head_stride", C.c_uint64), ("v_token_stride", C.c_uint64), ("v_head_stride", C.c_uint64),
+                ("d_q_start", C.c_void_p)]
 
 
 class AttendArgs(C.Structure):
@@ -87,6 +93,7 @@ class AttendArgs(C.Structure):
 
 
 _ATTEND_ARGS_BYTES = C.sizeof(AttendArgs)
+_KV_ROWS_BYTES = C.sizeof(KvRows)
 
 
 class ZcError(RuntimeError):
@@ -158,6 +165,9 @@ def lib():
         L.zc_attend_shared.argtypes = [C.POINTER(AttendArgs), C.POINTER(KvCache), C.POINTER(KvCache), vp, u64, vp]
         L.zc_evict.restype = C.c_int
         L.zc_evict.argtypes = [C.POINTER(KvCache), vp, u32, u32, u32, C.POINTER(KvCache), vp, vp, vp]
+        for call in (L.zc_kv_write, L.zc_kv_read):
+            call.restype = C.c_int
+            call.argtypes = [C.POINTER(KvRows), C.POINTER(KvCache), vp]
         L.zc_build_code.restype = C.c_int
         L.zc_build_code.argtypes = [C.POINTER(u64), u32, u32, C.POINTER(C.c_uint8), C.POINTER(C.c_uint16)]
         _lib = L
@@ -466,7 +476,9 @@ class Batch:
 
 
 _PAGE_TYPES = {FMT_BF16: (torch.bfloat16, torch.int16, torch.uint16), FMT_FP8_E4M3: (torch.uint8, torch.int8, torch.float8_e4m3fn),
-               FMT_FP8_E5M2: (torch.uint8, torch.int8, torch.float8_e5m2)}
+               FMT_FP8_E5M2: (torch.uint8, torch.int8, torch.float8_e5m2), FMT_FP4_E2M1_MX: (torch.uint8, torch.int8, torch.float4_e2m1fn_x2),
+               FMT_FP4_E2M1_NV: (torch.uint8, torch.int8, torch.float4_e2m1fn_x2)}
+_BLOCK_TYPES = {FMT_FP4_E2M1_MX: (torch.uint8, torch.int8, torch.float8_e8m0fnu), FMT_FP4_E2M1_NV: (torch.uint8, torch.int8, torch.float8_e4m3fn)}
 _ROW_TYPES = (torch.bfloat16, torch.int16, torch.uint16)
 
 
@@ -474,11 +486,12 @@ class PagedCache:
     """K and V of a batch of sequences in pages, as the attention and eviction calls take them.
 
     k_pages, v_pages: [n_pages, page_tokens, head_dim], contiguous, as stored (of the format's type, or as plain integers of
-    its size); table: int32 [n_seqs, n_heads, table_pages] of page numbers (one that is no page's: absent); lengths: int32
+    its size; FP4: head_dim / 2 bytes, with k_blocks, v_blocks: [n_pages, page_tokens, head_dim / 32] (MX) or head_dim / 16 (NV), the
+    block scales' bytes); table: int32 [n_seqs, n_heads, table_pages] of page numbers (one that is no page's: absent); lengths: int32
     [n_seqs], tokens in the cache; k_scales, v_scales: float32 [n_seqs, n_heads] or None.  The object holds the tensors
     and the descriptor; the lengths and the table are read on the device when a call runs, so they may change between calls."""
 
-    def __init__(self, k_pages, v_pages, table, lengths, fmt, k_scales=None, v_scales=None):
+    def __init__(self, k_pages, v_pages, table, lengths, fmt, k_scales=None, v_scales=None, k_blocks=None, v_blocks=None):
         for name, t, dtype, dims in (("table", table, torch.int32, 3), ("lengths", lengths, torch.int32, 1)):
             if t.dtype != dtype or t.dim() != dims or not t.is_contiguous():
                 raise ValueError("PagedCache: %s has to be a contiguous %s tensor of %d dimensions" % (name, dtype, dims))
@@ -493,13 +506,22 @@ class PagedCache:
         for t in (k_scales, v_scales):
             if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != tuple(table.shape[:2]) or not t.is_contiguous()):
                 raise ValueError("PagedCache: scales have to be contiguous float32 [n_seqs, n_heads]")
+        packed = 2 if fmt in _BLOCK_TYPES else 1                 # elements to an entry of the pages
+        if packed == 2 and k_blocks is None and v_blocks is None:
+            raise ZcError(ERR_UNSUPPORTED, "PagedCache: FP4 pages without block scales")
+        for t in (k_blocks, v_blocks):
+            if packed == 1 and t is not None:
+                raise ValueError("PagedCache: the format has no block scales")
+            if packed == 2 and (t is None or t.dtype not in _BLOCK_TYPES[fmt] or not t.is_contiguous() or
+                                tuple(t.shape) != tuple(k_pages.shape[:2]) + (k_pages.shape[2] * 2 // scale_block(fmt),)):
+                raise ValueError("PagedCache: block scales have to be contiguous [n_pages, page_tokens, head_dim / %d] bytes" % scale_block(fmt))
         self.device = k_pages.device
-        if any(t is not None and t.device != self.device for t in (v_pages, table, lengths, k_scales, v_scales)):
+        if any(t is not None and t.device != self.device for t in (v_pages, table, lengths, k_scales, v_scales, k_blocks, v_blocks)):
             raise ValueError("PagedCache: tensors are on different devices")
         self.k_pages, self.v_pages, self.table, self.lengths = k_pages, v_pages, table, lengths
-        self.k_scales, self.v_scales, self.fmt = k_scales, v_scales, fmt
+        self.k_scales, self.v_scales, self.k_blocks, self.v_blocks, self.fmt = k_scales, v_scales, k_blocks, v_blocks, fmt
         self.n_seqs, self.n_heads, self.table_pages = table.shape
-        self.n_pages, self.page_tokens, self.head_dim = k_pages.shape
+        self.n_pages, self.page_tokens, self.head_dim = k_pages.shape[0], k_pages.shape[1], k_pages.shape[2] * packed
         self.capacity = self.table_pages * self.page_tokens
         c = self.c = KvCache()
         c.struct_size, c.format = C.sizeof(KvCache), fmt
@@ -508,6 +530,8 @@ class PagedCache:
         c.d_k_pages, c.d_v_pages, c.d_table, c.d_lengths = k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), lengths.data_ptr()
         c.d_k_scales = k_scales.data_ptr() if k_scales is not None else None
         c.d_v_scales = v_scales.data_ptr() if v_scales is not None else None
+        c.d_k_block_scales = k_blocks.data_ptr() if k_blocks is not None else None
+        c.d_v_block_scales = v_blocks.data_ptr() if v_blocks is not None else None
         self.ref = C.byref(c)
 
 
@@ -519,6 +543,59 @@ def _check_numbers(what, **numbers):
     for name, x in numbers.items():
         if not 0 <= x <= _MOST:
             raise ValueError("%s: %s has to be in 0 .. 2^32 - 1, not %d" % (what, name, x))
+
+
+def _kv_rows(what, call, k, v, cache, q_start, written):
+    n = k.shape[0]
+    for name, t in (("k", k), ("v", v)):
+        if t.dim() != 3 or tuple(t.shape) != (n, cache.n_heads, cache.head_dim) or t.stride(2) != 1 or t.dtype not in _ROW_TYPES:
+            raise ValueError("%s: %s has to be [n_tokens, n_heads, head_dim] in BF16 with contiguous rows" % (what, name))
+        if not written:
+            reach = cache.head_dim                               # elements from a row's first to the next free one
+            for stride, size in sorted(zip(t.stride()[:2], t.shape[:2])):
+                if size > 1 and stride < reach:
+                    raise ValueError("%s: rows of %s overlap" % (what, name))
+                reach += stride * (size - 1) if size > 1 else 0
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError("%s: there is no gradient through a stored cache: detach %s, or call it under torch.no_grad()" % (what, name))
+    if q_start is None and n != cache.n_seqs:
+        raise ValueError("%s: without q_start there is one token per sequence" % what)
+    if q_start is not None and (q_start.dtype != torch.int32 or q_start.numel() != cache.n_seqs + 1 or not q_start.is_contiguous()):
+        raise ValueError("%s: q_start has to be contiguous int32 of n_seqs + 1 entries" % what)
+    device, current = k.device, torch._C._cuda_getDevice() if k.is_cuda else -1       # (the kernels go to the current GPU's stream)
+    if device.index != current or cache.device != device or v.device != device or (q_start is not None and q_start.device != device):
+        raise ValueError("%s: tensors have to be on one GPU, the current one" % what)
+    strides = [0 if size == 1 else stride for t in (k, v) for size, stride in zip(t.shape[:2], t.stride())]     # (of one element: any number)
+    a = KvRows(_KV_ROWS_BYTES, n, k.data_ptr(), v.data_ptr(), *strides, None if q_start is None else q_start.data_ptr())
+    st = call(C.byref(a), cache.ref, torch._C._cuda_getCurrentRawStream(current))
+    if st != OK:
+        raise ZcError(st, what)
+
+
+def write_kv(k, v, cache, q_start=None):
+    """Quantises BF16 keys and values [n_tokens, n_heads, head_dim] into the pages of a PagedCache: what the last tokens of every
+    sequence are, whose lengths count them already (as attend() takes its queries, so that a step is: lengths += 1, write_kv, attend).
+
+    q_start: int32 [n_seqs + 1], where each sequence's tokens begin (None: one token per sequence).  FP8: divided by the cache's
+    scales, the largest number where they are beyond it; FP4: with a scale for every block, which is written to k_blocks and v_blocks."""
+    _kv_rows("zc_kv_write", lib().zc_kv_write, k, v, cache, q_start, True)
+
+
+def read_kv(cache, q_start=None, n_tokens=None, k=None, v=None):
+    """The last tokens of every sequence of a PagedCache as attention sees them: (k, v), BF16 [n_tokens, n_heads, head_dim].
+
+    q_start: int32 [n_seqs + 1], where each sequence's tokens begin (None: one token, the last, per sequence); n_tokens: rows of the
+    results (needed with q_start unless k or v is given; rows of tokens of no sequence are left as they are); k, v: where the results go."""
+    if n_tokens is None:
+        n_tokens = k.shape[0] if k is not None else v.shape[0] if v is not None else cache.n_seqs
+        if k is None and v is None and q_start is not None:
+            raise ValueError("zc_kv_read: with q_start, n_tokens says how many rows there are")
+    _check_numbers("zc_kv_read", n_tokens=n_tokens)
+    k, v = (torch.empty((n_tokens, cache.n_heads, cache.head_dim), dtype=torch.bfloat16, device=cache.device) if t is None else t for t in (k, v))
+    if k.shape[0] != n_tokens:
+        raise ValueError("zc_kv_read: k has to be [n_tokens, n_heads, head_dim] in BF16 with contiguous rows")
+    _kv_rows("zc_kv_read", lib().zc_kv_read, k, v, cache, q_start, False)
+    return k, v
 
 
 def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, max_kv_len, max_prefix_len, out, lse, weights, weights_out, ws):
