@@ -62,15 +62,16 @@ bool same_shape(const zc_kv_cache &a, const zc_kv_cache &b) { return a.format ==
 // one pass over a cache: k_attend_many with tiles x 128 rows to a workgroup, or k_attend_few with tiles x 16
 struct Pass {
     bool many;
-    uint32_t tiles, row_blocks, even, splits;
+    uint32_t tiles, row_blocks, even, splits, long_part;
     uint64_t blocks;
 };
 
 // rows: of one (sequence, head), or of one head of the prefix; units: how many of those; longest: tokens that a row block may have to read;
 // only: the call has no other pass
-Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_splits, bool only)
+Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_splits, bool only, bool fp4)
 {
     Pass p;
+    p.long_part = fp4 ? kLongPart / 2 : kLongPart;
     // k_attend_few goes over a cache once for every 32 rows, k_attend_many once for 128.  Microseconds of the former against the latter, rows to a
     // K/V head in front, one query head each, 8 K/V heads: 64: 4 FP8 caches of 8,192 tokens 25.7 against 30.4, one 15.7 against 19.6, 4 BF16 ones
     // of 4,000 21.3 against 27.0, six E5M2 ones with heads of 64 and a window of 2,048 15.8 against 19.8, 16 BF16 ones of 1,000 with heads of 64
@@ -91,12 +92,17 @@ Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_sp
     // most kLongPart tokens, and what is left over of a shorter cache's parts ends at once: 31 FP8 caches of 1,000 tokens and one of 131,072
     // 1,077 -> 128 us, 64 of 0 to 32,768 444 -> 408 us; 64 of 8,192 188 us as before, 16 of 32,768 190 -> 198 us.  (At most 4,096: 109, 391,
     // 202 and 209 us.)  k_attend_many has row blocks enough where rows are many, and its parts would take their number times as much room.
-    const uint64_t enough = p.many ? 512 : 256;
+    // A part of an FP4 cache is half the bytes and nearly as much work, and a compute unit takes up to four of its workgroups: parts of at most 4,096
+    // tokens, and two for each compute unit where rows fill one tile.  Microseconds of one workgroup and 8,192 tokens, against 512 and 4,096 (MX, 8
+    // K/V heads of 128, 4 query heads to each): one cache of 131,072 tokens 48.0 and 38.7, 8 of 8,192 23.9 and 20.6, 24 of 15,005 98 and 86, 24 of 0 to
+    // 30,011 114 and 97, 64 of 0 to 32,768 264 and 238; 32 of 16,384 113.9 and 114.6; of 32 rows each, 4 of 8,192 21.8 and 23.1.
+    const bool fine = p.long_part < kLongPart;
+    const uint64_t enough = p.many || (fine && p.tiles == 1) ? 512 : 256;
     uint64_t even = groups ? (enough + groups - 1) / groups : 1;
     if (even > possible) even = possible;
     if (even > most_splits) even = most_splits;
     if (!even) even = 1;
-    const uint64_t least = p.many ? 1 : (longest + kLongPart - 1) / kLongPart, s = even > least ? even : least;
+    const uint64_t least = p.many ? 1 : (longest + p.long_part - 1) / p.long_part, s = even > least ? even : least;
     p.even = (uint32_t)even;
     p.splits = (uint32_t)(s < most_splits ? s : most_splits);
     p.blocks = groups * p.splits;
@@ -163,7 +169,7 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
         const uint64_t w = a.window ? (uint64_t)a.window + a.max_q_len + a.sinks + 64 : (uint64_t)limit;
         return w < (uint64_t)limit ? w : (uint64_t)limit;
     };
-    p.own_pass = plan_pass((uint64_t)a.max_q_len * a.group, (uint64_t)a.n_seqs * a.c.heads, reach(a.c.limit), shared ? 16 : kMaxSlots, !shared);
+    p.own_pass = plan_pass((uint64_t)a.max_q_len * a.group, (uint64_t)a.n_seqs * a.c.heads, reach(a.c.limit), shared ? 16 : kMaxSlots, !shared, fp4(cache->format));
     p.slots = p.own_pass.splits;
     if (shared) {
         AttendDev &b = p.pre;
@@ -178,9 +184,10 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
         b = a;
         b.c = pc;
         b.shared = 1;
-        p.pre_pass = plan_pass((uint64_t)a.n_tokens * a.group, a.c.heads, (uint64_t)pc.limit, 48, false);
+        p.pre_pass = plan_pass((uint64_t)a.n_tokens * a.group, a.c.heads, (uint64_t)pc.limit, 48, false, fp4(cache->format));
         b.splits = p.pre_pass.splits;
         b.even = p.pre_pass.even;
+        b.long_part = p.pre_pass.long_part;
         b.row_blocks = p.pre_pass.row_blocks;
         b.first_slot = 0;
         a.first_slot = b.splits;
@@ -188,6 +195,7 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
     } else if (x->max_prefix_len) return ZC_ERR_INVALID_ARG;
     a.splits = p.own_pass.splits;
     a.even = p.own_pass.even;
+    a.long_part = p.own_pass.long_part;
     a.row_blocks = p.own_pass.row_blocks;
     a.direct = p.slots == 1;
     if (p.own_pass.blocks + p.pre_pass.blocks > kMaxBlocks) return ZC_ERR_INVALID_ARG;

@@ -148,7 +148,7 @@ template <int FMT, int SEL> __device__ __forceinline__ uint32_t two_fp4_to_bf16(
     if constexpr (FMT == ZC_FMT_FP4_E2M1_MX) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, SEL));
     else {
         const f32x2 x = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, SEL));
-        return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(x[0] * scale), (__bf16)(x[1] * scale)});
+        return __builtin_amdgcn_perm(bits(x[1] * scale), bits(x[0] * scale), 0x07060302u);     // (nothing is cut off)
     }
 }
 template <int FMT, int SEL> __device__ __forceinline__ uint32_t two_fp4_to_values(uint32_t w, float scale)
@@ -167,17 +167,6 @@ template <int FMT> __device__ __forceinline__ u32x4_t eight_fp4_to_values(uint32
 {
     return u32x4_t{two_fp4_to_values<FMT, 0>(w, scale), two_fp4_to_values<FMT, 1>(w, scale), two_fp4_to_values<FMT, 2>(w, scale), two_fp4_to_values<FMT, 3>(w, scale)};
 }
-// one element as a float, without its block's scale
-__device__ __forceinline__ float e2m1_element(uint32_t code)
-{
-    return __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 0))[0];
-}
-template <int FMT> __device__ __forceinline__ float block_factor(uint32_t byte)      // what the elements are multiplied with, as a float
-{
-    if constexpr (FMT == ZC_FMT_FP4_E2M1_MX) return byte == 0 ? 0x1p-127f : byte == 255 ? __builtin_nanf("") : __uint_as_float(byte << 23);
-    else return block_scale<FMT>(byte);
-}
-
 // ones over those of a word's elements that are infinities or NaN
 template <int FMT> __device__ __forceinline__ uint32_t nonfinite_mask(uint32_t w)
 {
@@ -191,21 +180,31 @@ template <int FMT> __device__ __forceinline__ uint32_t nonfinite_mask(uint32_t w
         return (t >> 7) * 0xFFu;
     }
 }
-// One element of a row of values as a float, 0 where it is finite: what those rows that see its token add by themselves.  FP4: 0 only
-// where the block's scale is not wild (its finite elements have been left out with the others).
-template <int FMT, int D> __device__ __forceinline__ float wild_value(const PagesDev &c, uint64_t row, uint32_t dim)
+// Four consecutive elements of a row of values (the first a multiple of four) as floats, 0 where they are finite: what those rows that see the
+// token add by themselves.  FP4: 0 only where the block's scale is not wild (its finite elements have been left out with the others).
+template <int FMT, int D> __device__ __forceinline__ f32x4 wild_values(const PagesDev &c, uint64_t row, uint32_t dim)
 {
+    f32x4 x;
     if constexpr (kFp4<FMT>) {
         const uint32_t byte = c.v_blocks[row * kRowScales<FMT, D> + dim / kBlock<FMT>];
-        const uint32_t code = c.v[row * kRowBytes<FMT, D> + dim / 2] >> (dim & 1) * 4;
-        return wild_scale<FMT>(byte) ? e2m1_element(code) * block_factor<FMT>(byte) : 0.0f;
+        const uint32_t codes = *reinterpret_cast<const uint16_t *>(c.v + row * kRowBytes<FMT, D> + dim / 2);
+        const float scale = block_scale<FMT>(byte), factor = FMT == ZC_FMT_FP4_E2M1_MX ? scale : 1.0f;
+        const f32x2 lo = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, factor, 0)), hi = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, factor, 1));
+        x = f32x4{lo[0], lo[1], hi[0], hi[1]};
+        if constexpr (FMT == ZC_FMT_FP4_E2M1_NV) x *= scale;
+        const uint32_t keep = wild_scale<FMT>(byte) ? ~0u : 0u;
+#pragma unroll
+        for (int i = 0; i < 4; i++) x[i] = __uint_as_float(bits(x[i]) & keep);
     } else {
         const uint8_t *p = c.v + row * kRowBytes<FMT, D> + dim * (kElemBits<FMT> / 8);
-        float x;
-        if constexpr (FMT == ZC_FMT_BF16) x = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(p) << 16);
-        else x = __uint_as_float(two_to_bf16<FMT, false>(*p) << 16);
-        return fabsf(x) < __builtin_inff() ? 0.0f : x;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            if constexpr (FMT == ZC_FMT_BF16) x[i] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(p)[i] << 16);
+            else x[i] = __uint_as_float(two_to_bf16<FMT, false>(p[i]) << 16);
+            x[i] = fabsf(x[i]) < __builtin_inff() ? 0.0f : x[i];
+        }
     }
+    return x;
 }
 
 // 16 tokens of a page (bytes 0: none, what is asked for is 0)

@@ -59,11 +59,18 @@ template <int FMT, int VW> __device__ __forceinline__ u32x4_t value_operand(cons
     return r;
 }
 
-// The same for FP4, dimensions 2 SEL and 2 SEL + 1: the tokens' pairs of them, converted, with the tokens in pairs instead.
-template <int FMT, int SEL> __device__ __forceinline__ void value_operands4(const uint32_t (&v)[8], const uint32_t (&scale)[8], u32x4_t &even, u32x4_t &odd)
+// The same for FP4, dimensions 2 SEL and 2 SEL + 1.  MX: every token's pair of them is converted with its scale, then the tokens are paired.  NV: the
+// tokens are paired first, four bits each to a byte (`pairs`: of even dimensions, then of odd ones), converted, and multiplied with the two scales.
+template <int FMT, int SEL> __device__ __forceinline__ void value_operands4(const uint32_t (&v)[8], const uint32_t (&scale)[8], const uint32_t (&pairs)[4][2], u32x4_t &even, u32x4_t &odd)
 {
 #pragma unroll
     for (int p = 0; p < 4; p++) {
+        if constexpr (FMT == ZC_FMT_FP4_E2M1_NV) {
+            const halfx2 s = __builtin_bit_cast(halfx2, two_to_half<ZC_FMT_FP8_E4M3, false>(scale[2 * p + 1] << 8 | scale[2 * p]));
+            even[p] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(halfx2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(pairs[p][0], 1.0f, SEL)) * s);
+            odd[p] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(halfx2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(pairs[p][1], 1.0f, SEL)) * s);
+            continue;
+        }
         const uint32_t a = two_fp4_to_values<FMT, SEL>(v[2 * p], block_scale<FMT>(scale[2 * p])), b = two_fp4_to_values<FMT, SEL>(v[2 * p + 1], block_scale<FMT>(scale[2 * p + 1]));
         even[p] = __builtin_amdgcn_perm(b, a, 0x05040100u);
         odd[p] = __builtin_amdgcn_perm(b, a, 0x07060302u);
@@ -117,7 +124,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
     }
     const Blocks blocks = seen_blocks(32, last_max, from_min, sinks);
     // this workgroup's part, in steps that all wavefronts take part in
-    const int32_t even = min((blocks.count + (int32_t)a.even - 1) / (int32_t)a.even, (int32_t)kLongPart / 32), least = (blocks.count + (int32_t)a.splits - 1) / (int32_t)a.splits;
+    const int32_t even = min((blocks.count + (int32_t)a.even - 1) / (int32_t)a.even, (int32_t)a.long_part / 32), least = (blocks.count + (int32_t)a.splits - 1) / (int32_t)a.splits;
     const int32_t per_split = (max(even, least) + (int32_t)kWaves - 1) / (int32_t)kWaves * (int32_t)kWaves;
     const int32_t begin = min((int32_t)split * per_split, blocks.count), end = min(begin + per_split, blocks.count);
     if (begin == end && !a.direct) {                     // nothing left for this part (k_attend_join does not look at what its rows would be)
@@ -330,9 +337,10 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
 #pragma unroll
                     for (int cc = 0; cc < 4; cc++) {
 #pragma unroll
-                        for (int i = 0; i < DL; i++) {
-                            const float x = wild_value<FMT, D>(a.c, stored, (g * 4 + cc) * DL + i);
-                            o[t][i][cc] += mine && x != 0.0f ? weight * x : 0.0f;
+                        for (int i = 0; i < DL; i += 4) {
+                            const f32x4 x = wild_values<FMT, D>(a.c, stored, (g * 4 + cc) * DL + i);
+#pragma unroll
+                            for (int n4 = 0; n4 < 4; n4++) o[t][i + n4][cc] += mine && x[n4] != 0.0f ? weight * x[n4] : 0.0f;
                         }
                         __builtin_amdgcn_sched_barrier(0);       // a few at a time: this hardly ever runs and is to cost no registers
                     }
@@ -340,13 +348,22 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
             }
         }
         if constexpr (kFp4<FMT>) {
+            uint32_t pairs[4][2];
+            if constexpr (FMT == ZC_FMT_FP4_E2M1_NV) {
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const uint32_t x = r.v[2 * i], y = r.v[2 * i + 1];
+                    pairs[i][0] = (x & 0x0F0F0F0Fu) | (y << 4 & 0xF0F0F0F0u);
+                    pairs[i][1] = (x >> 4 & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u);
+                }
+            }
 #pragma unroll
             for (int i = 0; i < DL; i += 2) {
                 u32x4_t even, odd;
-                if (i == 0) value_operands4<FMT, 0>(r.v, r.v_scale, even, odd);
-                else if (i == 2) value_operands4<FMT, 1>(r.v, r.v_scale, even, odd);
-                else if (i == 4) value_operands4<FMT, 2>(r.v, r.v_scale, even, odd);
-                else value_operands4<FMT, 3>(r.v, r.v_scale, even, odd);
+                if (i == 0) value_operands4<FMT, 0>(r.v, r.v_scale, pairs, even, odd);
+                else if (i == 2) value_operands4<FMT, 1>(r.v, r.v_scale, pairs, even, odd);
+                else if (i == 4) value_operands4<FMT, 2>(r.v, r.v_scale, pairs, even, odd);
+                else value_operands4<FMT, 3>(r.v, r.v_scale, pairs, even, odd);
 #pragma unroll
                 for (int t = 0; t < QT; t++) {
                     o[t][i] = mma16_values<FMT>(even, p[t], o[t][i]);

@@ -6,55 +6,73 @@ namespace zc {
 
 namespace {
 
-// A row is D / 8 lanes, eight elements to each, so a workgroup takes 2,048 / D tokens of one head, K and V.
+// A row is D / 8 lanes, eight elements to each, so a workgroup takes 2,048 / D tokens of one head, K and V, at a time, and that P times over.
 template <int D> constexpr uint32_t kLanes = D / 8;
 template <int D> constexpr uint32_t kTokens = 256 / kLanes<D>;
 
-// where the lane's row lies: its (sequence, head), its number in the pools; ours: the token is a sequence's; there: so is its page
+// where a lane's row lies: its (sequence, head), its number in the pools; ours: the token is a sequence's; there: so is its page
 struct Place { uint32_t unit; uint64_t row; bool ours, there; };
 
-template <int D> __device__ __forceinline__ Place place_of(const RowsDev &r, uint32_t head, int32_t token)
+// the places of the lane's tokens, the P of which are kTokens apart
+template <int D, int P> __device__ __forceinline__ void find_places(const RowsDev &r, uint32_t head, int32_t token, Place (&p)[P])
 {
     const int32_t n = (int32_t)r.n_tokens;
-    Place p = {0, 0, false, false};
-    int32_t seq = token, before = 1;                           // tokens of the sequence from this one on
+    int32_t seq[P], before[P];                                 // tokens of the sequence from this one on
+#pragma unroll
+    for (int i = 0; i < P; i++) {
+        seq[i] = token + i * (int32_t)kTokens<D>;
+        before[i] = 1;
+    }
     if (r.q_start) {
         // the last sequence that begins at or before the token: the wavefront's tokens are counted against 64 beginnings at a time (a
         // binary search would wait for each of its steps)
         constexpr int kEach = 64 / (int)kLanes<D>;
         const uint32_t lane = threadIdx.x & 63;
         const int32_t first = __builtin_amdgcn_readfirstlane(token);
-        seq = -1;
+#pragma unroll
+        for (int i = 0; i < P; i++) seq[i] = -1;
         if (r.n_seqs <= 1024) {
             for (uint32_t c = 0; c < r.n_seqs; c += 64) {
                 const int32_t begin = c + lane < r.n_seqs ? r.q_start[c + lane] : INT32_MAX;
 #pragma unroll
-                for (int j = 0; j < kEach; j++) {
-                    const int32_t count = (int32_t)__popcll(__ballot(begin <= first + j));
-                    seq += token == first + j ? count : 0;
-                }
+                for (int i = 0; i < P; i++)
+#pragma unroll
+                    for (int j = 0; j < kEach; j++) {
+                        const int32_t count = (int32_t)__popcll(__ballot(begin <= first + i * (int32_t)kTokens<D> + j));
+                        seq[i] += token == first + j ? count : 0;
+                    }
             }
         } else {
-            int32_t lo = -1, hi = (int32_t)r.n_seqs;
-            while (hi - lo > 1) {
-                const int32_t mid = (lo + hi) / 2;
-                if (r.q_start[mid] <= token) lo = mid; else hi = mid;
+#pragma unroll
+            for (int i = 0; i < P; i++) {
+                int32_t lo = -1, hi = (int32_t)r.n_seqs;
+                while (hi - lo > 1) {
+                    const int32_t mid = (lo + hi) / 2;
+                    if (r.q_start[mid] <= token + i * (int32_t)kTokens<D>) lo = mid; else hi = mid;
+                }
+                seq[i] = lo;
             }
-            seq = lo;
         }
-        if (seq >= 0) before = min(max(r.q_start[seq + 1], 0), n) - token;
+#pragma unroll
+        for (int i = 0; i < P; i++) before[i] = seq[i] >= 0 ? min(max(r.q_start[seq[i] + 1], 0), n) - (token + i * (int32_t)kTokens<D>) : 0;
     }
-    p.ours = token < n && seq >= 0 && before > 0;
-    if (!p.ours) return p;
-    // (a length may be any number: differences of two are taken in 64 bits)
-    const int64_t position = (int64_t)max(r.c.lengths[seq], 0) - before;
-    p.unit = (uint32_t)seq * r.c.heads + head;
-    if (position < 0 || position >= r.c.capacity) return p;
-    const uint32_t at = (uint32_t)position;
-    const int32_t page = r.c.table[(uint64_t)p.unit * r.c.table_pages + (at >> r.c.page_shift)];
-    p.there = (uint32_t)page < r.c.n_pages;
-    p.row = ((uint64_t)(uint32_t)page << r.c.page_shift) + (at & ((1u << r.c.page_shift) - 1));
-    return p;
+    int64_t position[P];
+#pragma unroll
+    for (int i = 0; i < P; i++) {
+        p[i] = Place{0, 0, token + i * (int32_t)kTokens<D> < n && before[i] > 0, false};
+        position[i] = -1;
+        // (a length may be any number: differences of two are taken in 64 bits)
+        if (p[i].ours) position[i] = (int64_t)max(r.c.lengths[seq[i]], 0) - before[i];
+        p[i].unit = p[i].ours ? (uint32_t)seq[i] * r.c.heads + head : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < P; i++) {
+        if (position[i] < 0 || position[i] >= r.c.capacity) continue;
+        const uint32_t at = (uint32_t)position[i];
+        const int32_t page = r.c.table[(uint64_t)p[i].unit * r.c.table_pages + (at >> r.c.page_shift)];
+        p[i].there = (uint32_t)page < r.c.n_pages;
+        p[i].row = ((uint64_t)(uint32_t)page << r.c.page_shift) + (at & ((1u << r.c.page_shift) - 1));
+    }
 }
 
 // the largest of the lanes of a group of 2 or 4
@@ -68,6 +86,44 @@ template <int GROUP> __device__ __forceinline__ uint32_t max_over_group(uint32_t
 __device__ __forceinline__ float clamped(float x, float most) { return x != x ? x : fminf(fmaxf(x, -most), most); }
 
 constexpr uint32_t kInf = 0x7F800000u;
+
+__device__ __forceinline__ void floats_of_bf16(const u32x4_t &w, float (&y)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        y[2 * i] = __uint_as_float(w[i] << 16);
+        y[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+
+// y / s by one reciprocal of s (a normal number, its reciprocal too): the product's remainder, which the fused operation has exactly, corrects it, so
+// that a quotient of 24 bits comes out as it is: those half way between neighbours, which decide roundings, have few bits.
+__device__ __forceinline__ float quotient(float y, float s, float reciprocal)
+{
+    const float q = y * reciprocal;
+    return __builtin_fmaf(-__builtin_fmaf(q, s, -y), reciprocal, q);           // (this way round 0 keeps its sign where s is positive)
+}
+__device__ __forceinline__ float reciprocal_of(float s)
+{
+    const float x = __builtin_amdgcn_rcpf(s);
+    return __builtin_fmaf(__builtin_fmaf(-x, s, 1.0f), x, x);
+}
+
+// divided by the scale of sequence and head; 0 where that is 0
+template <int FMT> __device__ __forceinline__ void divide(float (&y)[8], float s)
+{
+    if (FMT != ZC_FMT_BF16 && __builtin_expect(fabsf(s) >= 0x1p-120f && fabsf(s) <= 0x1p120f, 1)) {
+        const float reciprocal = reciprocal_of(s);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float q = y[i] * reciprocal, better = quotient(y[i], s, reciprocal);
+            y[i] = __builtin_amdgcn_classf(q, 0x198) ? better : q;     // (a product other than 0, infinite or none)
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) y[i] = s == 0.0f ? 0.0f : y[i] / s;
+    }
+}
 
 // eight FP4 elements of y / scale, rounded to the nearest, ties to even, the largest where they are beyond it (`scale`: a power of two)
 __device__ __forceinline__ uint32_t eight_to_fp4(const float (&y)[8], float scale)
@@ -114,10 +170,10 @@ template <int FMT> __device__ __forceinline__ u32x4_t quantised(float (&y)[8], u
         } else {
             const float largest = fminf(__uint_as_float(top), 6.0f * 448.0f);
             scale = nan ? 0x7Fu : (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(largest / 6.0f, 0.0f, 0, false) & 0xFFu;
-            const float s = block_scale<FMT>(scale);
+            const float s = block_scale<FMT>(scale), reciprocal = reciprocal_of(s);
 #pragma unroll
-            for (int i = 0; i < 8; i++) y[i] = s == 0.0f ? 0.0f : y[i] / s;
-            w[0] = nan ? 0u : eight_to_fp4(y, 1.0f);
+            for (int i = 0; i < 8; i++) y[i] = quotient(__builtin_amdgcn_fmed3f(y[i], -0x1p20f, 0x1p20f), s, reciprocal);      // (6 times the largest scale is less than 2^12)
+            w[0] = nan || s == 0.0f ? 0u : eight_to_fp4(y, 1.0f);
         }
     }
     return w;
@@ -142,106 +198,111 @@ template <int FMT> __device__ __forceinline__ u32x4_t load_eight(const uint8_t *
     return w;
 }
 
+// Results that are more than the caches hold go past them.
+template <int P> __device__ __forceinline__ void store_result(uint16_t *to, const u32x4_t &w)
+{
+    u32x4_t *x = reinterpret_cast<u32x4_t *>(to);
+    if constexpr (P > 1) __builtin_nontemporal_store(w, x);
+    else *x = w;
+}
+
 // Every element is divided by the scale of its sequence and head (0: all become 0), rounded to the nearest, ties to even, the largest number where it is
 // beyond that.  NaN stays one; in an FP4 block it makes the block's scale NaN.
-template <int FMT, int D>
+template <int FMT, int D, int P>
 __global__ __launch_bounds__(256) void k_kv_write(RowsDev r)
 {
     const uint32_t head = blockIdx.x % r.c.heads, sub = threadIdx.x % kLanes<D>;
-    const int32_t token = (int32_t)(blockIdx.x / r.c.heads * kTokens<D> + threadIdx.x / kLanes<D>);
-    const uint64_t t = (uint64_t)min(token, (int32_t)r.n_tokens - 1);
-    u32x4_t x[2];
-    x[0] = *reinterpret_cast<const u32x4_t *>(r.k + t * r.k_token_stride + (uint64_t)head * r.k_head_stride + sub * 8);
-    x[1] = *reinterpret_cast<const u32x4_t *>(r.v + t * r.v_token_stride + (uint64_t)head * r.v_head_stride + sub * 8);
-    const Place p = place_of<D>(r, head, token);
+    const int32_t token = (int32_t)(blockIdx.x / r.c.heads * (P * kTokens<D>) + threadIdx.x / kLanes<D>);
+    u32x4_t x[P][2];
 #pragma unroll
-    for (int kv = 0; kv < 2; kv++) {
-        const float *scales = kv ? r.c.v_scales : r.c.k_scales;
-        float y[8];
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            y[2 * i] = __uint_as_float(x[kv][i] << 16);
-            y[2 * i + 1] = __uint_as_float(x[kv][i] & 0xFFFF0000u);
-        }
-        if (scales) {
-            const float s = scales[p.unit];
-#pragma unroll
-            for (int i = 0; i < 8; i++) y[i] = s == 0.0f ? 0.0f : y[i] / s;
-        }
-        uint32_t scale = 0;
-        u32x4_t w = quantised<FMT>(y, scale);
-        if constexpr (FMT == ZC_FMT_BF16) {
-            if (!scales) w = x[kv];                            // bit for bit
-        }
-        if (!p.there) continue;
-        store_eight<FMT>((kv ? r.v_pages : r.k_pages) + p.row * kRowBytes<FMT, D> + sub * kElemBits<FMT>, w);
-        if constexpr (kFp4<FMT>) {
-            constexpr uint32_t kGroup = kBlock<FMT> / 8;
-            if (sub % kGroup == 0) (kv ? r.v_scale_pages : r.k_scale_pages)[p.row * kRowScales<FMT, D> + sub / kGroup] = (uint8_t)scale;
-        }
+    for (int i = 0; i < P; i++) {
+        const uint64_t t = (uint64_t)min(token + i * (int32_t)kTokens<D>, (int32_t)r.n_tokens - 1);
+        x[i][0] = *reinterpret_cast<const u32x4_t *>(r.k + t * r.k_token_stride + (uint64_t)head * r.k_head_stride + sub * 8);
+        x[i][1] = *reinterpret_cast<const u32x4_t *>(r.v + t * r.v_token_stride + (uint64_t)head * r.v_head_stride + sub * 8);
     }
+    Place p[P];
+    find_places<D, P>(r, head, token, p);
+#pragma unroll
+    for (int i = 0; i < P; i++)
+#pragma unroll
+        for (int kv = 0; kv < 2; kv++) {
+            const float *scales = kv ? r.c.v_scales : r.c.k_scales;
+            float y[8];
+            floats_of_bf16(x[i][kv], y);
+            if (scales) divide<FMT>(y, scales[p[i].unit]);
+            uint32_t scale = 0;
+            u32x4_t w = quantised<FMT>(y, scale);
+            if constexpr (FMT == ZC_FMT_BF16) {
+                if (!scales) w = x[i][kv];                     // bit for bit
+            }
+            if (!p[i].there) continue;
+            store_eight<FMT>((kv ? r.v_pages : r.k_pages) + p[i].row * kRowBytes<FMT, D> + sub * kElemBits<FMT>, w);
+            if constexpr (kFp4<FMT>) {
+                constexpr uint32_t kGroup = kBlock<FMT> / 8;
+                if (sub % kGroup == 0) (kv ? r.v_scale_pages : r.k_scale_pages)[p[i].row * kRowScales<FMT, D> + sub / kGroup] = (uint8_t)scale;
+            }
+        }
 }
 
 // Element times its block's scale times that of its sequence and head, in 32 bits, rounded to BF16; 0 where the token's page is absent.
-template <int FMT, int D>
+template <int FMT, int D, int P>
 __global__ __launch_bounds__(256) void k_kv_read(RowsDev r)
 {
     const uint32_t head = blockIdx.x % r.c.heads, sub = threadIdx.x % kLanes<D>;
-    const int32_t token = (int32_t)(blockIdx.x / r.c.heads * kTokens<D> + threadIdx.x / kLanes<D>);
-    const Place p = place_of<D>(r, head, token);
-    if (!p.ours) return;
-    u32x4_t w[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-    uint32_t block[2] = {0, 0};
-    if (p.there) {
+    const int32_t token = (int32_t)(blockIdx.x / r.c.heads * (P * kTokens<D>) + threadIdx.x / kLanes<D>);
+    Place p[P];
+    find_places<D, P>(r, head, token, p);
+    u32x4_t w[P][2];
+    uint32_t block[P][2];
+    float s[P][2];
+#pragma unroll
+    for (int i = 0; i < P; i++)
 #pragma unroll
         for (int kv = 0; kv < 2; kv++) {
-            w[kv] = load_eight<FMT>((kv ? r.c.v : r.c.k) + p.row * kRowBytes<FMT, D> + sub * kElemBits<FMT>);
-            if constexpr (kFp4<FMT>) block[kv] = (kv ? r.c.v_blocks : r.c.k_blocks)[p.row * kRowScales<FMT, D> + sub / (kBlock<FMT> / 8)];
+            w[i][kv] = u32x4_t{0, 0, 0, 0};
+            block[i][kv] = 0;
+            s[i][kv] = 1.0f;
+            if (!p[i].there) continue;
+            w[i][kv] = load_eight<FMT>((kv ? r.c.v : r.c.k) + p[i].row * kRowBytes<FMT, D> + sub * kElemBits<FMT>);
+            if constexpr (kFp4<FMT>) block[i][kv] = (kv ? r.c.v_blocks : r.c.k_blocks)[p[i].row * kRowScales<FMT, D> + sub / (kBlock<FMT> / 8)];
+            const float *scales = kv ? r.c.v_scales : r.c.k_scales;
+            if (scales) s[i][kv] = scales[p[i].unit];
         }
-    }
 #pragma unroll
-    for (int kv = 0; kv < 2; kv++) {
-        const float *scales = kv ? r.c.v_scales : r.c.k_scales;
-        const float s = scales && p.there ? scales[p.unit] : 1.0f;
-        float y[8];
-        if constexpr (FMT == ZC_FMT_BF16) {
+    for (int i = 0; i < P; i++) {
+        if (!p[i].ours) continue;
+        const uint64_t t = (uint64_t)(token + i * (int32_t)kTokens<D>);
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                y[2 * i] = __uint_as_float(w[kv][i] << 16);
-                y[2 * i + 1] = __uint_as_float(w[kv][i] & 0xFFFF0000u);
+        for (int kv = 0; kv < 2; kv++) {
+            u32x4_t b;
+            if constexpr (FMT == ZC_FMT_BF16) b = w[i][kv];
+            else if constexpr (!kFp4<FMT>) b = eight_to_bf16<FMT>(w[i][kv][0], w[i][kv][1]);
+            else b = eight_fp4_to_bf16<FMT>(w[i][kv][0], block_scale<FMT>(block[i][kv]));
+            if (kv ? r.c.v_scales : r.c.k_scales) {            // (numbers as stored are exact in BF16: rounded once)
+                float y[8];
+                floats_of_bf16(b, y);
+#pragma unroll
+                for (int j = 0; j < 4; j++) b[j] = pack_bf16(y[2 * j] * s[i][kv], y[2 * j + 1] * s[i][kv]);
             }
-        } else if constexpr (!kFp4<FMT>) {
-            const u32x4_t b = eight_to_bf16<FMT>(w[kv][0], w[kv][1]);
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                y[2 * i] = __uint_as_float(b[i] << 16);
-                y[2 * i + 1] = __uint_as_float(b[i] & 0xFFFF0000u);
-            }
-        } else {
-            const u32x4_t b = eight_fp4_to_bf16<FMT>(w[kv][0], block_scale<FMT>(block[kv]));
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                y[2 * i] = __uint_as_float(b[i] << 16);
-                y[2 * i + 1] = __uint_as_float(b[i] & 0xFFFF0000u);
-            }
+            uint16_t *to = kv ? r.v + t * r.v_token_stride + (uint64_t)head * r.v_head_stride : r.k + t * r.k_token_stride + (uint64_t)head * r.k_head_stride;
+            store_result<P>(to + sub * 8, b);
         }
-        u32x4_t out;
-#pragma unroll
-        for (int i = 0; i < 4; i++) out[i] = pack_bf16(y[2 * i] * s, y[2 * i + 1] * s);
-        if constexpr (FMT == ZC_FMT_BF16) {
-            if (!scales) out = w[kv];
-        }
-        uint16_t *to = kv ? r.v + (uint64_t)token * r.v_token_stride + (uint64_t)head * r.v_head_stride : r.k + (uint64_t)token * r.k_token_stride + (uint64_t)head * r.k_head_stride;
-        *reinterpret_cast<u32x4_t *>(to + sub * 8) = out;
     }
 }
 
+// Calls whose workgroups fill the GPU (eight to a compute unit) take four times as many tokens to each.
+template <int FMT, int D, bool WRITE, int P> int launch_of(const RowsDev &r, hipStream_t s)
+{
+    constexpr uint32_t kEach = P * kTokens<D>;
+    const dim3 blocks((r.n_tokens + kEach - 1) / kEach * r.c.heads);
+    if constexpr (WRITE) hipLaunchKernelGGL((k_kv_write<FMT, D, P>), blocks, dim3(256), 0, s, r);
+    else hipLaunchKernelGGL((k_kv_read<FMT, D, P>), blocks, dim3(256), 0, s, r);
+    return (int)hipGetLastError();
+}
 template <int FMT, int D, bool WRITE> int launch(const RowsDev &r, hipStream_t s)
 {
-    const dim3 blocks((r.n_tokens + kTokens<D> - 1) / kTokens<D> * r.c.heads);
-    if constexpr (WRITE) hipLaunchKernelGGL((k_kv_write<FMT, D>), blocks, dim3(256), 0, s, r);
-    else hipLaunchKernelGGL((k_kv_read<FMT, D>), blocks, dim3(256), 0, s, r);
-    return (int)hipGetLastError();
+    const uint64_t blocks = ((uint64_t)r.n_tokens + kTokens<D> - 1) / kTokens<D> * r.c.heads;
+    return blocks >= 2048 ? launch_of<FMT, D, WRITE, 4>(r, s) : launch_of<FMT, D, WRITE, 1>(r, s);
 }
 template <int FMT, bool WRITE> int launch(const RowsDev &r, uint32_t head_dim, hipStream_t s)
 {
