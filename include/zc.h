@@ -426,7 +426,8 @@ typedef struct {
     const int32_t *d_q_start;
 } zc_kv_rows;
 
-/* Quantises rows into the cache's pages.  With S the scale of the sequence and head (NULL: 1), y = x / S in 32 bits (0 where S is 0) is stored
+/* Quantises rows into the cache's pages.  With S the scale of the sequence and head (NULL: 1), y = x * (1 / S) in 32 bits (1 / S at most the largest
+ * number; 0 where S is 0) is stored
  *   BF16, FP8   rounded to the nearest number, ties to even;
  *   FP4, MX     with e = floor(log2 m) - 2 (at least -127) of the block's largest magnitude m, E8M0 scale 2^e (m = 0: 2^-127), elements y / 2^e rounded likewise;
  *   FP4, NV     with the block's E4M3 scale s = m / 6 in 32 bits, rounded likewise (at most 448), elements y / s (0 where s is 0).

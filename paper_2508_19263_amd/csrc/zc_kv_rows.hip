@@ -75,17 +75,25 @@ template <int D, int P> __device__ __forceinline__ void find_places(const RowsDe
     }
 }
 
-// the largest of the lanes of a group of 2 or 4
-template <int GROUP> __device__ __forceinline__ uint32_t max_over_group(uint32_t x)
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+// the larger of two words' halves, each
+__device__ __forceinline__ uint32_t max_of_halves(uint32_t x, uint32_t y)
 {
-    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, false));                        // lanes 1 0 3 2 of every four
-    if constexpr (GROUP == 4) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, false));   // 2 3 0 1
-    return x;
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y)));
+}
+// The largest magnitude of the eight BF16 elements of each lane of a group of 2 or 4, as an integer: NaN above infinity above all numbers.
+template <int GROUP> __device__ __forceinline__ uint32_t largest_of_group(const u32x4_t &w)
+{
+    constexpr uint32_t kMagnitudes = 0x7FFF7FFFu;
+    uint32_t x = max_of_halves(max_of_halves(w[0] & kMagnitudes, w[1] & kMagnitudes), max_of_halves(w[2] & kMagnitudes, w[3] & kMagnitudes));
+    x = max_of_halves(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, false));                        // lanes 1 0 3 2 of every four
+    if constexpr (GROUP == 4) x = max_of_halves(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, false));   // 2 3 0 1
+    return max(x >> 16, x & 0xFFFFu);
 }
 
-__device__ __forceinline__ float clamped(float x, float most) { return x != x ? x : fminf(fmaxf(x, -most), most); }
-
-constexpr uint32_t kInf = 0x7F800000u;
+constexpr uint32_t kInf16 = 0x7F80u;
+constexpr float kLargest = 0x1.fffffep127f;
 
 __device__ __forceinline__ void floats_of_bf16(const u32x4_t &w, float (&y)[8])
 {
@@ -96,34 +104,19 @@ __device__ __forceinline__ void floats_of_bf16(const u32x4_t &w, float (&y)[8])
     }
 }
 
-// y / s by one reciprocal of s (a normal number, its reciprocal too): the product's remainder, which the fused operation has exactly, corrects it, so
-// that a quotient of 24 bits comes out as it is: those half way between neighbours, which decide roundings, have few bits.
+// y / s by one reciprocal of s (the scales of NV blocks, 2^-9 to 448): the product's remainder, which the fused operation has exactly, corrects it,
+// so that a quotient of few bits, as those half way between neighbours are, comes out as it is.
 __device__ __forceinline__ float quotient(float y, float s, float reciprocal)
 {
     const float q = y * reciprocal;
-    return __builtin_fmaf(-__builtin_fmaf(q, s, -y), reciprocal, q);           // (this way round 0 keeps its sign where s is positive)
+    return __builtin_fmaf(-__builtin_fmaf(q, s, -y), reciprocal, q);           // (this way round 0 keeps its sign)
 }
 __device__ __forceinline__ float reciprocal_of(float s)
 {
     const float x = __builtin_amdgcn_rcpf(s);
     return __builtin_fmaf(__builtin_fmaf(-x, s, 1.0f), x, x);
 }
-
-// divided by the scale of sequence and head; 0 where that is 0
-template <int FMT> __device__ __forceinline__ void divide(float (&y)[8], float s)
-{
-    if (FMT != ZC_FMT_BF16 && __builtin_expect(fabsf(s) >= 0x1p-120f && fabsf(s) <= 0x1p120f, 1)) {
-        const float reciprocal = reciprocal_of(s);
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const float q = y[i] * reciprocal, better = quotient(y[i], s, reciprocal);
-            y[i] = __builtin_amdgcn_classf(q, 0x198) ? better : q;     // (a product other than 0, infinite or none)
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; i++) y[i] = s == 0.0f ? 0.0f : y[i] / s;
-    }
-}
+__device__ __forceinline__ float clamped(float x, float most) { return x != x ? x : fminf(fmaxf(x, -most), most); }
 
 // eight FP4 elements of y / scale, rounded to the nearest, ties to even, the largest where they are beyond it (`scale`: a power of two)
 __device__ __forceinline__ uint32_t eight_to_fp4(const float (&y)[8], float scale)
@@ -134,11 +127,30 @@ __device__ __forceinline__ uint32_t eight_to_fp4(const float (&y)[8], float scal
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], scale, 2);
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], scale, 3);
 }
+// (an element of a vector goes to a variable first: the compiler takes a bit cast of the element itself as that of the first one)
+__device__ __forceinline__ bf16x2 bf16_pair(uint32_t w) { return __builtin_bit_cast(bf16x2, w); }
+__device__ __forceinline__ uint32_t eight_to_fp4(const u32x4_t &x, float scale)
+{
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, bf16_pair(x[0]), scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, bf16_pair(x[1]), scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, bf16_pair(x[2]), scale, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, bf16_pair(x[3]), scale, 3);
+}
 
-// y as stored; scale: FP4, the block's
-template <int FMT> __device__ __forceinline__ u32x4_t quantised(float (&y)[8], uint32_t &scale)
+// What eight BF16 elements times `factor` (if `times`) are stored as; scale: FP4, the block's.
+template <int FMT> __device__ __forceinline__ u32x4_t quantised(const u32x4_t &x, bool times, float factor, uint32_t &scale)
 {
     u32x4_t w = {0, 0, 0, 0};
+    if constexpr (FMT == ZC_FMT_BF16) {
+        if (!times) return x;
+    }
+    float y[8];
+    floats_of_bf16(x, y);
+    if (times) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) y[i] *= factor;
+    }
     if constexpr (FMT == ZC_FMT_BF16) {
 #pragma unroll
         for (int i = 0; i < 4; i++) w[i] = pack_bf16(y[2 * i], y[2 * i + 1]);
@@ -157,22 +169,25 @@ template <int FMT> __device__ __forceinline__ u32x4_t quantised(float (&y)[8], u
             }
         }
     } else {
-        uint32_t top = 0;                                      // magnitudes as integers: NaN above infinity above all numbers
-#pragma unroll
-        for (int i = 0; i < 8; i++) top = max(top, bits(y[i]) & 0x7FFFFFFFu);
-        top = max_over_group<kBlock<FMT> / 8>(top);
-        const bool nan = top > kInf;
+        const uint32_t top = largest_of_group<kBlock<FMT> / 8>(x);
+        // (the largest magnitude's product is the products' largest magnitude)
+        float largest = __uint_as_float(top << 16);
+        if (times) largest = fabsf(largest * factor);
+        const bool nan = top > kInf16 || largest != largest;
         if constexpr (FMT == ZC_FMT_FP4_E2M1_MX) {
             // 2^(floor(log2 of the largest) - 2); an infinity counts as the largest number
-            const int32_t e = (int32_t)min(top >> 23, 254u) - 2;
+            const int32_t e = (int32_t)min(bits(largest) >> 23, 254u) - 2;
             scale = nan ? 255u : (uint32_t)max(e, 0);
-            w[0] = nan ? 0u : eight_to_fp4(y, block_scale<FMT>(scale));
+            w[0] = nan ? 0u : times ? eight_to_fp4(y, block_scale<FMT>(scale)) : eight_to_fp4(x, block_scale<FMT>(scale));
         } else {
-            const float largest = fminf(__uint_as_float(top), 6.0f * 448.0f);
-            scale = nan ? 0x7Fu : (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(largest / 6.0f, 0.0f, 0, false) & 0xFFu;
+            scale = nan ? 0x7Fu : (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(fminf(largest, 6.0f * 448.0f) / 6.0f, 0.0f, 0, false) & 0xFFu;
+            if (__builtin_expect(__any(largest > 0x1p60f), 0)) {       // (whose quotients would not be finite: 6 times the largest scale is less than 2^12)
+#pragma unroll
+                for (int i = 0; i < 8; i++) y[i] = __builtin_amdgcn_fmed3f(y[i], -0x1p20f, 0x1p20f);
+            }
             const float s = block_scale<FMT>(scale), reciprocal = reciprocal_of(s);
 #pragma unroll
-            for (int i = 0; i < 8; i++) y[i] = quotient(__builtin_amdgcn_fmed3f(y[i], -0x1p20f, 0x1p20f), s, reciprocal);      // (6 times the largest scale is less than 2^12)
+            for (int i = 0; i < 8; i++) y[i] = quotient(y[i], s, reciprocal);
             w[0] = nan || s == 0.0f ? 0u : eight_to_fp4(y, 1.0f);
         }
     }
@@ -206,7 +221,7 @@ template <int P> __device__ __forceinline__ void store_result(uint16_t *to, cons
     else *x = w;
 }
 
-// Every element is divided by the scale of its sequence and head (0: all become 0), rounded to the nearest, ties to even, the largest number where it is
+// Every element is multiplied with the reciprocal of the scale of its sequence and head (at most the largest number; where the scale is 0, all become 0), rounded to the nearest, ties to even, the largest number where it is
 // beyond that.  NaN stays one; in an FP4 block it makes the block's scale NaN.
 template <int FMT, int D, int P>
 __global__ __launch_bounds__(256) void k_kv_write(RowsDev r)
@@ -227,14 +242,17 @@ __global__ __launch_bounds__(256) void k_kv_write(RowsDev r)
 #pragma unroll
         for (int kv = 0; kv < 2; kv++) {
             const float *scales = kv ? r.c.v_scales : r.c.k_scales;
-            float y[8];
-            floats_of_bf16(x[i][kv], y);
-            if (scales) divide<FMT>(y, scales[p[i].unit]);
-            uint32_t scale = 0;
-            u32x4_t w = quantised<FMT>(y, scale);
-            if constexpr (FMT == ZC_FMT_BF16) {
-                if (!scales) w = x[i][kv];                     // bit for bit
+            float factor = 1.0f;
+            if (scales) {
+                const float divisor = scales[p[i].unit];
+                factor = clamped(1.0f / divisor, kLargest);
+                if (divisor == 0.0f) {
+                    factor = 1.0f;
+                    x[i][kv] = u32x4_t{0, 0, 0, 0};
+                }
             }
+            uint32_t scale = 0;
+            const u32x4_t w = quantised<FMT>(x[i][kv], scales != nullptr, factor, scale);
             if (!p[i].there) continue;
             store_eight<FMT>((kv ? r.v_pages : r.k_pages) + p[i].row * kRowBytes<FMT, D> + sub * kElemBits<FMT>, w);
             if constexpr (kFp4<FMT>) {

@@ -545,28 +545,34 @@ def _check_numbers(what, **numbers):
             raise ValueError("%s: %s has to be in 0 .. 2^32 - 1, not %d" % (what, name, x))
 
 
-def _kv_rows(what, call, k, v, cache, q_start, written):
-    n = k.shape[0]
+def _kv_rows(what, call, k, v, cache, q_start, results):
+    """results: tensors of the caller's that are written to, 0 to 2 of (k, v)."""
+    shape, heads, dim = k.shape, cache.n_heads, cache.head_dim
+    n = shape[0] if len(shape) == 3 else 0
     for name, t in (("k", k), ("v", v)):
-        if t.dim() != 3 or tuple(t.shape) != (n, cache.n_heads, cache.head_dim) or t.stride(2) != 1 or t.dtype not in _ROW_TYPES:
+        if t.shape != (n, heads, dim) or t.stride(2) != 1 or t.dtype not in _ROW_TYPES:
             raise ValueError("%s: %s has to be [n_tokens, n_heads, head_dim] in BF16 with contiguous rows" % (what, name))
-        if not written:
-            reach = cache.head_dim                               # elements from a row's first to the next free one
-            for stride, size in sorted(zip(t.stride()[:2], t.shape[:2])):
-                if size > 1 and stride < reach:
-                    raise ValueError("%s: rows of %s overlap" % (what, name))
-                reach += stride * (size - 1) if size > 1 else 0
-        if t.requires_grad and torch.is_grad_enabled():
-            raise ValueError("%s: there is no gradient through a stored cache: detach %s, or call it under torch.no_grad()" % (what, name))
-    if q_start is None and n != cache.n_seqs:
-        raise ValueError("%s: without q_start there is one token per sequence" % what)
-    if q_start is not None and (q_start.dtype != torch.int32 or q_start.numel() != cache.n_seqs + 1 or not q_start.is_contiguous()):
+    for t in results:
+        reach = dim                                              # elements from a row's first to the next free one
+        for stride, size in sorted(zip(t.stride()[:2], shape)):
+            if size > 1 and stride < reach:
+                raise ValueError("%s: rows of %s overlap" % (what, "k" if t is k else "v"))
+            reach += stride * (size - 1) if size > 1 else 0
+    if (k.requires_grad or v.requires_grad) and torch.is_grad_enabled():
+        raise ValueError("%s: there is no gradient through a stored cache: detach k and v, or call it under torch.no_grad()" % what)
+    if q_start is None:
+        if n != cache.n_seqs:
+            raise ValueError("%s: without q_start there is one token per sequence" % what)
+    elif q_start.dtype != torch.int32 or q_start.numel() != cache.n_seqs + 1 or not q_start.is_contiguous():
         raise ValueError("%s: q_start has to be contiguous int32 of n_seqs + 1 entries" % what)
     device, current = k.device, torch._C._cuda_getDevice() if k.is_cuda else -1       # (the kernels go to the current GPU's stream)
     if device.index != current or cache.device != device or v.device != device or (q_start is not None and q_start.device != device):
         raise ValueError("%s: tensors have to be on one GPU, the current one" % what)
-    strides = [0 if size == 1 else stride for t in (k, v) for size, stride in zip(t.shape[:2], t.stride())]     # (of one element: any number)
-    a = KvRows(_KV_ROWS_BYTES, n, k.data_ptr(), v.data_ptr(), *strides, None if q_start is None else q_start.data_ptr())
+    (kt, kh, _), (vt, vh, _) = k.stride(), v.stride()
+    if n == 1 or heads == 1:                                     # the stride of a dimension of one element is any number
+        kt, vt = (0, 0) if n == 1 else (kt, vt)
+        kh, vh = (0, 0) if heads == 1 else (kh, vh)
+    a = KvRows(_KV_ROWS_BYTES, n, k.data_ptr(), v.data_ptr(), kt, kh, vt, vh, None if q_start is None else q_start.data_ptr())
     st = call(C.byref(a), cache.ref, torch._C._cuda_getCurrentRawStream(current))
     if st != OK:
         raise ZcError(st, what)
@@ -578,7 +584,7 @@ def write_kv(k, v, cache, q_start=None):
 
     q_start: int32 [n_seqs + 1], where each sequence's tokens begin (None: one token per sequence).  FP8: divided by the cache's
     scales, the largest number where they are beyond it; FP4: with a scale for every block, which is written to k_blocks and v_blocks."""
-    _kv_rows("zc_kv_write", lib().zc_kv_write, k, v, cache, q_start, True)
+    _kv_rows("zc_kv_write", lib().zc_kv_write, k, v, cache, q_start, ())
 
 
 def read_kv(cache, q_start=None, n_tokens=None, k=None, v=None):
@@ -591,10 +597,15 @@ def read_kv(cache, q_start=None, n_tokens=None, k=None, v=None):
         if k is None and v is None and q_start is not None:
             raise ValueError("zc_kv_read: with q_start, n_tokens says how many rows there are")
     _check_numbers("zc_kv_read", n_tokens=n_tokens)
-    k, v = (torch.empty((n_tokens, cache.n_heads, cache.head_dim), dtype=torch.bfloat16, device=cache.device) if t is None else t for t in (k, v))
-    if k.shape[0] != n_tokens:
+    results = [t for t in (k, v) if t is not None]
+    size = (n_tokens, cache.n_heads, cache.head_dim)
+    if k is None:
+        k = torch.empty(size, dtype=torch.bfloat16, device=cache.device)
+    elif k.shape[0] != n_tokens:
         raise ValueError("zc_kv_read: k has to be [n_tokens, n_heads, head_dim] in BF16 with contiguous rows")
-    _kv_rows("zc_kv_read", lib().zc_kv_read, k, v, cache, q_start, False)
+    if v is None:
+        v = torch.empty(size, dtype=torch.bfloat16, device=cache.device)
+    _kv_rows("zc_kv_read", lib().zc_kv_read, k, v, cache, q_start, results)
     return k, v
 
 

@@ -88,7 +88,8 @@ def expected(pages, k, v, q_lens, first=0):
             y = x[t].to(torch.float32)
             if pages.scales[name] is not None:
                 scale = pages.scales[name][s].unsqueeze(1)
-                y = torch.where(scale == 0, torch.zeros_like(y), y / scale)
+                most = torch.finfo(torch.float32).max
+                y = torch.where(scale == 0, torch.zeros_like(y), y * (1.0 / scale).clamp(-most, most))
             bits, blocks = quantised(y, pages.fmt)
             if pages.fmt == BF16 and pages.scales[name] is None:
                 bits = x[t].view(torch.int16)
