@@ -13,65 +13,79 @@ template <int D> constexpr uint32_t kTokens = 256 / kLanes<D>;
 // where a lane's row lies: its (sequence, head), its number in the pools; ours: the token is a sequence's; there: so is its page
 struct Place { uint32_t unit; uint64_t row; bool ours, there; };
 
-// the places of the lane's tokens, the P of which are kTokens apart
+// of a token whose sequence is `seq`, `before` its tokens from this one on (none where that is less than 1)
+__device__ __forceinline__ Place place_of(const RowsDev &r, uint32_t head, int32_t seq, int32_t before)
+{
+    Place p = {0, 0, before > 0, false};
+    if (!p.ours) return p;
+    p.unit = (uint32_t)seq * r.c.heads + head;
+    // (a length may be any number: differences of two are taken in 64 bits)
+    const int64_t position = (int64_t)max(r.c.lengths[seq], 0) - before;
+    if (position < 0 || position >= r.c.capacity) return p;
+    const uint32_t at = (uint32_t)position;
+    const int32_t page = r.c.table[(uint64_t)p.unit * r.c.table_pages + (at >> r.c.page_shift)];
+    p.there = (uint32_t)page < r.c.n_pages;
+    p.row = ((uint64_t)(uint32_t)page << r.c.page_shift) + (at & ((1u << r.c.page_shift) - 1));
+    return p;
+}
+template <int LANE> __device__ __forceinline__ uint32_t of_four(uint32_t x)       // of the LANE-th of every four lanes
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, LANE * 0x55, 0xF, 0xF, false);
+}
+template <int LANE> __device__ __forceinline__ Place of_four(const Place &p)
+{
+    const uint32_t flags = of_four<LANE>((p.ours ? 1u : 0u) | (p.there ? 2u : 0u));
+    return Place{of_four<LANE>(p.unit), (uint64_t)of_four<LANE>((uint32_t)(p.row >> 32)) << 32 | of_four<LANE>((uint32_t)p.row), (flags & 1) != 0, (flags & 2) != 0};
+}
+
+// The places of the lane's P tokens (1 or 4), which are kTokens apart.  A row has at least eight lanes, so of four tokens each of four lanes finds one.
+// The sequence is the last one that begins at or before the token: the wavefront's tokens are counted against 64 beginnings at a time (a
+// binary search waits for each of its steps: it is left to many sequences, and to four tokens to a lane where a sequence ends among them).
 template <int D, int P> __device__ __forceinline__ void find_places(const RowsDev &r, uint32_t head, int32_t token, Place (&p)[P])
 {
-    const int32_t n = (int32_t)r.n_tokens;
-    int32_t seq[P], before[P];                                 // tokens of the sequence from this one on
-#pragma unroll
-    for (int i = 0; i < P; i++) {
-        seq[i] = token + i * (int32_t)kTokens<D>;
-        before[i] = 1;
-    }
+    static_assert(P == 1 || P == 4, "");
+    constexpr int kEach = 64 / (int)kLanes<D>;
+    const uint32_t lane = threadIdx.x & 63;
+    const int32_t n = (int32_t)r.n_tokens, mine = token + (P == 4 ? (int32_t)(lane & 3) * (int32_t)kTokens<D> : 0);
+    int32_t seq = mine, before = mine < n ? 1 : 0;
     if (r.q_start) {
-        // the last sequence that begins at or before the token: the wavefront's tokens are counted against 64 beginnings at a time (a
-        // binary search would wait for each of its steps)
-        constexpr int kEach = 64 / (int)kLanes<D>;
-        const uint32_t lane = threadIdx.x & 63;
         const int32_t first = __builtin_amdgcn_readfirstlane(token);
-#pragma unroll
-        for (int i = 0; i < P; i++) seq[i] = -1;
+        int32_t lo = -1, hi = (int32_t)r.n_seqs;               // begins at or before the token; begins behind it
         if (r.n_seqs <= 1024) {
-            for (uint32_t c = 0; c < r.n_seqs; c += 64) {
-                const int32_t begin = c + lane < r.n_seqs ? r.q_start[c + lane] : INT32_MAX;
-#pragma unroll
-                for (int i = 0; i < P; i++)
+            if constexpr (P == 1) {
+                for (uint32_t c = 0; c < r.n_seqs; c += 64) {
+                    const int32_t begin = c + lane < r.n_seqs ? r.q_start[c + lane] : INT32_MAX;
 #pragma unroll
                     for (int j = 0; j < kEach; j++) {
-                        const int32_t count = (int32_t)__popcll(__ballot(begin <= first + i * (int32_t)kTokens<D> + j));
-                        seq[i] += token == first + j ? count : 0;
+                        const int32_t count = (int32_t)__popcll(__ballot(begin <= first + j));
+                        lo += mine == first + j ? count : 0;
                     }
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < P; i++) {
-                int32_t lo = -1, hi = (int32_t)r.n_seqs;
-                while (hi - lo > 1) {
-                    const int32_t mid = (lo + hi) / 2;
-                    if (r.q_start[mid] <= token + i * (int32_t)kTokens<D>) lo = mid; else hi = mid;
                 }
-                seq[i] = lo;
+                hi = lo + 1;
+            } else {
+                const int32_t last = first + (P - 1) * (int32_t)kTokens<D> + kEach - 1;
+                hi = 0;
+                for (uint32_t c = 0; c < r.n_seqs; c += 64) {
+                    const int32_t begin = c + lane < r.n_seqs ? r.q_start[c + lane] : INT32_MAX;
+                    lo += (int32_t)__popcll(__ballot(begin <= first));
+                    hi += (int32_t)__popcll(__ballot(begin <= last));
+                }
             }
         }
-#pragma unroll
-        for (int i = 0; i < P; i++) before[i] = seq[i] >= 0 ? min(max(r.q_start[seq[i] + 1], 0), n) - (token + i * (int32_t)kTokens<D>) : 0;
+        while (hi - lo > 1) {
+            const int32_t mid = (lo + hi) / 2;
+            if (r.q_start[mid] <= mine) lo = mid; else hi = mid;
+        }
+        seq = lo;
+        before = seq >= 0 && mine < n ? min(max(r.q_start[seq + 1], 0), n) - mine : 0;
     }
-    int64_t position[P];
-#pragma unroll
-    for (int i = 0; i < P; i++) {
-        p[i] = Place{0, 0, token + i * (int32_t)kTokens<D> < n && before[i] > 0, false};
-        position[i] = -1;
-        // (a length may be any number: differences of two are taken in 64 bits)
-        if (p[i].ours) position[i] = (int64_t)max(r.c.lengths[seq[i]], 0) - before[i];
-        p[i].unit = p[i].ours ? (uint32_t)seq[i] * r.c.heads + head : 0;
-    }
-#pragma unroll
-    for (int i = 0; i < P; i++) {
-        if (position[i] < 0 || position[i] >= r.c.capacity) continue;
-        const uint32_t at = (uint32_t)position[i];
-        const int32_t page = r.c.table[(uint64_t)p[i].unit * r.c.table_pages + (at >> r.c.page_shift)];
-        p[i].there = (uint32_t)page < r.c.n_pages;
-        p[i].row = ((uint64_t)(uint32_t)page << r.c.page_shift) + (at & ((1u << r.c.page_shift) - 1));
+    const Place q = place_of(r, head, seq, before);
+    if constexpr (P == 1) p[0] = q;
+    else {
+        p[0] = of_four<0>(q);
+        p[1] = of_four<1>(q);
+        p[2] = of_four<2>(q);
+        p[3] = of_four<3>(q);
     }
 }
 
@@ -138,16 +152,14 @@ __device__ __forceinline__ uint32_t eight_to_fp4(const u32x4_t &x, float scale)
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, bf16_pair(x[3]), scale, 3);
 }
 
-// What eight BF16 elements times `factor` (if `times`) are stored as; scale: FP4, the block's.
-template <int FMT> __device__ __forceinline__ u32x4_t quantised(const u32x4_t &x, bool times, float factor, uint32_t &scale)
+// What eight BF16 elements times `factor` (TIMES) are stored as; scale: FP4, the block's.
+template <int FMT, bool TIMES> __device__ __forceinline__ u32x4_t quantised(const u32x4_t &x, float factor, uint32_t &scale)
 {
     u32x4_t w = {0, 0, 0, 0};
-    if constexpr (FMT == ZC_FMT_BF16) {
-        if (!times) return x;
-    }
+    if constexpr (FMT == ZC_FMT_BF16 && !TIMES) return x;
     float y[8];
     floats_of_bf16(x, y);
-    if (times) {
+    if constexpr (TIMES) {
 #pragma unroll
         for (int i = 0; i < 8; i++) y[i] *= factor;
     }
@@ -172,22 +184,20 @@ template <int FMT> __device__ __forceinline__ u32x4_t quantised(const u32x4_t &x
         const uint32_t top = largest_of_group<kBlock<FMT> / 8>(x);
         // (the largest magnitude's product is the products' largest magnitude)
         float largest = __uint_as_float(top << 16);
-        if (times) largest = fabsf(largest * factor);
+        if constexpr (TIMES) largest = fabsf(largest * factor);
         const bool nan = top > kInf16 || largest != largest;
         if constexpr (FMT == ZC_FMT_FP4_E2M1_MX) {
             // 2^(floor(log2 of the largest) - 2); an infinity counts as the largest number
             const int32_t e = (int32_t)min(bits(largest) >> 23, 254u) - 2;
             scale = nan ? 255u : (uint32_t)max(e, 0);
-            w[0] = nan ? 0u : times ? eight_to_fp4(y, block_scale<FMT>(scale)) : eight_to_fp4(x, block_scale<FMT>(scale));
+            if constexpr (TIMES) w[0] = eight_to_fp4(y, block_scale<FMT>(scale));
+            else w[0] = eight_to_fp4(x, block_scale<FMT>(scale));
+            w[0] = nan ? 0u : w[0];
         } else {
-            scale = nan ? 0x7Fu : (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(fminf(largest, 6.0f * 448.0f) / 6.0f, 0.0f, 0, false) & 0xFFu;
-            if (__builtin_expect(__any(largest > 0x1p60f), 0)) {       // (whose quotients would not be finite: 6 times the largest scale is less than 2^12)
-#pragma unroll
-                for (int i = 0; i < 8; i++) y[i] = __builtin_amdgcn_fmed3f(y[i], -0x1p20f, 0x1p20f);
-            }
+            scale = nan ? 0x7Fu : (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(quotient(fminf(largest, 6.0f * 448.0f), 6.0f, 1.0f / 6.0f), 0.0f, 0, false) & 0xFFu;
             const float s = block_scale<FMT>(scale), reciprocal = reciprocal_of(s);
 #pragma unroll
-            for (int i = 0; i < 8; i++) y[i] = quotient(y[i], s, reciprocal);
+            for (int i = 0; i < 8; i++) y[i] = quotient(__builtin_amdgcn_fmed3f(y[i], -0x1p20f, 0x1p20f), s, reciprocal);      // (6 times the largest scale is less than 2^12)
             w[0] = nan || s == 0.0f ? 0u : eight_to_fp4(y, 1.0f);
         }
     }
@@ -223,7 +233,7 @@ template <int P> __device__ __forceinline__ void store_result(uint16_t *to, cons
 
 // Every element is multiplied with the reciprocal of the scale of its sequence and head (at most the largest number; where the scale is 0, all become 0), rounded to the nearest, ties to even, the largest number where it is
 // beyond that.  NaN stays one; in an FP4 block it makes the block's scale NaN.
-template <int FMT, int D, int P>
+template <int FMT, int D, int P, bool TIMES>
 __global__ __launch_bounds__(256) void k_kv_write(RowsDev r)
 {
     const uint32_t head = blockIdx.x % r.c.heads, sub = threadIdx.x % kLanes<D>;
@@ -232,8 +242,8 @@ __global__ __launch_bounds__(256) void k_kv_write(RowsDev r)
 #pragma unroll
     for (int i = 0; i < P; i++) {
         const uint64_t t = (uint64_t)min(token + i * (int32_t)kTokens<D>, (int32_t)r.n_tokens - 1);
-        x[i][0] = *reinterpret_cast<const u32x4_t *>(r.k + t * r.k_token_stride + (uint64_t)head * r.k_head_stride + sub * 8);
-        x[i][1] = *reinterpret_cast<const u32x4_t *>(r.v + t * r.v_token_stride + (uint64_t)head * r.v_head_stride + sub * 8);
+        x[i][0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(r.k + t * r.k_token_stride + (uint64_t)head * r.k_head_stride + sub * 8));
+        x[i][1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(r.v + t * r.v_token_stride + (uint64_t)head * r.v_head_stride + sub * 8));
     }
     Place p[P];
     find_places<D, P>(r, head, token, p);
@@ -241,18 +251,17 @@ __global__ __launch_bounds__(256) void k_kv_write(RowsDev r)
     for (int i = 0; i < P; i++)
 #pragma unroll
         for (int kv = 0; kv < 2; kv++) {
-            const float *scales = kv ? r.c.v_scales : r.c.k_scales;
+            [[maybe_unused]] const float *scales = kv ? r.c.v_scales : r.c.k_scales;
             float factor = 1.0f;
-            if (scales) {
-                const float divisor = scales[p[i].unit];
-                factor = clamped(1.0f / divisor, kLargest);
-                if (divisor == 0.0f) {
-                    factor = 1.0f;
-                    x[i][kv] = u32x4_t{0, 0, 0, 0};
-                }
+            if constexpr (TIMES) {
+                const float divisor = scales ? scales[p[i].unit] : 1.0f;
+                const uint32_t keep = divisor == 0.0f ? 0u : ~0u;
+                factor = divisor == 0.0f ? 1.0f : clamped(1.0f / divisor, kLargest);
+#pragma unroll
+                for (int j = 0; j < 4; j++) x[i][kv][j] &= keep;
             }
             uint32_t scale = 0;
-            const u32x4_t w = quantised<FMT>(x[i][kv], scales != nullptr, factor, scale);
+            const u32x4_t w = quantised<FMT, TIMES>(x[i][kv], factor, scale);
             if (!p[i].there) continue;
             store_eight<FMT>((kv ? r.v_pages : r.k_pages) + p[i].row * kRowBytes<FMT, D> + sub * kElemBits<FMT>, w);
             if constexpr (kFp4<FMT>) {
@@ -313,7 +322,10 @@ template <int FMT, int D, bool WRITE, int P> int launch_of(const RowsDev &r, hip
 {
     constexpr uint32_t kEach = P * kTokens<D>;
     const dim3 blocks((r.n_tokens + kEach - 1) / kEach * r.c.heads);
-    if constexpr (WRITE) hipLaunchKernelGGL((k_kv_write<FMT, D, P>), blocks, dim3(256), 0, s, r);
+    if constexpr (WRITE) {
+        if (r.c.k_scales || r.c.v_scales) hipLaunchKernelGGL((k_kv_write<FMT, D, P, true>), blocks, dim3(256), 0, s, r);
+        else hipLaunchKernelGGL((k_kv_write<FMT, D, P, false>), blocks, dim3(256), 0, s, r);
+    }
     else hipLaunchKernelGGL((k_kv_read<FMT, D, P>), blocks, dim3(256), 0, s, r);
     return (int)hipGetLastError();
 }
