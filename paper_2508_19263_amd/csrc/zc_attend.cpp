@@ -248,7 +248,8 @@ zc_status plan_rows(const zc_kv_rows *x, const zc_kv_cache *cache, RowsDev *out)
     const zc_status st = check_cache(cache, &r.c);
     if (st) return st;
     if (!x->d_q_start && x->n_tokens != cache->n_seqs) return ZC_ERR_INVALID_ARG;
-    if ((uint64_t)x->n_tokens * cache->n_heads > 0x3FFFFFFFu) return ZC_ERR_INVALID_ARG;
+    // (at least 8,192 elements of a head to a workgroup where there are many)
+    if ((uint64_t)x->n_tokens * cache->n_heads > 0x3FFFFFFFu || ((uint64_t)x->n_tokens * cache->head_dim + 8191) / 8192 * cache->n_heads > kMaxBlocks) return ZC_ERR_INVALID_ARG;
     if (x->n_tokens && (!x->d_k || !x->d_v)) return ZC_ERR_INVALID_ARG;
     if (!aligned16(x->d_k) || !aligned16(x->d_v) || !aligned4(x->d_q_start)) return ZC_ERR_INVALID_ARG;
     if ((x->k_token_stride | x->k_head_stride | x->v_token_stride | x->v_head_stride) & 7) return ZC_ERR_INVALID_ARG;

@@ -61,17 +61,21 @@ template <int FMT, int VW> __device__ __forceinline__ u32x4_t value_operand(cons
 
 // The same for FP4, dimensions 2 SEL and 2 SEL + 1.  MX: every token's pair of them is converted with its scale, then the tokens are paired.  NV: the
 // tokens are paired first, four bits each to a byte (`pairs`: of even dimensions, then of odd ones), converted, and multiplied with the two scales.
-template <int FMT, int SEL> __device__ __forceinline__ void value_operands4(const uint32_t (&v)[8], const uint32_t (&scale)[8], const uint32_t (&pairs)[4][2], u32x4_t &even, u32x4_t &odd)
+// my_block: where the lane's scale is in its tokens' words of them, in bits.
+template <int FMT, int D, int SEL> __device__ __forceinline__ void value_operands4(const uint32_t (&v)[8], const uint32_t (&scale)[8], const uint32_t (&pairs)[4][2], uint32_t my_block, u32x4_t &even, u32x4_t &odd)
 {
 #pragma unroll
     for (int p = 0; p < 4; p++) {
         if constexpr (FMT == ZC_FMT_FP4_E2M1_NV) {
-            const halfx2 s = __builtin_bit_cast(halfx2, two_to_half<ZC_FMT_FP8_E4M3, false>(scale[2 * p + 1] << 8 | scale[2 * p]));
+            const halfx2 s = __builtin_bit_cast(halfx2, two_to_half<ZC_FMT_FP8_E4M3, false>(
+                kRowScales<FMT, D> == 4 ? __builtin_amdgcn_perm(scale[2 * p + 1], scale[2 * p], my_block / 8 * 0x0101u + 0x0400u) : scale[2 * p + 1] << 8 | scale[2 * p]));
             even[p] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(halfx2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(pairs[p][0], 1.0f, SEL)) * s);
             odd[p] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(halfx2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(pairs[p][1], 1.0f, SEL)) * s);
             continue;
         }
-        const uint32_t a = two_fp4_to_values<FMT, SEL>(v[2 * p], block_scale<FMT>(scale[2 * p])), b = two_fp4_to_values<FMT, SEL>(v[2 * p + 1], block_scale<FMT>(scale[2 * p + 1]));
+        // (the byte comes to the exponent's place; sign and mantissa beside it do not count)
+        auto factor = [&](uint32_t x) { return __uint_as_float(kRowScales<FMT, D> == 4 ? __builtin_amdgcn_alignbit(x, x, my_block + 9) : x << 23); };
+        const uint32_t a = two_fp4_to_values<FMT, SEL>(v[2 * p], factor(scale[2 * p])), b = two_fp4_to_values<FMT, SEL>(v[2 * p + 1], factor(scale[2 * p + 1]));
         even[p] = __builtin_amdgcn_perm(b, a, 0x05040100u);
         odd[p] = __builtin_amdgcn_perm(b, a, 0x07060302u);
     }
@@ -139,6 +143,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
 
     const int32_t *table = a.c.table + (uint64_t)(unit) * a.c.table_pages;
     const uint32_t page_mask = (1u << a.c.page_shift) - 1;
+    [[maybe_unused]] const uint32_t my_block = kFp4<FMT> && kRowScales<FMT, D> == 4 ? n16 / 4 * 8 : 0;
     const uint32_t k_lane = n16 * kRow + g * (kFp4<FMT> ? kRow / 4 : 16), v_lane = g * 4 * kRow + n16 * (kRow / 16);
 
     // page ids of the wavefront's next 32 steps: lane 2i + h has that of half h of step i (-1: absent)
@@ -227,9 +232,18 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
                 const __amdgpu_buffer_rsrc_t scales = sixteen_tokens(a.c.v_blocks + x.at[h] * kScales, x.there >> h & 1 ? 16 * kScales : 0);
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
+                    if constexpr (kScales == 4) break;
+                    r.v_scale[h * 4 + j] = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)((g * 4 + j) * kScales + n16 * kScales / 16), 0, 0);
+                }
+                if constexpr (kScales == 4) {            // all of a token's four scales
+                    const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(scales, (int)(g * 16), 0, 0);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) r.v_scale[h * 4 + j] = x[j];
+                }
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
                     if constexpr (DL == 8) r.v[h * 4 + j] = __builtin_amdgcn_raw_buffer_load_b32(from, (int)(v_lane + j * kRow), 0, 0);
                     else r.v[h * 4 + j] = __builtin_amdgcn_raw_buffer_load_b16(from, (int)(v_lane + j * kRow), 0, 0);
-                    r.v_scale[h * 4 + j] = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)((g * 4 + j) * kScales + n16 * kScales / 16), 0, 0);
                 }
             } else {
 #pragma unroll
@@ -276,7 +290,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
             for (int j = 0; j < 8; j++) {
                 const uint32_t keep = bit_as_mask(used, j), some = ~bit_as_mask(by_all, j);
                 if constexpr (kFp4<FMT>) {               // (a scale that is not finite takes its block's elements along)
-                    const uint32_t scale = r.v_scale[j] & keep, wild = wild_scale<FMT>(scale) ? some : 0u;
+                    const uint32_t scale = r.v_scale[j] & keep, wild = wild_scale<FMT>(scale >> my_block & 0xFFu) ? some : 0u;
                     bad |= wild ? 1u << j : 0u;
                     r.v_scale[j] = scale & ~wild;
                     r.v[j] &= keep & ~wild;
@@ -360,10 +374,10 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
 #pragma unroll
             for (int i = 0; i < DL; i += 2) {
                 u32x4_t even, odd;
-                if (i == 0) value_operands4<FMT, 0>(r.v, r.v_scale, pairs, even, odd);
-                else if (i == 2) value_operands4<FMT, 1>(r.v, r.v_scale, pairs, even, odd);
-                else if (i == 4) value_operands4<FMT, 2>(r.v, r.v_scale, pairs, even, odd);
-                else value_operands4<FMT, 3>(r.v, r.v_scale, pairs, even, odd);
+                if (i == 0) value_operands4<FMT, D, 0>(r.v, r.v_scale, pairs, my_block, even, odd);
+                else if (i == 2) value_operands4<FMT, D, 1>(r.v, r.v_scale, pairs, my_block, even, odd);
+                else if (i == 4) value_operands4<FMT, D, 2>(r.v, r.v_scale, pairs, my_block, even, odd);
+                else value_operands4<FMT, D, 3>(r.v, r.v_scale, pairs, my_block, even, odd);
 #pragma unroll
                 for (int t = 0; t < QT; t++) {
                     o[t][i] = mma16_values<FMT>(even, p[t], o[t][i]);
