@@ -36,11 +36,11 @@ template <int FMT, int D> struct BlockRegs4 {
 template <int FMT, int D, bool FP4 = kFp4<FMT>> struct FewRegs { typedef BlockRegs<FMT, D> Type; };
 template <int FMT, int D> struct FewRegs<FMT, D, true> { typedef BlockRegs4<FMT, D> Type; };
 
-template <int N> __device__ __forceinline__ void load_words(uint32_t (&to)[N], __amdgpu_buffer_rsrc_t from, uint32_t at)
+template <int AUX, int N> __device__ __forceinline__ void load_words(uint32_t (&to)[N], __amdgpu_buffer_rsrc_t from, uint32_t at)
 {
-    if constexpr (N == 1) to[0] = __builtin_amdgcn_raw_buffer_load_b32(from, (int)at, 0, 0);
-    else if constexpr (N == 2) { const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(from, (int)at, 0, 0); to[0] = x[0]; to[1] = x[1]; }
-    else { const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(from, (int)at, 0, 0); to[0] = x[0]; to[1] = x[1]; to[2] = x[2]; to[3] = x[3]; }
+    if constexpr (N == 1) to[0] = __builtin_amdgcn_raw_buffer_load_b32(from, (int)at, 0, AUX);
+    else if constexpr (N == 2) { const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(from, (int)at, 0, AUX); to[0] = x[0]; to[1] = x[1]; }
+    else { const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(from, (int)at, 0, AUX); to[0] = x[0]; to[1] = x[1]; to[2] = x[2]; to[3] = x[3]; }
 }
 
 // The operand for dimension i of a lane's DL: 8 tokens' elements of it.
@@ -86,12 +86,16 @@ template <int D, int QT> struct FewShared {
     alignas(16) float ob[kWaves][16][D + 4];
 };
 
-template <int FMT, int D, int QT, bool LOGITS>
+// PAST: pages go past the caches (kPastCaches)
+constexpr int kPastCaches = 2;                 // the non-temporal bit of buffer loads
+
+template <int FMT, int D, int QT, bool LOGITS, bool PAST>
 __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, uint32_t split, uint32_t row_block, FewShared<D, QT> &shared)
 {
     using Regs = typename FewRegs<FMT, D>::Type;
     constexpr int DL = Regs::DL, KS = D / 32;
     constexpr uint32_t kRow = kRowBytes<FMT, D>;
+    constexpr int AUX = PAST ? kPastCaches : 0;
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
     const uint32_t head = unit % a.c.heads, seq = unit / a.c.heads;              // a shared prefix's one "sequence" is 0
 
@@ -213,13 +217,13 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
             if constexpr (kFp4<FMT>) {
                 constexpr uint32_t kScales = kRowScales<FMT, D>;
                 const __amdgpu_buffer_rsrc_t scales = sixteen_tokens(a.c.k_blocks + x.at[h] * kScales, x.there >> h & 1 ? 16 * kScales : 0);
-                load_words(r.k[h], from, k_lane);
+                load_words<AUX>(r.k[h], from, k_lane);
                 // a quarter of a key has two scales, one, or half of one
                 if constexpr (kScales == 8) r.k_scale[h] = __builtin_amdgcn_raw_buffer_load_b16(scales, (int)(n16 * 8 + g * 2), 0, 0);
                 else r.k_scale[h] = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)(n16 * kScales + g * kScales / 4), 0, 0);
             } else {
 #pragma unroll
-                for (int u = 0; u < Regs::NK; u++) r.k[h][u] = __builtin_amdgcn_raw_buffer_load_b128(from, (int)(k_lane + u * 64), 0, 0);
+                for (int u = 0; u < Regs::NK; u++) r.k[h][u] = __builtin_amdgcn_raw_buffer_load_b128(from, (int)(k_lane + u * 64), 0, AUX);
             }
         }
     };
@@ -242,12 +246,12 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
                 }
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
-                    if constexpr (DL == 8) r.v[h * 4 + j] = __builtin_amdgcn_raw_buffer_load_b32(from, (int)(v_lane + j * kRow), 0, 0);
-                    else r.v[h * 4 + j] = __builtin_amdgcn_raw_buffer_load_b16(from, (int)(v_lane + j * kRow), 0, 0);
+                    if constexpr (DL == 8) r.v[h * 4 + j] = __builtin_amdgcn_raw_buffer_load_b32(from, (int)(v_lane + j * kRow), 0, AUX);
+                    else r.v[h * 4 + j] = __builtin_amdgcn_raw_buffer_load_b16(from, (int)(v_lane + j * kRow), 0, AUX);
                 }
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; j++) load_words(r.v[h * 4 + j], from, v_lane + j * kRow);
+                for (int j = 0; j < 4; j++) load_words<AUX>(r.v[h * 4 + j], from, v_lane + j * kRow);
             }
         }
     };

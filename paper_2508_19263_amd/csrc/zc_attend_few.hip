@@ -5,21 +5,26 @@ namespace zc {
 
 namespace {
 
-template <int FMT, int D, int QT, bool LOGITS>
+template <int FMT, int D, int QT, bool LOGITS, bool PAST>
 __global__ __launch_bounds__(kWaves * 64, 2) void k_attend_few(AttendDev a)
 {
     __shared__ FewShared<D, QT> shared;
     // Each part begins with another unit: workgroups that lie a round apart go to the same compute unit, where the parts of a long
     // cache would meet (one FP8 cache of 131,072 tokens and 31 of 1,000: 168 -> 128 us, six of 100 to 3,001 13.6 -> 12.4 us).
-    attend_few<FMT, D, QT, LOGITS>(a, (blockIdx.x + blockIdx.y * 13) % gridDim.x, blockIdx.y, blockIdx.z, shared);
+    attend_few<FMT, D, QT, LOGITS, PAST>(a, (blockIdx.x + blockIdx.y * 13) % gridDim.x, blockIdx.y, blockIdx.z, shared);
 }
 
+template <int FMT, int D, int QT, bool LOGITS> void launch_of(const AttendDev &a, dim3 blocks, hipStream_t s)
+{
+    if (a.past_caches) hipLaunchKernelGGL((k_attend_few<FMT, D, QT, LOGITS, true>), blocks, dim3(kWaves * 64), 0, s, a);
+    else hipLaunchKernelGGL((k_attend_few<FMT, D, QT, LOGITS, false>), blocks, dim3(kWaves * 64), 0, s, a);
+}
 template <int FMT, int D> int launch(const AttendDev &a, uint32_t tiles, dim3 blocks, hipStream_t s)
 {
-    if (a.logits && tiles == 1) hipLaunchKernelGGL((k_attend_few<FMT, D, 1, true>), blocks, dim3(kWaves * 64), 0, s, a);
-    else if (a.logits) hipLaunchKernelGGL((k_attend_few<FMT, D, 2, true>), blocks, dim3(kWaves * 64), 0, s, a);
-    else if (tiles == 1) hipLaunchKernelGGL((k_attend_few<FMT, D, 1, false>), blocks, dim3(kWaves * 64), 0, s, a);
-    else hipLaunchKernelGGL((k_attend_few<FMT, D, 2, false>), blocks, dim3(kWaves * 64), 0, s, a);
+    if (a.logits && tiles == 1) launch_of<FMT, D, 1, true>(a, blocks, s);
+    else if (a.logits) launch_of<FMT, D, 2, true>(a, blocks, s);
+    else if (tiles == 1) launch_of<FMT, D, 1, false>(a, blocks, s);
+    else launch_of<FMT, D, 2, false>(a, blocks, s);
     return (int)hipGetLastError();
 }
 template <int FMT> int launch(const AttendDev &a, uint32_t head_dim, uint32_t tiles, dim3 blocks, hipStream_t s)

@@ -25,10 +25,10 @@ __global__ __launch_bounds__(256, 2) void k_attend_shared(AttendDev pre, AttendD
             __shared__ ManyNotes notes;
             attend_many<FMT, D>(pre, blockIdx.x, *reinterpret_cast<ManyTile<D> *>(room), tile1, notes);
         }
-        else attend_few<FMT, D, QT, false>(pre, blockIdx.x % units, id % pre.splits, id / pre.splits, *reinterpret_cast<FewShared<D, QT> *>(room));
+        else attend_few<FMT, D, QT, false, false>(pre, blockIdx.x % units, id % pre.splits, id / pre.splits, *reinterpret_cast<FewShared<D, QT> *>(room));
     } else {
         const uint32_t units = own.n_seqs * own.c.heads, id = (blockIdx.x - pre_blocks) / units;
-        attend_few<FMT, D, QT, false>(own, (blockIdx.x - pre_blocks) % units, id % own.splits, id / own.splits, *reinterpret_cast<FewShared<D, QT> *>(room));
+        attend_few<FMT, D, QT, false, false>(own, (blockIdx.x - pre_blocks) % units, id % own.splits, id / own.splits, *reinterpret_cast<FewShared<D, QT> *>(room));
     }
 }
 

@@ -294,8 +294,6 @@ __global__ __launch_bounds__(256) void k_evict_move(EvictDev e, uint32_t blocks_
     }
 }
 
-constexpr uint64_t kMemorySideCache = 256u << 20;
-
 template <uint32_t PIECES> void launch_move(const EvictDev &e, uint32_t blocks, uint32_t per_head, bool stream_past, hipStream_t s)
 {
     if (stream_past) hipLaunchKernelGGL((k_evict_move<PIECES, true>), dim3(blocks), dim3(256), 0, s, e, per_head);
