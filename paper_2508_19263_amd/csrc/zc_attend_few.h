@@ -10,9 +10,16 @@
 // head_dim / 16 consecutive dimensions.  At the end the wavefronts' (m, l, O) are joined in LDS; parts of a cache that went
 // to different workgroups are joined by k_attend_join.
 //
-// Measured with 8 K/V heads of 128 in random pages of 16 tokens, one query token, joins included (a kernel that only reads reaches
-// 6.1 TB/s): 64 FP8 caches of 8,192 tokens 189 us, 5.7 TB/s; 48 BF16 ones of 12,000 418 us, 5.6 TB/s; 4 FP8 ones of 8,192 16.7 us,
-// 4.0 TB/s, and 17.5 replayed from a graph; one with 512 tokens in sight 8.5 us, all latency.
+// Measured with 8 K/V heads of 128 in random pages of 16 tokens, one query token, 4 query heads to each, joins included (a large copy
+// reaches 6.2 TB/s): 64 FP8 caches of 8,192 tokens 167 us, 6.4 TB/s (past the caches; 212 where their memory lies less well, which no address
+// tells); 48 BF16 ones of 12,000 373 - 420 us, 5.6 - 6.3 TB/s; 4 FP8 ones of 8,192 16.5 us, 4.1 TB/s; one with 512 tokens in sight 8.5 us, all latency.
+//
+// FP4 elements are converted as they are used, with their block's scale: MX to BF16, an instruction for two keys, two for two values (the tokens
+// have to be paired); NV keys to BF16 (four instructions), values to half precision (two and a quarter).  64 MXFP4 caches of 8,192 tokens
+// 103 us, 5.5 TB/s of what they hold: the read, 200 vector instructions for 32 tokens, which take 43 % of the time beside it; NVFP4 120 us, 5.0
+// TB/s, 340 instructions, which take 75 %.  (NV keys and queries in half precision, where queries have to be brought to its range and rows that
+// do not fit it need a loop of their own, are 80 instructions less: 32 caches of 16,384 125.4 -> 128.6 us, shorter ones the same.  A step
+// more ahead, in two sets of registers: MX 113 -> 120, NV 126 -> 130.)
 #pragma once
 #include "zc_attend_device.h"
 

@@ -3,7 +3,8 @@
 // k_attend_few), which fill the places that the former leave.  Replayed from a graph, one pass after the other against one launch: 64 answers
 // (8 K/V heads of 128, 4 query heads to each, FP8) of 16 to 777 tokens under 32,768, 76 against 72 - 75 us; five answers (BF16) under 1,531,
 // 19.2 against 12.9.  Under a kernel trace 59 us of the former are this kernel's, 590 TFLOP/s, bound like k_attend_many but with tiles
-// converted for only two row blocks, and 9 the join of 33 slots; of the latter, 11 and 4, bound by latency.
+// converted for only two row blocks, and 9 the join of 33 slots; of the latter, 11 and 4, bound by latency.  64 answers over MXFP4 pages 62 - 67 us,
+// NVFP4 68.
 #include "zc_attend_few.h"
 #include "zc_attend_many.h"
 

@@ -1,5 +1,13 @@
 // Rows of keys and values to the pages of a K/V cache and back: k_kv_write quantises as it writes, k_kv_read gives what attention
 // will see, in BF16.
+//
+// Both read each element once and write it once.  Measured with 8 K/V heads of 128 in random pages of 16 tokens: reading 84,051 MXFP4 tokens
+// 87 us, 5.0 TB/s, nearly four fifths of it writing (a large copy reaches 6.2, a fill 6.8; through the caches 95 us); 24,000 tokens BF16 36, FP8
+// 24, MX 21, NV 22 us; writing these from every sixth row of a wider tensor BF16 28, FP8 33, MX 25, NV 35 us (with inputs through the caches 2 to
+// 6 us more).  FP8 and NV with a scale for each sequence and head are bound by instructions as much as by memory: NV 1,070 of them for 64 rows of K
+// and V, 44 us for 31,385 tokens.  A token of each of 32 sequences is 2.9 us of latencies one after the other, either way.
+// (Rows in the order of the caller's tensors, the heads of a token in one workgroup, instead of tokens of one head, which share a page: the
+// 84,051 tokens 85 -> 99 us.)
 #include "zc_attend_device.h"
 
 namespace zc {
@@ -223,7 +231,7 @@ template <int FMT> __device__ __forceinline__ u32x4_t load_eight(const uint8_t *
     return w;
 }
 
-// Results that are more than the caches hold go past them.
+// Results of large calls go past the caches (84,051 tokens 94 -> 85 us; smaller ones that would stay there lose nothing: 24,000 tokens 27 -> 21).
 template <int P> __device__ __forceinline__ void store_result(uint16_t *to, const u32x4_t &w)
 {
     u32x4_t *x = reinterpret_cast<u32x4_t *>(to);
@@ -317,7 +325,8 @@ __global__ __launch_bounds__(256) void k_kv_read(RowsDev r)
     }
 }
 
-// Calls whose workgroups fill the GPU (eight to a compute unit) take four times as many tokens to each.
+// Calls whose workgroups fill the GPU (eight to a compute unit) take four times as many tokens to each, whose loads are on their way together and
+// whose places are found once: 84,051 MXFP4 tokens read 141 -> 95 us, 31,385 NVFP4 ones written and read 102 -> 78.
 template <int FMT, int D, bool WRITE, int P> int launch_of(const RowsDev &r, hipStream_t s)
 {
     constexpr uint32_t kEach = P * kTokens<D>;
