@@ -16,8 +16,8 @@
 //
 // FP4 elements are converted as they are used, with their block's scale: MX to BF16, an instruction for two keys, two for two values (the tokens
 // have to be paired); NV keys to BF16 (four instructions), values to half precision (two and a quarter).  64 MXFP4 caches of 8,192 tokens
-// 103 us, 5.5 TB/s of what they hold: the read, 200 vector instructions for 32 tokens, which take 43 % of the time beside it; NVFP4 120 us, 5.0
-// TB/s, 340 instructions, which take 75 %.  (NV keys and queries in half precision, where queries have to be brought to its range and rows that
+// 103 us, 5.5 TB/s of what they hold: the read, and 200 vector instructions for 32 tokens, which take 53 % of the time beside it; NVFP4 120 us,
+// 5.0 TB/s, 340 instructions, which take 62 %.  (NV keys and queries in half precision, where queries have to be brought to its range and rows that
 // do not fit it need a loop of their own, are 80 instructions less: 32 caches of 16,384 125.4 -> 128.6 us, shorter ones the same.  A step
 // more ahead, in two sets of registers: MX 113 -> 120, NV 126 -> 130.)
 #pragma once

@@ -17,7 +17,7 @@
 // under it; here it goes from 2.2 to 1.9.  The matrix unit is busy 51 % of the cycles (FP8: 38 %), the exponentials and what belongs to
 // them take about as many (two wavefronts to a SIMD; registers and LDS have room for no more); other orders of the same instructions
 // give the same time.  FP4 tiles are converted like FP8 ones, a piece of 32 (16) elements and its scales to a lane: the same pieces of prompts
-// over MXFP4 137 - 147 us, NVFP4 157; a whole prompt of 8,192 without a window 553 us (MX, 994 TFLOP/s) and 588 - 603 (NV).
+// over MXFP4 137 - 148 us, NVFP4 149 - 152; a whole prompt of 8,192 without a window 550 - 575 us (MX, 960 - 1,000 TFLOP/s) and 590 - 615 (NV).
 #pragma once
 #include "zc_attend_device.h"
 
