@@ -417,7 +417,8 @@ typedef struct {
 
 /* Rows of the last tokens of every sequence.  Sequence s has the tokens d_q_start[s] .. d_q_start[s + 1] (non-decreasing; NULL:
  * n_tokens == n_seqs, token s is sequence s's); as in attention the i-th of n is at position length - n + i of the cache, so a length counts the
- * tokens that are written already when they are. */
+ * tokens that are written already when they are.  (Here a length beyond the table's room is taken as it is: tokens whose positions are past
+ * the room have none, and no other token's place.) */
 typedef struct {
     uint32_t struct_size;       /* = sizeof(zc_kv_rows) */
     uint32_t n_tokens;

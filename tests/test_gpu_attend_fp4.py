@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2508_19263_amd import zc
-from tests.paged import agree, attention, gen, starts
+from tests.paged import Cache, agree, attention, gen, starts
 from tests.paged4 import MX, NV, Cache4
 from tests.test_gpu_attend import check, queries
 
@@ -189,3 +189,109 @@ def test_eviction_moves_elements_and_block_scales(fmt, dim, page, into_page):
                     if (s, h) == (0, 1):
                         want[[i for i, t in enumerate(at.tolist()) if t in gone]] = 0
                     assert torch.equal(got, want)
+
+
+def with_room(cache, tokens):
+    """The cache with a table that has room for more tokens; the pages behind its own are absent."""
+    seqs, heads, have = cache.table.shape
+    more = torch.full((seqs, heads, -(-tokens // cache.page) - have), -1, dtype=torch.int32, device="cuda")
+    cache.table = torch.cat([cache.table, more], dim=2).contiguous()
+    p = cache.paged
+    cache.paged = zc.PagedCache(p.k_pages, p.v_pages, cache.table, cache.lengths, p.fmt, p.k_scales, p.v_scales, p.k_blocks, p.v_blocks)
+    return cache
+
+
+@pytest.mark.parametrize("fmt,dim", [(MX, 128), (NV, 128), (MX, 64), (zc.FMT_BF16, 64), (zc.FMT_BF16, 128), (zc.FMT_FP8_E4M3, 64), (zc.FMT_FP8_E5M2, 128)])
+@pytest.mark.parametrize("q_len", [1, 3, 8])
+@pytest.mark.parametrize("weights", [False, True])
+def test_room_for_more_than_the_caches_hold(fmt, dim, q_len, weights):
+    """What may be read is more than 256 MB: these pages are loaded in another way (but for rows of less than 64 bytes)."""
+    kind = Cache4 if fmt in (MX, NV) else Cache
+    lens = [300, 1, 0, 1037, 64, 4099, 16, 17]
+    cache = with_room(kind(lens, 8, dim, fmt), 40000)
+    small = kind(lens, 8, dim, fmt)
+    q_lens = [q_len] * len(lens)
+    _, out, lse = check(cache, q_lens, 4, 0, 0, weights=weights)
+    check(cache, q_lens, 4, 200, 5, weights=weights)             # (a window: less)
+    want, want_lse = zc.attend(queries(len(lens) * q_len, 32, dim), small.paged, q_start=starts(q_lens), max_q_len=q_len)
+    _, _, _, tol, tol_lse, _ = attention(queries(len(lens) * q_len, 32, dim), q_lens, small)
+    agree(out, want.to(torch.float64), 2 * tol, "out")
+    agree(lse, want_lse.to(torch.float64), 2 * tol_lse, "lse")
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_rooms_and_longest_lengths(fmt):
+    """Lengths past the room and past what the call was told is the longest, below zero: as with other formats."""
+    cache = Cache4([100, 33, 64, 0], 2, 128, fmt)
+    q = queries(4, 8, 128)
+    want, want_lse = zc.attend(q, cache.paged)
+    cache.lengths.copy_(torch.tensor([100, 33, 64, -7], dtype=torch.int32))
+    got, lse = zc.attend(q, cache.paged)
+    assert torch.equal(got, want) and torch.equal(lse, want_lse)
+    full = Cache4([112, 112, 112, 112], 2, 128, fmt)
+    want, want_lse = zc.attend(q, full.paged)
+    full.lengths.fill_(2 ** 31 - 1)
+    got, lse = zc.attend(q, full.paged)
+    assert torch.equal(got, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("q_lens", [[1, 1], [40, 7], [300, 133]])
+def test_negative_block_scales(dim, q_lens):
+    """NV block scales are E4M3 numbers, and so may be negative (zc_kv_write gives none)."""
+    def edit(c):
+        for name in "kv":
+            c.blocks[name] |= torch.randint(0, 2, c.blocks[name].shape, generator=gen(6), device="cuda").to(torch.uint8) << 7
+    cache = Cache4([700, 133], 2, dim, NV, edit=edit)
+    check(cache, q_lens, 4, weights=True)
+    k, v = zc.read_kv(cache.paged, starts([700, 133]), 833)
+    for s, first in ((0, 0), (1, 700)):
+        for h in range(2):
+            for name, got in (("k", k), ("v", v)):
+                x = getattr(cache, name)[s, h, :cache.lens[s]].to(torch.float32) * getattr(cache, name + "s")[s, h]
+                assert torch.equal(got[first:first + cache.lens[s], h], x.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("length", [4095, 4096, 4097, 8191, 8192, 8193, 12288])
+def test_where_long_caches_are_cut(fmt, length):
+    check(Cache4([length, 5], 1, 128, fmt), [1, 1], 4, single=True)
+    check(Cache4([length], 2, 64, fmt), [2], 3, length - 1, 1)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_on_another_stream_with_scratch_of_its_own_and_in_two_graphs(fmt):
+    """Two graphs of one scratch, replayed in turn with the program's own work between them."""
+    cache, prefix = Cache4([9000, 37, 500], 2, 128, fmt), Cache4([700], 2, 128, fmt, seed=3)
+    q, big = queries(3, 8, 128), queries(211, 8, 128, 9)
+    many = dict(q_start=starts([200, 1, 10]), max_q_len=200)
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    outs = [torch.zeros_like(q), torch.zeros_like(big), torch.zeros_like(q)]
+    calls = [lambda o, **m: zc.attend(q, cache.paged, out=o, **m), lambda o, **m: zc.attend(big, cache.paged, out=o, **many, **m),
+             lambda o, **m: zc.attend_shared(q, prefix.paged, cache.paged, out=o, **m)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for call, o in zip(calls, outs):
+            call(o, ws=ws)
+    side.synchronize()
+    want = [torch.zeros_like(o) for o in outs]
+    for call, o in zip(calls, want):
+        call(o)
+    for o, w in zip(outs, want):
+        assert torch.equal(o, w)
+    graphs = []
+    for call, o in zip(calls, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call(o, ws=ws)
+    for i in range(4):
+        q.copy_(torch.randn(q.shape, generator=gen(i), device="cuda"))
+        big.copy_(torch.randn(big.shape, generator=gen(i + 9), device="cuda"))
+        for graph in graphs:
+            graph.replay()
+        if i % 2:
+            torch.cuda.synchronize()
+        for call, o, w in zip(calls, outs, want):
+            call(w)
+            assert torch.equal(o, w)
