@@ -545,6 +545,25 @@ def _check_numbers(what, **numbers):
             raise ValueError("%s: %s has to be in 0 .. 2^32 - 1, not %d" % (what, name, x))
 
 
+def _rows_meet(k, v):
+    """Whether rows of two BF16 tensors [n, heads, dim], none of which overlap among themselves, have elements in common."""
+    (n, heads, dim), off = k.shape, (v.data_ptr() - k.data_ptr()) // 2
+    reach = [sum(stride * (size - 1) for stride, size in zip(t.stride()[:2], t.shape)) + dim for t in (k, v)]
+    if not n or off >= reach[0] or -off >= reach[1]:
+        return False
+    if k.stride() == v.stride():                                 # heads or tokens of one tensor: rows meet where they begin less than a row apart
+        token, head = k.stride()[:2]
+        for j in range(1 - heads, heads):
+            x = off + j * head
+            i = 0 if n == 1 else min(max(-(x // token), 1 - n), n - 1)
+            if any(abs(x + a * token) < dim for a in (i, i - 1) if abs(a) < n):
+                return True
+        return False
+    first = [torch.arange(n).view(-1, 1) * t.stride(0) + torch.arange(heads) * t.stride(1) for t in (k, v)]
+    begins = torch.cat([first[0].flatten(), first[1].flatten() + off]).sort().values
+    return bool((begins.diff() < dim).any())
+
+
 def _kv_rows(what, call, k, v, cache, q_start, results):
     """results: tensors of the caller's that are written to, 0 to 2 of (k, v)."""
     shape, heads, dim = k.shape, cache.n_heads, cache.head_dim
@@ -558,6 +577,8 @@ def _kv_rows(what, call, k, v, cache, q_start, results):
             if size > 1 and stride < reach:
                 raise ValueError("%s: rows of %s overlap" % (what, "k" if t is k else "v"))
             reach += stride * (size - 1) if size > 1 else 0
+    if len(results) == 2 and _rows_meet(k, v):
+        raise ValueError("%s: rows of k and v overlap" % what)
     if (k.requires_grad or v.requires_grad) and torch.is_grad_enabled():
         raise ValueError("%s: there is no gradient through a stored cache: detach k and v, or call it under torch.no_grad()" % what)
     if q_start is None:

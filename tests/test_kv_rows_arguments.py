@@ -167,3 +167,32 @@ def test_heads_on_top_of_the_next_token():
     for shape, strides in (((2, 2, 64), (128, 64, 1)), ((2, 2, 64), (64, 128, 1))):
         with pytest.raises(ValueError, match="GPU"):
             zc.read_kv(c, k=some(shape=(1000,)).as_strided(shape, strides))
+
+
+def meet(k, v):
+    """The elements that two tensors have in common, one by one."""
+    a, b = (set((t.data_ptr() // 2 + torch.cat([torch.arange(t.shape[2]) + i * t.stride(0) + j * t.stride(1) for i in range(t.shape[0]) for j in range(t.shape[1])])).tolist())
+            for t in (k, v))
+    return bool(a & b)
+
+
+@pytest.mark.parametrize("shape", [(1, 1), (1, 3), (2, 1), (2, 2), (5, 3)])
+@pytest.mark.parametrize("k_strides", [(200, 64), (64, 400), (720, 72), (400, 128), (136, 680)])
+def test_keys_on_top_of_values(shape, k_strides):
+    """Every place of V's first row around K's, with K's strides and with others: what has elements in common is refused, what goes between is not."""
+    room, (n, heads) = some(shape=(40000,)), shape
+    c = paged(table=torch.zeros((2, heads, 2), dtype=torch.int32))
+    start, seen = torch.zeros(3, dtype=torch.int32), set()
+    if (n > 1 and heads > 1) and not (k_strides[0] >= k_strides[1] * (heads - 1) + 64 or k_strides[1] >= k_strides[0] * (n - 1) + 64):
+        return                                                   # (K's own rows would overlap)
+    for v_strides in (k_strides, (k_strides[0] * 2 + 8, k_strides[1] * 2 + 8)):
+        if n > 1 and heads > 1 and not (v_strides[0] >= v_strides[1] * (heads - 1) + 64 or v_strides[1] >= v_strides[0] * (n - 1) + 64):
+            continue
+        k = room.as_strided((n, heads, 64), k_strides + (1,), 20000)
+        for off in list(range(-1600, 1601, 8)) + [-65, -63, 63, 65]:
+            v = room.as_strided((n, heads, 64), v_strides + (1,), 20000 + off)
+            both = meet(k, v)
+            seen.add(both)
+            with pytest.raises(ValueError, match="rows of k and v overlap" if both else "GPU"):
+                zc.read_kv(c, start, k=k, v=v)
+    assert seen == {True, False}
