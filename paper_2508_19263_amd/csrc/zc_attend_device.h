@@ -26,12 +26,12 @@ constexpr float kLeastFactor = 0x1p-126f;
 // A row's running maximum is replaced, and what has been added up scaled, only where a weight would be more than 2^kSlack times its: the
 // 32-bit sums and the operands' types (half precision to 2^16) hold what is below that with the same relative error.
 constexpr float kSlack = 8.0f;
-// Weights in half precision (FP8 values) are all 2^kLift of what they are, and the sum that they are divided by is too.  Half
-// precision ends at 2^-24, but the sum counts what is below: many light tokens beside a heavy one would lose their share.  With both
-// powers weights reach 2^15 of half precision's 2^16, and end at 2^-31 of a row's heaviest.
 template <int FMT> constexpr bool kFp4 = FMT == ZC_FMT_FP4_E2M1_MX || FMT == ZC_FMT_FP4_E2M1_NV;
 // Values are multiplied in BF16 where their range goes to no other two-byte type (BF16; MXFP4, whose scales are any power of two).
 template <int FMT> constexpr bool kValuesBf16 = FMT == ZC_FMT_BF16 || FMT == ZC_FMT_FP4_E2M1_MX;
+// Weights in half precision (FP8 and NVFP4 values) are all 2^kLift of what they are, and the sum that they are divided by is too.  Half
+// precision ends at 2^-24, but the sum counts what is below: many light tokens beside a heavy one would lose their share.  With both
+// powers weights reach 2^15 of half precision's 2^16, and end at 2^-31 of a row's heaviest.
 template <int FMT> constexpr float kLift = kValuesBf16<FMT> ? 0.0f : 7.0f;
 
 template <int FMT> constexpr int kElemBits = FMT == ZC_FMT_BF16 ? 16 : kFp4<FMT> ? 4 : 8;

@@ -358,7 +358,7 @@ __device__ __forceinline__ void attend_many(const AttendDev &a, uint32_t id, Man
                 for (int d = 0; d < DT; d++)
 #pragma unroll
                     for (int kk = 0; kk < 16; kk += 4) {
-const f32x4 x = wild_values<FMT, D>(a.c, stored, d * 32 + kk * 2 + g * 4);
+                        const f32x4 x = wild_values<FMT, D>(a.c, stored, d * 32 + kk * 2 + g * 4);
 #pragma unroll
                         for (int k = 0; k < 4; k++) o[d][kk + k] += mine && x[k] != 0.0f ? weight * x[k] : 0.0f;
                         __builtin_amdgcn_sched_barrier(0);       // a few at a time: this hardly ever runs and is to cost no registers
