@@ -21,6 +21,25 @@ template <int D> constexpr uint32_t kTokens = 256 / kLanes<D>;
 // where a lane's row lies: its (sequence, head), its number in the pools; ours: the token is a sequence's; there: so is its page
 struct Place { uint32_t unit; uint64_t row; bool ours, there; };
 
+__device__ __forceinline__ float clamped(float x, float most) { return x != x ? x : fminf(fmaxf(x, -most), most); }
+constexpr float kLargest = 0x1.fffffep127f;
+
+// what a row's K and V are multiplied with before they are stored, where the cache has scales; zero: bit 0, 1: K, V become 0
+struct Factors { float of[2]; uint32_t zero; };
+
+__device__ __forceinline__ Factors factors_of(const RowsDev &r, const Place &p)
+{
+    Factors f = {{1.0f, 1.0f}, 0};
+#pragma unroll
+    for (int kv = 0; kv < 2; kv++) {
+        const float *scales = kv ? r.c.v_scales : r.c.k_scales;
+        const float divisor = scales ? scales[p.unit] : 1.0f;
+        f.of[kv] = divisor == 0.0f ? 1.0f : clamped(1.0f / divisor, kLargest);
+        f.zero |= divisor == 0.0f ? 1u << kv : 0u;
+    }
+    return f;
+}
+
 // of a token whose sequence is `seq`, `before` its tokens from this one on (none where that is less than 1)
 __device__ __forceinline__ Place place_of(const RowsDev &r, uint32_t head, int32_t seq, int32_t before)
 {
@@ -45,11 +64,15 @@ template <int LANE> __device__ __forceinline__ Place of_four(const Place &p)
     const uint32_t flags = of_four<LANE>((p.ours ? 1u : 0u) | (p.there ? 2u : 0u));
     return Place{of_four<LANE>(p.unit), (uint64_t)of_four<LANE>((uint32_t)(p.row >> 32)) << 32 | of_four<LANE>((uint32_t)p.row), (flags & 1) != 0, (flags & 2) != 0};
 }
+template <int LANE> __device__ __forceinline__ Factors of_four(const Factors &f)
+{
+    return Factors{{__uint_as_float(of_four<LANE>(bits(f.of[0]))), __uint_as_float(of_four<LANE>(bits(f.of[1])))}, of_four<LANE>(f.zero)};
+}
 
-// The places of the lane's P tokens (1 or 4), which are kTokens apart.  A row has at least eight lanes, so of four tokens each of four lanes finds one.
+// The places (TIMES: and factors) of the lane's P tokens (1 or 4), which are kTokens apart.  A row has at least eight lanes, so of four tokens each of four lanes finds one.
 // The sequence is the last one that begins at or before the token: the wavefront's tokens are counted against 64 beginnings at a time (a
 // binary search waits for each of its steps: it is left to many sequences, and to four tokens to a lane where a sequence ends among them).
-template <int D, int P> __device__ __forceinline__ void find_places(const RowsDev &r, uint32_t head, int32_t token, Place (&p)[P])
+template <int D, int P, bool TIMES> __device__ __forceinline__ void find_places(const RowsDev &r, uint32_t head, int32_t token, Place (&p)[P], Factors (&f)[P])
 {
     static_assert(P == 1 || P == 4, "");
     constexpr int kEach = 64 / (int)kLanes<D>;
@@ -95,6 +118,16 @@ template <int D, int P> __device__ __forceinline__ void find_places(const RowsDe
         p[2] = of_four<2>(q);
         p[3] = of_four<3>(q);
     }
+    if constexpr (TIMES) {
+        const Factors own = factors_of(r, q);
+        if constexpr (P == 1) f[0] = own;
+        else {
+            f[0] = of_four<0>(own);
+            f[1] = of_four<1>(own);
+            f[2] = of_four<2>(own);
+            f[3] = of_four<3>(own);
+        }
+    }
 }
 
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
@@ -104,18 +137,17 @@ __device__ __forceinline__ uint32_t max_of_halves(uint32_t x, uint32_t y)
 {
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y)));
 }
-// The largest magnitude of the eight BF16 elements of each lane of a group of 2 or 4, as an integer: NaN above infinity above all numbers.
+// The largest magnitude of the eight BF16 elements of each lane of a group of 1, 2 or 4, as an integer: NaN above infinity above all numbers.
 template <int GROUP> __device__ __forceinline__ uint32_t largest_of_group(const u32x4_t &w)
 {
     constexpr uint32_t kMagnitudes = 0x7FFF7FFFu;
     uint32_t x = max_of_halves(max_of_halves(w[0] & kMagnitudes, w[1] & kMagnitudes), max_of_halves(w[2] & kMagnitudes, w[3] & kMagnitudes));
-    x = max_of_halves(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, false));                        // lanes 1 0 3 2 of every four
+    if constexpr (GROUP > 1) x = max_of_halves(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, false));    // lanes 1 0 3 2 of every four
     if constexpr (GROUP == 4) x = max_of_halves(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, false));   // 2 3 0 1
     return max(x >> 16, x & 0xFFFFu);
 }
 
 constexpr uint32_t kInf16 = 0x7F80u;
-constexpr float kLargest = 0x1.fffffep127f;
 
 __device__ __forceinline__ void floats_of_bf16(const u32x4_t &w, float (&y)[8])
 {
@@ -138,7 +170,6 @@ __device__ __forceinline__ float reciprocal_of(float s)
     const float x = __builtin_amdgcn_rcpf(s);
     return __builtin_fmaf(__builtin_fmaf(-x, s, 1.0f), x, x);
 }
-__device__ __forceinline__ float clamped(float x, float most) { return x != x ? x : fminf(fmaxf(x, -most), most); }
 
 // eight FP4 elements of y / scale, rounded to the nearest, ties to even, the largest where they are beyond it (`scale`: a power of two)
 __device__ __forceinline__ uint32_t eight_to_fp4(const float (&y)[8], float scale)
@@ -204,8 +235,12 @@ template <int FMT, bool TIMES> __device__ __forceinline__ u32x4_t quantised(cons
         } else {
             scale = nan ? 0x7Fu : (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(quotient(fminf(largest, 6.0f * 448.0f), 6.0f, 1.0f / 6.0f), 0.0f, 0, false) & 0xFFu;
             const float s = block_scale<FMT>(scale), reciprocal = reciprocal_of(s);
+            if (__any(largest > 0x1p20f)) {                      // whose quotients might not be numbers (6 times the largest scale is less than 2^12)
 #pragma unroll
-            for (int i = 0; i < 8; i++) y[i] = quotient(__builtin_amdgcn_fmed3f(y[i], -0x1p20f, 0x1p20f), s, reciprocal);      // (6 times the largest scale is less than 2^12)
+                for (int i = 0; i < 8; i++) y[i] = __builtin_amdgcn_fmed3f(y[i], -0x1p20f, 0x1p20f);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; i++) y[i] = quotient(y[i], s, reciprocal);
             w[0] = nan || s == 0.0f ? 0u : eight_to_fp4(y, 1.0f);
         }
     }
@@ -254,22 +289,20 @@ __global__ __launch_bounds__(256) void k_kv_write(RowsDev r)
         x[i][1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(r.v + t * r.v_token_stride + (uint64_t)head * r.v_head_stride + sub * 8));
     }
     Place p[P];
-    find_places<D, P>(r, head, token, p);
+    Factors f[P];
+    find_places<D, P, TIMES>(r, head, token, p, f);
 #pragma unroll
     for (int i = 0; i < P; i++)
 #pragma unroll
         for (int kv = 0; kv < 2; kv++) {
-            [[maybe_unused]] const float *scales = kv ? r.c.v_scales : r.c.k_scales;
-            float factor = 1.0f;
-            if constexpr (TIMES) {
-                const float divisor = scales ? scales[p[i].unit] : 1.0f;
-                const uint32_t keep = divisor == 0.0f ? 0u : ~0u;
-                factor = divisor == 0.0f ? 1.0f : clamped(1.0f / divisor, kLargest);
-#pragma unroll
-                for (int j = 0; j < 4; j++) x[i][kv][j] &= keep;
-            }
             uint32_t scale = 0;
-            const u32x4_t w = quantised<FMT, TIMES>(x[i][kv], factor, scale);
+            u32x4_t w = quantised<FMT, TIMES>(x[i][kv], TIMES ? f[i].of[kv] : 1.0f, scale);
+            if constexpr (TIMES) {
+                const uint32_t keep = ~bit_as_mask(f[i].zero, kv);
+#pragma unroll
+                for (int j = 0; j < 4; j++) w[j] &= keep;
+                scale &= keep;
+            }
             if (!p[i].there) continue;
             store_eight<FMT>((kv ? r.v_pages : r.k_pages) + p[i].row * kRowBytes<FMT, D> + sub * kElemBits<FMT>, w);
             if constexpr (kFp4<FMT>) {
@@ -286,7 +319,8 @@ __global__ __launch_bounds__(256) void k_kv_read(RowsDev r)
     const uint32_t head = blockIdx.x % r.c.heads, sub = threadIdx.x % kLanes<D>;
     const int32_t token = (int32_t)(blockIdx.x / r.c.heads * (P * kTokens<D>) + threadIdx.x / kLanes<D>);
     Place p[P];
-    find_places<D, P>(r, head, token, p);
+    Factors none[P];
+    find_places<D, P, false>(r, head, token, p, none);
     u32x4_t w[P][2];
     uint32_t block[P][2];
     float s[P][2];
