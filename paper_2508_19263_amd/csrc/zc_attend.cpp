@@ -71,7 +71,6 @@ struct Pass {
 Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_splits, bool only, bool fp4)
 {
     Pass p;
-    p.long_part = fp4 ? kLongPart / 2 : kLongPart;
     // k_attend_few goes over a cache once for every 32 rows, k_attend_many once for 128.  Microseconds of the former against the latter, rows to a
     // K/V head in front, one query head each, 8 K/V heads: 64: 4 FP8 caches of 8,192 tokens 25.7 against 30.4, one 15.7 against 19.6, 4 BF16 ones
     // of 4,000 21.3 against 27.0, six E5M2 ones with heads of 64 and a window of 2,048 15.8 against 19.8, 16 BF16 ones of 1,000 with heads of 64
@@ -96,8 +95,13 @@ Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_sp
     // tokens, and two for each compute unit where rows fill one tile.  Microseconds of one workgroup and 8,192 tokens, against 512 and 4,096 (MX, 8
     // K/V heads of 128, 4 query heads to each): one cache of 131,072 tokens 48.0 and 38.7, 8 of 8,192 23.9 and 20.6, 24 of 15,005 98 and 86, 24 of 0 to
     // 30,011 114 and 97, 64 of 0 to 32,768 264 and 238; 32 of 16,384 113.9 and 114.6; of 32 rows each, 4 of 8,192 21.8 and 23.1.
-    const bool fine = p.long_part < kLongPart;
-    const uint64_t enough = p.many || (fine && p.tiles == 1) ? 512 : 256;
+    // Where rows fill one tile and there are fewer than two (sequence, head)s for each compute unit, whose parts end at very different times, parts are of at
+    // most 2,560 tokens.  Microseconds of 4,096 against 2,560: 24 NVFP4 caches of 0 to 30,011 94.4 and 91.1, with weights 130 and 127, 17 of 0 to 23,302
+    // 75.5 and 56.1, 16 of 16,384 62.0 and 58.9; 17 MXFP4 ones of 0 to 29,067 84.9 and 62.9, of 17,109 72.5 and 64.8, 40 of 8,348 74.5 and 66.8, but 32 of 16,384 99.1 and 102.9, 40 of 3,000 to 20,000 100 and
+    // 107; where there are more: 64 NVFP4 ones of 0 to 5,606 52.2 and 54.7, MXFP4 of 8,192 99.4 and 103.3, of 0 to 6,576 56.5 and 54.9;
+    // seven NVFP4 ones of 3,000 to 20,000, 64 rows, 69 and 77.  (2,048: those of 16,384 105 and, NV, 63.)
+    p.long_part = !fp4 ? kLongPart : p.tiles == 1 && groups < 512 ? kShortPart : kLongPart / 2;
+    const uint64_t enough = p.many || (fp4 && p.tiles == 1) ? 512 : 256;
     uint64_t even = groups ? (enough + groups - 1) / groups : 1;
     if (even > possible) even = possible;
     if (even > most_splits) even = most_splits;

@@ -253,10 +253,18 @@ def test_negative_block_scales(dim, q_lens):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("length", [4095, 4096, 4097, 8191, 8192, 8193, 12288])
+@pytest.mark.parametrize("length", [2559, 2560, 2561, 4095, 4096, 4097, 5120, 5121, 8191, 8192, 8193, 12288])
 def test_where_long_caches_are_cut(fmt, length):
     check(Cache4([length, 5], 1, 128, fmt), [1, 1], 4, single=True)
     check(Cache4([length], 2, 64, fmt), [2], 3, length - 1, 1)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("seqs", [31, 32, 33])
+def test_parts_of_many_heads(fmt, seqs):
+    """512 (sequence, head)s, from which on parts are longer, one sequence less and one more; lengths of both kinds of parts and none."""
+    lens = [0, 1, 2560, 2561, 4097, 5121, 6001] + [(i * 271) % 4000 for i in range(seqs - 7)]
+    check(Cache4(lens, 16, 64, fmt), [1] * seqs, 4, single=True, weights=seqs != 32)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
