@@ -3,9 +3,10 @@
 //
 // Both read each element once and write it once.  Measured with 8 K/V heads of 128 in random pages of 16 tokens: reading 84,051 MXFP4 tokens
 // 87 us, 5.0 TB/s, nearly four fifths of it writing (a large copy reaches 6.2, a fill 6.8; through the caches 95 us); 24,000 tokens BF16 36, FP8
-// 24, MX 21, NV 22 us; writing these from every sixth row of a wider tensor BF16 28, FP8 33, MX 25, NV 35 us (with inputs through the caches 2 to
-// 6 us more).  FP8 and NV with a scale for each sequence and head are bound by instructions as much as by memory: NV 1,070 of them for 64 rows of K
-// and V, 44 us for 31,385 tokens.  A token of each of 32 sequences is 2.9 us of latencies one after the other, either way.
+// 24, MX 21, NV 22 us; writing these from every sixth row of a wider tensor BF16 28, MX 25 us (with inputs through the caches 2 to 6 us more), 22,617 of them
+// with a scale for each sequence and head FP8 30, NV 32.  NV is bound by instructions as much as by memory: 900 of them to a wavefront for 16 rows of K
+// and V, 42 us for 31,385 tokens (44 with 1,070: a reciprocal of the scale for every row, every number brought into range).  A token of each of 32
+// sequences is 2.9 us of latencies one after the other, either way.
 // (Rows in the order of the caller's tensors, the heads of a token in one workgroup, instead of tokens of one head, which share a page: the
 // 84,051 tokens 85 -> 99 us.)
 #include "zc_attend_device.h"
@@ -274,8 +275,8 @@ template <int P> __device__ __forceinline__ void store_result(uint16_t *to, cons
     else *x = w;
 }
 
-// Every element is multiplied with the reciprocal of the scale of its sequence and head (at most the largest number; where the scale is 0, all become 0), rounded to the nearest, ties to even, the largest number where it is
-// beyond that.  NaN stays one; in an FP4 block it makes the block's scale NaN.
+// Every element is multiplied with the reciprocal of the scale of its sequence and head (at most the largest number; where the scale is 0, all become
+// 0), rounded to the nearest, ties to even, the largest number where it is beyond that.  NaN stays one; in an FP4 block it makes the block's scale NaN.
 template <int FMT, int D, int P, bool TIMES>
 __global__ __launch_bounds__(256) void k_kv_write(RowsDev r)
 {
