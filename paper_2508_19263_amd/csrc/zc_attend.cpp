@@ -63,12 +63,13 @@ bool same_shape(const zc_kv_cache &a, const zc_kv_cache &b) { return a.format ==
 struct Pass {
     bool many;
     uint32_t tiles, row_blocks, even, splits, long_part;
+    bool eight;                                // k_attend_short
     uint64_t blocks;
 };
 
 // rows: of one (sequence, head), or of one head of the prefix; units: how many of those; longest: tokens that a row block may have to read;
 // only: the call has no other pass
-Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_splits, bool only, bool fp4)
+Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_splits, bool only, bool fp4, bool weights)
 {
     Pass p;
     // k_attend_few goes over a cache once for every 32 rows, k_attend_many once for 128.  Microseconds of the former against the latter, rows to a
@@ -86,7 +87,13 @@ Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_sp
     // k_attend_few: 4 FP8 caches of 8,192 tokens 17.6 against 18.3 us, 32 BF16 ones with a window of 4,096 94 against 100 us; with
     // parts of two steps against four: one cache with a window of 512 9.0 against 9.6 us, 1,531 shared tokens 19.1 against 21.4 us.
     // A call's only pass is left in one part up to 640 tokens: a second launch costs what its part of the work takes.
-    const uint64_t groups = units * p.row_blocks, part = 256, possible = only && longest <= 640 ? 1 : (longest + part - 1) / part;
+    const uint64_t groups = units * p.row_blocks, part = 256;
+    // FP4, up to a workgroup for each compute unit: k_attend_short, whose eight wavefronts take what four of k_attend_few and a join take longer for.
+    // Microseconds of calls one after the other, those against it, 8 K/V heads of 128, 4 query heads to each: one MXFP4 cache of 260 tokens 6.4 and 6.1, 640
+    // 7.5 and 7.0, 700 8.6 and 7.9, 1,000 9.0 and 8.8, 1,280 8.7 and 9.5; NVFP4 640 8.6 and 7.7, 1,000 9.1 and 10.3 (from Python, which takes longer for two
+    // launches and scratch than the GPU does, 15 and 11); 32 MXFP4 ones of 1,000 12.7 and 9.7, 2,048 18.1 and 15.6, NVFP4 19.2 and 17.0.  (128 tokens 5.2 and 5.5.)
+    const bool may_be_eight = fp4 && only && !weights && rows <= 16 && groups <= 256;
+    const uint64_t one_part = !may_be_eight ? 640 : groups <= 128 ? 1024 : 2048, possible = only && longest <= one_part ? 1 : (longest + part - 1) / part;
     // Lengths are not known here, only the longest.  So that one long cache among short ones does not keep everyone waiting, parts are at
     // most kLongPart tokens, and what is left over of a shorter cache's parts ends at once: 31 FP8 caches of 1,000 tokens and one of 131,072
     // 1,077 -> 128 us, 64 of 0 to 32,768 444 -> 408 us; 64 of 8,192 188 us as before, 16 of 32,768 190 -> 198 us.  (At most 4,096: 109, 391,
@@ -109,6 +116,7 @@ Pass plan_pass(uint64_t rows, uint64_t units, uint64_t longest, uint32_t most_sp
     const uint64_t least = p.many ? 1 : (longest + p.long_part - 1) / p.long_part, s = even > least ? even : least;
     p.even = (uint32_t)even;
     p.splits = (uint32_t)(s < most_splits ? s : most_splits);
+    p.eight = may_be_eight && p.splits == 1 && longest > 256;
     p.blocks = groups * p.splits;
     return p;
 }
@@ -173,7 +181,7 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
         const uint64_t w = a.window ? (uint64_t)a.window + a.max_q_len + a.sinks + 64 : (uint64_t)limit;
         return w < (uint64_t)limit ? w : (uint64_t)limit;
     };
-    p.own_pass = plan_pass((uint64_t)a.max_q_len * a.group, (uint64_t)a.n_seqs * a.c.heads, reach(a.c.limit), shared ? 16 : kMaxSlots, !shared, fp4(cache->format));
+    p.own_pass = plan_pass((uint64_t)a.max_q_len * a.group, (uint64_t)a.n_seqs * a.c.heads, reach(a.c.limit), shared ? 16 : kMaxSlots, !shared, fp4(cache->format), x->d_weights_out);
     p.slots = p.own_pass.splits;
     if (shared) {
         AttendDev &b = p.pre;
@@ -188,7 +196,7 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
         b = a;
         b.c = pc;
         b.shared = 1;
-        p.pre_pass = plan_pass((uint64_t)a.n_tokens * a.group, a.c.heads, (uint64_t)pc.limit, 48, false, fp4(cache->format));
+        p.pre_pass = plan_pass((uint64_t)a.n_tokens * a.group, a.c.heads, (uint64_t)pc.limit, 48, false, fp4(cache->format), false);
         b.splits = p.pre_pass.splits;
         b.even = p.pre_pass.even;
         b.long_part = p.pre_pass.long_part;
@@ -202,6 +210,7 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
     a.long_part = p.own_pass.long_part;
     a.row_blocks = p.own_pass.row_blocks;
     a.direct = p.slots == 1;
+    a.eight = p.own_pass.eight;
     // Pages that are read once and are more than the memory-side cache holds go past the caches.  Microseconds of a decoding step through them against
     // past them (8 K/V heads of 128, 64 caches of 8,192 tokens): BF16 371 and 330, FP8 184 and 167, MXFP4 113 and 103, NVFP4 127 and 120; 32 MXFP4 ones (285
     // MB) 60 and 57; 16 (142 MB) 33 and 32, 8 of MXFP4 20 and 21.5, 4 FP8 ones 16.6 and 18.6, which find them there again.  Rows of less than 64 bytes lie

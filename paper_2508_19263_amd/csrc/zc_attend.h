@@ -39,6 +39,7 @@ struct AttendDev {
     uint32_t even, long_part;          // k_attend_few: parts that what a sequence sees is divided into if these have no more than so many tokens
     uint32_t row_blocks;               // row blocks per (sequence, head), or per head of the prefix
     uint32_t past_caches;              // k_attend_few: 1: what the pass reads is more than the caches hold
+    uint32_t eight;                    // 1: k_attend_short in k_attend_few's place
     uint32_t direct;                   // 1: one slot in all, the pass writes out and lse itself
 };
 

@@ -25,7 +25,7 @@
 
 namespace zc {
 
-constexpr uint32_t kWaves = 4;                 // wavefronts per workgroup (k_attend_few: with eight, batches were 1 us slower and single sequences 0.6 us faster)
+constexpr uint32_t kWaves = 4;                 // wavefronts per workgroup (k_attend_few: with eight, batches were 1 us slower and single sequences 0.6 us faster: see k_attend_short)
 
 template <int FMT, int D> struct BlockRegs {
     static constexpr int NK = D * kElemBits<FMT> / 512;              // 16-byte pieces of a key per lane
@@ -88,16 +88,16 @@ template <int FMT, int D, int SEL> __device__ __forceinline__ void value_operand
     }
 }
 
-template <int D, int QT> struct FewShared {
-    float ml[kWaves][QT * 16][2];
-    alignas(16) float ob[kWaves][16][D + 4];
+template <int D, int QT, uint32_t WAVES = kWaves> struct FewShared {
+    float ml[WAVES][QT * 16][2];
+    alignas(16) float ob[WAVES][16][D + 4];
 };
 
 // PAST: pages go past the caches (kPastCaches)
 constexpr int kPastCaches = 2;                 // the non-temporal bit of buffer loads
 
-template <int FMT, int D, int QT, bool LOGITS, bool PAST>
-__device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, uint32_t split, uint32_t row_block, FewShared<D, QT> &shared)
+template <int FMT, int D, int QT, bool LOGITS, bool PAST, uint32_t WAVES = kWaves>
+__device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, uint32_t split, uint32_t row_block, FewShared<D, QT, WAVES> &shared)
 {
     using Regs = typename FewRegs<FMT, D>::Type;
     constexpr int DL = Regs::DL, KS = D / 32;
@@ -140,7 +140,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
     const Blocks blocks = seen_blocks(32, last_max, from_min, sinks);
     // this workgroup's part, in steps that all wavefronts take part in
     const int32_t even = min((blocks.count + (int32_t)a.even - 1) / (int32_t)a.even, (int32_t)a.long_part / 32), least = (blocks.count + (int32_t)a.splits - 1) / (int32_t)a.splits;
-    const int32_t per_split = (max(even, least) + (int32_t)kWaves - 1) / (int32_t)kWaves * (int32_t)kWaves;
+    const int32_t per_split = (max(even, least) + (int32_t)WAVES - 1) / (int32_t)WAVES * (int32_t)WAVES;
     const int32_t begin = min((int32_t)split * per_split, blocks.count), end = min(begin + per_split, blocks.count);
     if (begin == end && !a.direct) {                     // nothing left for this part (k_attend_join does not look at what its rows would be)
         const uint32_t r = first_row + threadIdx.x, i = r / a.group;
@@ -160,7 +160,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
     // page ids of the wavefront's next 32 steps: lane 2i + h has that of half h of step i (-1: absent)
     int32_t ids = -1, ids_from = begin + (int32_t)wave;
     auto fetch_ids = [&](int32_t b) {
-        const int32_t mine = b + (int32_t)(lane >> 1) * (int32_t)kWaves;
+        const int32_t mine = b + (int32_t)(lane >> 1) * (int32_t)WAVES;
         const uint32_t page = ((uint32_t)blocks.at(mine) * 32 + (lane & 1) * 16) >> a.c.page_shift;
         ids = -1;
         if (mine < end && page < a.c.table_pages) ids = table[page];
@@ -206,8 +206,8 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
     auto place_of = [&](int32_t b) {
         Place x = {{0, 0}, 0, 0};
         if (b >= end) return x;
-        if (b - ids_from >= 32 * (int32_t)kWaves) fetch_ids(b);
-        const int32_t i = (b - ids_from) / (int32_t)kWaves * 2;
+        if (b - ids_from >= 32 * (int32_t)WAVES) fetch_ids(b);
+        const int32_t i = (b - ids_from) / (int32_t)WAVES * 2;
         x.t0 = blocks.at(b) * 32;
 #pragma unroll
         for (int h = 0; h < 2; h++) {
@@ -269,10 +269,10 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
     Place place = place_of(b);
     load_keys(place, r);
     load_values(place, r);
-    for (; b < end; b += (int32_t)kWaves) {
+    for (; b < end; b += (int32_t)WAVES) {
         const int32_t t0 = place.t0;
         const uint32_t there = place.there;
-        place = place_of(b + (int32_t)kWaves);
+        place = place_of(b + (int32_t)WAVES);
         f32x4 s[QT][2];
 #pragma unroll
         for (int t = 0; t < QT; t++) s[t][0] = s[t][1] = f32x4{0, 0, 0, 0};
@@ -415,14 +415,14 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
         if (g == 0) { ml[wave][t * 16 + n16][0] = part_base(base[t], l[t]); ml[wave][t * 16 + n16][1] = l[t]; }
     }
     __syncthreads();
-    constexpr uint32_t kPerRow = kWaves * 4, DP = D / kPerRow;     // threads per row, dimensions per thread
+    constexpr uint32_t kPerRow = WAVES * 4, DP = D / kPerRow;     // threads per row, dimensions per thread
     const uint32_t row16 = threadIdx.x / kPerRow, piece = threadIdx.x % kPerRow;
 #pragma unroll
     for (int t = 0; t < QT; t++) {
         const float mine = ml[wave][t * 16 + n16][0];
         float top = kNegInf;
 #pragma unroll
-        for (uint32_t w = 0; w < kWaves; w++) top = fmaxf(top, ml[w][t * 16 + n16][0]);
+        for (uint32_t w = 0; w < WAVES; w++) top = fmaxf(top, ml[w][t * 16 + n16][0]);
         const float f = __builtin_amdgcn_exp2f(mine - (top == kNegInf ? 0.0f : top));
 #pragma unroll
         for (int cc = 0; cc < 4; cc++)
@@ -440,14 +440,14 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
             if (a.shared && tok >= 0 && sequence_of(a, tok) < 0) tok = -1;
             float big = kNegInf, sum = 0.0f;
 #pragma unroll
-            for (uint32_t w = 0; w < kWaves; w++) big = fmaxf(big, ml[w][t * 16 + row16][0]);
+            for (uint32_t w = 0; w < WAVES; w++) big = fmaxf(big, ml[w][t * 16 + row16][0]);
 #pragma unroll
-            for (uint32_t w = 0; w < kWaves; w++) sum += ml[w][t * 16 + row16][1] * __builtin_amdgcn_exp2f(ml[w][t * 16 + row16][0] - (big == kNegInf ? 0.0f : big));
+            for (uint32_t w = 0; w < WAVES; w++) sum += ml[w][t * 16 + row16][1] * __builtin_amdgcn_exp2f(ml[w][t * 16 + row16][0] - (big == kNegInf ? 0.0f : big));
             float x[DP];
 #pragma unroll
             for (uint32_t d = 0; d < DP; d++) x[d] = 0.0f;
 #pragma unroll
-            for (uint32_t w = 0; w < kWaves; w++)
+            for (uint32_t w = 0; w < WAVES; w++)
 #pragma unroll
                 for (uint32_t d = 0; d < DP; d++) x[d] += ob[w][row16][piece * DP + d];
             if (tok >= 0) {

@@ -621,11 +621,13 @@ def read_kv(cache, q_start=None, n_tokens=None, k=None, v=None):
     results = [t for t in (k, v) if t is not None]
     size = (n_tokens, cache.n_heads, cache.head_dim)
     if k is None:
-        k = torch.empty(size, dtype=torch.bfloat16, device=cache.device)
+        k = cache.k_pages.new_empty(size, dtype=torch.bfloat16)
+        if v is None:
+            v = torch.empty_like(k)
     elif k.shape[0] != n_tokens:
         raise ValueError("zc_kv_read: k has to be [n_tokens, n_heads, head_dim] in BF16 with contiguous rows")
     if v is None:
-        v = torch.empty(size, dtype=torch.bfloat16, device=cache.device)
+        v = cache.k_pages.new_empty(size, dtype=torch.bfloat16)
     _kv_rows("zc_kv_read", lib().zc_kv_read, k, v, cache, q_start, results)
     return k, v
 
@@ -641,7 +643,7 @@ def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, ma
     elif (n > 1 and out.stride(0) < dim) or (heads > 1 and out.stride(1) < dim):
         raise ValueError("%s: rows of out overlap" % what)
     if lse is None:
-        lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
+        lse = q.new_empty((n, heads), dtype=torch.float32)
     elif lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous():
         raise ValueError("%s: lse has to be contiguous float32 [n_tokens, n_q_heads]" % what)
     if q_start is not None and (q_start.dtype != torch.int32 or q_start.numel() != cache.n_seqs + 1 or not q_start.is_contiguous()):

@@ -259,6 +259,27 @@ def test_where_long_caches_are_cut(fmt, length):
     check(Cache4([length], 2, 64, fmt), [2], 3, length - 1, 1)
 
 
+@pytest.mark.parametrize("fmt,dim", [(MX, 128), (NV, 128), (MX, 64), (NV, 64)])
+@pytest.mark.parametrize("length", [255, 256, 257, 639, 641, 1024, 1025])
+def test_short_caches(fmt, dim, length):
+    """On both sides of the lengths between which a part has eight wavefronts; up to 16 rows and more."""
+    cache = Cache4([length], 2, dim, fmt)
+    check(cache, [1], 4, single=True)
+    check(cache, [1], 16, length // 2, 5)
+    check(cache, [3], 5)
+    check(cache, [2], 9)
+    cache.table[0, 1, ::3] = -1
+    check(cache, [2], 7)
+
+
+@pytest.mark.parametrize("fmt,dim", [(MX, 128), (NV, 64)])
+@pytest.mark.parametrize("seqs,heads,length", [(8, 16, 1024), (43, 3, 1025), (8, 16, 1025), (16, 16, 2048), (16, 16, 2049), (257, 1, 700)])
+def test_short_caches_of_many_heads(fmt, dim, seqs, heads, length):
+    """128 and 256 (sequence, head)s, up to which longer caches are one part, and one more; lengths of all kinds and none."""
+    lens = [length, 0, 1, 33, length - 1, 128] + [(i * 97) % (length if seqs < 99 else 60) for i in range(seqs - 6)]
+    check(Cache4(lens, heads, dim, fmt), [1] * seqs, 4, single=True)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("seqs", [31, 32, 33])
 def test_parts_of_many_heads(fmt, seqs):
