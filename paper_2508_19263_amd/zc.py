@@ -7,6 +7,7 @@ library handle raises.
 """
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -94,6 +95,9 @@ class AttendArgs(C.Structure):
 
 _ATTEND_ARGS_BYTES = C.sizeof(AttendArgs)
 _KV_ROWS_BYTES = C.sizeof(KvRows)
+# The members in their order: a structure made of packed bytes takes half the time of one whose members are set one by one (0.9 us, of calls of 10).
+_pack_attend_args = struct.Struct("=8IfI10Q").pack
+_pack_kv_rows = struct.Struct("=2I7Q").pack
 
 
 class ZcError(RuntimeError):
@@ -593,7 +597,7 @@ def _kv_rows(what, call, k, v, cache, q_start, results):
     if n == 1 or heads == 1:                                     # the stride of a dimension of one element is any number
         kt, vt = (0, 0) if n == 1 else (kt, vt)
         kh, vh = (0, 0) if heads == 1 else (kh, vh)
-    a = KvRows(_KV_ROWS_BYTES, n, k.data_ptr(), v.data_ptr(), kt, kh, vt, vh, None if q_start is None else q_start.data_ptr())
+    a = KvRows.from_buffer_copy(_pack_kv_rows(_KV_ROWS_BYTES, n, k.data_ptr(), v.data_ptr(), kt, kh, vt, vh, 0 if q_start is None else q_start.data_ptr()))
     st = call(C.byref(a), cache.ref, torch._C._cuda_getCurrentRawStream(current))
     if st != OK:
         raise ZcError(st, what)
@@ -660,16 +664,16 @@ def _attend(what, q, prefix, cache, q_start, max_q_len, window, sinks, scale, ma
     if (q.requires_grad or (weights is not None and weights.requires_grad)) and torch.is_grad_enabled():
         raise ValueError("%s: there is no gradient through a stored cache: detach q and weights, or call it under torch.no_grad()" % what)
     device, current = q.device, torch._C._cuda_getDevice() if q.is_cuda else -1       # (the kernels go to the current GPU's stream)
-    if device.index != current or cache.device != device or any(t is not None and t.device != device for t in (out, lse, q_start, weights, weights_out, ws)) or \
-            (prefix is not None and prefix.device != device):
+    if device.index != current or cache.device != device or out.device != device or lse.device != device or \
+            any(t is not None and t.device != device for t in (q_start, weights, weights_out, ws, prefix)):
         raise ValueError("%s: tensors have to be on one GPU, the current one" % what)
     strides = q.stride()[:2] + out.stride()[:2]
     if n == 1 or heads == 1:                                     # the stride of a dimension of one element is any number
         strides = [0 if size == 1 else stride for size, stride in zip((n, heads, n, heads), strides)]
-    a = AttendArgs(_ATTEND_ARGS_BYTES, n, heads, max_q_len, window, sinks, max_kv_len, max_prefix_len, dim ** -0.5 if scale is None else scale, 0,
-                   q.data_ptr(), out.data_ptr(), *strides,
-                   None if q_start is None else q_start.data_ptr(), lse.data_ptr(),
-                   None if weights is None else weights.data_ptr(), None if weights_out is None else weights_out.data_ptr())
+    a = AttendArgs.from_buffer_copy(_pack_attend_args(
+        _ATTEND_ARGS_BYTES, n, heads, max_q_len, window, sinks, max_kv_len, max_prefix_len, dim ** -0.5 if scale is None else C.c_float(scale).value, 0,
+        q.data_ptr(), out.data_ptr(), *strides, 0 if q_start is None else q_start.data_ptr(), lse.data_ptr(),
+        0 if weights is None else weights.data_ptr(), 0 if weights_out is None else weights_out.data_ptr()))
     L, ref = lib(), C.byref(a)
     at, size = (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
     if ws is None:

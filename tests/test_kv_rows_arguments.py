@@ -196,3 +196,11 @@ def test_keys_on_top_of_values(shape, k_strides):
             with pytest.raises(ValueError, match="rows of k and v overlap" if both else "GPU"):
                 zc.read_kv(c, start, k=k, v=v)
     assert seen == {True, False}
+
+
+def test_packed_arguments_are_the_structures():
+    """The binding packs a call's arguments itself: every member is where the structure has it."""
+    for kind, pack in ((zc.KvRows, zc._pack_kv_rows), (zc.AttendArgs, zc._pack_attend_args)):
+        values = [i + 1 for i in range(len(kind._fields_))]
+        a = kind.from_buffer_copy(pack(*values))
+        assert [getattr(a, name) for name, _ in kind._fields_] == values and len(pack(*values)) == C.sizeof(kind)
