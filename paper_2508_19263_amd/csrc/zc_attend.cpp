@@ -215,7 +215,7 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
     // past them (8 K/V heads of 128, 64 caches of 8,192 tokens): BF16 371 and 330, FP8 184 and 167, MXFP4 113 and 103, NVFP4 127 and 120; 32 MXFP4 ones (285
     // MB) 60 and 57; 16 (142 MB) 33 and 32, 8 of MXFP4 20 and 21.5, 4 FP8 ones 16.6 and 18.6, which find them there again.  Rows of less than 64 bytes lie
     // four to a line that several loads take parts of: 64 MXFP4 caches of 16,384 tokens, 64 dimensions, 134 and 140.
-    a.past_caches = !p.own_pass.many && p.own_pass.row_blocks == 1 && row_bytes(*cache) >= 64 &&
+    a.past_caches = !p.own_pass.many && p.own_pass.row_blocks == 1 && row_bytes(*cache) >= kLeastPast &&
                     (uint64_t)a.n_seqs * a.c.heads * reach(a.c.limit) * 2 * (row_bytes(*cache) + row_scales(*cache)) > kMemorySideCache;
     if (p.own_pass.blocks + p.pre_pass.blocks > kMaxBlocks) return ZC_ERR_INVALID_ARG;
     if (p.slots > 1) {

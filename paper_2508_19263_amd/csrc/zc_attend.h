@@ -44,6 +44,7 @@ struct AttendDev {
 };
 
 constexpr uint64_t kMemorySideCache = 256u << 20;     // bytes
+constexpr uint32_t kLeastPast = 64;    // bytes of a row that goes past them
 constexpr uint32_t kMostParts = 16;
 constexpr uint32_t kLogitRows = 24;    // rows whose logits k_attend_few leaves
 constexpr uint32_t kLongPart = 8192;   // tokens; of FP4 half of it, or

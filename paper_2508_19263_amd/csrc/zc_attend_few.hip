@@ -25,8 +25,13 @@ __global__ __launch_bounds__(512, 2) void k_attend_short(AttendDev a)
 
 template <int FMT, int D, int QT, bool LOGITS> void launch_of(const AttendDev &a, dim3 blocks, hipStream_t s)
 {
-    if (a.past_caches) hipLaunchKernelGGL((k_attend_few<FMT, D, QT, LOGITS, true>), blocks, dim3(kWaves * 64), 0, s, a);
-    else hipLaunchKernelGGL((k_attend_few<FMT, D, QT, LOGITS, false>), blocks, dim3(kWaves * 64), 0, s, a);
+    if constexpr (kRowBytes<FMT, D> >= kLeastPast) {
+        if (a.past_caches) {
+            hipLaunchKernelGGL((k_attend_few<FMT, D, QT, LOGITS, true>), blocks, dim3(kWaves * 64), 0, s, a);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((k_attend_few<FMT, D, QT, LOGITS, false>), blocks, dim3(kWaves * 64), 0, s, a);
 }
 template <int FMT, int D> int launch(const AttendDev &a, uint32_t tiles, dim3 blocks, hipStream_t s)
 {
