@@ -475,8 +475,8 @@ uint64_t zc_attend_workspace_bytes(const zc_attend_args *args, const zc_kv_cache
  * weights_out[s][h][t] = weights_in[s][h][t] + sum exp(s_t - lse) for t below the length; entries behind it are left untouched.
  * The sums have one order: the same call gives the same bits.
  * Kernels are chosen by max_q_len: sequences that go on by a token or a few are best given a call of their own, apart from those
- * that bring a prompt, and max_kv_len decides into how many parts a cache is split and how much scratch is asked for, so it is best
- * close to the longest length.  Weights of up to 24 query rows per K/V head take 4 bytes of scratch per row and token of that length where
+ * that bring a prompt, and max_kv_len decides into how many parts a cache is split, how much scratch is asked for and, over FP4 pages,
+ * whether these are taken for more than the GPU's caches hold, so it is best close to the longest length.  Weights of up to 24 query rows per K/V head take 4 bytes of scratch per row and token of that length where
  * this is at most 1 GiB in all; where it would be more they are slower (the keys are read again). */
 zc_status zc_attend(const zc_attend_args *args, const zc_kv_cache *cache, void *d_ws, uint64_t ws_bytes, void *stream);
 

@@ -212,11 +212,20 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
     a.direct = p.slots == 1;
     a.eight = p.own_pass.eight;
     // Pages that are read once and are more than the memory-side cache holds go past the caches.  Microseconds of a decoding step through them against
-    // past them (8 K/V heads of 128, 64 caches of 8,192 tokens): BF16 371 and 330, FP8 184 and 167, MXFP4 113 and 103, NVFP4 127 and 120; 32 MXFP4 ones (285
-    // MB) 60 and 57; 16 (142 MB) 33 and 32, 8 of MXFP4 20 and 21.5, 4 FP8 ones 16.6 and 18.6, which find them there again.  Rows of less than 64 bytes lie
-    // four to a line that several loads take parts of: 64 MXFP4 caches of 16,384 tokens, 64 dimensions, 134 and 140.
-    a.past_caches = !p.own_pass.many && p.own_pass.row_blocks == 1 && row_bytes(*cache) >= kLeastPast &&
-                    (uint64_t)a.n_seqs * a.c.heads * reach(a.c.limit) * 2 * (row_bytes(*cache) + row_scales(*cache)) > kMemorySideCache;
+    // past them (8 K/V heads of 128): 64 caches of 8,192 tokens BF16 361 and 320, FP8 186 and 167, MXFP4 113 and 103, NVFP4 124 and 113; 200 FP8 ones of 2,000
+    // 151 and 138, 24 of 0 to 30,011 160 and 167; 32 MXFP4 ones (285 MB) 60 and 57; 16 (142 MB) 33 and 32, 8 of MXFP4 20 and 21.5, 4 FP8 ones 16.6 and 18.6,
+    // which find them there again.  Rows of less than 64 bytes lie four to a line that several loads take parts of: 64 MXFP4 caches of 16,384 tokens, 64
+    // dimensions, 134 and 140.
+    // The host knows the room and the pools, and a pool that the caches hold is never read past them.  BF16 and FP8 go on by the lengths and the table, on the
+    // device (past_caches): 4 caches of 8,192 tokens in tables for 131,072, BF16 25.7 us through the caches and 27.0 past them, FP8 16.6 and 17.5; 64 of 8,192
+    // that have their first 8,000 in the same pages BF16 145 and 188, FP8 89 and 95, the first 6,144 BF16 189 and 213, FP8 104 and 113, the first 4,096 BF16 243
+    // and 241, FP8 139 and 131.  FP4 goes by the room: a workgroup's choice takes two loads one after the other, 3 to 5 % of what it has to do then (200
+    // caches of 2,000 MXFP4 81.5 -> 84.4 us, NVFP4 88.8 -> 92.7, 24 of 0 to 30,011 88.9 -> 92.3 and 92.8 -> 96.5; BF16 less than 0.5 %), where 4 of 8,192 in too much
+    // room lose no more (MXFP4 13.2 and 13.8, NVFP4 14.6 and 15.0) and 64 of 8,192 that share 6,144 a tenth (68 and 75, 91 and 98).
+    const uint64_t held = kMemorySideCache / ((uint64_t)a.c.heads * 2 * (row_bytes(*cache) + row_scales(*cache)));       // tokens
+    a.reach = (int32_t)reach(a.c.limit);
+    if (!p.own_pass.many && p.own_pass.row_blocks == 1 && row_bytes(*cache) >= kLeastPast && (uint64_t)a.n_seqs * (uint64_t)a.reach > held &&
+        ((uint64_t)a.c.n_pages << a.c.page_shift) > held * a.c.heads) a.past_caches = held ? (uint32_t)held : 1;
     if (p.own_pass.blocks + p.pre_pass.blocks > kMaxBlocks) return ZC_ERR_INVALID_ARG;
     if (p.slots > 1) {
         const uint64_t rows = (uint64_t)a.n_tokens * a.q_heads * p.slots;

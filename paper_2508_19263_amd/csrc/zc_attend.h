@@ -38,13 +38,14 @@ struct AttendDev {
     uint32_t splits, first_slot;       // this pass's slots are first_slot .. first_slot + splits
     uint32_t even, long_part;          // k_attend_few: parts that what a sequence sees is divided into if these have no more than so many tokens
     uint32_t row_blocks;               // row blocks per (sequence, head), or per head of the prefix
-    uint32_t past_caches;              // k_attend_few: 1: what the pass reads is more than the caches hold
+    uint32_t past_caches;              // k_attend_few: tokens of all sequences above which pages go past the caches; 0: none do
+    int32_t reach;                     // tokens of a sequence that are read, at most
     uint32_t eight;                    // 1: k_attend_short in k_attend_few's place
     uint32_t direct;                   // 1: one slot in all, the pass writes out and lse itself
 };
 
 constexpr uint64_t kMemorySideCache = 256u << 20;     // bytes
-constexpr uint32_t kLeastPast = 64;    // bytes of a row that goes past them
+constexpr uint32_t kLeastPast = 64;    // bytes of a row that may go past them
 constexpr uint32_t kMostParts = 16;
 constexpr uint32_t kLogitRows = 24;    // rows whose logits k_attend_few leaves
 constexpr uint32_t kLongPart = 8192;   // tokens; of FP4 half of it, or

@@ -93,8 +93,22 @@ template <int D, int QT, uint32_t WAVES = kWaves> struct FewShared {
     alignas(16) float ob[WAVES][16][D + 4];
 };
 
-// PAST: pages go past the caches (kPastCaches)
-constexpr int kPastCaches = 2;                 // the non-temporal bit of buffer loads
+// Whether a call whose pages may go past the caches (plan_attend) has them do so, for one (sequence, head): all sequences together have more tokens than
+// a.past_caches, counting those that are read, and the page in the middle of them is not also the next 64 sequences' (which would find it in the caches).
+__device__ __forceinline__ bool past_caches(const AttendDev &a, uint32_t unit)
+{
+    const uint32_t lane = threadIdx.x & 63, head = unit % a.c.heads, seq = unit / a.c.heads;
+    float tokens = 0.0f;
+    for (uint32_t s = lane; s < a.n_seqs; s += 64) tokens += (float)clamped_length(a.c.lengths, s, a.reach);
+    const int32_t length = clamped_length(a.c.lengths, seq, a.c.limit);
+    const uint32_t middle = (uint32_t)max(min(length - min(length, a.reach) / 2, length - 1), 0) >> a.c.page_shift;
+    const uint32_t other = lane + 1 < a.n_seqs ? (seq + 1 + lane) % a.n_seqs : seq;
+    const int32_t mine = a.c.table[(uint64_t)unit * a.c.table_pages + middle], its = a.c.table[((uint64_t)other * a.c.heads + head) * a.c.table_pages + middle];
+    return !__any(other != seq && its == mine) && uniform(sum_over_wave(tokens) > (float)a.past_caches ? 1 : 0);
+}
+
+// PAST: pages go past the caches
+constexpr int kNonTemporal = 2;                // the bit of buffer loads
 
 template <int FMT, int D, int QT, bool LOGITS, bool PAST, uint32_t WAVES = kWaves>
 __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, uint32_t split, uint32_t row_block, FewShared<D, QT, WAVES> &shared)
@@ -102,7 +116,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
     using Regs = typename FewRegs<FMT, D>::Type;
     constexpr int DL = Regs::DL, KS = D / 32;
     constexpr uint32_t kRow = kRowBytes<FMT, D>;
-    constexpr int AUX = PAST ? kPastCaches : 0;
+    constexpr int AUX = PAST ? kNonTemporal : 0;
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
     const uint32_t head = unit % a.c.heads, seq = unit / a.c.heads;              // a shared prefix's one "sequence" is 0
 

@@ -5,13 +5,22 @@ namespace zc {
 
 namespace {
 
-template <int FMT, int D, int QT, bool LOGITS, bool PAST>
+enum Pages { kThrough, kPast, kChoose };       // the caches; kChoose: as past_caches says
+
+template <int FMT, int D, int QT, bool LOGITS, Pages PAGES>
 __global__ __launch_bounds__(kWaves * 64, 2) void k_attend_few(AttendDev a)
 {
     __shared__ FewShared<D, QT> shared;
     // Each part begins with another unit: workgroups that lie a round apart go to the same compute unit, where the parts of a long
     // cache would meet (one FP8 cache of 131,072 tokens and 31 of 1,000: 168 -> 128 us, six of 100 to 3,001 13.6 -> 12.4 us).
-    attend_few<FMT, D, QT, LOGITS, PAST>(a, (blockIdx.x + blockIdx.y * 13) % gridDim.x, blockIdx.y, blockIdx.z, shared);
+    const uint32_t unit = (blockIdx.x + blockIdx.y * 13) % gridDim.x;
+    if constexpr (PAGES == kChoose) {
+        if (past_caches(a, unit)) {
+            attend_few<FMT, D, QT, LOGITS, true>(a, unit, blockIdx.y, blockIdx.z, shared);
+            return;
+        }
+    }
+    attend_few<FMT, D, QT, LOGITS, PAGES == kPast>(a, unit, blockIdx.y, blockIdx.z, shared);
 }
 
 // Short FP4 caches, one part and up to 16 rows each, few enough for a compute unit to each: eight wavefronts, every one an eighth of the steps (one cache
@@ -27,11 +36,11 @@ template <int FMT, int D, int QT, bool LOGITS> void launch_of(const AttendDev &a
 {
     if constexpr (kRowBytes<FMT, D> >= kLeastPast) {
         if (a.past_caches) {
-            hipLaunchKernelGGL((k_attend_few<FMT, D, QT, LOGITS, true>), blocks, dim3(kWaves * 64), 0, s, a);
+            hipLaunchKernelGGL((k_attend_few<FMT, D, QT, LOGITS, kFp4<FMT> ? kPast : kChoose>), blocks, dim3(kWaves * 64), 0, s, a);
             return;
         }
     }
-    hipLaunchKernelGGL((k_attend_few<FMT, D, QT, LOGITS, false>), blocks, dim3(kWaves * 64), 0, s, a);
+    hipLaunchKernelGGL((k_attend_few<FMT, D, QT, LOGITS, kThrough>), blocks, dim3(kWaves * 64), 0, s, a);
 }
 template <int FMT, int D> int launch(const AttendDev &a, uint32_t tiles, dim3 blocks, hipStream_t s)
 {

@@ -38,3 +38,16 @@ def test_no_build_loads_short_rows_past_the_caches(kernels):
     for (fmt, dim, _, _, _), listing in kernels.items():
         assert ROW_BYTES[fmt] * dim >= 64 or not re.search(r"buffer_load.* nt\b", listing), (fmt, dim)
     assert any(re.search(r"buffer_load.* nt\b", listing) for listing in kernels.values())
+
+
+@pytest.mark.parametrize("fmt", [zc.FMT_BF16, zc.FMT_FP8_E4M3, zc.FMT_FP8_E5M2])
+def test_kernels_that_load_past_the_caches_can_load_through_them(kernels, fmt):
+    """BF16 and FP8: what a call reads is known when the lengths and the table are, on the device, so no kernel can only go past the caches."""
+    both = 0
+    for key, listing in kernels.items():
+        loads = re.findall(r"buffer_load_(?:dword|dwordx2|dwordx4) .*", listing)
+        past = [x for x in loads if re.search(r" nt\b", x)]
+        if key[0] == fmt and past:
+            assert len(loads) >= 2 * len(past), (key, len(loads), len(past))
+            both += 1
+    assert both == 8                                           # two sizes of heads, one tile or two, with logits or without
