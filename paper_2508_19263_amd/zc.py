@@ -479,10 +479,15 @@ class Batch:
         return self.out
 
 
-_PAGE_TYPES = {FMT_BF16: (torch.bfloat16, torch.int16, torch.uint16), FMT_FP8_E4M3: (torch.uint8, torch.int8, torch.float8_e4m3fn),
-               FMT_FP8_E5M2: (torch.uint8, torch.int8, torch.float8_e5m2), FMT_FP4_E2M1_MX: (torch.uint8, torch.int8, torch.float4_e2m1fn_x2),
-               FMT_FP4_E2M1_NV: (torch.uint8, torch.int8, torch.float4_e2m1fn_x2)}
-_BLOCK_TYPES = {FMT_FP4_E2M1_MX: (torch.uint8, torch.int8, torch.float8_e8m0fnu), FMT_FP4_E2M1_NV: (torch.uint8, torch.int8, torch.float8_e4m3fn)}
+def _types(*names):
+    """Those of torch's types that this torch has (formats can be held as plain integers without them)."""
+    return tuple(getattr(torch, name) for name in names if hasattr(torch, name))
+
+
+_PAGE_TYPES = {FMT_BF16: _types("bfloat16", "int16", "uint16"), FMT_FP8_E4M3: _types("uint8", "int8", "float8_e4m3fn"),
+               FMT_FP8_E5M2: _types("uint8", "int8", "float8_e5m2"), FMT_FP4_E2M1_MX: _types("uint8", "int8", "float4_e2m1fn_x2"),
+               FMT_FP4_E2M1_NV: _types("uint8", "int8", "float4_e2m1fn_x2")}
+_BLOCK_TYPES = {FMT_FP4_E2M1_MX: _types("uint8", "int8", "float8_e8m0fnu"), FMT_FP4_E2M1_NV: _types("uint8", "int8", "float8_e4m3fn")}
 _ROW_TYPES = (torch.bfloat16, torch.int16, torch.uint16)
 
 
