@@ -554,23 +554,48 @@ def _check_numbers(what, **numbers):
             raise ValueError("%s: %s has to be in 0 .. 2^32 - 1, not %d" % (what, name, x))
 
 
+def _least_in(a, m, lo, hi):
+    """The least x >= 0 with lo <= a * x mod m <= hi (0 <= lo <= hi < m), or None.  Where no multiple of a is in the interval, a * x - m * y is in it for
+    the least y for which m * y mod a is in the interval's negative: a smaller question of the same kind, as in Euclid's algorithm."""
+    if lo == 0:
+        return 0
+    a %= m
+    if a == 0:
+        return None
+    x = -(-lo // a)
+    if a * x <= hi:
+        return x
+    y = _least_in(m % a, a, -hi % a, -lo % a)
+    return None if y is None else -(-(lo + m * y) // a)
+
+
+def _tokens_meet(off, n, a, b, dim):
+    """Whether rows of dim elements at i * a and off + j * b (i, j < n; a, b >= dim) have elements in common."""
+    if n == 1:
+        return abs(off) < dim
+    first, last = max(0, -((off + dim - 1) // b)), min(n - 1, ((n - 1) * a + dim - 1 - off) // b)      # the j whose rows reach what lies between the others' ends
+    if first > last or a < 2 * dim:                              # (gaps of less than dim: no row fits)
+        return first <= last
+    lo = -(off + first * b + dim - 1) % a
+    x = 0 if lo + 2 * dim - 2 >= a else _least_in(b, a, lo, lo + 2 * dim - 2)
+    return x is not None and x <= last - first
+
+
 def _rows_meet(k, v):
     """Whether rows of two BF16 tensors [n, heads, dim], none of which overlap among themselves, have elements in common."""
     (n, heads, dim), off = k.shape, (v.data_ptr() - k.data_ptr()) // 2
-    reach = [sum(stride * (size - 1) for stride, size in zip(t.stride()[:2], t.shape)) + dim for t in (k, v)]
+    strides = [t.stride()[:2] for t in (k, v)]
+    reach = [a * (n - 1) + b * (heads - 1) + dim for a, b in strides]
     if not n or off >= reach[0] or -off >= reach[1]:
         return False
-    if k.stride() == v.stride():                                 # heads or tokens of one tensor: rows meet where they begin less than a row apart
-        token, head = k.stride()[:2]
-        for j in range(1 - heads, heads):
-            x = off + j * head
-            i = 0 if n == 1 else min(max(-(x // token), 1 - n), n - 1)
-            if any(abs(x + a * token) < dim for a in (i, i - 1) if abs(a) < n):
-                return True
-        return False
-    first = [torch.arange(n).view(-1, 1) * t.stride(0) + torch.arange(heads) * t.stride(1) for t in (k, v)]
-    begins = torch.cat([first[0].flatten(), first[1].flatten() + off]).sort().values
-    return bool((begins.diff() < dim).any())
+    levels = [(a, size) for a, b, size in zip(*strides, (n, heads)) if size > 1 and a == b]
+    if len(levels) == (n > 1) + (heads > 1):                     # tokens and heads of one tensor: the differences next to 0 are among these
+        near = [off]
+        for stride, size in sorted(levels, reverse=True):
+            near = [x + i * stride for x in near for i in (-(x // stride), -(x // stride) - 1) if -size < i < size]
+        return any(abs(x) < dim for x in near)
+    (a, a_head), (b, b_head) = strides
+    return any(_tokens_meet(off + j * b_head - i * a_head, n, a, b, dim) for i in range(heads) for j in range(heads))
 
 
 def _kv_rows(what, call, k, v, cache, q_start, results):
