@@ -434,7 +434,8 @@ typedef struct {
  *   FP4, NV     with the block's E4M3 scale s = m / 6 in 32 bits, rounded likewise (at most 448), elements y / s (0 where s is 0).
  * FP8 and FP4: what is beyond the largest number becomes that, infinities included.  NaN stays NaN; FP4: the block's scale is NaN and its
  * elements 0.  Tokens of no sequence are skipped, and so is a row whose page is absent or whose position is negative or past the table's room.
- * Nothing but the rows (and FP4 block scales) of these tokens is written; a page that tokens are written to is named once in the table. */
+ * Nothing but the rows (and FP4 block scales) of these tokens is written; a page that tokens are written to is named once in the table.  K and V
+ * (and their block scales) do not overlap in memory: one pool for both is refused, unless d_k and d_v, their strides and scales are the same too. */
 zc_status zc_kv_write(const zc_kv_rows *rows, const zc_kv_cache *cache, void *stream);
 
 /* Reads rows back: element * block scale * S in 32 bits, rounded to BF16.  A row whose page is absent or whose position is negative or past the

@@ -350,6 +350,10 @@ extern "C" zc_status zc_kv_write(const zc_kv_rows *rows, const zc_kv_cache *cach
     zc::RowsDev r;
     const zc_status st = zc::plan_rows(rows, cache, &r);
     if (st) return st;
+    // (K and V have the same page numbers: in one pool they would overwrite each other, unless they are the same bits)
+    const bool tied = r.k == r.v && r.k_token_stride == r.v_token_stride && r.k_head_stride == r.v_head_stride && r.c.k_scales == r.c.v_scales;
+    const bool one_pool = r.k_pages == r.v_pages, one_scale_pool = r.k_scale_pages && r.k_scale_pages == r.v_scale_pages;
+    if (!tied && (one_pool || one_scale_pool)) return ZC_ERR_INVALID_ARG;
     if (r.n_tokens) LAUNCH_TRY(zc::launch_kv_write(r, cache->format, cache->head_dim, stream));
     return ZC_OK;
 }
