@@ -490,7 +490,7 @@ zc_status zc_attend_shared(const zc_attend_args *args, const zc_kv_cache *prefix
  * `recent` (sinks + recent <= keep) and, of those between, the ones with the largest d_weights, keep in all; of equal ones those
  * that come first; NaN counts as lowest.  They keep their order.  d_kept: [n_seqs][n_heads][keep], the numbers of the tokens that
  * remain, ascending, -1 behind the last.  Keys, values and weights of the tokens that remain go to the pages of `to` (same
- * sequences, heads, head_dim and format; pages that `from` does not name; room for min(keep, tokens of from's table)) and to
+ * sequences, heads, head_dim and format; pages that `from` does not name, one pool for K and V only where `from` has one; room for min(keep, tokens of from's table)) and to
  * d_weights_to ([n_seqs][n_heads][to's table_pages * page_tokens], or NULL, not d_weights); to's d_lengths (not from's) becomes
  * min(length, keep).  The first length tokens' pages have to be there in both tables: a row from an absent page is zero, one to an
  * absent page is not written.  Scales belong to sequence and head and stay as they are. */

@@ -376,6 +376,9 @@ extern "C" zc_status zc_evict(const zc_kv_cache *from, const float *d_weights, u
     if (!st) st = zc::check_cache(to, &e.to);
     if (st) return st;
     if (!zc::same_shape(*from, *to) || from->n_seqs != to->n_seqs || from->d_lengths == to->d_lengths) return ZC_ERR_INVALID_ARG;
+    // (keys and values that lie apart would overwrite each other in one pool)
+    if (to->d_k_pages == to->d_v_pages && from->d_k_pages != from->d_v_pages) return ZC_ERR_INVALID_ARG;
+    if (e.to.k_blocks && e.to.k_blocks == e.to.v_blocks && e.from.k_blocks != e.from.v_blocks) return ZC_ERR_INVALID_ARG;
     if (!d_weights || (keep && !d_kept) || !zc::aligned4(d_weights) || !zc::aligned4(d_weights_to) || !zc::aligned4(d_kept)) return ZC_ERR_INVALID_ARG;
     if (d_weights_to == d_weights || (uint64_t)sinks + recent > keep || keep >= zc::kMaxTokens) return ZC_ERR_INVALID_ARG;
     const uint64_t most = keep < (uint32_t)e.from.capacity ? keep : (uint32_t)e.from.capacity;     // rows per sequence and head
