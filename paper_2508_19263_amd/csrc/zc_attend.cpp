@@ -219,12 +219,15 @@ zc_status plan_attend(const zc_attend_args *x, const zc_kv_cache *prefix, const 
     // The host knows the room and the pools, and a pool that the caches hold is never read past them.  BF16 and FP8 go on by the lengths and the table, on the
     // device (past_caches): 4 caches of 8,192 tokens in tables for 131,072, BF16 25.7 us through the caches and 27.0 past them, FP8 16.6 and 17.5; 64 of 8,192
     // that have their first 8,000 in the same pages BF16 145 and 188, FP8 89 and 95, the first 6,144 BF16 189 and 213, FP8 104 and 113, the first 4,096 BF16 243
-    // and 241, FP8 139 and 131.  FP4 goes by the room: a workgroup's choice takes two loads one after the other, 3 to 5 % of what it has to do then (200
-    // caches of 2,000 MXFP4 81.5 -> 84.4 us, NVFP4 88.8 -> 92.7, 24 of 0 to 30,011 88.9 -> 92.3 and 92.8 -> 96.5; BF16 less than 0.5 %), where 4 of 8,192 in too much
-    // room lose no more (MXFP4 13.2 and 13.8, NVFP4 14.6 and 15.0) and 64 of 8,192 that share 6,144 a tenth (68 and 75, 91 and 98).
+    // and 241, FP8 139 and 131.  The choice takes two loads one after the other, which parts of less than kLeastChoice tokens do without: 4,000 BF16 caches
+    // of 250 tokens 743 us through the caches, 779 past them, 877 with a choice for each, 2,000 of 500 716, 665 and 707, 1,200 of 800 670, 611 and 620, 1,000 of
+    // 1,000 696, 633 and 636; FP8 405, 418 and 503; 375, 373 and 403; 349, 328 and 338; 359, 338 and 345.  FP4 goes by the room: its parts end sooner (with a choice 200
+    // caches of 2,000 MXFP4 81.5 -> 84.4 us, NVFP4 88.8 -> 92.7, 24 of 0 to 30,011 88.9 -> 92.3 and 92.8 -> 96.5), and 4 of 8,192 in too much room lose no more
+    // (MXFP4 13.2 and 13.8, NVFP4 14.6 and 15.0), 64 of 8,192 that share 6,144 a tenth (68 and 75, 91 and 98).
     const uint64_t held = kMemorySideCache / ((uint64_t)a.c.heads * 2 * (row_bytes(*cache) + row_scales(*cache)));       // tokens
     a.reach = (int32_t)reach(a.c.limit);
     if (!p.own_pass.many && p.own_pass.row_blocks == 1 && row_bytes(*cache) >= kLeastPast && (uint64_t)a.n_seqs * (uint64_t)a.reach > held &&
+        (fp4(cache->format) || a.reach >= kLeastChoice) &&
         ((uint64_t)a.c.n_pages << a.c.page_shift) > held * a.c.heads) a.past_caches = held ? (uint32_t)held : 1;
     if (p.own_pass.blocks + p.pre_pass.blocks > kMaxBlocks) return ZC_ERR_INVALID_ARG;
     if (p.slots > 1) {

@@ -46,6 +46,7 @@ struct AttendDev {
 
 constexpr uint64_t kMemorySideCache = 256u << 20;     // bytes
 constexpr uint32_t kLeastPast = 64;    // bytes of a row that may go past them
+constexpr int32_t kLeastChoice = 768;  // tokens of a part that is worth choosing for
 constexpr uint32_t kMostParts = 16;
 constexpr uint32_t kLogitRows = 24;    // rows whose logits k_attend_few leaves
 constexpr uint32_t kLongPart = 8192;   // tokens; of FP4 half of it, or

@@ -93,18 +93,31 @@ template <int D, int QT, uint32_t WAVES = kWaves> struct FewShared {
     alignas(16) float ob[WAVES][16][D + 4];
 };
 
-// Whether a call whose pages may go past the caches (plan_attend) has them do so, for one (sequence, head): all sequences together have more tokens than
-// a.past_caches, counting those that are read, and the page in the middle of them is not also the next 64 sequences' (which would find it in the caches).
-__device__ __forceinline__ bool past_caches(const AttendDev &a, uint32_t unit)
+// Blocks of 32 tokens that a part of `count` of them has: steps that all wavefronts take part in.
+template <uint32_t WAVES> __device__ __forceinline__ int32_t blocks_per_part(const AttendDev &a, int32_t count)
 {
-    const uint32_t lane = threadIdx.x & 63, head = unit % a.c.heads, seq = unit / a.c.heads;
+    const int32_t even = min((count + (int32_t)a.even - 1) / (int32_t)a.even, (int32_t)a.long_part / 32), least = (count + (int32_t)a.splits - 1) / (int32_t)a.splits;
+    return (max(even, least) + (int32_t)WAVES - 1) / (int32_t)WAVES * (int32_t)WAVES;
+}
+
+// Whether a call whose pages may go past the caches (plan_attend) has them do so, for one part of one (sequence, head): all sequences together have more
+// tokens than a.past_caches, counting those that are read (of many sequences by the next 256), and the page in the middle of them is not also the next 64
+// sequences' (which would find it in the caches).  A part of less than kLeastChoice tokens does not wait for that.
+__device__ __forceinline__ bool past_caches(const AttendDev &a, uint32_t unit, uint32_t split)
+{
+    const uint32_t lane = threadIdx.x & 63, head = unit % a.c.heads, seq = unit / a.c.heads, n = min(a.n_seqs, 256u);
+    const int32_t length = clamped_length(a.c.lengths, seq, a.c.limit), read = min(length, a.reach);
+    const int32_t blocks = (read + 31) / 32, per_part = blocks_per_part<kWaves>(a, blocks);
+    if (min(blocks - (int32_t)split * per_part, per_part) * 32 < kLeastChoice) return false;
+    auto behind = [&](uint32_t i) { return seq + i < a.n_seqs ? seq + i : seq + i - a.n_seqs; };     // the i-th sequence behind this one, i below n_seqs
     float tokens = 0.0f;
-    for (uint32_t s = lane; s < a.n_seqs; s += 64) tokens += (float)clamped_length(a.c.lengths, s, a.reach);
-    const int32_t length = clamped_length(a.c.lengths, seq, a.c.limit);
-    const uint32_t middle = (uint32_t)max(min(length - min(length, a.reach) / 2, length - 1), 0) >> a.c.page_shift;
-    const uint32_t other = lane + 1 < a.n_seqs ? (seq + 1 + lane) % a.n_seqs : seq;
+#pragma unroll
+    for (uint32_t i = 0; i < 4; i++)
+        if (i * 64 + lane < n) tokens += (float)clamped_length(a.c.lengths, behind(i * 64 + lane), a.reach);
+    const uint32_t middle = (uint32_t)(length - (read + 1) / 2) >> a.c.page_shift;
+    const uint32_t other = lane + 1 < a.n_seqs ? behind(lane + 1) : seq;
     const int32_t mine = a.c.table[(uint64_t)unit * a.c.table_pages + middle], its = a.c.table[((uint64_t)other * a.c.heads + head) * a.c.table_pages + middle];
-    return !__any(other != seq && its == mine) && uniform(sum_over_wave(tokens) > (float)a.past_caches ? 1 : 0);
+    return !__any(other != seq && its == mine) && uniform(sum_over_wave(tokens) > (float)a.past_caches * ((float)n / (float)a.n_seqs) ? 1 : 0);
 }
 
 // PAST: pages go past the caches
@@ -153,8 +166,7 @@ __device__ __forceinline__ void attend_few(const AttendDev &a, uint32_t unit, ui
     }
     const Blocks blocks = seen_blocks(32, last_max, from_min, sinks);
     // this workgroup's part, in steps that all wavefronts take part in
-    const int32_t even = min((blocks.count + (int32_t)a.even - 1) / (int32_t)a.even, (int32_t)a.long_part / 32), least = (blocks.count + (int32_t)a.splits - 1) / (int32_t)a.splits;
-    const int32_t per_split = (max(even, least) + (int32_t)WAVES - 1) / (int32_t)WAVES * (int32_t)WAVES;
+    const int32_t per_split = blocks_per_part<WAVES>(a, blocks.count);
     const int32_t begin = min((int32_t)split * per_split, blocks.count), end = min(begin + per_split, blocks.count);
     if (begin == end && !a.direct) {                     // nothing left for this part (k_attend_join does not look at what its rows would be)
         const uint32_t r = first_row + threadIdx.x, i = r / a.group;

@@ -15,7 +15,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_attend_few(AttendDev a)
     // cache would meet (one FP8 cache of 131,072 tokens and 31 of 1,000: 168 -> 128 us, six of 100 to 3,001 13.6 -> 12.4 us).
     const uint32_t unit = (blockIdx.x + blockIdx.y * 13) % gridDim.x;
     if constexpr (PAGES == kChoose) {
-        if (past_caches(a, unit)) {
+        if (past_caches(a, unit, blockIdx.y)) {
             attend_few<FMT, D, QT, LOGITS, true>(a, unit, blockIdx.y, blockIdx.z, shared);
             return;
         }

@@ -162,3 +162,22 @@ def test_a_pool_that_the_caches_hold():
     p = cache.paged
     cache.table, cache.paged = room, zc.PagedCache(p.k_pages, p.v_pages, room, cache.lengths, BF16)
     check(cache, [1] * 8, 4, 0, 0, weights=True)
+
+
+@pytest.mark.parametrize("length", [767, 768, 800])
+def test_many_short_caches(length):
+    """Parts on both sides of what is worth choosing for; more sequences than are looked at."""
+    heads, dim = 2, 128
+    seqs = HELD // (2 * heads * dim * 2) // 700
+    big = Big(BF16, dim, heads, seqs, length + 33)
+    q = queries(seqs, heads * 4, dim)
+    lens = [length, 1, 0] + [length + (i % 67) - 33 for i in range(seqs - 3)]
+    big.set(lens)
+    out, lse = zc.attend(q, big.paged)
+    close(big, q, out, lse, (0, 1, 3, 36, 37, seqs // 2, seqs - 1))
+    assert bool((out[2] == 0).all())
+    half = [n if i % 300 == 0 else 0 for i, n in enumerate(lens)]
+    big.set(half)
+    again, again_lse = zc.attend(q, big.paged)
+    on = torch.tensor([n > 0 for n in half], device="cuda")
+    assert torch.equal(again[on], out[on]) and torch.equal(again_lse[on], lse[on]) and bool((again[~on] == 0).all())
