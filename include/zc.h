@@ -439,7 +439,7 @@ typedef struct {
 zc_status zc_kv_write(const zc_kv_rows *rows, const zc_kv_cache *cache, void *stream);
 
 /* Reads rows back: element * block scale * S in 32 bits, rounded to BF16.  A row whose page is absent or whose position is negative or past the
- * table's room is 0; rows of tokens of no sequence are left untouched. */
+ * table's room is 0; rows of tokens of no sequence are left untouched.  d_k and d_v do not overlap each other nor the cache. */
 zc_status zc_kv_read(const zc_kv_rows *rows, const zc_kv_cache *cache, void *stream);
 
 /* Attention of n_tokens query tokens.  Sequence s has the query tokens d_q_start[s] .. d_q_start[s + 1] (at most max_q_len of
@@ -451,7 +451,8 @@ zc_status zc_kv_read(const zc_kv_rows *rows, const zc_kv_cache *cache, void *str
  * a query that sees nothing (or nothing with a logit above minus infinity) has out = 0 and lse = -infinity.  Products are
  * accumulated, and the softmax is held, in 32 bits; its weights are rounded to the type the values are multiplied in (BF16 for
  * BF16 and MXFP4 pages; half precision for FP8 and NVFP4 pages, to within 2^-32 of a row's largest weight where they are below 2^-21 of it), the result
- * once to BF16.  Query tokens of no sequence are left untouched. */
+ * once to BF16.  Values are added up with weights of up to 2^8 and divided at the end: where 2^8 times the sum of a dimension's values over all tokens
+ * seen passes 2^128, a result may be infinite.  Query tokens of no sequence are left untouched. */
 typedef struct {
     uint32_t struct_size;       /* = sizeof(zc_attend_args) */
     uint32_t n_tokens, n_q_heads, max_q_len;

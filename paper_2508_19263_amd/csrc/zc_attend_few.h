@@ -10,8 +10,8 @@
 // head_dim / 16 consecutive dimensions.  At the end the wavefronts' (m, l, O) are joined in LDS; parts of a cache that went
 // to different workgroups are joined by k_attend_join.
 //
-// Measured with 8 K/V heads of 128 in random pages of 16 tokens, one query token, 4 query heads to each, joins included (a large copy
-// reaches 6.2 TB/s): 64 FP8 caches of 8,192 tokens 167 us, 6.4 TB/s (past the caches; 212 where their memory lies less well, which no address
+// Measured with 8 K/V heads of 128 in random pages of 16 tokens, one query token, 4 query heads to each, joins included (a large element-wise
+// pass reaches 6.2 TB/s): 64 FP8 caches of 8,192 tokens 167 us, 6.4 TB/s (past the caches; 212 where their memory lies less well, which no address
 // tells); 48 BF16 ones of 12,000 373 - 420 us, 5.6 - 6.3 TB/s; 4 FP8 ones of 8,192 16.5 us, 4.1 TB/s; one with 512 tokens in sight 8.5 us, all latency.
 //
 // FP4 elements are converted as they are used, with their block's scale: MX to BF16, an instruction for two keys, two for two values (the tokens

@@ -13,11 +13,11 @@
 //
 // Measured with 8 K/V heads of 128 and 4 query heads to each: two BF16 prompts of 8,192 and 7,001 tokens with a window of 4,096 and 16
 // sinks 790 - 850 us, 880 - 945 TFLOP/s (counted are the products of tokens that are seen); pieces of 1,024 and 511 tokens behind 7,977
-// and 7,680 FP8 ones 137 - 147 us, 700 - 750 TFLOP/s.  A library product of 8,192^3 reaches 1,136 on this card, and its clock goes down to 1.5 GHz
-// under it; here it goes from 2.2 to 1.9.  The matrix unit is busy 51 % of the cycles (FP8: 38 %), the exponentials and what belongs to
+// and 7,680 FP8 ones 137 - 147 us, 700 - 750 TFLOP/s.  A library product of 8,192^3 reaches 1,380 on this card when several follow each other, and its clock goes
+// down to 1.5 GHz under it; here it goes from 2.2 to 1.9.  The matrix unit is busy 51 % of the cycles (FP8: 38 %), the exponentials and what belongs to
 // them take about as many (two wavefronts to a SIMD; registers and LDS have room for no more); other orders of the same instructions
 // give the same time.  FP4 tiles are converted like FP8 ones, a piece of 32 (16) elements and its scales to a lane: the same pieces of prompts
-// over MXFP4 137 - 148 us, NVFP4 149 - 152; a whole prompt of 8,192 without a window 550 - 575 us (MX, 960 - 1,000 TFLOP/s) and 590 - 615 (NV).
+// over MXFP4 132 - 148 us, NVFP4 143 - 152; a whole prompt of 8,192 without a window 540 - 575 us (MX, 960 - 1,020 TFLOP/s) and 581 - 615 (NV).
 #pragma once
 #include "zc_attend_device.h"
 
@@ -43,6 +43,7 @@ template <int FMT> __device__ __forceinline__ u32x4_t eight_to_half(uint32_t lo,
 
 // Byte offset in a tile of 64 tokens x D two-byte elements of values: byte x of a token's row, moved in pieces of 64 bytes and of 16 within these: the
 // former for the transposing reads, the latter for the stores of converted tiles, whose lanes' pieces of 32 or 64 bytes would meet in a bank.
+// (Without the latter BF16 prompts take 812 us and FP8 pieces of prompts 140, with it 813 and 140.)
 template <int D> __device__ __forceinline__ uint32_t value_place(uint32_t token, uint32_t x)
 {
     return D == 128 ? token * 256 + (x ^ ((token & 3) * 0x50)) : token * 128 + (x ^ ((token >> 1 & 1) * 0x50));
