@@ -105,7 +105,7 @@ def test_under_a_default_device():
 def test_long_results_are_answered_at_once():
     """A million tokens: nothing is done for each of them."""
     k = Rows((1 << 20, 8, 128), (4096, 128), 0)
-    # a token of V lies 1,024 or 3,072 behind one of K, whose heads take 1,024 (64 less: the last of them is touched); or 8 further with each
+    # a token of V lies 1,024 (or 2,048 more) behind one of K, whose heads take 1,024 (64 less: the last of them is touched); or 8 further with each
     for v, want in ((Rows(k.shape, (6144, 128), 1024), False), (Rows(k.shape, (6144, 128), 960), True), (Rows(k.shape, (8192, 128), 1024), False),
                     (Rows(k.shape, (8200, 128), 1024), True)):
         asked = []
